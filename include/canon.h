@@ -8,7 +8,7 @@
  *     with Algorithm 2 (binary-carry tree fold) across replicas, the ascending-shard reduce-scatter order
  *     and averages taken as reciprocal multiplies (appendix "Deterministic Gradient Reduction");
  *   - AdamW is widened to fp32 and rounded to bf16 once (training recipe, optimizer-state precision).
- * The order itself (rules R0-R12, "CANON-v1") is stated with each entry point below.
+ * The order itself (rules R0-R22, "CANON-v1") is stated with each entry point below.
  *
  * Conventions for every entry point:
  *   - Tensor pointers are DEVICE memory owned by the caller.  bf16 tensors are uint16_t bit patterns.
@@ -21,8 +21,8 @@
  *     synchronisation.
  *   - Invalid arguments return CANON_EINVAL and enqueue nothing.  Valid requests outside what this
  *     version implements return CANON_EUNSUPPORTED.  A failed launch returns CANON_EDEVICE.
- *   - Calls on different streams may run concurrently; calls that share output buffers must be ordered
- *     by the caller.
+ *   - Calls on different streams may run concurrently; calls that share output buffers or a workspace must be
+ *     ordered by the caller.
  */
 #ifndef CANON_H
 #define CANON_H
@@ -415,6 +415,111 @@ canon_status canon_embed_bwd(const canon_order* order, int64_t T, int64_t V, int
 canon_status canon_lsq_step_grad_noalloc(const canon_order* order, int64_t T, int64_t K, const uint16_t* x,
                                          const float* s, const float* dx, float* grad, void* stream);
 int64_t canon_lsq_step_grad_noalloc_max_terms(void);
+
+/* ------------------------------------------------------------------------------------------------ */
+/* Activations kept in 8 bits between the forward and the backward pass (R21).  A matrix [rows][cols] is kept as
+   codes, int8 [rows][cols], and steps, fp32 [rows][ceil(cols / group)]: every `group` consecutive elements of a row
+   (32, 64, 128 or 256; a row's last group may be shorter) get the step s = RN(amax * RN(1/127)), amax their largest
+   |value| by bit pattern, and the codes clamp(rne(RN(x / s)), -128, 127) of canon_quantize; they stand for the values
+   RN(s * code), at most s/2 (and the quotient's rounding) from x.  A group with an infinity or a NaN stands for NaNs, a
+   group whose step is zero once flushed for zeros.  Device pointers of any alignment that their types allow; the struct
+   is read during the call.  canon_act8_groups: ceil(cols / group), or 0 for a group that is none of the four.
+     canon_act8_pack: x [rows][cols], fp32 (CANON_F32) or bf16 (CANON_BF16), into *kept.
+     canon_act8_unpack: the values that *kept stands for into out [rows][cols], fp32 or (rounded once more) bf16.
+   rows * cols up to 2^40 (else CANON_EUNSUPPORTED); an output that overlaps an input or another output returns
+   CANON_EINVAL, here and for every entry point below. */
+typedef struct {
+  int32_t group;
+  int8_t* codes;
+  float* steps;
+} canon_act8;
+int64_t canon_act8_groups(int64_t cols, int32_t group);
+canon_status canon_act8_pack(int64_t rows, int64_t cols, int32_t in_dtype, const void* x, const canon_act8* kept,
+                             void* stream);
+canon_status canon_act8_unpack(int64_t rows, int64_t cols, const canon_act8* kept, int32_t out_dtype, void* out,
+                               void* stream);
+
+/* SwiGLU (R4's rule, as inside the decoder block): gu [T][2 F], gate columns first, fp32 or bf16;
+   a (bf16 [T][F]) = bf16(RN(silu(g) u)).  kept (may be NULL): also keeps gu in 8 bits, gate and up of a token as two rows
+   of F: codes int8 [2 T][F] (the layout of gu), steps fp32 [2 T][canon_act8_groups(F, group)].
+   canon_swiglu_bwd: from da (fp32 [T][F]) and either gu (kept NULL) or what it was kept as (gu NULL; in_dtype unused), the
+   gradient dgu (bf16 [T][2 F]): du = bf16(RN(da silu(g))), dg = bf16(RN(RN(da u) dsg)), dsg = RN(sig RN(1 + RN(g RN(1 -
+   sig)))).  a (may be NULL): the activation again, of the same values (the down projection's weight gradient reads it, so
+   that the forward's need not be kept). */
+canon_status canon_swiglu(int64_t T, int64_t F, int32_t in_dtype, const void* gu, uint16_t* a, const canon_act8* kept,
+                          void* stream);
+canon_status canon_swiglu_bwd(int64_t T, int64_t F, int32_t in_dtype, const void* gu, const canon_act8* kept,
+                              const float* da, uint16_t* dgu, uint16_t* a, void* stream);
+
+/* ------------------------------------------------------------------------------------------------ */
+/* Layer norm rows (R20), x [rows][cols] fp32 or bf16; gain and bias bf16 [cols], bias may be NULL (none).  With n = cols
+   and inv = RN(1/n):
+     forward:  mean = RN(R1(x) inv), d = RN(x - mean), rstd = CRdiv(1, CRsqrt(RN(RN(R1(RN(d d)) inv) + eps))),
+               xh = RN(d rstd), y = RN(RN(xh gain) + bias) (y = RN(xh gain) without a bias), fp32 or bf16 by y_dtype.
+               mean and rstd: fp32 [rows].  kept (may be NULL): also keeps x in 8 bits, in the same pass.
+     backward: from dy (fp32 [rows][cols]), the forward's mean and rstd, and either x (kept NULL) or what it was kept as
+               (x NULL; x_dtype unused; xh is then that of the kept values): gy = RN(dy gain), m1 = RN(R1(gy) inv),
+               m2 = RN(R1(RN(gy xh)) inv), dx = RN(rstd RN(RN(gy - m1) - RN(xh m2))), fp32 [rows][cols];
+               dgain (fp32 [cols], may be NULL) = R1 over rows of RN(dy xh); dbias (fp32 [cols], may be NULL) = R1 over
+               rows of dy.  workspace: device memory of canon_layernorm_bwd_workspace_bytes(rows, cols) bytes, 256-byte
+               aligned (the chains' sums; not needed where dgain and dbias are both NULL).
+   cols up to 32768, rows up to 2^26 (else CANON_EUNSUPPORTED).  rows = 0 writes dgain and dbias as +0. */
+canon_status canon_layernorm(const canon_order* order, int64_t rows, int64_t cols, int32_t x_dtype, const void* x,
+                             const uint16_t* gain, const uint16_t* bias, float eps, int32_t y_dtype, void* y,
+                             float* mean, float* rstd, const canon_act8* kept, void* stream);
+canon_status canon_layernorm_bwd(const canon_order* order, int64_t rows, int64_t cols, int32_t x_dtype, const void* x,
+                                 const canon_act8* kept, const uint16_t* gain, const float* mean, const float* rstd,
+                                 const float* dy, float* dx, float* dgain, float* dbias, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+size_t canon_layernorm_bwd_workspace_bytes(int64_t rows, int64_t cols);
+
+/* ------------------------------------------------------------------------------------------------ */
+/* Attention rows with a learned relative position bias (R22).  Scores, probabilities and their gradients are
+   [batch][n_heads][q_len][ld], row (b, h, i) holding its k_len keys first (ld >= k_len; 0: ld = k_len; what follows them is
+   neither read nor written).  Query i of sequence b is at position pos = q_start + i (or q_starts[b] + i), key j at
+   position j.  It sees the keys j < k_len with
+     j < k_lens[b] (if given), j <= pos (if causal), |pos - j| < window (if window > 0),
+   and none if i >= q_lens[b] (if given).  q_starts, q_lens, k_lens: device int32 [batch], each may be NULL; any values.
+   Training takes q_len = k_len and q_start = 0; the next token of sequences of different lengths takes q_len = 1 and
+   q_starts = k_lens - 1.
+
+   Buckets: start[0] = 0 <= start[1] <= ... are the distances at which the n_starts buckets of one side begin; a distance
+   falls into the last bucket that begins at or before it (of equal starts only the last is ever used).  Without
+   `bidirectional` there are n_starts buckets and a key after the query counts as distance 0; with it there are 2 n_starts,
+   keys after the query taking the second half.  n_starts in [1, 128], start[n_starts - 1] <= 1024.
+   canon_relbias_log fills the record: n_buckets in all (even if bidirectional), n = those of a side; every distance below
+   n / 2 has its own, then bucket n / 2 + i begins at the first whole d with d >= (n/2) (max_distance / (n/2))^(i / (n -
+   n/2)), decided exactly.  max_distance > n / 2, at most 1024.  Host only.
+
+   table: bf16 [buckets][n_heads].  Forward: z = RN(RN(x scale) + table[bucket][h]) of the keys that are seen, m their
+   largest (0 if that is -inf), e = cexp(RN(z - m)), S = R1 over all k_len keys of e, the others as +0 terms,
+   probs (bf16) = bf16(RN(e CRdiv(1, S))), +0 for the keys that are not seen and in rows with S = 0 (no key seen, or
+   only scores of -inf).  Backward, from probs and dprobs (fp32): D = R1 over the keys of RN(p dp), ds = RN(p RN(dp - D)),
+   dscores (bf16) = bf16(RN(ds scale)), +0 for keys that are not seen; dtable (fp32 [buckets][n_heads], may be NULL) = R1
+   over the rows (b, i) of [R1 over the keys of ds, those of other buckets as +0 terms].  Whatever stands in places that are
+   not seen (infinities, NaN) is not used.
+   k_len up to 32768 and batch * n_heads * q_len up to 2^31 (else CANON_EUNSUPPORTED); window >= 0; |q_start| up to 2^30.
+   workspace: device memory of canon_softmax_relbias_bwd_workspace_bytes(rows, bias) bytes, 256-byte aligned (the rows' sums
+   per bucket; not needed where dtable is NULL). */
+#define CANON_RELBIAS_MAX_STARTS 128
+typedef struct {
+  int32_t n_starts, bidirectional;
+  int32_t start[CANON_RELBIAS_MAX_STARTS];
+} canon_relbias;
+typedef struct {
+  int64_t batch, n_heads, q_len, k_len;
+  int64_t ld, q_start, window;
+  int32_t causal;
+  float scale;
+  const int32_t *q_starts, *q_lens, *k_lens;
+} canon_attn_rows;
+canon_status canon_relbias_log(int32_t n_buckets, int32_t bidirectional, int32_t max_distance, canon_relbias* bias);
+canon_status canon_softmax_relbias(const canon_order* order, const canon_attn_rows* rows, const canon_relbias* bias,
+                                   const uint16_t* table, const float* scores, uint16_t* probs, void* stream);
+canon_status canon_softmax_relbias_bwd(const canon_order* order, const canon_attn_rows* rows, const canon_relbias* bias,
+                                       const uint16_t* probs, const float* dprobs, uint16_t* dscores, float* dtable,
+                                       void* workspace, size_t workspace_bytes, void* stream);
+size_t canon_softmax_relbias_bwd_workspace_bytes(const canon_attn_rows* rows, const canon_relbias* bias);
 
 /* Device evaluation of the R0/R4 primitives, element by element, for testing the device math against
    the oracle: op 0 add, 1 sub, 2 mul, 3 fma(a,b,c), 4 div, 5 sqrt, 6 cexp, 7 clog, 8 sigmoid, 9 silu,

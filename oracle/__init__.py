@@ -5,7 +5,7 @@ TEST INFRASTRUCTURE.  Only ``tests/``, ``__graft_entry__.smoke()`` and the
 (the GPU library and its binding) never imports it, and it never imports the
 product path; the only shared code is the seeded input generator.
 
-Thin ctypes binding over ``liboracle.so`` (plain C, ``canon_ref.c``).  Arrays
+Thin ctypes binding over ``liboracle.so`` (plain C, ``canon_ref.c`` and ``block_ref.c``).  Arrays
 are numpy; bf16 tensors are uint16 bit patterns.
 """
 from __future__ import annotations
@@ -17,7 +17,7 @@ import subprocess
 import numpy as np
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
-_SRC = os.path.join(_HERE, "canon_ref.c")
+_SRCS = [os.path.join(_HERE, "canon_ref.c"), os.path.join(_HERE, "block_ref.c")]
 _LIB = os.path.join(_HERE, "liboracle.so")
 _lib = None
 
@@ -27,7 +27,7 @@ CFLAGS = ["-O2", "-fPIC", "-shared", "-fopenmp", "-ffp-contract=off", "-fno-fast
 
 def build() -> str:
     tmp = _LIB + ".tmp"
-    subprocess.run(["gcc", *CFLAGS, "-o", tmp, _SRC, "-lm"], check=True)
+    subprocess.run(["gcc", *CFLAGS, "-o", tmp, *_SRCS, "-lm"], check=True)
     os.replace(tmp, _LIB)  # a process that has the old library loaded keeps its copy
     return _LIB
 
@@ -100,6 +100,12 @@ def _load():
             "cref_embed_bwd": (ctypes.c_int, [i64, i64, i64, vp, vp, vp]),
             "cref_inv_sqrt_int": (f, [i64]),
             "cref_swiglu": (ctypes.c_int, [i64, vp, vp, vp, vp, vp, vp]),
+            "cref_act8_pack": (ctypes.c_int, [i64, i64, i32, vp, vp, vp]),
+            "cref_act8_unpack": (ctypes.c_int, [i64, i64, i32, vp, vp, vp]),
+            "cref_layernorm_fwd": (ctypes.c_int, [i64, i64, vp, vp, vp, f, vp, vp, vp]),
+            "cref_layernorm_bwd": (ctypes.c_int, [i64, i64, vp, vp, vp, vp, vp, vp, vp, vp]),
+            "cref_relbias_fwd": (ctypes.c_int, [vp, i64, i32, vp, f, vp, vp, vp, vp, vp, vp]),
+            "cref_relbias_bwd": (ctypes.c_int, [vp, i64, i32, vp, f, vp, vp, vp, vp, vp, vp, vp]),
             "cref_num_threads": (ctypes.c_int, []),
             "cref_set_threads": (None, [ctypes.c_int]),
         }
@@ -451,3 +457,72 @@ def set_threads(n: int) -> None:
 
 def num_threads() -> int:
     return int(_load().cref_num_threads())
+
+
+def act8_pack(x: np.ndarray, group: int):
+    """R21: (codes, steps) of float32 rows; bf16 input is widened by the caller."""
+    x = np.ascontiguousarray(x, dtype=np.float32)
+    rows, cols = x.shape
+    codes, steps = np.empty((rows, cols), dtype=np.int8), np.empty((rows, -(-cols // group)), dtype=np.float32)
+    _check(_load().cref_act8_pack(rows, cols, group, _p(x), _p(codes), _p(steps)))
+    return codes, steps
+
+
+def act8_unpack(codes: np.ndarray, steps: np.ndarray, group: int) -> np.ndarray:
+    rows, cols = codes.shape
+    out = np.empty((rows, cols), dtype=np.float32)
+    _check(_load().cref_act8_unpack(rows, cols, group, _p(np.ascontiguousarray(codes)), _p(np.ascontiguousarray(steps)),
+                                    _p(out)))
+    return out
+
+
+def layernorm_fwd(x, gain, bias, eps: float):
+    """R20: (y float32, mean, rstd) of float32 rows; gain and bias (or None) as bf16 bit patterns."""
+    x = np.ascontiguousarray(x, dtype=np.float32)
+    rows, cols = x.shape
+    y, mean, rstd = np.empty((rows, cols), np.float32), np.empty(rows, np.float32), np.empty(rows, np.float32)
+    b = None if bias is None else np.ascontiguousarray(bias, dtype=np.uint16)
+    _check(_load().cref_layernorm_fwd(rows, cols, _p(x), _p(np.ascontiguousarray(gain, dtype=np.uint16)),
+                                      None if b is None else _p(b), eps, _p(y), _p(mean), _p(rstd)))
+    return y, mean, rstd
+
+
+def layernorm_bwd(x, gain, mean, rstd, dy):
+    """R20: (dx, dgain, dbias)."""
+    x, dy = np.ascontiguousarray(x, dtype=np.float32), np.ascontiguousarray(dy, dtype=np.float32)
+    rows, cols = x.shape
+    dx, dg, db = np.empty((rows, cols), np.float32), np.empty(cols, np.float32), np.empty(cols, np.float32)
+    _check(_load().cref_layernorm_bwd(rows, cols, _p(x), _p(np.ascontiguousarray(gain, dtype=np.uint16)), _p(mean),
+                                      _p(rstd), _p(dy), _p(dx), _p(dg), _p(db)))
+    return dx, dg, db
+
+
+def _relbias_args(shape, starts, bidirectional, causal, window, scale, q_starts, q_lens, k_lens):
+    b, _, q, k = shape
+    lens = [np.ascontiguousarray(np.full(b, d) if v is None else v, dtype=np.int32)
+            for v, d in ((q_starts, 0), (q_lens, q), (k_lens, k))]
+    cfg = np.array([*shape, window, int(causal)], dtype=np.int64)
+    start = np.array(starts, dtype=np.int32)
+    return (cfg, start, *lens), (_p(cfg), len(starts), int(bidirectional), _p(start), scale, *(_p(v) for v in lens))
+
+
+def relbias_fwd(scores, table, starts, bidirectional=False, causal=True, window=0, scale=1.0, q_starts=None, q_lens=None,
+                k_lens=None) -> np.ndarray:
+    """R22: probabilities (bf16 bit patterns) of float32 scores [batch][heads][q][k]; table as bf16 bit patterns."""
+    scores = np.ascontiguousarray(scores, dtype=np.float32)
+    held, args = _relbias_args(scores.shape, starts, bidirectional, causal, window, scale, q_starts, q_lens, k_lens)
+    p = np.empty(scores.shape, dtype=np.uint16)
+    _check(_load().cref_relbias_fwd(*args, _p(np.ascontiguousarray(table, dtype=np.uint16)), _p(scores), _p(p)))
+    return p
+
+
+def relbias_bwd(probs, dprobs, starts, bidirectional=False, causal=True, window=0, scale=1.0, q_starts=None, q_lens=None,
+                k_lens=None):
+    """R22: (dscores as bf16 bit patterns, dtable [buckets][heads])."""
+    probs = np.ascontiguousarray(probs, dtype=np.uint16)
+    dprobs = np.ascontiguousarray(dprobs, dtype=np.float32)
+    held, args = _relbias_args(probs.shape, starts, bidirectional, causal, window, scale, q_starts, q_lens, k_lens)
+    ds = np.empty(probs.shape, dtype=np.uint16)
+    dt = np.empty((len(starts) * (2 if bidirectional else 1), probs.shape[1]), dtype=np.float32)
+    _check(_load().cref_relbias_bwd(*args, _p(probs), _p(dprobs), _p(ds), _p(dt)))
+    return ds, dt

@@ -194,6 +194,21 @@ int cref_num_threads(void);
 /* threads of the parallel loops (each parallel loop runs over independent outputs) */
 void cref_set_threads(int n);
 
+/* ---- layer norm, activations kept in 8 bits, attention rows with a relative position bias (block_ref.c) ---- */
+int cref_act8_pack(int64_t rows, int64_t cols, int32_t group, const float* x, int8_t* codes, float* steps);
+int cref_act8_unpack(int64_t rows, int64_t cols, int32_t group, const int8_t* codes, const float* steps, float* out);
+int cref_layernorm_fwd(int64_t rows, int64_t cols, const float* x, const uint16_t* gain, const uint16_t* bias, float eps,
+                       float* y, float* mean, float* rstd);
+int cref_layernorm_bwd(int64_t rows, int64_t cols, const float* x, const uint16_t* gain, const float* mean,
+                       const float* rstd, const float* dy, float* dx, float* dgain, float* dbias);
+/* cfg: batch, heads, q_len, k_len, window, causal; q_starts, q_lens, k_lens [batch] */
+int cref_relbias_fwd(const int64_t* cfg, int64_t n_starts, int32_t bidirectional, const int32_t* start, float scale,
+                     const int32_t* q_starts, const int32_t* q_lens, const int32_t* k_lens, const uint16_t* table,
+                     const float* scores, uint16_t* probs);
+int cref_relbias_bwd(const int64_t* cfg, int64_t n_starts, int32_t bidirectional, const int32_t* start, float scale,
+                     const int32_t* q_starts, const int32_t* q_lens, const int32_t* k_lens, const uint16_t* probs,
+                     const float* dprobs, uint16_t* dscores, float* dtable);
+
 #ifdef __cplusplus
 }
 #endif

@@ -114,6 +114,18 @@ def _lib():
             "canon_embed_bwd": (i32, [vp, i64, i64, i64, vp, vp, vp, vp, sz, vp]),
             "canon_embed_bwd_workspace_bytes": (sz, [i64, i64]),
             "canon_lsq_step_grad_noalloc_max_terms": (i64, []),
+            "canon_act8_groups": (i64, [i64, i32]),
+            "canon_act8_pack": (i32, [i64, i64, i32, vp, vp, vp]),
+            "canon_act8_unpack": (i32, [i64, i64, vp, i32, vp, vp]),
+            "canon_swiglu": (i32, [i64, i64, i32, vp, vp, vp, vp]),
+            "canon_swiglu_bwd": (i32, [i64, i64, i32, vp, vp, vp, vp, vp, vp]),
+            "canon_layernorm": (i32, [vp, i64, i64, i32, vp, vp, vp, f32, i32, vp, vp, vp, vp, vp]),
+            "canon_layernorm_bwd": (i32, [vp, i64, i64, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
+            "canon_layernorm_bwd_workspace_bytes": (sz, [i64, i64]),
+            "canon_relbias_log": (i32, [i32, i32, i32, vp]),
+            "canon_softmax_relbias": (i32, [vp, vp, vp, vp, vp, vp, vp]),
+            "canon_softmax_relbias_bwd": (i32, [vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
+            "canon_softmax_relbias_bwd_workspace_bytes": (sz, [vp, vp]),
             "canon_status_str": (ctypes.c_char_p, [i32]),
             "canon_version": (i32, []),
         }
@@ -372,6 +384,184 @@ def state_hash(tensors, digest, workspace, stream=None):
 def devmath(op: str, n, a, b=None, c=None, out=None, stream=None):
     _check(_lib().canon_devmath(DEVMATH_OPS[op], n, _ptr(a), _ptr(b), _ptr(c), _ptr(out), _stream(stream)),
            "canon_devmath")
+
+
+# ---- activations kept in 8 bits, SwiGLU, layer norm, attention rows with a relative position bias ----------------
+#
+# These calls take sizes and element types from their arguments, so they check them: a tensor of another type, size or
+# device than the call needs raises ValueError and enqueues nothing.
+
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _arg(t, what, numel, *dtypes):
+    """The device address of an argument of `numel` elements (None: 0 pointer)."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes:
+        raise ValueError(f"{what}: a tensor of {' or '.join(map(str, dtypes))} is needed")
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{what}: a tensor on the current device is needed, not on {t.device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous tensor is needed")
+    if t.numel() != numel:
+        raise ValueError(f"{what}: {numel} elements are needed, not {t.numel()}")
+    return t.data_ptr()
+
+
+def _scratch(ws):
+    """(address, bytes) of a workspace; without one, none."""
+    if ws is None:
+        return None, 0
+    return _arg(ws, "workspace", ws.numel(), ws.dtype), ws.numel() * ws.element_size()
+
+
+class Act8(ctypes.Structure):
+    """A matrix [rows][cols] kept in 8 bits: codes int8 [rows, cols] and steps fp32 [rows, act8_groups(cols, group)]."""
+    _fields_ = [("group", ctypes.c_int32), ("codes", ctypes.c_void_p), ("steps", ctypes.c_void_p)]
+
+    def __init__(self, group, codes, steps):
+        super().__init__(group, codes.data_ptr(), steps.data_ptr())
+        self.tensors = codes, steps
+
+    def _of(self, rows, cols):
+        """The record's address, once its tensors are those of [rows][cols]."""
+        groups = act8_groups(cols, self.group)
+        if not groups and cols:
+            raise ValueError("group: 32, 64, 128 or 256 is needed")
+        _arg(self.tensors[0], "codes", rows * cols, torch.int8)
+        _arg(self.tensors[1], "steps", rows * groups, torch.float32)
+        return ctypes.byref(self)
+
+
+def act8_groups(cols, group) -> int:
+    return int(_lib().canon_act8_groups(cols, group))
+
+
+def act8_pack(rows, cols, x, kept: Act8, stream=None):
+    px = _arg(x, "x", rows * cols, torch.float32, torch.bfloat16)
+    _check(_lib().canon_act8_pack(rows, cols, _DTYPES[x.dtype], px, kept._of(rows, cols), _stream(stream)),
+           "canon_act8_pack")
+
+
+def act8_unpack(rows, cols, kept: Act8, out, stream=None):
+    po = _arg(out, "out", rows * cols, torch.float32, torch.bfloat16)
+    _check(_lib().canon_act8_unpack(rows, cols, kept._of(rows, cols), _DTYPES[out.dtype], po, _stream(stream)),
+           "canon_act8_unpack")
+
+
+def swiglu(T, F, gu, a, keep: Act8 | None = None, stream=None):
+    """a = silu(gate) up from gu [T, 2F]; keep: also keeps gu in 8 bits, as the matrix [2T][F]."""
+    pg = _arg(gu, "gu", 2 * T * F, torch.float32, torch.bfloat16)
+    _check(_lib().canon_swiglu(T, F, _DTYPES[gu.dtype], pg, _arg(a, "a", T * F, torch.bfloat16),
+                               None if keep is None else keep._of(2 * T, F), _stream(stream)), "canon_swiglu")
+
+
+def swiglu_bwd(T, F, gu, da, dgu, a=None, stream=None):
+    """gu: the forward's input, or the Act8 that it was kept as."""
+    kept = gu._of(2 * T, F) if isinstance(gu, Act8) else None
+    pg = None if kept else _arg(gu, "gu", 2 * T * F, torch.float32, torch.bfloat16)
+    _check(_lib().canon_swiglu_bwd(T, F, F32 if kept else _DTYPES[gu.dtype], pg, kept,
+                                   _arg(da, "da", T * F, torch.float32), _arg(dgu, "dgu", 2 * T * F, torch.bfloat16),
+                                   _arg(a, "a", T * F, torch.bfloat16), _stream(stream)), "canon_swiglu_bwd")
+
+
+def layernorm(rows, cols, x, gain, bias, eps, y, mean, rstd, keep: Act8 | None = None, order=ORDER_V1, stream=None):
+    px = _arg(x, "x", rows * cols, torch.float32, torch.bfloat16)
+    py = _arg(y, "y", rows * cols, torch.float32, torch.bfloat16)
+    _check(_lib().canon_layernorm(ctypes.byref(order), rows, cols, _DTYPES[x.dtype], px,
+                                  _arg(gain, "gain", cols, torch.bfloat16), _arg(bias, "bias", cols, torch.bfloat16), eps,
+                                  _DTYPES[y.dtype], py, _arg(mean, "mean", rows, torch.float32),
+                                  _arg(rstd, "rstd", rows, torch.float32),
+                                  None if keep is None else keep._of(rows, cols), _stream(stream)), "canon_layernorm")
+
+
+def layernorm_bwd_workspace_bytes(rows, cols) -> int:
+    return int(_lib().canon_layernorm_bwd_workspace_bytes(rows, cols))
+
+
+def layernorm_bwd(rows, cols, x, gain, mean, rstd, dy, dx, workspace=None, dgain=None, dbias=None, order=ORDER_V1,
+                  stream=None):
+    """x: the forward's input, or the Act8 that it was kept as.  workspace: needed for dgain and dbias."""
+    kept = x._of(rows, cols) if isinstance(x, Act8) else None
+    px = None if kept else _arg(x, "x", rows * cols, torch.float32, torch.bfloat16)
+    ws, ws_bytes = _scratch(workspace)
+    _check(_lib().canon_layernorm_bwd(ctypes.byref(order), rows, cols, F32 if kept else _DTYPES[x.dtype], px, kept,
+                                      _arg(gain, "gain", cols, torch.bfloat16), _arg(mean, "mean", rows, torch.float32),
+                                      _arg(rstd, "rstd", rows, torch.float32),
+                                      _arg(dy, "dy", rows * cols, torch.float32),
+                                      _arg(dx, "dx", rows * cols, torch.float32),
+                                      _arg(dgain, "dgain", cols, torch.float32),
+                                      _arg(dbias, "dbias", cols, torch.float32), ws, ws_bytes, _stream(stream)),
+           "canon_layernorm_bwd")
+
+
+RELBIAS_MAX_STARTS = 128
+
+
+class RelBias(ctypes.Structure):
+    """The buckets of a relative position bias: the distances at which those of one side begin."""
+    _fields_ = [("n_starts", ctypes.c_int32), ("bidirectional", ctypes.c_int32),
+                ("start", ctypes.c_int32 * RELBIAS_MAX_STARTS)]
+
+    def __init__(self, starts=(), bidirectional=False):
+        if len(starts) > RELBIAS_MAX_STARTS:
+            raise ValueError(f"starts: at most {RELBIAS_MAX_STARTS}")
+        super().__init__(len(starts), int(bidirectional), (ctypes.c_int32 * RELBIAS_MAX_STARTS)(*starts))
+
+    @property
+    def buckets(self) -> int:
+        return self.n_starts * (2 if self.bidirectional else 1)
+
+
+def relbias_log(n_buckets, max_distance, bidirectional=False) -> RelBias:
+    """Buckets that widen with the distance: n_buckets in all, the last of a side from about max_distance on."""
+    r = RelBias()
+    _check(_lib().canon_relbias_log(n_buckets, int(bidirectional), max_distance, ctypes.byref(r)), "canon_relbias_log")
+    return r
+
+
+class AttnRows(ctypes.Structure):
+    """The rows of attention [batch][n_heads][q_len][ld >= k_len] and the keys that each sees; q_starts, q_lens and k_lens
+    are int32 device tensors [batch] or None."""
+    _fields_ = [(n, ctypes.c_int64) for n in ("batch", "n_heads", "q_len", "k_len", "ld", "q_start", "window")] + \
+               [("causal", ctypes.c_int32), ("scale", ctypes.c_float)] + \
+               [(n, ctypes.c_void_p) for n in ("q_starts", "q_lens", "k_lens")]
+
+    def __init__(self, batch, n_heads, q_len, k_len, causal=True, window=0, scale=1.0, ld=0, q_start=0, q_starts=None,
+                 q_lens=None, k_lens=None):
+        self.tensors = q_starts, q_lens, k_lens
+        super().__init__(batch, n_heads, q_len, k_len, ld, q_start, window, int(causal), scale,
+                         *(_arg(t, w, batch, torch.int32) for t, w in zip(self.tensors, ("q_starts", "q_lens", "k_lens"))))
+
+    def _matrix(self, t, what, dtype):
+        """A matrix of these rows: all of them, `ld` apart."""
+        return _arg(t, what, self.batch * self.n_heads * self.q_len * (self.ld or self.k_len), dtype)
+
+
+def softmax_relbias(rows: AttnRows, bias: RelBias, table, scores, probs, order=ORDER_V1, stream=None):
+    """probs (bf16) of the raw scores (fp32), with table (bf16 [buckets, n_heads]) added by distance."""
+    _check(_lib().canon_softmax_relbias(ctypes.byref(order), ctypes.byref(rows), ctypes.byref(bias),
+                                        _arg(table, "table", bias.buckets * rows.n_heads, torch.bfloat16),
+                                        rows._matrix(scores, "scores", torch.float32),
+                                        rows._matrix(probs, "probs", torch.bfloat16), _stream(stream)),
+           "canon_softmax_relbias")
+
+
+def softmax_relbias_bwd_workspace_bytes(rows: AttnRows, bias: RelBias) -> int:
+    return int(_lib().canon_softmax_relbias_bwd_workspace_bytes(ctypes.byref(rows), ctypes.byref(bias)))
+
+
+def softmax_relbias_bwd(rows: AttnRows, bias: RelBias, probs, dprobs, dscores, workspace=None, dtable=None,
+                        order=ORDER_V1, stream=None):
+    """dscores (bf16) and dtable (fp32 [buckets, n_heads]); workspace: needed for dtable."""
+    ws, ws_bytes = _scratch(workspace)
+    _check(_lib().canon_softmax_relbias_bwd(ctypes.byref(order), ctypes.byref(rows), ctypes.byref(bias),
+                                            rows._matrix(probs, "probs", torch.bfloat16),
+                                            rows._matrix(dprobs, "dprobs", torch.float32),
+                                            rows._matrix(dscores, "dscores", torch.bfloat16),
+                                            _arg(dtable, "dtable", bias.buckets * rows.n_heads, torch.float32), ws, ws_bytes,
+                                            _stream(stream)), "canon_softmax_relbias_bwd")
 
 
 def version() -> int:

@@ -214,4 +214,55 @@ hipError_t lsq_scratch(float** out);
 int64_t lsq_noalloc_max_terms();
 hipError_t set_nan_if_launch(const int32_t* flag, float* x, hipStream_t s);
 
+// Activations as an operator's input: fp32, bf16, or kept in 8 bits (R21: int8 codes [rows][cols] and one fp32 step for
+// every 2^lg consecutive elements of a row, ceil(cols / 2^lg) to a row).
+enum { ACT_F32 = 0, ACT_BF16 = 1, ACT_Q8 = 2 };
+struct ActIn {
+  const void* x;
+  const float* steps;
+  int32_t src, lg;
+};
+// where to keep an activation in 8 bits; codes null: nowhere
+struct ActKeep {
+  int8_t* codes;
+  float* steps;
+  int32_t lg;
+};
+// act8.hip
+hipError_t act8_pack_launch(int64_t rows, int64_t cols, const ActIn& x, const ActKeep& k, hipStream_t s);
+hipError_t act8_unpack_launch(int64_t rows, int64_t cols, const ActIn& k, int out_bf16, void* out, hipStream_t s);
+hipError_t swiglu_keep_launch(int64_t T, int64_t F, const ActIn& gu, uint16_t* a, const ActKeep& k, hipStream_t s);
+hipError_t swiglu_grad_launch(int64_t T, int64_t F, const ActIn& gu, const float* da, uint16_t* dgu, uint16_t* a,
+                              hipStream_t s);
+// layernorm.hip
+hipError_t layernorm_fwd_launch(int64_t rows, int64_t cols, const ActIn& x, const uint16_t* gain, const uint16_t* bias,
+                                float eps, int y_bf16, void* y, float* mean, float* rstd, const ActKeep& k,
+                                hipStream_t s);
+// part: scratch of layernorm_part_floats(rows, cols) floats, unused where neither dgain nor dbias is asked for
+int64_t layernorm_part_floats(int64_t rows, int64_t cols);
+hipError_t layernorm_bwd_launch(int64_t rows, int64_t cols, const ActIn& x, const uint16_t* gain, const float* mean,
+                                const float* rstd, const float* dy, float* dx, float* dgain, float* dbias, float* part,
+                                hipStream_t s);
+// out[c] = Algorithm 2 over the ceil(rows / 32) partials part[][c] of each of cols columns (0 for no rows); with
+// inner > 0 column c goes to out[(c % inner) * (cols / inner) + c / inner]
+hipError_t column_fold_launch(int64_t rows, int64_t cols, int64_t inner, const float* part, float* out, hipStream_t s);
+// relbias.hip: attention rows with a learned relative position bias (R22)
+constexpr int kRelStarts = 128;     // buckets on one side
+constexpr int kRelFar = 1024;       // the last bucket's first distance
+constexpr int kRelShort = 32;       // a bucket of up to this many distances is summed by one lane
+struct RelBiasArgs {
+  int64_t batch, heads, q_len, k_len, ld, q_start, window;
+  const int32_t *q_starts, *q_lens, *k_lens;
+  const uint16_t* table;  // [buckets][heads]
+  float scale;
+  int32_t causal, n_side, bidirectional, n_long;
+  int32_t start[kRelStarts];
+  uint8_t longs[2 * kRelStarts];  // the buckets of more than kRelShort distances
+};
+hipError_t relbias_fwd_launch(const RelBiasArgs& a, const float* scores, uint16_t* probs, hipStream_t s);
+// rowsum: scratch of relbias_scratch_floats floats, unused where dtable is null
+int64_t relbias_scratch_floats(int64_t rows, int64_t heads, int64_t buckets);
+hipError_t relbias_bwd_launch(const RelBiasArgs& a, const uint16_t* probs, const float* dprobs, uint16_t* dscores,
+                              float* dtable, float* rowsum, hipStream_t s);
+
 }  // namespace canon

@@ -151,4 +151,25 @@ __device__ __forceinline__ float reg_row_sum(RegStage& st, const float (&e)[Q][4
   return __shfl(wave_fold(p, nc), 0, 64);
 }
 
+// The R1 sum of a row spread over a workgroup of NW wavefronts, wavefront w holding its terms 2048 w .. 2048 w + 2047:
+// 64 chunks, a complete subtree of Algorithm 2 wherever a later one follows, so the wavefronts' sums are folded by the
+// same rule.  slot: NW floats of LDS, not written again before every wavefront has passed another barrier (NW = 1: one
+// wavefront per row, no barrier).
+template <int NW>
+__device__ __forceinline__ float wide_row_sum(RegStage& st, const float (&e)[kRegQ][4], int64_t n, float* slot) {
+  if constexpr (NW == 1) {
+    return reg_row_sum(st, e, n);
+  } else {
+    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int64_t left = n - w * kRegCols;
+    float p = 0.0f;
+    if (left > 0) p = reg_row_sum(st, e, left < kRegCols ? left : kRegCols);
+    if (lane == 0) slot[w] = p;
+    __syncthreads();
+    const int parts = (int)((n + kRegCols - 1) / kRegCols);
+    p = lane < parts ? slot[lane] : 0.0f;
+    return __shfl(wave_fold(p, parts), 0, 64);
+  }
+}
+
 }  // namespace canon

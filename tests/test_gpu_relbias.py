@@ -1,0 +1,278 @@
+"""canon_softmax_relbias and its backward: bit-identical to the oracle over lengths, masks and bucket schemes, rows without
+keys, junk in masked places, and near the formula in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import paper_2609_17380_amd.canon as C
+import paper_2609_17380_amd.inputs as I
+from gpu_util import DEV, assert_bits, dev_bf16, dev_f32, dev_i32, host_f32, host_u16, poisoned_workspace
+from test_gpu_layernorm import host_bf16, off, sum_error
+
+pytestmark = pytest.mark.gpu
+
+LOG32 = list(C.relbias_log(32, 128).start)[:32]
+LOG16 = list(C.relbias_log(32, 128, True).start)[:16]
+FAR = list(C.relbias_log(8, 1024).start)[:8]         # wide buckets, summed chunk by chunk
+WIDE = [0, 1, 33, 66, 200, 1000]
+EQUAL = [0, 0, 3, 3, 3, 10]                          # buckets that begin together
+
+
+def seen_mask(B, Q, K, causal, window, q_starts, q_lens, k_lens):
+    pos = np.arange(Q)[None, :, None] + (np.zeros(B) if q_starts is None else np.asarray(q_starts))[:, None, None]
+    j = np.arange(K)[None, None, :]
+    m = np.broadcast_to(j < (np.full(B, K) if k_lens is None else np.asarray(k_lens))[:, None, None], (B, Q, K)).copy()
+    m &= np.arange(Q)[None, :, None] < (np.full(B, Q) if q_lens is None else np.asarray(q_lens))[:, None, None]
+    if causal:
+        m &= j <= pos
+    if window:
+        m &= np.abs(pos - j) < window
+    return m[:, None]
+
+
+def case_inputs(B, H, Q, K, starts, bidirectional, seed=0):
+    nb = len(starts) * (2 if bidirectional else 1)
+    return (I.normal_f32((B, H, Q, K), seed, 11) * np.float32(8), I.normal_bf16((nb, H), seed, 12),
+            I.normal_f32((B, H, Q, K), seed, 13))
+
+
+def lay(a, ld, fill):
+    """[B, H, Q, K] into rows ld apart, off any alignment, the rest `fill`."""
+    if ld and ld > a.shape[-1]:
+        b = np.full(a.shape[:-1] + (ld,), fill, dtype=a.dtype)
+        b[..., :a.shape[-1]] = a
+        a = b
+    return a
+
+
+def run(B, H, Q, K, starts, bidirectional, scores, table, dprobs, probs=None, ld=0, scale=0.125, **masks):
+    dev = {k: (dev_i32(np.asarray(v)) if k in ("q_starts", "q_lens", "k_lens") and v is not None else v) for k, v in masks.items()}
+    rows = C.AttnRows(B, H, Q, K, scale=scale, ld=ld, **dev)
+    bias = C.RelBias(starts, bidirectional)
+    full = (B, H, Q, ld or K)
+    p = off(torch.full(full, 7.0, dtype=torch.bfloat16, device=DEV))
+    C.softmax_relbias(rows, bias, off(dev_bf16(table)), off(dev_f32(lay(scores, ld, np.nan))), p)
+    torch.cuda.synchronize()
+    got_p = host_u16(p)
+    if probs is not None:
+        p = off(dev_bf16(lay(probs, ld, 0x7FC0)))
+    ds = off(torch.full(full, 7.0, dtype=torch.bfloat16, device=DEV))
+    dt = off(torch.full((bias.buckets, H), float("nan"), dtype=torch.float32, device=DEV))
+    ws = poisoned_workspace(C.softmax_relbias_bwd_workspace_bytes(rows, bias))
+    C.softmax_relbias_bwd(rows, bias, p, off(dev_f32(lay(dprobs, ld, np.nan))), ds, ws, dtable=dt)
+    torch.cuda.synchronize()
+    got_ds = host_u16(ds)
+    if ld and ld > K:  # what lies behind the keys is left as it was
+        assert (got_p[..., K:] == 0x40E0).all() and (got_ds[..., K:] == 0x40E0).all()
+    return np.ascontiguousarray(got_p[..., :K]), np.ascontiguousarray(got_ds[..., :K]), host_f32(dt)
+
+
+def check(B, H, Q, K, starts, bidirectional, seed=0, ld=0, **masks):
+    print(f"relbias {B}x{H}x{Q}x{K} {len(starts)} starts bidirectional={bidirectional} ld={ld} {masks}", flush=True)
+    scores, table, dprobs = case_inputs(B, H, Q, K, starts, bidirectional, seed)
+    want_p = oracle.relbias_fwd(scores, table, starts, bidirectional, scale=0.125, **masks)
+    want_ds, want_dt = oracle.relbias_bwd(want_p, dprobs, starts, bidirectional, scale=0.125, **masks)
+    # junk where nothing is seen: none of it may show
+    hidden = ~np.broadcast_to(seen_mask(B, Q, K, masks.get("causal", True), masks.get("window", 0), masks.get("q_starts"),
+                                        masks.get("q_lens"), masks.get("k_lens")), scores.shape)
+    junk = np.array([np.nan, np.inf, -np.inf, np.finfo(np.float32).min], np.float32)
+    scores = np.where(hidden, junk[np.arange(scores.size).reshape(scores.shape) % 4], scores)
+    dprobs = np.where(hidden, junk[np.arange(scores.size).reshape(scores.shape) % 3], dprobs)
+    probs = np.where(hidden, np.uint16(0x7FC0), want_p)
+    p, ds, dt = run(B, H, Q, K, starts, bidirectional, scores, table, dprobs, probs=probs, ld=ld, **masks)
+    assert_bits(p, want_p, "probs")
+    assert_bits(ds, want_ds, "dscores")
+    assert_bits(dt, want_dt, "dtable")
+    assert not p[hidden].any() and not (ds[hidden] & 0x7FFF).any()
+
+
+@pytest.mark.parametrize("s", [1, 2, 3, 31, 33, 64, 255, 257, 300])
+@pytest.mark.parametrize("starts,bidirectional,causal,window",
+                         [(LOG32, False, True, 0), (LOG16, True, False, 0), (LOG16, True, False, 20), (LOG32, False, True, 40),
+                          (LOG32, False, False, 0), (LOG16, True, True, 0), (WIDE, True, False, 0), (EQUAL, True, False, 0),
+                          (EQUAL, False, False, 0), ([0], False, True, 0), ([0, 0], True, False, 1)])
+def test_square_rows(s, starts, bidirectional, causal, window):
+    check(2, 3, s, s, starts, bidirectional, causal=causal, window=window)
+
+
+@pytest.mark.parametrize("q,k", [(5, 2047), (5, 2048), (3, 2049), (6, 2052), (2, 4095), (3, 4096), (2, 4097), (2, 8192), (1, 8197),
+                                 (2, 16384), (1, 16390), (1, 32768), (5, 32767)])
+@pytest.mark.parametrize("starts,bidirectional", [(LOG32, False), (FAR, True)])
+def test_long_rows(q, k, starts, bidirectional):
+    check(1, 2, q, k, starts, bidirectional, causal=not bidirectional, q_starts=[k - q])
+    check(1, 1, q, k, starts, bidirectional, causal=False, q_starts=[k // 2], window=k // 3)
+
+
+def test_padded_batch_with_empty_sequences():
+    lens = [70, 0, 1, 33]
+    for starts, bidirectional in ((LOG32, False), (LOG16, True)):
+        check(4, 2, 70, 70, starts, bidirectional, causal=not bidirectional, q_lens=lens, k_lens=lens)
+    check(4, 2, 60, 2500, LOG16, True, causal=False, q_lens=[60, 0, 1, 5], k_lens=[2500, 2500, 0, 2049])
+
+
+def test_lengths_outside_the_rows():
+    # any values: longer than the rows, negative, positions far off
+    check(5, 1, 9, 40, LOG16, True, causal=False, k_lens=[41, -3, 2 ** 31 - 1, -2 ** 31, 40], q_lens=[9, 9, 100, 9, -1])
+    check(5, 1, 9, 40, LOG32, False, causal=True, q_starts=[-5, -2 ** 31, 2 ** 31 - 1, 39, 35])
+    check(4, 1, 9, 40, LOG16, True, causal=False, window=2 ** 31 - 100, q_starts=[2 ** 31 - 1, -2 ** 31, 0, 100])
+
+
+@pytest.mark.parametrize("k", [1, 40, 2500])
+def test_the_next_token(k):
+    lens = np.array([k, max(1, k // 2), 1, max(1, k - 1)])
+    check(4, 4, 1, k, LOG32, False, causal=True, q_starts=lens - 1, k_lens=lens)
+    check(4, 4, 1, k, LOG32, False, causal=True, window=17, q_starts=lens - 1, k_lens=lens)
+
+
+@pytest.mark.parametrize("ld", [301, 304, 512])
+def test_rows_apart(ld):
+    check(2, 2, 65, 300, LOG32, False, ld=ld)
+    check(1, 2, 3, 300, LOG16, True, ld=ld, causal=False)
+
+
+def test_many_rows_of_a_bucket():
+    # around the chains of 32 rows and the fold's blocks
+    for b, q in ((1, 33), (3, 31), (2, 600), (40, 1)):
+        check(b, 2, q, 50, LOG32, False, causal=False, q_starts=list(range(b)))
+
+
+def test_scores_of_minus_infinity():
+    # all of a row's seen scores at -inf, or at the type's lowest value; a NaN among them
+    B, H, Q, K = 1, 1, 6, 70
+    scores, table, dprobs = case_inputs(B, H, Q, K, LOG32, False)
+    scores[0, 0, 0, :] = -np.inf
+    scores[0, 0, 1, :] = np.finfo(np.float32).min
+    scores[0, 0, 2, :] = -np.inf
+    scores[0, 0, 2, 3] = np.nan
+    scores[0, 0, 3, :40] = -np.inf
+    scores[0, 0, 4, 9] = np.inf
+    p, ds, dt = run(B, H, Q, K, LOG32, False, scores, table, dprobs, scale=1.0, causal=False)
+    v = I.bf16_bits_to_f32(p)[0, 0]
+    assert not v[0].any() and not (ds[0, 0, 0] & 0x7FFF).any()  # p = +0 times a negative number is -0
+    assert np.isfinite(v[1]).all() and abs(v[1].astype(np.float64).sum() - 1) < 2.0 ** -8
+    assert np.isnan(v[2]).all() and np.isnan(v[4]).all()
+    assert not v[3, :40].any() and v[3, 40:].any()
+    assert_bits(p[:, :, [0, 1, 3, 5]], oracle.relbias_fwd(scores, table, LOG32, False, causal=False, scale=1.0)[:, :, [0, 1, 3, 5]], "probs")
+
+
+@pytest.mark.parametrize("bidirectional", [False, True])
+def test_near_the_formula_in_64_bits(bidirectional):
+    B, H, Q, K = 2, 2, 150, 150
+    starts = LOG16
+    scores, table, dprobs = case_inputs(B, H, Q, K, starts, bidirectional, seed=5)
+    scores *= np.float32(0.25)
+    lens = [150, 90]
+    p, _, _ = run(B, H, Q, K, starts, bidirectional, scores, table, dprobs, causal=not bidirectional, q_lens=lens, k_lens=lens)
+    seen = np.broadcast_to(seen_mask(B, Q, K, not bidirectional, 0, None, lens, lens), scores.shape)
+    rel = np.arange(K)[None, :] - np.arange(Q)[:, None]
+    d = np.abs(rel) if bidirectional else np.maximum(-rel, 0)
+    which = np.searchsorted(starts, d, side="right") - 1 + (len(starts) * (rel > 0) if bidirectional else 0)
+    T = I.bf16_bits_to_f32(table).astype(np.float64)
+    z = scores.astype(np.float64) * 0.125 + T[which].transpose(2, 0, 1)[None]
+    z = np.where(seen, z, -np.inf)
+    with np.errstate(invalid="ignore"):
+        e = np.exp(z - np.where(seen.any(-1, keepdims=True), z.max(-1, keepdims=True), 0))
+    total = e.sum(-1, keepdims=True)
+    want = e / np.where(total == 0, 1, total)
+    # z and z - m are off by half a unit of the largest of them (below 16: 2^-20 each), e by those and 3 units of 2^-23 of
+    # the exponential, their sum by its own; then the bf16 rounding
+    top = np.abs(z[seen]).max()
+    tol = 4 * top * 2.0 ** -23 + 6 * 2.0 ** -23 + 2 * sum_error(K)
+    got = I.bf16_bits_to_f32(p).astype(np.float64)
+    assert np.all(np.abs(got - want) <= want * (tol + 2.0 ** -8) + 2.0 ** -126)
+    # the backward from the probabilities as they were stored
+    _, ds, dt = run(B, H, Q, K, starts, bidirectional, scores, table, dprobs, probs=p, causal=not bidirectional, q_lens=lens, k_lens=lens)
+    dp = dprobs.astype(np.float64)
+    D = (got * dp).sum(-1, keepdims=True)
+    w = got * (dp - D)
+    tol_d = (sum_error(K) + 2.0 ** -24) * np.abs(got * dp).sum(-1, keepdims=True)
+    err = got * (tol_d + 2.0 ** -24 * (np.abs(dp) + np.abs(D))) + 2.0 ** -24 * np.abs(w) * 1.01
+    assert np.all(np.abs(I.bf16_bits_to_f32(ds) - w * 0.125) <= np.abs(w) * 0.125 * (2.0 ** -8) * 1.01 + err * 0.125 * 1.01)
+    for n in range(len(T)):
+        inside = seen & (which == n)[None, None]
+        wt = np.where(inside, w, 0).sum((0, 2, 3))
+        # two sums, of keys and of rows
+        lim = np.where(inside, err, 0).sum((0, 2, 3)) + (sum_error(K) + sum_error(B * Q)) * np.where(inside, np.abs(w), 0).sum((0, 2, 3))
+        assert np.all(np.abs(dt[n] - wt) <= lim * 1.01)
+
+
+def test_table_gradient_against_differences():
+    # d loss / d table by central differences in 64 bits of the loss sum(w softmax): the bf16 probabilities that the
+    # backward reads are 2^-9 off, so its gradient is up to 2^-8 of the magnitudes that it sums away from them
+    B, H, Q, K = 1, 1, 40, 40
+    starts = LOG16
+    scores, table, dprobs = case_inputs(B, H, Q, K, starts, False, seed=6)
+    _, _, dt = run(B, H, Q, K, starts, False, scores, table, dprobs, causal=True)
+    rel = np.arange(K)[None, :] - np.arange(Q)[:, None]
+    which = np.searchsorted(starts, np.maximum(-rel, 0), side="right") - 1
+    T = I.bf16_bits_to_f32(table).astype(np.float64)[:, 0]
+
+    def probs(t):
+        z = np.where(rel <= 0, scores[0, 0].astype(np.float64) * 0.125 + t[which], -np.inf)
+        e = np.exp(z - z.max(-1, keepdims=True))
+        return e / e.sum(-1, keepdims=True)
+
+    W = dprobs[0, 0].astype(np.float64)
+    P = probs(T)
+    mags = P * (np.abs(W) + (P * np.abs(W)).sum(-1, keepdims=True))
+    for n in range(len(starts)):
+        h = np.zeros(len(starts))
+        h[n] = 1e-5
+        want = ((probs(T + h) - probs(T - h)) * W).sum() / 2e-5
+        assert abs(dt[n, 0] - want) <= 2.0 ** -8 * mags[(which == n) & (rel <= 0)].sum() + 1e-6
+
+
+def test_without_the_table_gradient():
+    B, H, Q, K = 2, 2, 5, 2500  # rows of two wavefronts, several to a workgroup
+    scores, table, dprobs = case_inputs(B, H, Q, K, LOG32, False, seed=7)
+    p = oracle.relbias_fwd(scores, table, LOG32, False, scale=0.125, q_starts=[2490] * 2)
+    want, _ = oracle.relbias_bwd(p, dprobs, LOG32, False, scale=0.125, q_starts=[2490] * 2)
+    rows = C.AttnRows(B, H, Q, K, scale=0.125, q_start=2490)
+    ds = torch.empty((B, H, Q, K), dtype=torch.bfloat16, device=DEV)
+    C.softmax_relbias_bwd(rows, C.RelBias(LOG32), dev_bf16(p), dev_f32(dprobs), ds)
+    torch.cuda.synchronize()
+    assert_bits(host_u16(ds), want, "dscores")
+
+
+def test_no_rows_and_no_keys():
+    bias = C.RelBias(LOG32)
+    for shape in ((0, 2, 5, 5), (2, 2, 0, 5), (2, 2, 5, 0)):
+        rows = C.AttnRows(*shape)
+        z = torch.empty(0, dtype=torch.float32, device=DEV)
+        zb = torch.empty(0, dtype=torch.bfloat16, device=DEV)
+        dt = torch.full((32, 2), float("nan"), device=DEV)
+        C.softmax_relbias(rows, bias, torch.zeros((32, 2), dtype=torch.bfloat16, device=DEV), z, zb)
+        C.softmax_relbias_bwd(rows, bias, zb, z, zb, poisoned_workspace(C.softmax_relbias_bwd_workspace_bytes(rows, bias)), dtable=dt)
+        torch.cuda.synchronize()
+        assert not host_f32(dt).view(np.uint32).any()
+
+
+def test_captured_with_an_eager_call_between():
+    B, H, Q, K = 2, 2, 100, 100
+    scores, table, dprobs = case_inputs(B, H, Q, K, LOG32, False, seed=8)
+    want_p = oracle.relbias_fwd(scores, table, LOG32, False, scale=0.125)
+    want_ds, want_dt = oracle.relbias_bwd(want_p, dprobs, LOG32, False, scale=0.125)
+    rows, bias = C.AttnRows(B, H, Q, K, scale=0.125), C.RelBias(LOG32)
+    x, t, dp = torch.zeros((B, H, Q, K), device=DEV), dev_bf16(table), dev_f32(dprobs)
+    p, ds = (torch.empty((B, H, Q, K), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    dt = torch.empty((32, H), device=DEV)
+    ws = poisoned_workspace(C.softmax_relbias_bwd_workspace_bytes(rows, bias))
+
+    def both():
+        C.softmax_relbias(rows, bias, t, x, p)
+        C.softmax_relbias_bwd(rows, bias, p, dp, ds, ws, dtable=dt)
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    for _ in range(3):
+        x.zero_()
+        both()
+        x.copy_(dev_f32(scores))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert_bits(host_u16(p), want_p, "probs")
+        assert_bits(host_u16(ds), want_ds, "dscores")
+        assert_bits(host_f32(dt), want_dt, "dtable")
