@@ -161,8 +161,9 @@ def _ptrs(ts):
 def _stream(stream=None) -> int:
     if isinstance(stream, int):  # a raw hipStream_t (0: the null stream)
         return stream
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return s.cuda_stream
+    if stream is None:  # the current stream's handle, without a Stream object around it
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return stream.cuda_stream
 
 
 # ---- entry points (same names as the C ABI, without the prefix) -------------------------------------
@@ -395,17 +396,15 @@ _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 
 
 def _arg(t, what, numel, *dtypes):
-    """The device address of an argument of `numel` elements (None: 0 pointer)."""
+    """The device address of an argument of `numel` elements (None: no pointer)."""
     if t is None:
         return None
     if not isinstance(t, torch.Tensor) or t.dtype not in dtypes:
         raise ValueError(f"{what}: a tensor of {' or '.join(map(str, dtypes))} is needed")
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+    if t.get_device() < 0 or t.get_device() != torch._C._cuda_getDevice():
         raise ValueError(f"{what}: a tensor on the current device is needed, not on {t.device}")
-    if not t.is_contiguous():
-        raise ValueError(f"{what}: a contiguous tensor is needed")
-    if t.numel() != numel:
-        raise ValueError(f"{what}: {numel} elements are needed, not {t.numel()}")
+    if t.numel() != numel or not t.is_contiguous():
+        raise ValueError(f"{what}: {numel} elements are needed, contiguous, not {tuple(t.shape)} of strides {t.stride()}")
     return t.data_ptr()
 
 

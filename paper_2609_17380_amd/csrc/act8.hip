@@ -58,10 +58,7 @@ __global__ __launch_bounds__(256) void act8_unpack_kernel(int64_t rows, int64_t 
       const int64_t j = j0 + 256 * q;
       if (j >= cols) continue;
       if (BF16) {
-        uint16_t h[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) h[t] = f32_to_bf16(v[q][t]);
-        stb4<TAIL>((uint16_t*)out + row * cols, j, cols, h);
+        stb4_arith<TAIL>((uint16_t*)out + row * cols, j, cols, v[q]);
       } else {
         stf4<TAIL>((float*)out + row * cols, j, cols, v[q]);
       }
@@ -100,13 +97,13 @@ __global__ __launch_bounds__(256) void swiglu_keep_kernel(int64_t T, int64_t F, 
         keep4<TAIL>(u[q], j, F, k.lg, k.codes + (2 * t + 1) * F, k.steps + (2 * t + 1) * groups);
       }
       if (j >= F) continue;
-      uint16_t h[4];
+      float h[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float sl = csilu(g[q][i]);
-        h[i] = f32_to_bf16(sl * u[q][i]);
+        h[i] = sl * u[q][i];
       }
-      stb4<TAIL>(a + t * F, j, F, h);
+      stb4_arith<TAIL>(a + t * F, j, F, h);
     }
   }
 }
@@ -134,7 +131,7 @@ __global__ __launch_bounds__(256) void swiglu_grad_kernel(int64_t T, int64_t F, 
     for (int q = 0; q < kGluQ; ++q) {
       const int64_t j = j0 + 256 * q;
       if (j >= F) continue;
-      uint16_t hg[4], hu[4], ha[4];
+      float hg[4], hu[4], ha[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float sig = csigmoid(g[q][i]);
@@ -144,13 +141,13 @@ __global__ __launch_bounds__(256) void swiglu_grad_kernel(int64_t T, int64_t F, 
         const float ops = 1.0f + gs;
         const float dsg = sig * ops;
         const float du = d[q][i] * u[q][i];
-        hg[i] = f32_to_bf16(du * dsg);
-        hu[i] = f32_to_bf16(d[q][i] * sl);
-        ha[i] = f32_to_bf16(sl * u[q][i]);
+        hg[i] = du * dsg;
+        hu[i] = d[q][i] * sl;
+        ha[i] = sl * u[q][i];
       }
-      stb4<TAIL>(dgu + 2 * t * F, j, F, hg);
-      stb4<TAIL>(dgu + (2 * t + 1) * F, j, F, hu);
-      if (a) stb4<TAIL>(a + t * F, j, F, ha);
+      stb4_arith<TAIL>(dgu + 2 * t * F, j, F, hg);
+      stb4_arith<TAIL>(dgu + (2 * t + 1) * F, j, F, hu);
+      if (a) stb4_arith<TAIL>(a + t * F, j, F, ha);
     }
   }
 }

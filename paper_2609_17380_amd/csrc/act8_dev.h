@@ -15,42 +15,70 @@ struct __attribute__((packed, aligned(1))) B4 {
   uint32_t x;
 };
 
-// the largest of m over each aligned set of `lanes` lanes (a power of two from 8 to 64)
-__device__ __forceinline__ uint32_t lanes_max(uint32_t m, int lanes) {
-#pragma unroll
-  for (int s = 1; s < 64; s <<= 1) {
-    if (s >= lanes) break;
-    const uint32_t o = __shfl_xor(m, s, 64);
-    m = o > m ? o : m;
-  }
-  return m;
-}
-
 // Elements j .. j + 3 of a row of n (j a multiple of 4 whose lanes run through whole groups; v holds 0 beyond n) into
 // codes and their group's step.  Every lane of the wavefront takes part.  The magnitudes are compared as bit patterns,
 // so that a NaN ranks above every number.
-template <bool TAIL>
-__device__ __forceinline__ void keep4(const float (&v)[4], int64_t j, int64_t n, int lg, int8_t* codes, float* steps) {
+__device__ __forceinline__ uint32_t codes4(const float (&v)[4], int lg, float& s) {
   uint32_t m = 0;
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
     const uint32_t a = __float_as_uint(v[t]) & 0x7FFFFFFFu;
     m = a > m ? a : m;
   }
-  m = lanes_max(m, 1 << (lg - 2));
-  const float s = __uint_as_float(m) * __uint_as_float(kInv127Bits);
+  m = lanes_join(m, 1 << (lg - 2), [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+  s = __uint_as_float(m) * __uint_as_float(kInv127Bits);
   const bool recip = recip_step_ok(s);
   const float rs = recip ? 1.0f / s : 0.0f;
   uint32_t w[1];
   quant_pack<4>(v, s, rs, recip, w);
+  return w[0];
+}
+template <bool TAIL>
+__device__ __forceinline__ void keep4(const float (&v)[4], int64_t j, int64_t n, int lg, int8_t* codes, float* steps) {
+  float s;
+  const uint32_t w = codes4(v, lg, s);
   if (j >= n) return;
   if ((j & ((1 << lg) - 1)) == 0) steps[j >> lg] = s;
   if (!TAIL || j + 4 <= n) {
-    reinterpret_cast<B4*>(codes + j)->x = w[0];
+    reinterpret_cast<B4*>(codes + j)->x = w;
   } else {
 #pragma unroll
     for (int t = 0; t < 4; ++t)
-      if (j + t < n) codes[j + t] = (int8_t)(w[0] >> (8 * t));
+      if (j + t < n) codes[j + t] = (int8_t)(w >> (8 * t));
+  }
+}
+// the same of a part of a row (part_load): v holds 0 beyond n
+template <bool TAIL>
+__device__ __forceinline__ void part_keep(const float (&v)[kRegQ][4], int n, int lg, int8_t* codes, float* steps) {
+  const int at = 4 * (threadIdx.x & 63);
+  const int mine = TAIL && (n & 3) && n > 0 && at == (n & 252) ? n >> 8 : -1;
+  uint32_t cut = 0;
+#pragma unroll
+  for (int q = 0; q < kRegQ; ++q) {
+    if (256 * q >= n) break;
+    const int j = 256 * q + at;
+    float s;
+    const uint32_t w = codes4(v[q], lg, s);
+    if (j < n && (j & ((1 << lg) - 1)) == 0) steps[j >> lg] = s;
+    if (j + 4 <= n) reinterpret_cast<B4*>(codes + j)->x = w;
+    cut = q == mine ? w : cut;
+  }
+  if (mine >= 0) {
+#pragma unroll
+    for (int t = 0; t < 3; ++t)
+      if (t < (n & 3)) codes[(n & ~3) + t] = (int8_t)(cut >> (8 * t));
+  }
+}
+
+// results of arithmetic to bf16, elements j .. j + 3 of a row of n
+template <bool TAIL>
+__device__ __forceinline__ void stb4_arith(uint16_t* row, int64_t j, int64_t n, const float (&f)[4]) {
+  if (!TAIL || j + 4 <= n) {
+    stb_arith(row + j, f);
+  } else {
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+      if (j + t < n) row[j + t] = bf16_arith(f[t]);
   }
 }
 
@@ -69,12 +97,56 @@ __device__ __forceinline__ void kept4(const int8_t* codes, const float* steps, i
   }
 }
 
-// four elements of row `row` of an activation: fp32, bf16 or kept in 8 bits
+// elements j .. j + 3 of row `row` of an activation (fp32, bf16 or kept in 8 bits), for arithmetic
 template <int SRC, bool TAIL>
 __device__ __forceinline__ void act4(const ActIn& a, int64_t row, int64_t j, int64_t n, float (&f)[4]) {
   if constexpr (SRC == ACT_F32) ldf4<TAIL>((const float*)a.x + row * n, j, n, f);
-  else if constexpr (SRC == ACT_BF16) ldb4<TAIL>((const uint16_t*)a.x + row * n, j, n, f);
+  else if constexpr (SRC == ACT_BF16) {
+    const uint16_t* p = (const uint16_t*)a.x + row * n + j;
+    if (!TAIL || j + 4 <= n) {
+      ldb_wide(p, f);
+    } else {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) f[t] = j + t < n ? bf16_wide(p[t]) : 0.0f;
+    }
+  }
   else kept4<TAIL>((const int8_t*)a.x + row * n, a.steps + row * ((n + (1 << a.lg) - 1) >> a.lg), j, n, a.lg, f);
 }
+
+// a part of a row of an activation, from element `seg` (a multiple of 256) on
+template <int SRC>
+struct PartIn {
+  const void* p;
+  const float* steps;
+  int lg;
+  __device__ __forceinline__ PartIn(const ActIn& a, int64_t row, int64_t cols, int seg) {
+    const int64_t at = row * cols + seg;
+    lg = a.lg;
+    steps = nullptr;
+    if constexpr (SRC == ACT_F32) p = (const float*)a.x + at;
+    else if constexpr (SRC == ACT_BF16) p = (const uint16_t*)a.x + at;
+    else {
+      p = (const int8_t*)a.x + at;
+      steps = a.steps + row * ((cols + (1 << lg) - 1) >> lg) + (seg >> lg);
+    }
+  }
+  __device__ __forceinline__ void load4(int j, float (&f)[4]) const {
+    if constexpr (SRC == ACT_F32) {
+      ldf<4>((const float*)p + j, f);
+    } else if constexpr (SRC == ACT_BF16) {
+      ldb_wide((const uint16_t*)p + j, f);
+    } else {
+      const float s = steps[j >> lg];
+      const uint32_t w = reinterpret_cast<const B4*>((const int8_t*)p + j)->x;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) f[t] = (float)(int8_t)(w >> (8 * t)) * s;
+    }
+  }
+  __device__ __forceinline__ float load1(int j) const {
+    if constexpr (SRC == ACT_F32) return ((const float*)p)[j];
+    else if constexpr (SRC == ACT_BF16) return bf16_wide(((const uint16_t*)p)[j]);
+    else return (float)((const int8_t*)p)[j] * steps[j >> lg];
+  }
+};
 
 }  // namespace canon

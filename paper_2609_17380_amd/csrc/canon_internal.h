@@ -244,8 +244,10 @@ hipError_t layernorm_bwd_launch(int64_t rows, int64_t cols, const ActIn& x, cons
                                 const float* rstd, const float* dy, float* dx, float* dgain, float* dbias, float* part,
                                 hipStream_t s);
 // out[c] = Algorithm 2 over the ceil(rows / 32) partials part[][c] of each of cols columns (0 for no rows); with
-// inner > 0 column c goes to out[(c % inner) * (cols / inner) + c / inner]
-hipError_t column_fold_launch(int64_t rows, int64_t cols, int64_t inner, const float* part, float* out, hipStream_t s);
+// inner > 0 column c goes to out[(c % inner) * (cols / inner) + c / inner].  out1: the same of a second set of partials that
+// follows the first; either may be null.
+hipError_t column_fold_launch(int64_t rows, int64_t cols, int64_t inner, const float* part, float* out, float* out1,
+                              hipStream_t s);
 // relbias.hip: attention rows with a learned relative position bias (R22)
 constexpr int kRelStarts = 128;     // buckets on one side
 constexpr int kRelFar = 1024;       // the last bucket's first distance

@@ -16,116 +16,117 @@ namespace canon {
 
 namespace {
 
-template <int SRC, int NW, bool TAIL>
-__global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void layernorm_fwd_kernel(
-    int64_t rows, int64_t cols, ActIn x, const uint16_t* __restrict__ gain, const uint16_t* __restrict__ bias, float eps,
+template <int SRC, int NW, bool TAIL, bool KEEP>
+__global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, NW == 1 ? 4 : 1) void layernorm_fwd_kernel(
+    int64_t rows, int cols, ActIn x, const uint16_t* __restrict__ gain, const uint16_t* __restrict__ bias, float eps,
     float inv_d, int y_bf16, void* __restrict__ y, float* __restrict__ mean, float* __restrict__ rstd, ActKeep k) {
   constexpr int kRows = NW == 1 ? 4 : 1;  // rows of a workgroup
   __shared__ __attribute__((aligned(16))) RegStage st[NW == 1 ? 4 : NW];
   __shared__ float slot[2][NW];
-  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t c0 = NW == 1 ? 4 * lane : w * kRegCols + 4 * lane;  // this lane's first column
+  const int w = wave_id(), lane = threadIdx.x & 63;
+  const int seg = NW == 1 ? 0 : w * (int)kRegCols;  // this wavefront's part of the row
+  const int n = cols - seg < (int)kRegCols ? cols - seg : (int)kRegCols;
   for (int64_t row = (int64_t)blockIdx.x * kRows + (NW == 1 ? w : 0); row < rows; row += (int64_t)gridDim.x * kRows) {
+    const PartIn<SRC> in(x, row, cols, seg);
     float xv[kRegQ][4];
-#pragma unroll
-    for (int q = 0; q < kRegQ; ++q) {
-#pragma unroll
-      for (int t = 0; t < 4; ++t) xv[q][t] = 0.0f;
-      if (c0 + 256 * q < cols) act4<SRC, TAIL>(x, row, c0 + 256 * q, cols, xv[q]);
-    }
+    part_load<TAIL>(n, xv, [&](int j, float(&v)[4]) { in.load4(j, v); }, [&](int j) { return in.load1(j); });
     const float sum = wide_row_sum<NW>(st[w], xv, cols, slot[0]);
     const float mu = sum * inv_d;
-    float sq[kRegQ][4];
+    float sq[kRegQ][4];  // what lies behind the row's end is not read by the chains
 #pragma unroll
     for (int q = 0; q < kRegQ; ++q)
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         const float d = xv[q][t] - mu;
-        sq[q][t] = !TAIL || c0 + 256 * q + t < cols ? d * d : 0.0f;  // terms past the end are not read by the chains
+        sq[q][t] = d * d;
       }
     const float ss = wide_row_sum<NW>(st[w], sq, cols, slot[1]);
     const float var = ss * inv_d;
     const float v = var + eps;
     const float r = 1.0f / __builtin_sqrtf(v);
-    if (lane == 0 && (NW == 1 || w == 0)) {
+    if (lane == 0 && seg == 0) {
       mean[row] = mu;
       rstd[row] = r;
     }
+    if (KEEP)
+      part_keep<TAIL>(xv, n, k.lg, k.codes + row * cols + seg,
+                      k.steps + row * ((cols + (1 << k.lg) - 1) >> k.lg) + (seg >> k.lg));
+    uint16_t* yh = (uint16_t*)y + row * cols + seg;
+    float* yf = (float*)y + row * cols + seg;
+    part_store<TAIL>(n,
+                     [&](int q, float(&o)[4]) {
 #pragma unroll
-    for (int q = 0; q < kRegQ; ++q) {
-      const int64_t j = c0 + 256 * q;
-      if (k.codes)
-        keep4<TAIL>(xv[q], j, cols, k.lg, k.codes + row * cols, k.steps + row * ((cols + (1 << k.lg) - 1) >> k.lg));
-      if (j >= cols) continue;
-      float gv[4], bv[4] = {0.0f, 0.0f, 0.0f, 0.0f}, o[4];
-      ldb4<TAIL>(gain, j, cols, gv);
-      if (bias) ldb4<TAIL>(bias, j, cols, bv);
+                       for (int t = 0; t < 4; ++t) {
+                         const float d = xv[q][t] - mu;
+                         o[t] = d * r;
+                       }
+                     },
+                     [&](int j, float(&o)[4]) {
+                       float gv[4];
+                       ldb_wide(gain + seg + j, gv);
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const float d = xv[q][t] - mu;
-        const float xh = d * r;
-        o[t] = xh * gv[t];
-        if (bias) o[t] = o[t] + bv[t];
-      }
-      if (y_bf16) {
-        uint16_t h[4];
+                       for (int t = 0; t < 4; ++t) o[t] = o[t] * gv[t];
+                       if (bias) {
+                         ldb_wide(bias + seg + j, gv);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) h[t] = f32_to_bf16(o[t]);
-        stb4<TAIL>((uint16_t*)y + row * cols, j, cols, h);
-      } else {
-        stf4<TAIL>((float*)y + row * cols, j, cols, o);
-      }
-    }
+                         for (int t = 0; t < 4; ++t) o[t] = o[t] + gv[t];
+                       }
+                       if (y_bf16) stb_arith(yh + j, o);
+                       else stf<4>(yf + j, o);
+                     },
+                     [&](int j, float xh) {
+                       float o = xh * bf16_wide(gain[seg + j]);
+                       if (bias) o = o + bf16_wide(bias[seg + j]);
+                       if (y_bf16) yh[j] = bf16_arith(o);
+                       else yf[j] = o;
+                     });
   }
 }
 
 // dx = RN(r RN(RN(gy - m1) - RN(xh m2))): gy = RN(dy g), m1 and m2 the row's means of gy and of RN(gy xh)
 template <int SRC, int NW, bool TAIL>
-__global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void layernorm_dx_kernel(
-    int64_t rows, int64_t cols, ActIn x, const uint16_t* __restrict__ gain, const float* __restrict__ mean,
+__global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, NW == 1 ? 4 : 1) void layernorm_dx_kernel(
+    int64_t rows, int cols, ActIn x, const uint16_t* __restrict__ gain, const float* __restrict__ mean,
     const float* __restrict__ rstd, const float* __restrict__ dy, float inv_d, float* __restrict__ dx) {
   constexpr int kRows = NW == 1 ? 4 : 1;
   __shared__ __attribute__((aligned(16))) RegStage st[NW == 1 ? 4 : NW];
   __shared__ float slot[2][NW];
-  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t c0 = NW == 1 ? 4 * lane : w * kRegCols + 4 * lane;
+  const int w = wave_id();
+  const int seg = NW == 1 ? 0 : w * (int)kRegCols;
+  const int n = cols - seg < (int)kRegCols ? cols - seg : (int)kRegCols;
   for (int64_t row = (int64_t)blockIdx.x * kRows + (NW == 1 ? w : 0); row < rows; row += (int64_t)gridDim.x * kRows) {
     const float mu = mean[row], r = rstd[row];
+    const PartIn<SRC> in(x, row, cols, seg);
+    const float* dr = dy + row * cols + seg;
     float xh[kRegQ][4], gy[kRegQ][4], tm[kRegQ][4];
+    part_load<TAIL>(n, xh, [&](int j, float(&v)[4]) { in.load4(j, v); }, [&](int j) { return in.load1(j); });
+    part_load<TAIL>(n, gy, [&](int j, float(&v)[4]) { ldf<4>(dr + j, v); }, [&](int j) { return dr[j]; });
+    part_load<TAIL>(n, tm, [&](int j, float(&v)[4]) { ldb_wide(gain + seg + j, v); },
+                    [&](int j) { return bf16_wide(gain[seg + j]); });
 #pragma unroll
-    for (int q = 0; q < kRegQ; ++q) {
-      const int64_t j = c0 + 256 * q;
-      float xv[4] = {0.0f, 0.0f, 0.0f, 0.0f}, dv[4] = {0.0f, 0.0f, 0.0f, 0.0f}, gv[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-      if (j < cols) {
-        act4<SRC, TAIL>(x, row, j, cols, xv);
-        ldf4<TAIL>(dy + row * cols, j, cols, dv);
-        ldb4<TAIL>(gain, j, cols, gv);
-      }
+    for (int q = 0; q < kRegQ; ++q)
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        const float d = xv[t] - mu;
+        const float d = xh[q][t] - mu;
         xh[q][t] = d * r;
-        gy[q][t] = dv[t] * gv[t];
+        gy[q][t] = gy[q][t] * tm[q][t];
         tm[q][t] = gy[q][t] * xh[q][t];
       }
-    }
     const float s1 = wide_row_sum<NW>(st[w], gy, cols, slot[0]);
     const float s2 = wide_row_sum<NW>(st[w], tm, cols, slot[1]);
     const float m1 = s1 * inv_d, m2 = s2 * inv_d;
+    float* out = dx + row * cols + seg;
+    part_store<TAIL>(n,
+                     [&](int q, float(&o)[4]) {
 #pragma unroll
-    for (int q = 0; q < kRegQ; ++q) {
-      const int64_t j = c0 + 256 * q;
-      if (j >= cols) continue;
-      float o[4];
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const float a = gy[q][t] - m1;
-        const float b = xh[q][t] * m2;
-        const float c = a - b;
-        o[t] = r * c;
-      }
-      stf4<TAIL>(dx + row * cols, j, cols, o);
-    }
+                       for (int t = 0; t < 4; ++t) {
+                         const float a = gy[q][t] - m1;
+                         const float b = xh[q][t] * m2;
+                         const float c = a - b;
+                         o[t] = r * c;
+                       }
+                     },
+                     [&](int j, const float(&o)[4]) { stf<4>(out + j, o); }, [&](int j, float o) { out[j] = o; });
   }
 }
 
@@ -185,8 +186,11 @@ __global__ __launch_bounds__(256 / V) void layernorm_part_kernel(int64_t rows, i
 constexpr int kFoldBlocks = 16;
 __global__ __launch_bounds__(64 * kFoldBlocks) void column_fold_kernel(int64_t nc, int64_t cols, int64_t inner,
                                                                        const float* __restrict__ part,
-                                                                       float* __restrict__ out) {
+                                                                       float* __restrict__ out0, float* __restrict__ out1) {
   __shared__ float res[kFoldBlocks][64];
+  float* out = blockIdx.y ? out1 : out0;
+  if (!out) return;
+  part += blockIdx.y * nc * cols;
   const int lane = threadIdx.x & 63, g = threadIdx.x >> 6;
   const int64_t col = (int64_t)blockIdx.x * 64 + lane;
   const int64_t G = block_chunks(nc, kFoldBlocks);
@@ -229,10 +233,11 @@ int row_waves(int64_t cols) {
 
 }  // namespace
 
-hipError_t column_fold_launch(int64_t rows, int64_t cols, int64_t inner, const float* part, float* out, hipStream_t s) {
+hipError_t column_fold_launch(int64_t rows, int64_t cols, int64_t inner, const float* part, float* out, float* out1,
+                              hipStream_t s) {
   if (cols == 0) return hipSuccess;
-  hipLaunchKernelGGL(column_fold_kernel, dim3((unsigned)((cols + 63) / 64)), dim3(64 * kFoldBlocks), 0, s,
-                     (rows + kChunk - 1) / kChunk, cols, inner, part, out);
+  hipLaunchKernelGGL(column_fold_kernel, dim3((unsigned)((cols + 63) / 64), out1 ? 2 : 1), dim3(64 * kFoldBlocks), 0, s,
+                     (rows + kChunk - 1) / kChunk, cols, inner, part, out, out1);
   return hipGetLastError();
 }
 
@@ -253,14 +258,18 @@ hipError_t layernorm_fwd_launch(int64_t rows, int64_t cols, const ActIn& x, cons
   const int nw = row_waves(cols);
   const int64_t blocks = nw == 1 ? (rows + 3) / 4 : rows;
   const dim3 grid((unsigned)(blocks < kMaxBlocks ? blocks : kMaxBlocks)), wg(nw == 1 ? 256 : 64 * nw);
-#define CANON_LN(SRC, NW)                                                                                           \
-  do {                                                                                                              \
-    if (cols % 4 == 0)                                                                                              \
-      hipLaunchKernelGGL((layernorm_fwd_kernel<SRC, NW, false>), grid, wg, 0, s, rows, cols, x, gain, bias, eps,    \
-                         inv_d, y_bf16, y, mean, rstd, k);                                                          \
-    else                                                                                                            \
-      hipLaunchKernelGGL((layernorm_fwd_kernel<SRC, NW, true>), grid, wg, 0, s, rows, cols, x, gain, bias, eps,     \
-                         inv_d, y_bf16, y, mean, rstd, k);                                                          \
+#define CANON_LN_K(SRC, NW, TAIL, KEEP)                                                                                \
+  hipLaunchKernelGGL((layernorm_fwd_kernel<SRC, NW, TAIL, KEEP>), grid, wg, 0, s, rows, (int)cols, x, gain, bias, eps, \
+                     inv_d, y_bf16, y, mean, rstd, k)
+#define CANON_LN(SRC, NW)                          \
+  do {                                             \
+    if (cols % 4 == 0) {                           \
+      if (k.codes) CANON_LN_K(SRC, NW, false, true); \
+      else CANON_LN_K(SRC, NW, false, false);      \
+    } else {                                       \
+      if (k.codes) CANON_LN_K(SRC, NW, true, true);  \
+      else CANON_LN_K(SRC, NW, true, false);       \
+    }                                              \
   } while (0)
   if (x.src == ACT_F32) {
     CANON_LN_WAVES(CANON_LN, ACT_F32)
@@ -268,6 +277,7 @@ hipError_t layernorm_fwd_launch(int64_t rows, int64_t cols, const ActIn& x, cons
     CANON_LN_WAVES(CANON_LN, ACT_BF16)
   }
 #undef CANON_LN
+#undef CANON_LN_K
   return hipGetLastError();
 }
 
@@ -296,12 +306,8 @@ hipError_t layernorm_bwd_launch(int64_t rows, int64_t cols, const ActIn& x, cons
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (dgain) {
-    hipError_t e = column_fold_launch(rows, cols, 0, part, dgain, s);
-    if (e != hipSuccess) return e;
-  }
-  if (dbias) {
-    hipError_t e = column_fold_launch(rows, cols, 0, part + nc * cols, dbias, s);
+  if (dgain || dbias) {
+    hipError_t e = column_fold_launch(rows, cols, 0, part, dgain, dbias, s);
     if (e != hipSuccess) return e;
   }
   if (rows == 0) return hipSuccess;
@@ -311,11 +317,11 @@ hipError_t layernorm_bwd_launch(int64_t rows, int64_t cols, const ActIn& x, cons
 #define CANON_LN(SRC, NW)                                                                                              \
   do {                                                                                                                 \
     if (cols % 4 == 0)                                                                                                 \
-      hipLaunchKernelGGL((layernorm_dx_kernel<SRC, NW, false>), grid, wg, 0, s, rows, cols, x, gain, mean, rstd, dy,   \
-                         inv_d, dx);                                                                                   \
+      hipLaunchKernelGGL((layernorm_dx_kernel<SRC, NW, false>), grid, wg, 0, s, rows, (int)cols, x, gain, mean, rstd,  \
+                         dy, inv_d, dx);                                                                                   \
     else                                                                                                               \
-      hipLaunchKernelGGL((layernorm_dx_kernel<SRC, NW, true>), grid, wg, 0, s, rows, cols, x, gain, mean, rstd, dy,    \
-                         inv_d, dx);                                                                                   \
+      hipLaunchKernelGGL((layernorm_dx_kernel<SRC, NW, true>), grid, wg, 0, s, rows, (int)cols, x, gain, mean, rstd,   \
+                         dy, inv_d, dx);                                                                                   \
   } while (0)
   if (x.src == ACT_F32) {
     CANON_LN_WAVES(CANON_LN, ACT_F32)

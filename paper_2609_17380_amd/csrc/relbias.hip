@@ -54,18 +54,16 @@ __device__ __forceinline__ Query query_of(const RelBiasArgs& a, int64_t b, int64
 }
 
 template <int NW, bool TAIL>
-__global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void relbias_fwd_kernel(RelBiasArgs a, int64_t blocks,
-                                                                              int64_t per_head,
-                                                                              const float* __restrict__ scores,
-                                                                              uint16_t* __restrict__ probs) {
+__global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, NW == 1 ? 4 : 1) void relbias_fwd_kernel(
+    RelBiasArgs a, int64_t blocks, int64_t per_head, const float* __restrict__ scores, uint16_t* __restrict__ probs) {
   constexpr int kRows = NW == 1 ? 4 : 1;
   __shared__ __attribute__((aligned(16))) RegStage st[NW == 1 ? 4 : NW];
   __shared__ float slot[2][NW], top[NW];
   extern __shared__ float near_[];  // bias by position: of the key less the query's, the near side of the last buckets
-  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int w = wave_id(), lane = threadIdx.x & 63;
   const int far = a.start[a.n_side - 1], right = a.bidirectional ? far : 0;
-  const int seg = NW == 1 ? 0 : w * (int)kRegCols;
-  const int64_t ld = a.ld;
+  const int seg = NW == 1 ? 0 : w * (int)kRegCols;  // this wavefront's part of the row
+  const int n = (int)a.k_len - seg < (int)kRegCols ? (int)a.k_len - seg : (int)kRegCols;
   int turn = 0;  // rows in turn take one of two slots, so that a barrier lies between a slot's reads and its next writes
   for (int64_t blk = blockIdx.x; blk < blocks; blk += gridDim.x) {
     const int64_t bh = blk / per_head, b = bh / a.heads, h = bh - b * a.heads;
@@ -73,88 +71,79 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void relbias_fwd_kernel(Re
     __syncthreads();  // the last block's biases are read
     for (int e = threadIdx.x; e <= far + right; e += blockDim.x) {
       const int d = far - e;  // query less key: far .. -right
-      const int n = d >= 0 ? bucket_of(a.start, a.n_side, d) : a.n_side + bucket_of(a.start, a.n_side, -d);
-      near_[e] = bf16_to_f32(a.table[n * a.heads + h]);
+      const int k = d >= 0 ? bucket_of(a.start, a.n_side, d) : a.n_side + bucket_of(a.start, a.n_side, -d);
+      near_[e] = bf16_to_f32(a.table[k * a.heads + h]);
     }
     __syncthreads();
     for (int it = 0; it < kQueries; ++it) {
       const int64_t i = i0 + it * kRows + (NW == 1 ? w : 0);
       if (i >= a.q_len) break;  // the same for every wavefront that shares the row
       const Query qy = query_of(a, b, i);
-      const int j0 = qy.j0, j1 = qy.j1;
-      const int64_t row = bh * a.q_len + i;
-      const float* rr = scores + row * ld;
-      auto any = [&](int q) { return seg + 256 * q < j1 && seg + 256 * q + 255 >= j0; };
-      auto all = [&](int q) { return seg + 256 * q + 255 < j1 && seg + 256 * q >= j0; };
+      const int j0 = qy.j0 - seg, span = qy.j1 - qy.j0, first = far + seg - qy.pos;  // near_ entry of the part's first key
+      const float* rr = scores + (bh * a.q_len + i) * a.ld + seg;
+      auto any = [&](int q) { return 256 * q < j0 + span && 256 * q + 255 >= j0; };
       float e[kRegQ][4];
-#pragma unroll
-      for (int q = 0; q < kRegQ; ++q) {
-#pragma unroll
-        for (int t = 0; t < 4; ++t) e[q][t] = 0.0f;
-        const int j = seg + 256 * q + 4 * lane;
-        if (any(q) && j < j1 && j + 3 >= j0) ldf4<TAIL>(rr, j, a.k_len, e[q]);
-      }
+      part_load<TAIL>(n < j0 + span ? n : j0 + span + 3 < n ? j0 + span + 3 : n, e,
+                      [&](int j, float(&v)[4]) {
+                        if (j + 3 >= j0) ldf<4>(rr + j, v);
+                        else v[0] = v[1] = v[2] = v[3] = 0.0f;
+                      },
+                      [&](int j) { return rr[j]; });
       float m = -__builtin_inff();
 #pragma unroll
       for (int q = 0; q < kRegQ; ++q) {
-        if (!any(q)) continue;
-        const int j = seg + 256 * q + 4 * lane;
-        // entry of key j: far + j - pos, cut to the table's ends
-        const int at = far + j - qy.pos;
-        if (far + seg + 256 * q + 255 - qy.pos <= 0 || far + seg + 256 * q - qy.pos >= far + right) {
-          const float bias = near_[far + seg + 256 * q + 255 - qy.pos <= 0 ? 0 : far + right];
+        if (!any(q)) {
 #pragma unroll
-          for (int t = 0; t < 4; ++t) {
-            const float x = e[q][t] * a.scale;
-            e[q][t] = x + bias;
-          }
+          for (int t = 0; t < 4; ++t) e[q][t] = -__builtin_inff();
+          continue;
+        }
+        const int j = 256 * q + 4 * lane;
+        const bool left = first + 256 * q + 255 <= 0;
+        float bias[4];
+        if (left || first + 256 * q >= far + right) {
+          bias[0] = bias[1] = bias[2] = bias[3] = near_[left ? 0 : far + right];
         } else {
 #pragma unroll
           for (int t = 0; t < 4; ++t) {
-            const int k = at + t < 0 ? 0 : at + t > far + right ? far + right : at + t;
-            const float x = e[q][t] * a.scale;
-            e[q][t] = x + near_[k];
+            const int k = first + j + t;
+            bias[t] = near_[k < 0 ? 0 : k > far + right ? far + right : k];
           }
         }
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
-          if (all(q) || (j + t < j1 && j + t >= j0)) m = fmaxf(m, e[q][t]);
+        for (int t = 0; t < 4; ++t) {
+          const float x = e[q][t] * a.scale;
+          const float z = x + bias[t];
+          e[q][t] = (unsigned)(j + t - j0) < (unsigned)span ? z : -__builtin_inff();  // unseen: an e of +0
+          m = fmaxf(m, e[q][t]);
+        }
       }
-#pragma unroll
-      for (int s = 32; s >= 1; s >>= 1) m = fmaxf(m, __shfl_xor(m, s, 64));
+      m = wave_most(m);
       if constexpr (NW > 1) {
         if (lane == 0) top[w] = m;
         __syncthreads();
-        m = lane < NW ? top[lane] : -__builtin_inff();
-#pragma unroll
-        for (int s = 32; s >= 1; s >>= 1) m = fmaxf(m, __shfl_xor(m, s, 64));
+        m = wave_most(lane < NW ? top[lane] : -__builtin_inff());
       }
       // a row whose seen scores are all -inf has e = cexp(-inf) = +0, not cexp(-inf - -inf)
       m = m == -__builtin_inff() ? 0.0f : m;
 #pragma unroll
       for (int q = 0; q < kRegQ; ++q) {
-        if (!any(q)) continue;
-        const int j = seg + 256 * q + 4 * lane;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const float x = cexp_neg(e[q][t] - m);
-          e[q][t] = all(q) || (j + t < j1 && j + t >= j0) ? x : 0.0f;  // masked keys enter the chain as +0 terms
-        }
+        for (int t = 0; t < 4; ++t) e[q][t] = any(q) ? cexp_neg(e[q][t] - m) : 0.0f;
       }
       turn ^= 1;
-      const float S = wide_row_sum<NW>(st[w], e, a.k_len, slot[turn]);
+      const float S = wide_row_sum<NW>(st[w], e, (int)a.k_len, slot[turn]);
       const float rcp = S == 0.0f ? 0.0f : 1.0f / S;
+      uint16_t* pr = probs + (bh * a.q_len + i) * a.ld + seg;
+      if (S == S) {
+        part_store<TAIL>(n,
+                         [&](int q, float(&o)[4]) {
 #pragma unroll
-      for (int q = 0; q < kRegQ; ++q) {
-        const int j = seg + 256 * q + 4 * lane;
-        if (j >= a.k_len) continue;
-        uint16_t o[4] = {0, 0, 0, 0};
-        if (any(q)) {  // a masked key's +0 rcp is a NaN where S is one: its zero is kept
-#pragma unroll
-          for (int t = 0; t < 4; ++t)
-            if (all(q) || (j + t < j1 && j + t >= j0)) o[t] = f32_to_bf16(e[q][t] * rcp);
-        }
-        stb4<TAIL>(probs + row * ld, j, a.k_len, o);
+                           for (int t = 0; t < 4; ++t) o[t] = e[q][t] * rcp;
+                         },
+                         [&](int j, const float(&o)[4]) { stb_arith(pr + j, o); },
+                         [&](int j, float o) { pr[j] = bf16_arith(o); });
+      } else {  // a NaN among the seen: every seen key's, and still +0 elsewhere
+        for (int j = lane; j < n; j += 64) pr[j] = (unsigned)(j - j0) < (unsigned)span ? 0x7FC0 : 0;
       }
     }
   }
@@ -165,33 +154,33 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void relbias_fwd_kernel(Re
 // two chunks, whose chains one lane runs and adds (their sum is the fold whatever lies between); a longer one is summed
 // chunk by chunk, a lane to a chunk, like the row.
 template <int NW, bool TAIL>
-__global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void relbias_bwd_kernel(RelBiasArgs a, int64_t blocks,
-                                                                              int64_t per_head,
-                                                                              const uint16_t* __restrict__ probs,
-                                                                              const float* __restrict__ dprobs,
-                                                                              uint16_t* __restrict__ dscores,
-                                                                              float* __restrict__ rowsum) {
+__global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, NW == 1 ? 4 : 1) void relbias_bwd_kernel(
+    RelBiasArgs a, int64_t blocks, int64_t per_head, const uint16_t* __restrict__ probs,
+    const float* __restrict__ dprobs, uint16_t* __restrict__ dscores, float* __restrict__ rowsum) {
   constexpr int kRows = NW == 1 ? 4 : 1;
   __shared__ __attribute__((aligned(16))) RegStage st[NW == 1 ? 4 : NW];
   __shared__ float slot[2][NW];
   __shared__ float part[2][NW];
-  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  __shared__ int lo_[2 * kRelStarts], hi_[2 * kRelStarts];  // the keys of a bucket, less the query's position: lo <= . < hi
+  const int w = wave_id(), lane = threadIdx.x & 63;
   const int seg = NW == 1 ? 0 : w * (int)kRegCols;
+  const int n = (int)a.k_len - seg < (int)kRegCols ? (int)a.k_len - seg : (int)kRegCols;
   const int nb = a.n_side * (a.bidirectional ? 2 : 1);
-  const int64_t ld = a.ld;
   int turn = 0;  // as above
-  // the keys of bucket n, less the query's position: lo <= j - pos < hi
-  auto range = [&](int n, int& lo, int& hi) {
-    const int m = n < a.n_side ? n : n - a.n_side;
-    const int d0 = a.start[m], d1 = m + 1 < a.n_side ? a.start[m + 1] : 2 * (int)kFarPos;
-    if (n < a.n_side) {
-      lo = 1 - d1;
-      hi = d0 == d1 ? lo : d0 == 0 && !a.bidirectional ? 2 * (int)kFarPos : 1 - d0;
-    } else {
-      lo = d0 > 0 ? d0 : 1;
-      hi = d1;
+  if (rowsum) {
+    for (int k = threadIdx.x; k < nb; k += blockDim.x) {
+      const int side = k < a.n_side ? k : k - a.n_side;
+      const int d0 = a.start[side], d1 = side + 1 < a.n_side ? a.start[side + 1] : 2 * (int)kFarPos;
+      if (k < a.n_side) {
+        lo_[k] = 1 - d1;
+        hi_[k] = d0 == d1 ? 1 - d1 : d0 == 0 && !a.bidirectional ? 2 * (int)kFarPos : 1 - d0;
+      } else {
+        lo_[k] = d0 > 0 ? d0 : 1;
+        hi_[k] = d1;
+      }
     }
-  };
+    __syncthreads();
+  }
   for (int64_t blk = blockIdx.x; blk < blocks; blk += gridDim.x) {
     const int64_t bh = blk / per_head, b = bh / a.heads, h = bh - b * a.heads;
     const int64_t i0 = (blk - bh * per_head) * (kRows * kQueries);
@@ -199,48 +188,51 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void relbias_bwd_kernel(Re
       const int64_t i = i0 + it * kRows + (NW == 1 ? w : 0);
       if (i >= a.q_len) break;
       const Query qy = query_of(a, b, i);
-      const int j0 = qy.j0, j1 = qy.j1;
-      const int64_t row = bh * a.q_len + i;
-      auto any = [&](int q) { return seg + 256 * q < j1 && seg + 256 * q + 255 >= j0; };
-      auto all = [&](int q) { return seg + 256 * q + 255 < j1 && seg + 256 * q >= j0; };
+      const int j0 = qy.j0 - seg, span = qy.j1 - qy.j0;
+      const int64_t at = (bh * a.q_len + i) * a.ld + seg;
+      const uint16_t* pr = probs + at;
+      const float* dr = dprobs + at;
+      const int upto = n < j0 + span ? n : j0 + span + 3 < n ? j0 + span + 3 : n;  // whole vectors of what is seen
       float p[kRegQ][4], dp[kRegQ][4], e[kRegQ][4];
+      part_load<TAIL>(upto, p,
+                      [&](int j, float(&v)[4]) {
+                        if (j + 3 >= j0) ldb_wide(pr + j, v);
+                        else v[0] = v[1] = v[2] = v[3] = 0.0f;
+                      },
+                      [&](int j) { return bf16_wide(pr[j]); });
+      part_load<TAIL>(upto, dp,
+                      [&](int j, float(&v)[4]) {
+                        if (j + 3 >= j0) ldf<4>(dr + j, v);
+                        else v[0] = v[1] = v[2] = v[3] = 0.0f;
+                      },
+                      [&](int j) { return dr[j]; });
+      auto seen = [&](int q, int t, int first) { return (unsigned)(256 * q + 4 * lane + t - first) < (unsigned)span; };
 #pragma unroll
-      for (int q = 0; q < kRegQ; ++q) {
-#pragma unroll
-        for (int t = 0; t < 4; ++t) p[q][t] = dp[q][t] = 0.0f;
-        const int j = seg + 256 * q + 4 * lane;
-        if (any(q) && j < j1 && j + 3 >= j0) {
-          ldb4<TAIL>(probs + row * ld, j, a.k_len, p[q]);
-          ldf4<TAIL>(dprobs + row * ld, j, a.k_len, dp[q]);
-        }
-      }
-#pragma unroll
-      for (int q = 0; q < kRegQ; ++q) {
-        const int j = seg + 256 * q + 4 * lane;
+      for (int q = 0; q < kRegQ; ++q)
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           const float x = p[q][t] * dp[q][t];
-          e[q][t] = any(q) && (all(q) || (j + t < j1 && j + t >= j0)) ? x : 0.0f;
+          e[q][t] = seen(q, t, j0) ? x : 0.0f;
         }
-      }
       turn ^= 1;
-      const float D = wide_row_sum<NW>(st[w], e, a.k_len, slot[turn]);
+      const float D = wide_row_sum<NW>(st[w], e, (int)a.k_len, slot[turn]);
+      const int first = again(j0);
 #pragma unroll
-      for (int q = 0; q < kRegQ; ++q) {
-        const int j = seg + 256 * q + 4 * lane;
+      for (int q = 0; q < kRegQ; ++q)
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           const float d = dp[q][t] - D;
           const float x = p[q][t] * d;
-          e[q][t] = any(q) && (all(q) || (j + t < j1 && j + t >= j0)) ? x : 0.0f;
+          e[q][t] = seen(q, t, first) ? x : 0.0f;
         }
-        if (j < a.k_len) {
-          uint16_t o[4];
+      uint16_t* sr = dscores + at;
+      part_store<TAIL>(n,
+                       [&](int q, float(&o)[4]) {
 #pragma unroll
-          for (int t = 0; t < 4; ++t) o[t] = f32_to_bf16(e[q][t] * a.scale);
-          stb4<TAIL>(dscores + row * ld, j, a.k_len, o);
-        }
-      }
+                         for (int t = 0; t < 4; ++t) o[t] = e[q][t] * a.scale;
+                       },
+                       [&](int j, const float(&o)[4]) { stb_arith(sr + j, o); },
+                       [&](int j, float o) { sr[j] = bf16_arith(o); });
       if (!rowsum) continue;
       float* out = rowsum + ((b * a.q_len + i) * a.heads + h) * nb;
       // the row's ds, a chunk to a row of LDS (a wavefront's own, its LDS operations in order)
@@ -251,43 +243,51 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW) void relbias_bwd_kernel(Re
       }
       if constexpr (NW > 1) __syncthreads();
       else __builtin_amdgcn_wave_barrier();
-      for (int n = NW == 1 ? lane : (int)threadIdx.x; n < nb; n += NW == 1 ? 64 : 64 * NW) {
-        int lo, hi;
-        range(n, lo, hi);
+      for (int k = NW == 1 ? lane : (int)threadIdx.x; k < nb; k += NW == 1 ? 64 : 64 * NW) {
+        const int lo = lo_[k], hi = hi_[k];
         if (hi - lo > kRelShort) continue;
-        const int b0 = qy.pos + lo > j0 ? qy.pos + lo : j0, b1 = qy.pos + hi < j1 ? qy.pos + hi : j1;
+        const int b0 = qy.pos + lo > qy.j0 ? qy.pos + lo : qy.j0, b1 = qy.pos + hi < qy.j1 ? qy.pos + hi : qy.j1;
         const int mid = (b0 | 31) + 1;  // the next chunk's first key
         float s0 = 0.0f, s1 = 0.0f;
-        for (int j = b0; j < b1 && j < mid; ++j) s0 = s0 + st[NW == 1 ? w : j >> 11].t[(j >> 5) & 63][j & 31];
-        for (int j = mid; j < b1; ++j) s1 = s1 + st[NW == 1 ? w : j >> 11].t[(j >> 5) & 63][j & 31];
-        out[n] = s0 + s1;
+        for (int j = b0; j < b1; j += 4) {
+          float v[4];
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            const int u = j + t < b1 ? j + t : b0;
+            v[t] = st[NW == 1 ? w : u >> 11].t[(u >> 5) & 63][u & 31];
+          }
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            s0 = s0 + (j + t < b1 && j + t < mid ? v[t] : 0.0f);
+            s1 = s1 + (j + t < b1 && j + t >= mid ? v[t] : 0.0f);
+          }
+        }
+        out[k] = s0 + s1;
       }
       for (int l = 0; l < a.n_long; ++l) {
-        const int n = a.longs[l];
-        int lo, hi;
-        range(n, lo, hi);
-        const int b0 = qy.pos + lo > j0 ? qy.pos + lo : j0, b1 = qy.pos + hi < j1 ? qy.pos + hi : j1;
+        const int k = a.longs[l];
+        const int lo = lo_[k], hi = hi_[k];
+        const int b0 = (qy.pos + lo > qy.j0 ? qy.pos + lo : qy.j0) - seg, b1 = (qy.pos + hi < qy.j1 ? qy.pos + hi : qy.j1) - seg;
         float sum = 0.0f;
-        if (b0 < b1 && b0 < seg + (int)kRegCols && b1 > seg) {  // the same for the whole wavefront
-          const int first = b0 - seg - 32 * lane, last = b1 - seg - 32 * lane;
+        if (b0 < b1 && b0 < (int)kRegCols && b1 > 0) {  // the same for the whole wavefront
+          const int c0 = b0 - 32 * lane, len = b1 - b0;
 #pragma unroll
-          for (int k = 0; k < kChunk; k += 4) {
-            const float4 v = *reinterpret_cast<const float4*>(&st[w].t[lane][k]);
-            sum = sum + (k >= first && k < last ? v.x : 0.0f);
-            sum = sum + (k + 1 >= first && k + 1 < last ? v.y : 0.0f);
-            sum = sum + (k + 2 >= first && k + 2 < last ? v.z : 0.0f);
-            sum = sum + (k + 3 >= first && k + 3 < last ? v.w : 0.0f);
+          for (int t = 0; t < kChunk; t += 4) {
+            const float4 v = *reinterpret_cast<const float4*>(&st[w].t[lane][t]);
+            sum = sum + ((unsigned)(t - c0) < (unsigned)len ? v.x : 0.0f);
+            sum = sum + ((unsigned)(t + 1 - c0) < (unsigned)len ? v.y : 0.0f);
+            sum = sum + ((unsigned)(t + 2 - c0) < (unsigned)len ? v.z : 0.0f);
+            sum = sum + ((unsigned)(t + 3 - c0) < (unsigned)len ? v.w : 0.0f);
           }
-          const int64_t left = a.k_len - seg < kRegCols ? a.k_len - seg : kRegCols;
-          sum = wave_fold(sum, (int)((left + kChunk - 1) / kChunk));
+          sum = wave_total(sum);
         }
         if constexpr (NW > 1) {
           if (lane == 0) part[l & 1][w] = sum;
           __syncthreads();
-          const int parts = (int)((a.k_len + kRegCols - 1) / kRegCols);
-          sum = wave_fold(lane < parts ? part[l & 1][lane] : 0.0f, parts);
+          const int parts = ((int)a.k_len + (int)kRegCols - 1) / (int)kRegCols;
+          sum = wave_total(lane < parts ? part[l & 1][lane] : 0.0f);
         }
-        if (lane == 0 && (NW == 1 || w == 0)) out[n] = sum;
+        if (lane == 0 && (NW == 1 || w == 0)) out[k] = sum;
       }
       if constexpr (NW > 1) __syncthreads();  // the row's ds are read
     }
@@ -396,7 +396,7 @@ hipError_t relbias_bwd_launch(const RelBiasArgs& a, const uint16_t* probs, const
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  return column_fold_launch(rows, cols, nb, part, dtable, s);
+  return column_fold_launch(rows, cols, nb, part, dtable, nullptr, s);
 }
 
 }  // namespace canon

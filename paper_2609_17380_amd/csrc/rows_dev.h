@@ -106,6 +106,44 @@ __device__ __forceinline__ void stb4(uint16_t* row, int64_t j, int64_t n, const 
   }
 }
 
+// A lane's value joined with that of its partner at distance 1, 2, 4, .. 32 in turn, so that every lane ends with the whole
+// wavefront's (or, of fewer steps, its aligned set's).  The steps within 16 lanes are register moves between lanes (the
+// partner at distance 4 and 8 may be any lane of the other half: those hold the same by then), the last two swap rows of
+// 16 and halves; no LDS operation, whose latency a shuffle has each time.
+template <int CTRL>
+__device__ __forceinline__ uint32_t lane_move(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true);
+}
+template <class Join>
+__device__ __forceinline__ uint32_t lanes_join(uint32_t x, int lanes, Join join) {
+  x = join(x, lane_move<0xB1>(x));   // lanes 1 0 3 2 of each four
+  x = join(x, lane_move<0x4E>(x));   // lanes 2 3 0 1
+  x = join(x, lane_move<0x141>(x));  // each eight mirrored
+  if (lanes > 8) x = join(x, lane_move<0x140>(x));  // each sixteen mirrored
+  if (lanes > 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = join(r[0], r[1]);
+  }
+  if (lanes > 32) {
+    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    x = join(r[0], r[1]);
+  }
+  return x;
+}
+// Algorithm 2 over 64 chunk partials, one per lane, of which those past the last chunk are +0: adding them is the
+// pass-through rule (no partial is -0).  The sum in every lane.
+__device__ __forceinline__ float wave_total(float p) {
+  return __uint_as_float(lanes_join(__float_as_uint(p), 64, [](uint32_t a, uint32_t b) {
+    const float s = __uint_as_float(a) + __uint_as_float(b);
+    return __float_as_uint(s);
+  }));
+}
+__device__ __forceinline__ float wave_most(float m) {
+  return __uint_as_float(lanes_join(__float_as_uint(m), 64, [](uint32_t a, uint32_t b) {
+    return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+  }));
+}
+
 // Register-resident rows (cols <= 2048, or the part H of 2048 terms of a longer one): lane l holds terms
 // 4l + 256q .. +3 of its row, read from memory once.  The chunk chains still run one per lane over an LDS transpose
 // (rows of 36 floats: 16-byte stores and reads without bank conflicts; a wavefront's LDS operations complete in order).
@@ -136,7 +174,6 @@ __device__ __forceinline__ float reg_row_sum(RegStage& st, const float (&e)[Q][4
     }
   }
   __builtin_amdgcn_wave_barrier();
-  const int nc = (int)((n + kChunk - 1) / kChunk);
   float p = 0.0f;
   const int k1 = (int)n - lane * kChunk;
   if (k1 >= kChunk) {
@@ -148,27 +185,104 @@ __device__ __forceinline__ float reg_row_sum(RegStage& st, const float (&e)[Q][4
   } else {
     for (int i = 0; i < k1; ++i) p = p + st.t[lane][i];
   }
-  return __shfl(wave_fold(p, nc), 0, 64);
+  return wave_total(p);
 }
 
-// The R1 sum of a row spread over a workgroup of NW wavefronts, wavefront w holding its terms 2048 w .. 2048 w + 2047:
-// 64 chunks, a complete subtree of Algorithm 2 wherever a later one follows, so the wavefronts' sums are folded by the
-// same rule.  slot: NW floats of LDS, not written again before every wavefront has passed another barrier (NW = 1: one
-// wavefront per row, no barrier).
+// ---- a part of a row in a wavefront's registers: n <= 2048 elements, lane l holding 256 q + 4 l .. +3 -----------------
+// Vectors that lie inside the part are moved whole; the one that its end cuts (TAIL: n is no multiple of 4) belongs to one
+// lane of one q and is moved by element beside the loop, so that the loop has a single condition per vector (with the
+// cut vector's branches in every iteration the masks spilled: padded rows of 1001 keys 109 us, now 72).
+template <bool TAIL, class Load4, class Load1>
+__device__ __forceinline__ void part_load(int n, float (&v)[kRegQ][4], Load4 load4, Load1 load1) {
+  const int at = 4 * (threadIdx.x & 63);
+#pragma unroll
+  for (int q = 0; q < kRegQ; ++q) {
+    if (256 * q + at + 4 <= n) {
+      load4(256 * q + at, v[q]);
+    } else {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) v[q][t] = 0.0f;
+    }
+  }
+  if (TAIL && n > 0 && (n & 3)) {
+    const int base = n & ~3;
+    float c[3] = {0.0f, 0.0f, 0.0f};
+    const int mine = at == (base & 255) ? base >> 8 : -1;  // the cut vector's q, in its lane
+    if (mine >= 0) {
+#pragma unroll
+      for (int t = 0; t < 3; ++t)
+        if (base + t < n) c[t] = load1(base + t);
+    }
+#pragma unroll
+    for (int q = 0; q < kRegQ; ++q)
+#pragma unroll
+      for (int t = 0; t < 3; ++t) v[q][t] = q == mine ? c[t] : v[q][t];
+  }
+}
+// value(q, o) makes vector q, store4(j, o) moves the one at element j, store1(j, o) an element
+template <bool TAIL, class Value, class Store4, class Store1>
+__device__ __forceinline__ void part_store(int n, Value value, Store4 store4, Store1 store1) {
+  const int at = 4 * (threadIdx.x & 63);
+  const int mine = TAIL && (n & 3) && n > 0 && at == (n & 252) ? n >> 8 : -1;
+  float c[3] = {0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int q = 0; q < kRegQ; ++q) {
+    if (256 * q >= n) break;
+    float o[4];
+    value(q, o);
+    if (256 * q + at + 4 <= n) store4(256 * q + at, o);
+    if (TAIL) {
+#pragma unroll
+      for (int t = 0; t < 3; ++t) c[t] = q == mine ? o[t] : c[t];
+    }
+  }
+  if (mine >= 0) {
+#pragma unroll
+    for (int t = 0; t < 3; ++t)
+      if (t < (n & 3)) store1((n & ~3) + t, c[t]);
+  }
+}
+
+// bf16 to fp32 where arithmetic follows at once, which reads a subnormal as zero by itself
+__device__ __forceinline__ float bf16_wide(uint16_t h) { return __uint_as_float((uint32_t)h << 16); }
+__device__ __forceinline__ void ldb_wide(const uint16_t* p, float (&f)[4]) {
+  const H4 u = *reinterpret_cast<const H4*>(p);
+  f[0] = __uint_as_float(u.x << 16); f[1] = __uint_as_float(u.x & 0xFFFF0000u);
+  f[2] = __uint_as_float(u.y << 16); f[3] = __uint_as_float(u.y & 0xFFFF0000u);
+}
+// results of arithmetic (never subnormal) to bf16
+__device__ __forceinline__ void stb_arith(uint16_t* p, const float (&f)[4]) {
+  *reinterpret_cast<H4*>(p) = H4{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3])};
+}
+__device__ __forceinline__ uint16_t bf16_arith(float f) { return (uint16_t)pack_bf16(f, 0.0f); }
+
+// a value that the compiler does not know to be the same as before: masks made from it are made again instead of being
+// held in scalar registers from their first use to the next, which spills them
+__device__ __forceinline__ int again(int x) {
+  asm("" : "+s"(x));
+  return x;
+}
+
+// this wavefront's place in its workgroup, known to be the same for all its lanes
+__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
+
+// The R1 sum of a row of n terms spread over a workgroup of NW wavefronts, wavefront w holding its part from 2048 w on: 64
+// chunks, a complete subtree of Algorithm 2 wherever a later part follows, so the parts' sums are folded by the same rule.
+// slot: NW floats of LDS, not written again before every wavefront has passed another barrier (NW = 1: one wavefront per
+// row, no barrier).
 template <int NW>
-__device__ __forceinline__ float wide_row_sum(RegStage& st, const float (&e)[kRegQ][4], int64_t n, float* slot) {
+__device__ __forceinline__ float wide_row_sum(RegStage& st, const float (&e)[kRegQ][4], int n, float* slot) {
   if constexpr (NW == 1) {
     return reg_row_sum(st, e, n);
   } else {
-    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int64_t left = n - w * kRegCols;
+    const int w = wave_id(), lane = threadIdx.x & 63;
+    const int left = n - w * (int)kRegCols;
     float p = 0.0f;
-    if (left > 0) p = reg_row_sum(st, e, left < kRegCols ? left : kRegCols);
+    if (left > 0) p = reg_row_sum(st, e, left < (int)kRegCols ? left : (int)kRegCols);
     if (lane == 0) slot[w] = p;
     __syncthreads();
-    const int parts = (int)((n + kRegCols - 1) / kRegCols);
-    p = lane < parts ? slot[lane] : 0.0f;
-    return __shfl(wave_fold(p, parts), 0, 64);
+    const int parts = (n + (int)kRegCols - 1) / (int)kRegCols;
+    return wave_total(lane < parts ? slot[lane] : 0.0f);
   }
 }
 
