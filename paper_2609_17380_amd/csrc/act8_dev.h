@@ -18,7 +18,7 @@ struct __attribute__((packed, aligned(1))) B4 {
 // Elements j .. j + 3 of a row of n (j a multiple of 4 whose lanes run through whole groups; v holds 0 beyond n) into
 // codes and their group's step.  Every lane of the wavefront takes part.  The magnitudes are compared as bit patterns,
 // so that a NaN ranks above every number.
-__device__ __forceinline__ uint32_t codes4(const float (&v)[4], int lg, float& s) {
+__device__ __forceinline__ float step4(const float (&v)[4], int lg) {
   uint32_t m = 0;
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
@@ -26,7 +26,10 @@ __device__ __forceinline__ uint32_t codes4(const float (&v)[4], int lg, float& s
     m = a > m ? a : m;
   }
   m = lanes_join(m, 1 << (lg - 2), [](uint32_t a, uint32_t b) { return a > b ? a : b; });
-  s = __uint_as_float(m) * __uint_as_float(kInv127Bits);
+  return __uint_as_float(m) * __uint_as_float(kInv127Bits);
+}
+__device__ __forceinline__ uint32_t codes4(const float (&v)[4], int lg, float& s) {
+  s = step4(v, lg);
   const bool recip = recip_step_ok(s);
   const float rs = recip ? 1.0f / s : 0.0f;
   uint32_t w[1];
@@ -47,21 +50,50 @@ __device__ __forceinline__ void keep4(const float (&v)[4], int64_t j, int64_t n,
       if (j + t < n) codes[j + t] = (int8_t)(w >> (8 * t));
   }
 }
-// the same of a part of a row (part_load): v holds 0 beyond n
-template <bool TAIL>
-__device__ __forceinline__ void part_keep(const float (&v)[kRegQ][4], int n, int lg, int8_t* codes, float* steps) {
+// The same of a part of a row (part_load): v holds 0 beyond n.  Every code is taken through the reciprocal first; the few
+// vectors with a value that it does not decide (quant_pack's rule) are remembered and done exactly behind the loop, in one
+// branch instead of one per vector, whose masks spilled.
+template <bool TAIL, int Q>
+__device__ __forceinline__ void part_keep(const float (&v)[Q][4], int n, int lg, int8_t* codes, float* steps) {
   const int at = 4 * (threadIdx.x & 63);
+  uint32_t w[Q], undecided = 0;
+  float s[Q];
+#pragma unroll
+  for (int q = 0; q < Q; ++q) {
+    if (256 * q >= n) break;
+    s[q] = step4(v[q], lg);
+    const bool recip = recip_step_ok(s[q]);
+    const float rs = recip ? 1.0f / s[q] : 0.0f;
+    bool sure = recip;
+    uint32_t x = 0;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const float y = v[q][t] * rs, k = __builtin_rintf(y);
+      sure &= fabsf(y - k) < 0.5f - 0x1p-15f;
+      x = __builtin_amdgcn_cvt_pk_u8_f32(k + 128.0f, t, x);
+    }
+    w[q] = x ^ 0x80808080u;
+    undecided |= sure ? 0u : 1u << q;
+  }
+  if (undecided) {
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+      if (undecided & (1u << q)) {
+        uint32_t x = 0;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) x |= (uint32_t)(uint8_t)quant1(v[q][t], s[q]) << (8 * t);
+        w[q] = x;
+      }
+  }
   const int mine = TAIL && (n & 3) && n > 0 && at == (n & 252) ? n >> 8 : -1;
   uint32_t cut = 0;
 #pragma unroll
-  for (int q = 0; q < kRegQ; ++q) {
+  for (int q = 0; q < Q; ++q) {
     if (256 * q >= n) break;
     const int j = 256 * q + at;
-    float s;
-    const uint32_t w = codes4(v[q], lg, s);
-    if (j < n && (j & ((1 << lg) - 1)) == 0) steps[j >> lg] = s;
-    if (j + 4 <= n) reinterpret_cast<B4*>(codes + j)->x = w;
-    cut = q == mine ? w : cut;
+    if (j < n && (j & ((1 << lg) - 1)) == 0) steps[j >> lg] = s[q];
+    if (j + 4 <= n) reinterpret_cast<B4*>(codes + j)->x = w[q];
+    cut = q == mine ? w[q] : cut;
   }
   if (mine >= 0) {
 #pragma unroll
@@ -130,17 +162,49 @@ struct PartIn {
       steps = a.steps + row * ((cols + (1 << lg) - 1) >> lg) + (seg >> lg);
     }
   }
-  __device__ __forceinline__ void load4(int j, float (&f)[4]) const {
+  // four elements as they are stored, to be widened when they are needed, so that nothing waits for them before
+  struct Raw {
+    float f[SRC == ACT_F32 ? 4 : 1];  // fp32; in 8 bits the step
+    uint32_t w[SRC == ACT_BF16 ? 2 : 1];
+  };
+  __device__ __forceinline__ void load4(int j, Raw& r) const {
     if constexpr (SRC == ACT_F32) {
-      ldf<4>((const float*)p + j, f);
+      ldf<4>((const float*)p + j, r.f);
     } else if constexpr (SRC == ACT_BF16) {
-      ldb_wide((const uint16_t*)p + j, f);
+      const H4 h = *reinterpret_cast<const H4*>((const uint16_t*)p + j);
+      r.w[0] = h.x; r.w[1] = h.y;
     } else {
-      const float s = steps[j >> lg];
-      const uint32_t w = reinterpret_cast<const B4*>((const int8_t*)p + j)->x;
-#pragma unroll
-      for (int t = 0; t < 4; ++t) f[t] = (float)(int8_t)(w >> (8 * t)) * s;
+      r.f[0] = steps[j >> lg];
+      r.w[0] = reinterpret_cast<const B4*>((const int8_t*)p + j)->x;
     }
+  }
+  // element j + t into place t
+  __device__ __forceinline__ void load1(int j, int t, Raw& r) const {
+    if constexpr (SRC == ACT_F32) {
+      r.f[t] = ((const float*)p)[j + t];
+    } else if constexpr (SRC == ACT_BF16) {
+      r.w[t >> 1] |= (uint32_t)((const uint16_t*)p)[j + t] << (16 * (t & 1));
+    } else {
+      r.f[0] = steps[j >> lg];
+      r.w[0] |= (uint32_t)((const uint8_t*)p)[j + t] << (8 * t);
+    }
+  }
+  static __device__ __forceinline__ void wide(const Raw& r, float (&f)[4]) {
+    if constexpr (SRC == ACT_F32) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) f[t] = r.f[t];
+    } else if constexpr (SRC == ACT_BF16) {
+      f[0] = __uint_as_float(r.w[0] << 16); f[1] = __uint_as_float(r.w[0] & 0xFFFF0000u);
+      f[2] = __uint_as_float(r.w[1] << 16); f[3] = __uint_as_float(r.w[1] & 0xFFFF0000u);
+    } else {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) f[t] = (float)(int8_t)(r.w[0] >> (8 * t)) * r.f[0];
+    }
+  }
+  __device__ __forceinline__ void load4(int j, float (&f)[4]) const {
+    Raw r{};
+    load4(j, r);
+    wide(r, f);
   }
   __device__ __forceinline__ float load1(int j) const {
     if constexpr (SRC == ACT_F32) return ((const float*)p)[j];

@@ -290,6 +290,8 @@ RelBiasArgs args_of(const canon_attn_rows* r, const canon_relbias* bias, const u
   a.table = table; a.scale = r->scale; a.causal = r->causal;
   a.n_side = bias->n_starts; a.bidirectional = bias->bidirectional;
   memcpy(a.start, bias->start, sizeof(int32_t) * (size_t)bias->n_starts);
+  for (int n = 0, d = 0; n < a.n_side; ++n)
+    for (const int end = n + 1 < a.n_side ? a.start[n + 1] : a.start[n] + 1; d < end; ++d) a.bucket[d] = (uint8_t)n;
   // buckets without an end, or of more than kRelShort distances
   for (int side = 0; side < (bias->bidirectional ? 2 : 1); ++side)
     for (int n = 0; n < a.n_side; ++n) {

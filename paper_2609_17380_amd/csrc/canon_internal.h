@@ -260,6 +260,7 @@ struct RelBiasArgs {
   int32_t causal, n_side, bidirectional, n_long;
   int32_t start[kRelStarts];
   uint8_t longs[2 * kRelStarts];  // the buckets of more than kRelShort distances
+  uint8_t bucket[kRelFar + 1];    // of the distances up to the last bucket's first, on one side
 };
 hipError_t relbias_fwd_launch(const RelBiasArgs& a, const float* scores, uint16_t* probs, hipStream_t s);
 // rowsum: scratch of relbias_scratch_floats floats, unused where dtable is null

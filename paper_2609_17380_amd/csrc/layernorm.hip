@@ -16,25 +16,44 @@ namespace canon {
 
 namespace {
 
-template <int SRC, int NW, bool TAIL, bool KEEP>
-__global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, NW == 1 ? 4 : 1) void layernorm_fwd_kernel(
+constexpr bool layernorm_ahead(bool keep) { return !keep; }
+
+template <int SRC, int Q, int NW, bool TAIL, bool KEEP>
+__global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void layernorm_fwd_kernel(
     int64_t rows, int cols, ActIn x, const uint16_t* __restrict__ gain, const uint16_t* __restrict__ bias, float eps,
     float inv_d, int y_bf16, void* __restrict__ y, float* __restrict__ mean, float* __restrict__ rstd, ActKeep k) {
   constexpr int kRows = NW == 1 ? 4 : 1;  // rows of a workgroup
-  __shared__ __attribute__((aligned(16))) RegStage st[NW == 1 ? 4 : NW];
+  __shared__ __attribute__((aligned(16))) RowStage<Q> st[NW == 1 ? 4 : NW];
   __shared__ float slot[2][NW];
   const int w = wave_id(), lane = threadIdx.x & 63;
-  const int seg = NW == 1 ? 0 : w * (int)kRegCols;  // this wavefront's part of the row
-  const int n = cols - seg < (int)kRegCols ? cols - seg : (int)kRegCols;
-  for (int64_t row = (int64_t)blockIdx.x * kRows + (NW == 1 ? w : 0); row < rows; row += (int64_t)gridDim.x * kRows) {
+  const int seg = NW == 1 ? 0 : w * 256 * Q;  // this wavefront's part of the row
+  const int n = cols - seg < 256 * Q ? cols - seg : 256 * Q;
+  auto load = [&](int64_t row, float(&v)[Q][4]) __attribute__((always_inline)) {
     const PartIn<SRC> in(x, row, cols, seg);
-    float xv[kRegQ][4];
-    part_load<TAIL>(n, xv, [&](int j, float(&v)[4]) { in.load4(j, v); }, [&](int j) { return in.load1(j); });
+    part_load<TAIL>(0, row < rows ? n : 0, v, [&](int j, float(&f)[4]) { in.load4(j, f); }, [&](int j) { return in.load1(j); });
+  };
+  const int64_t step = (int64_t)gridDim.x * kRows;
+  // the next row is on its way while one is summed and written, where the registers allow it
+  constexpr bool kAhead = layernorm_ahead(KEEP);
+  float next[Q][4];
+  int64_t row = (int64_t)blockIdx.x * kRows + (NW == 1 ? w : 0);
+  if (kAhead) load(row, next);
+  for (; row < rows; row += step) {
+    float xv[Q][4];
+    if (kAhead) {
+#pragma unroll
+      for (int q = 0; q < Q; ++q)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) xv[q][t] = next[q][t];
+      load(row + step, next);
+    } else {
+      load(row, xv);
+    }
     const float sum = wide_row_sum<NW>(st[w], xv, cols, slot[0]);
     const float mu = sum * inv_d;
-    float sq[kRegQ][4];  // what lies behind the row's end is not read by the chains
+    float sq[Q][4];  // what lies behind the row's end is not read by the chains
 #pragma unroll
-    for (int q = 0; q < kRegQ; ++q)
+    for (int q = 0; q < Q; ++q)
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         const float d = xv[q][t] - mu;
@@ -53,7 +72,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, NW == 1 ? 4 : 1) void laye
                       k.steps + row * ((cols + (1 << k.lg) - 1) >> k.lg) + (seg >> k.lg));
     uint16_t* yh = (uint16_t*)y + row * cols + seg;
     float* yf = (float*)y + row * cols + seg;
-    part_store<TAIL>(n,
+    part_store<TAIL, Q>(n,
                      [&](int q, float(&o)[4]) {
 #pragma unroll
                        for (int t = 0; t < 4; ++t) {
@@ -84,27 +103,27 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, NW == 1 ? 4 : 1) void laye
 }
 
 // dx = RN(r RN(RN(gy - m1) - RN(xh m2))): gy = RN(dy g), m1 and m2 the row's means of gy and of RN(gy xh)
-template <int SRC, int NW, bool TAIL>
-__global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, NW == 1 ? 4 : 1) void layernorm_dx_kernel(
+template <int SRC, int Q, int NW, bool TAIL>
+__global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void layernorm_dx_kernel(
     int64_t rows, int cols, ActIn x, const uint16_t* __restrict__ gain, const float* __restrict__ mean,
     const float* __restrict__ rstd, const float* __restrict__ dy, float inv_d, float* __restrict__ dx) {
   constexpr int kRows = NW == 1 ? 4 : 1;
-  __shared__ __attribute__((aligned(16))) RegStage st[NW == 1 ? 4 : NW];
+  __shared__ __attribute__((aligned(16))) RowStage<Q> st[NW == 1 ? 4 : NW];
   __shared__ float slot[2][NW];
   const int w = wave_id();
-  const int seg = NW == 1 ? 0 : w * (int)kRegCols;
-  const int n = cols - seg < (int)kRegCols ? cols - seg : (int)kRegCols;
+  const int seg = NW == 1 ? 0 : w * 256 * Q;
+  const int n = cols - seg < 256 * Q ? cols - seg : 256 * Q;
   for (int64_t row = (int64_t)blockIdx.x * kRows + (NW == 1 ? w : 0); row < rows; row += (int64_t)gridDim.x * kRows) {
     const float mu = mean[row], r = rstd[row];
     const PartIn<SRC> in(x, row, cols, seg);
     const float* dr = dy + row * cols + seg;
-    float xh[kRegQ][4], gy[kRegQ][4], tm[kRegQ][4];
-    part_load<TAIL>(n, xh, [&](int j, float(&v)[4]) { in.load4(j, v); }, [&](int j) { return in.load1(j); });
-    part_load<TAIL>(n, gy, [&](int j, float(&v)[4]) { ldf<4>(dr + j, v); }, [&](int j) { return dr[j]; });
-    part_load<TAIL>(n, tm, [&](int j, float(&v)[4]) { ldb_wide(gain + seg + j, v); },
+    float xh[Q][4], gy[Q][4], tm[Q][4];
+    part_load<TAIL>(0, n, xh, [&](int j, float(&v)[4]) { in.load4(j, v); }, [&](int j) { return in.load1(j); });
+    part_load<TAIL>(0, n, gy, [&](int j, float(&v)[4]) { ldf<4>(dr + j, v); }, [&](int j) { return dr[j]; });
+    part_load<TAIL>(0, n, tm, [&](int j, float(&v)[4]) { ldb_wide(gain + seg + j, v); },
                     [&](int j) { return bf16_wide(gain[seg + j]); });
 #pragma unroll
-    for (int q = 0; q < kRegQ; ++q)
+    for (int q = 0; q < Q; ++q)
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         const float d = xh[q][t] - mu;
@@ -116,7 +135,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, NW == 1 ? 4 : 1) void laye
     const float s2 = wide_row_sum<NW>(st[w], tm, cols, slot[1]);
     const float m1 = s1 * inv_d, m2 = s2 * inv_d;
     float* out = dx + row * cols + seg;
-    part_store<TAIL>(n,
+    part_store<TAIL, Q>(n,
                      [&](int q, float(&o)[4]) {
 #pragma unroll
                        for (int t = 0; t < 4; ++t) {
@@ -181,9 +200,151 @@ __global__ __launch_bounds__(256 / V) void layernorm_part_kernel(int64_t rows, i
   }
 }
 
+// The whole backward in one pass over x and dy: a workgroup takes a chain of 32 rows, wavefront w the columns 256 w .. +255
+// of them, four rows at a time.  A lane's four columns run through the 32 rows in order, so it holds their chains of dgain
+// and dbias; a row's own sums, two to a row, are cut into 8 chunks to a wavefront, 64 chains in all, a lane to a chain over
+// an LDS transpose, folded over the wavefront's 8 chunks and then over the wavefronts.  The next four rows are loaded
+// before the barrier that the sums wait at.
+constexpr int kPassRows = 4;
+template <int SRC, int NW, bool TAIL>
+__global__ __launch_bounds__(64 * NW) void layernorm_pass_kernel(int64_t rows, int cols, ActIn x,
+                                                                 const uint16_t* __restrict__ gain,
+                                                                 const float* __restrict__ mean,
+                                                                 const float* __restrict__ rstd,
+                                                                 const float* __restrict__ dy, float inv_d,
+                                                                 float* __restrict__ dx, float* __restrict__ part) {
+  __shared__ __attribute__((aligned(16))) RegStage st[NW];
+  __shared__ float slot[2][2 * kPassRows][NW];
+  const int w = wave_id(), lane = threadIdx.x & 63;
+  const int j = 256 * w + 4 * lane;  // this lane's first column
+  const int n = cols - j < 4 ? cols - j : 4;  // and how many of its four there are
+  const int64_t nc = (rows + kChunk - 1) / kChunk;
+  // this lane's columns of a row, x as it is stored; 0 where there are none
+  using In = PartIn<SRC>;
+  auto load = [&](int64_t row, typename In::Raw& xr, float(&dv)[4]) __attribute__((always_inline)) {
+    xr = typename In::Raw{};
+#pragma unroll
+    for (int t = 0; t < 4; ++t) dv[t] = 0.0f;
+    if (row >= rows) return;
+    const In in(x, row, cols, 0);
+    const float* dr = dy + row * cols;
+    if (n == 4) {
+      in.load4(j, xr);
+      ldf<4>(dr + j, dv);
+    } else if (TAIL) {
+#pragma unroll
+      for (int t = 0; t < 3; ++t)
+        if (t < n) {
+          in.load1(j, t, xr);
+          dv[t] = dr[j + t];
+        }
+    }
+  };
+  float gv[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+    if (t < n) gv[t] = bf16_wide(gain[j + t]);
+  for (int64_t c = blockIdx.x; c < nc; c += gridDim.x) {
+    const int64_t t0 = c * kChunk;
+    typename In::Raw xr[kPassRows];
+    float dv[kPassRows][4], sg[4] = {0.0f, 0.0f, 0.0f, 0.0f}, sb[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int r = 0; r < kPassRows; ++r) load(t0 + r, xr[r], dv[r]);
+    for (int k = 0; k < kChunk / kPassRows; ++k) {
+      const int64_t t = t0 + kPassRows * k;
+      if (t >= rows) break;
+      float xh[kPassRows][4], gy[kPassRows][4], rs[kPassRows];
+#pragma unroll
+      for (int r = 0; r < kPassRows; ++r) {
+        const int64_t row = t + r < rows ? t + r : rows - 1;
+        const float mu = mean[row];
+        rs[r] = rstd[row];
+        float tm[4], xv[4];
+        In::wide(xr[r], xv);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float d = xv[i] - mu;
+          xh[r][i] = d * rs[r];
+          gy[r][i] = dv[r][i] * gv[i];
+          tm[i] = gy[r][i] * xh[r][i];
+          if (i >= n) gy[r][i] = tm[i] = 0.0f;  // no column: a term of +0
+          const float pr = dv[r][i] * xh[r][i];
+          if (t + r < rows) {
+            sg[i] = sg[i] + pr;
+            sb[i] = sb[i] + dv[r][i];
+          }
+        }
+        st[w].put(2 * r, lane, gy[r]);
+        st[w].put(2 * r + 1, lane, tm);
+      }
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int r = 0; r < kPassRows; ++r) load(t + kPassRows + r < t0 + kChunk ? t + kPassRows + r : rows, xr[r], dv[r]);
+      float p = 0.0f;  // the chain of chunk lane % 8 of sum lane / 8
+#pragma unroll
+      for (int i = 0; i < kChunk / 4; ++i) {
+        const float4 v = st[w].vec(lane, i);
+        p = p + v.x; p = p + v.y; p = p + v.z; p = p + v.w;
+      }
+      auto add = [](uint32_t a, uint32_t b) {
+        const float s = __uint_as_float(a) + __uint_as_float(b);
+        return __float_as_uint(s);
+      };
+      p = __uint_as_float(lanes_join(__float_as_uint(p), 8, add));
+      if ((lane & 7) == 0) slot[k & 1][lane >> 3][w] = p;
+      __syncthreads();
+      float m[2 * kPassRows];
+      if constexpr (NW <= 8) {
+        float s = (lane & 7) < NW ? slot[k & 1][lane >> 3][lane & 7] : 0.0f;
+        s = __uint_as_float(lanes_join(__float_as_uint(s), 8, add)) * inv_d;
+#pragma unroll
+        for (int i = 0; i < 2 * kPassRows; ++i) m[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(s), 8 * i));
+      } else {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          float s = slot[k & 1][4 * half + (lane >> 4)][lane & 15];
+          s = __uint_as_float(lanes_join(__float_as_uint(s), 16, add)) * inv_d;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            m[4 * half + i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(s), 16 * i));
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < kPassRows; ++r) {
+        if (t + r >= rows) break;
+        float o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float a = gy[r][i] - m[2 * r];
+          const float b = xh[r][i] * m[2 * r + 1];
+          const float d = a - b;
+          o[i] = rs[r] * d;
+        }
+        float* out = dx + (t + r) * cols + j;
+        if (n == 4) {
+          stf<4>(out, o);
+        } else if (TAIL) {
+#pragma unroll
+          for (int i = 0; i < 3; ++i)
+            if (i < n) out[i] = o[i];
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < n) {
+        part[c * cols + j + i] = sg[i];
+        part[(nc + c) * cols + j + i] = sb[i];
+      }
+  }
+}
+
 // Algorithm 2 over the chunk partials of a column: 16 wavefronts take 64 columns, wavefront g folds the aligned
-// power-of-two block of chunks [g G, g G + G), and the block results are folded with the pass-through rule.
+// power-of-two block of chunks [g G, g G + G), and the block results are folded with the pass-through rule.  Within a block
+// 16 partials at a time are loaded and folded as a tree, those past the last chunk as +0 (no partial is -0); only blocks of
+// more need Algorithm 2's stack (whose levels are indexed in scratch memory).
 constexpr int kFoldBlocks = 16;
+constexpr int kFoldUnit = 16;
 __global__ __launch_bounds__(64 * kFoldBlocks) void column_fold_kernel(int64_t nc, int64_t cols, int64_t inner,
                                                                        const float* __restrict__ part,
                                                                        float* __restrict__ out0, float* __restrict__ out1) {
@@ -191,23 +352,31 @@ __global__ __launch_bounds__(64 * kFoldBlocks) void column_fold_kernel(int64_t n
   float* out = blockIdx.y ? out1 : out0;
   if (!out) return;
   part += blockIdx.y * nc * cols;
-  const int lane = threadIdx.x & 63, g = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, g = wave_id();
   const int64_t col = (int64_t)blockIdx.x * 64 + lane;
   const int64_t G = block_chunks(nc, kFoldBlocks);
   const int64_t c0 = g * G, c1 = c0 + G < nc ? c0 + G : nc;
-  LocalFoldN<22> f;
-  if (col < cols) {
-    int64_t c = c0;
-    for (; c + 8 <= c1; c += 8) {
-      float p[8];
+  auto unit = [&](int64_t c) __attribute__((always_inline)) {
+    float p[kFoldUnit];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) p[i] = part[(c + i) * cols + col];
+    for (int i = 0; i < kFoldUnit; ++i) p[i] = c + i < c1 ? part[(c + i) * cols + col] : 0.0f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) f.push(p[i]);
+    for (int d = 1; d < kFoldUnit; d <<= 1)
+#pragma unroll
+      for (int i = 0; i + d < kFoldUnit; i += 2 * d) p[i] = p[i] + p[i + d];
+    return p[0];
+  };
+  float r = 0.0f;
+  if (col < cols && c0 < c1) {
+    if (G <= kFoldUnit) {
+      r = unit(c0);
+    } else {
+      LocalFoldN<18> f;
+      for (int64_t c = c0; c < c1; c += kFoldUnit) f.push(unit(c));
+      r = f.result();
     }
-    for (; c < c1; ++c) f.push(part[c * cols + col]);
   }
-  res[g][lane] = f.result();
+  res[g][lane] = r;
   __syncthreads();
   if (g == 0 && col < cols) {
     float v[kFoldBlocks];
@@ -216,20 +385,13 @@ __global__ __launch_bounds__(64 * kFoldBlocks) void column_fold_kernel(int64_t n
 #pragma unroll
     for (int d = 1; d < kFoldBlocks; d <<= 1)
 #pragma unroll
-      for (int q = 0; q + d < kFoldBlocks; q += 2 * d)
-        if ((q + d) * G < nc) v[q] = v[q] + v[q + d];
+      for (int q = 0; q + d < kFoldBlocks; q += 2 * d) v[q] = v[q] + v[q + d];
     out[inner > 0 ? (col % inner) * (cols / inner) + col / inner : col] = v[0];
   }
 }
 
 constexpr int64_t kMaxBlocks = 1 << 20;
-
-// wavefronts that hold a row of cols terms
-int row_waves(int64_t cols) {
-  int nw = 1;
-  while (nw * kRegCols < cols) nw <<= 1;
-  return nw;
-}
+constexpr int64_t kPassCols = 4096;  // 16 wavefronts of 256 columns
 
 }  // namespace
 
@@ -241,13 +403,15 @@ hipError_t column_fold_launch(int64_t rows, int64_t cols, int64_t inner, const f
   return hipGetLastError();
 }
 
-#define CANON_LN_WAVES(K, SRC)                \
-  switch (row_waves(cols)) {                  \
-    case 1: K(SRC, 1); break;                 \
-    case 2: K(SRC, 2); break;                 \
-    case 4: K(SRC, 4); break;                 \
-    case 8: K(SRC, 8); break;                 \
-    default: K(SRC, 16); break;               \
+#define CANON_LN_ROWS(K, SRC)                 \
+  switch (row_shape(cols)) {                  \
+    case 2: K(SRC, 2, 1); break;              \
+    case 4: K(SRC, 4, 1); break;              \
+    case 8: K(SRC, 8, 1); break;              \
+    case 16: K(SRC, 8, 2); break;             \
+    case 32: K(SRC, 8, 4); break;             \
+    case 64: K(SRC, 8, 8); break;             \
+    default: K(SRC, 8, 16); break;            \
   }
 
 hipError_t layernorm_fwd_launch(int64_t rows, int64_t cols, const ActIn& x, const uint16_t* gain, const uint16_t* bias,
@@ -257,24 +421,26 @@ hipError_t layernorm_fwd_launch(int64_t rows, int64_t cols, const ActIn& x, cons
   const float inv_d = (float)(1.0 / (double)cols);  // RN32(1/cols), correctly rounded
   const int nw = row_waves(cols);
   const int64_t blocks = nw == 1 ? (rows + 3) / 4 : rows;
-  const dim3 grid((unsigned)(blocks < kMaxBlocks ? blocks : kMaxBlocks)), wg(nw == 1 ? 256 : 64 * nw);
-#define CANON_LN_K(SRC, NW, TAIL, KEEP)                                                                                \
-  hipLaunchKernelGGL((layernorm_fwd_kernel<SRC, NW, TAIL, KEEP>), grid, wg, 0, s, rows, (int)cols, x, gain, bias, eps, \
+  // rows that are loaded ahead: no more workgroups than are on the chip at once (16 wavefronts to a CU)
+  const int64_t most = layernorm_ahead(k.codes) ? device_cus() * (nw == 1 ? 4 : 16 / nw) : kMaxBlocks;
+  const dim3 grid((unsigned)(blocks < most ? blocks : most)), wg(nw == 1 ? 256 : 64 * nw);
+#define CANON_LN_K(SRC, Q, NW, TAIL, KEEP)                                                                               \
+  hipLaunchKernelGGL((layernorm_fwd_kernel<SRC, Q, NW, TAIL, KEEP>), grid, wg, 0, s, rows, (int)cols, x, gain, bias, eps, \
                      inv_d, y_bf16, y, mean, rstd, k)
-#define CANON_LN(SRC, NW)                          \
+#define CANON_LN(SRC, Q, NW)                         \
   do {                                             \
     if (cols % 4 == 0) {                           \
-      if (k.codes) CANON_LN_K(SRC, NW, false, true); \
-      else CANON_LN_K(SRC, NW, false, false);      \
+      if (k.codes) CANON_LN_K(SRC, Q, NW, false, true); \
+      else CANON_LN_K(SRC, Q, NW, false, false);      \
     } else {                                       \
-      if (k.codes) CANON_LN_K(SRC, NW, true, true);  \
-      else CANON_LN_K(SRC, NW, true, false);       \
+      if (k.codes) CANON_LN_K(SRC, Q, NW, true, true);  \
+      else CANON_LN_K(SRC, Q, NW, true, false);       \
     }                                              \
   } while (0)
   if (x.src == ACT_F32) {
-    CANON_LN_WAVES(CANON_LN, ACT_F32)
+    CANON_LN_ROWS(CANON_LN, ACT_F32)
   } else {
-    CANON_LN_WAVES(CANON_LN, ACT_BF16)
+    CANON_LN_ROWS(CANON_LN, ACT_BF16)
   }
 #undef CANON_LN
 #undef CANON_LN_K
@@ -288,6 +454,36 @@ hipError_t layernorm_bwd_launch(int64_t rows, int64_t cols, const ActIn& x, cons
                                 hipStream_t s) {
   const float inv_d = (float)(1.0 / (double)cols);
   const int64_t nc = (rows + kChunk - 1) / kChunk;
+  // One pass over x and dy where its workgroups, one to 32 rows, are enough to fill the chip: 8192 x 2048 in 45 us against
+  // 66 in two passes, 2048 x 2048 (64 workgroups) in 29 against 21.
+  const bool once = (dgain || dbias) && cols <= kPassCols && nc >= device_cus();
+  if (once) {
+    const dim3 grid((unsigned)(nc < kMaxBlocks ? nc : kMaxBlocks));
+#define CANON_LN_PASS(SRC, NW)                                                                                          \
+  do {                                                                                                                  \
+    if (cols % 4 == 0)                                                                                                  \
+      hipLaunchKernelGGL((layernorm_pass_kernel<SRC, NW, false>), grid, dim3(64 * NW), 0, s, rows, (int)cols, x, gain,  \
+                         mean, rstd, dy, inv_d, dx, part);                                                              \
+    else                                                                                                                \
+      hipLaunchKernelGGL((layernorm_pass_kernel<SRC, NW, true>), grid, dim3(64 * NW), 0, s, rows, (int)cols, x, gain,   \
+                         mean, rstd, dy, inv_d, dx, part);                                                              \
+  } while (0)
+#define CANON_LN_PASS_WAVES(SRC)                   \
+  do {                                             \
+    if (cols <= 512) CANON_LN_PASS(SRC, 2);        \
+    else if (cols <= 1024) CANON_LN_PASS(SRC, 4);  \
+    else if (cols <= 2048) CANON_LN_PASS(SRC, 8);  \
+    else CANON_LN_PASS(SRC, 16);                   \
+  } while (0)
+    if (x.src == ACT_F32) CANON_LN_PASS_WAVES(ACT_F32);
+    else if (x.src == ACT_BF16) CANON_LN_PASS_WAVES(ACT_BF16);
+    else CANON_LN_PASS_WAVES(ACT_Q8);
+#undef CANON_LN_PASS_WAVES
+#undef CANON_LN_PASS
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    return column_fold_launch(rows, cols, 0, part, dgain, dbias, s);
+  }
   if ((dgain || dbias) && rows > 0) {
     const dim3 grid((unsigned)((cols + 255) / 256), (unsigned)(nc < 65535 ? nc : 65535));
 #define CANON_LN_PART(SRC)                                                                                            \
@@ -314,21 +510,21 @@ hipError_t layernorm_bwd_launch(int64_t rows, int64_t cols, const ActIn& x, cons
   const int nw = row_waves(cols);
   const int64_t blocks = nw == 1 ? (rows + 3) / 4 : rows;
   const dim3 grid((unsigned)(blocks < kMaxBlocks ? blocks : kMaxBlocks)), wg(nw == 1 ? 256 : 64 * nw);
-#define CANON_LN(SRC, NW)                                                                                              \
+#define CANON_LN(SRC, Q, NW)                                                                                             \
   do {                                                                                                                 \
     if (cols % 4 == 0)                                                                                                 \
-      hipLaunchKernelGGL((layernorm_dx_kernel<SRC, NW, false>), grid, wg, 0, s, rows, (int)cols, x, gain, mean, rstd,  \
+      hipLaunchKernelGGL((layernorm_dx_kernel<SRC, Q, NW, false>), grid, wg, 0, s, rows, (int)cols, x, gain, mean, rstd,  \
                          dy, inv_d, dx);                                                                                   \
     else                                                                                                               \
-      hipLaunchKernelGGL((layernorm_dx_kernel<SRC, NW, true>), grid, wg, 0, s, rows, (int)cols, x, gain, mean, rstd,   \
+      hipLaunchKernelGGL((layernorm_dx_kernel<SRC, Q, NW, true>), grid, wg, 0, s, rows, (int)cols, x, gain, mean, rstd,   \
                          dy, inv_d, dx);                                                                                   \
   } while (0)
   if (x.src == ACT_F32) {
-    CANON_LN_WAVES(CANON_LN, ACT_F32)
+    CANON_LN_ROWS(CANON_LN, ACT_F32)
   } else if (x.src == ACT_BF16) {
-    CANON_LN_WAVES(CANON_LN, ACT_BF16)
+    CANON_LN_ROWS(CANON_LN, ACT_BF16)
   } else {
-    CANON_LN_WAVES(CANON_LN, ACT_Q8)
+    CANON_LN_ROWS(CANON_LN, ACT_Q8)
   }
 #undef CANON_LN
   return hipGetLastError();

@@ -4,7 +4,7 @@
 // A row of up to 2048 keys is held by one wavefront, a longer one by a workgroup of up to 16 (wide_row_sum): scores,
 // probabilities and their gradient are read from memory once.  The keys that a query sees are one range j0 <= j < j1
 // (lengths, causality and the window all cut it from an end), so no mask is read.  A head's biases, by distance up to
-// the last bucket's first, are laid out in LDS once for the queries of a workgroup.  Bound: HBM.
+// the last bucket's first, are laid out in LDS while the row is on its way.  Bound: HBM.
 #include <hip/hip_runtime.h>
 
 #include "canon_dev.h"
@@ -15,9 +15,10 @@ namespace canon {
 
 namespace {
 
+constexpr int kEdge = 256;              // entries of either end of the bias table again, for the keys of a vector across it
 constexpr int kQueries = 4;             // queries that a wavefront (or, of longer rows, a workgroup) takes in turn
 constexpr int64_t kFarPos = 1 << 20;    // beyond every key's distance and the last bucket
-constexpr int64_t kMaxBlocks = 1 << 20;
+constexpr int64_t kMaxBlocks = 1 << 20;  // of up to 1024 threads: 2^30 of 2^32
 
 // bucket of a distance on one side: the last one that begins at or before it
 __device__ __forceinline__ int bucket_of(const int32_t* start, int n, int d) {
@@ -30,7 +31,7 @@ __device__ __forceinline__ int bucket_of(const int32_t* start, int n, int d) {
   return lo;
 }
 
-// The keys j0 <= j < j1 that query i of sequence b sees, and its position (cut to +-kFarPos, which leaves every bucket as
+// The keys j0 <= j < j1 that query i of sequence b sees (none behind the last query), and its position (cut to +-kFarPos, which leaves every bucket as
 // it is).
 struct Query {
   int j0, j1, pos;
@@ -44,7 +45,7 @@ __device__ __forceinline__ Query query_of(const RelBiasArgs& a, int64_t b, int64
     lo = pos - a.window + 1 > lo ? pos - a.window + 1 : lo;
     hi = pos + a.window < hi ? pos + a.window : hi;
   }
-  if (a.q_lens && i >= a.q_lens[b]) hi = 0;
+  if (i >= a.q_len || (a.q_lens && i >= a.q_lens[b])) hi = 0;
   if (hi <= lo) lo = hi = 0;
   Query q;
   q.j0 = __builtin_amdgcn_readfirstlane((int)lo);
@@ -53,244 +54,239 @@ __device__ __forceinline__ Query query_of(const RelBiasArgs& a, int64_t b, int64
   return q;
 }
 
-template <int NW, bool TAIL>
-__global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, NW == 1 ? 4 : 1) void relbias_fwd_kernel(
+// What a query sees of a wavefront's part of the row, n keys from `seg` on: its elements from .. end - 1, all of them in
+// the vectors q0 .. q1 - 1; upto: the end of the vectors that hold them, within the part.
+struct Part {
+  int from, end, upto, q0, q1;
+  __device__ __forceinline__ bool sees(int j) const { return (unsigned)(j - from) < (unsigned)(end - from); }
+};
+__device__ __forceinline__ Part part_of(const Query& q, int seg, int n) {
+  Part p;
+  p.from = q.j0 - seg > 0 ? q.j0 - seg : 0;
+  p.end = q.j1 - seg < n ? q.j1 - seg : n;
+  if (p.end <= p.from) p.from = p.end = 0;
+  p.upto = p.end + 3 < n ? (p.end + 3) & ~3 : n;
+  if (p.end == 0) p.upto = 0;
+  p.q0 = p.from >> 8;
+  p.q1 = (p.end + 255) >> 8;
+  return p;
+}
+
+template <int Q, int NW, bool TAIL>
+__global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbias_fwd_kernel(
     RelBiasArgs a, int64_t blocks, int64_t per_head, const float* __restrict__ scores, uint16_t* __restrict__ probs) {
   constexpr int kRows = NW == 1 ? 4 : 1;
-  __shared__ __attribute__((aligned(16))) RegStage st[NW == 1 ? 4 : NW];
+  __shared__ __attribute__((aligned(16))) RowStage<Q> st[NW == 1 ? 4 : NW];
   __shared__ float slot[2][NW], top[NW];
-  extern __shared__ float near_[];  // bias by position: of the key less the query's, the near side of the last buckets
+  extern __shared__ float near_[];  // bias by place: key less query, from -far to `right`, and kEdge more on either side
   const int w = wave_id(), lane = threadIdx.x & 63;
   const int far = a.start[a.n_side - 1], right = a.bidirectional ? far : 0;
-  const int seg = NW == 1 ? 0 : w * (int)kRegCols;  // this wavefront's part of the row
-  const int n = (int)a.k_len - seg < (int)kRegCols ? (int)a.k_len - seg : (int)kRegCols;
+  const int seg = NW == 1 ? 0 : w * 256 * Q;  // this wavefront's part of the row
+  const int n = (int)a.k_len - seg < 256 * Q ? (int)a.k_len - seg : 256 * Q;
+  const int parts = ((int)a.k_len + 256 * Q - 1) / (256 * Q);
   int turn = 0;  // rows in turn take one of two slots, so that a barrier lies between a slot's reads and its next writes
   for (int64_t blk = blockIdx.x; blk < blocks; blk += gridDim.x) {
     const int64_t bh = blk / per_head, b = bh / a.heads, h = bh - b * a.heads;
-    const int64_t i0 = (blk - bh * per_head) * (kRows * kQueries);
-    __syncthreads();  // the last block's biases are read
-    for (int e = threadIdx.x; e <= far + right; e += blockDim.x) {
-      const int d = far - e;  // query less key: far .. -right
-      const int k = d >= 0 ? bucket_of(a.start, a.n_side, d) : a.n_side + bucket_of(a.start, a.n_side, -d);
-      near_[e] = bf16_to_f32(a.table[k * a.heads + h]);
+    const int64_t i = (blk - bh * per_head) * kRows + (NW == 1 ? w : 0);
+    const Query qy = query_of(a, b, i);
+    const Part pt = part_of(qy, seg, n);
+    const int64_t row = (bh * a.q_len + i) * a.ld + seg;
+    const float* rr = scores + row;
+    uint16_t* pr = probs + row;
+    float e[Q][4];
+    part_load<TAIL>(pt.from, pt.upto, e, [&](int j, float(&v)[4]) { ldf<4>(rr + j, v); }, [&](int j) { return rr[j]; });
+    if (blk != (int64_t)blockIdx.x) __syncthreads();  // the last row's biases are read
+    for (int k = threadIdx.x; k <= far + right + 2 * kEdge; k += blockDim.x) {
+      int d = far + kEdge - k;  // query less key
+      d = d > far ? far : d < -right ? -right : d;
+      near_[k] = bf16_to_f32(a.table[(d >= 0 ? a.bucket[d] : a.n_side + a.bucket[-d]) * a.heads + h]);
     }
     __syncthreads();
-    for (int it = 0; it < kQueries; ++it) {
-      const int64_t i = i0 + it * kRows + (NW == 1 ? w : 0);
-      if (i >= a.q_len) break;  // the same for every wavefront that shares the row
-      const Query qy = query_of(a, b, i);
-      const int j0 = qy.j0 - seg, span = qy.j1 - qy.j0, first = far + seg - qy.pos;  // near_ entry of the part's first key
-      const float* rr = scores + (bh * a.q_len + i) * a.ld + seg;
-      auto any = [&](int q) { return 256 * q < j0 + span && 256 * q + 255 >= j0; };
-      float e[kRegQ][4];
-      part_load<TAIL>(n < j0 + span ? n : j0 + span + 3 < n ? j0 + span + 3 : n, e,
-                      [&](int j, float(&v)[4]) {
-                        if (j + 3 >= j0) ldf<4>(rr + j, v);
-                        else v[0] = v[1] = v[2] = v[3] = 0.0f;
-                      },
-                      [&](int j) { return rr[j]; });
-      float m = -__builtin_inff();
+    if (i >= a.q_len) continue;  // NW = 1: a wavefront without a row
+    const int first = far + seg - qy.pos;  // the part's first key in near_, behind its edge
+    float m = -__builtin_inff();
 #pragma unroll
-      for (int q = 0; q < kRegQ; ++q) {
-        if (!any(q)) {
+    for (int q = 0; q < Q; ++q) {
+      if (q < pt.q0 || q >= pt.q1) continue;
+      const int j = 256 * q + 4 * lane;
+      float bias[4];
+      if (first + 256 * q <= -255) {
+        bias[0] = bias[1] = bias[2] = bias[3] = near_[0];
+      } else if (first + 256 * q >= far + right) {
+        bias[0] = bias[1] = bias[2] = bias[3] = near_[far + right + kEdge];
+      } else {
 #pragma unroll
-          for (int t = 0; t < 4; ++t) e[q][t] = -__builtin_inff();
-          continue;
-        }
-        const int j = 256 * q + 4 * lane;
-        const bool left = first + 256 * q + 255 <= 0;
-        float bias[4];
-        if (left || first + 256 * q >= far + right) {
-          bias[0] = bias[1] = bias[2] = bias[3] = near_[left ? 0 : far + right];
-        } else {
-#pragma unroll
-          for (int t = 0; t < 4; ++t) {
-            const int k = first + j + t;
-            bias[t] = near_[k < 0 ? 0 : k > far + right ? far + right : k];
-          }
-        }
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const float x = e[q][t] * a.scale;
-          const float z = x + bias[t];
-          e[q][t] = (unsigned)(j + t - j0) < (unsigned)span ? z : -__builtin_inff();  // unseen: an e of +0
-          m = fmaxf(m, e[q][t]);
-        }
+        for (int t = 0; t < 4; ++t) bias[t] = near_[first + kEdge + j + t];
       }
-      m = wave_most(m);
-      if constexpr (NW > 1) {
-        if (lane == 0) top[w] = m;
-        __syncthreads();
-        m = wave_most(lane < NW ? top[lane] : -__builtin_inff());
-      }
-      // a row whose seen scores are all -inf has e = cexp(-inf) = +0, not cexp(-inf - -inf)
-      m = m == -__builtin_inff() ? 0.0f : m;
 #pragma unroll
-      for (int q = 0; q < kRegQ; ++q) {
-#pragma unroll
-        for (int t = 0; t < 4; ++t) e[q][t] = any(q) ? cexp_neg(e[q][t] - m) : 0.0f;
+      for (int t = 0; t < 4; ++t) {
+        const float x = e[q][t] * a.scale;
+        const float z = x + bias[t];
+        e[q][t] = pt.sees(j + t) ? z : -__builtin_inff();  // unseen: an e of +0
+        m = fmaxf(m, e[q][t]);
       }
-      turn ^= 1;
-      const float S = wide_row_sum<NW>(st[w], e, (int)a.k_len, slot[turn]);
-      const float rcp = S == 0.0f ? 0.0f : 1.0f / S;
-      uint16_t* pr = probs + (bh * a.q_len + i) * a.ld + seg;
-      if (S == S) {
-        part_store<TAIL>(n,
-                         [&](int q, float(&o)[4]) {
+    }
+    m = wave_most(m);
+    if constexpr (NW > 1) {
+      if (lane == 0) top[w] = m;
+      __syncthreads();
+      m = wave_most(lane < NW ? top[lane] : -__builtin_inff());
+    }
+    // a row whose seen scores are all -inf has e = cexp(-inf) = +0, not cexp(-inf - -inf)
+    m = m == -__builtin_inff() ? 0.0f : m;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      if (q < pt.q0 || q >= pt.q1) continue;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) e[q][t] = cexp_neg(e[q][t] - m);
+      st[w].put(q, lane, e[q]);
+    }
+    turn ^= 1;
+    const float S = wide_join<NW>(st[w].span_sum(pt.q0, pt.q1), parts, slot[turn]);
+    const float rcp = S == 0.0f ? 0.0f : 1.0f / S;
+    if (S == S) {
+      part_store<TAIL, Q>(n,
+                       [&](int q, float(&o)[4]) {
+                         if (q >= pt.q0 && q < pt.q1) {
 #pragma unroll
                            for (int t = 0; t < 4; ++t) o[t] = e[q][t] * rcp;
-                         },
-                         [&](int j, const float(&o)[4]) { stb_arith(pr + j, o); },
-                         [&](int j, float o) { pr[j] = bf16_arith(o); });
-      } else {  // a NaN among the seen: every seen key's, and still +0 elsewhere
-        for (int j = lane; j < n; j += 64) pr[j] = (unsigned)(j - j0) < (unsigned)span ? 0x7FC0 : 0;
-      }
+                         } else {
+                           o[0] = o[1] = o[2] = o[3] = 0.0f;
+                         }
+                       },
+                       [&](int j, const float(&o)[4]) { stb_arith(pr + j, o); },
+                       [&](int j, float o) { pr[j] = bf16_arith(o); });
+    } else {  // a NaN among the seen: every seen key's, and still +0 elsewhere
+      for (int j = lane; j < n; j += 64) pr[j] = pt.sees(j) ? 0x7FC0 : 0;
     }
   }
 }
 
 // ds = RN(P RN(dP - D)), D = R1 over the keys of RN(P dP); dS = bf16(RN(ds scale)).  rowsum [batch][q_len][heads][buckets]:
 // for every bucket R1 over the keys of ds, those outside it as +0 terms.  A bucket of up to 32 distances touches at most
-// two chunks, whose chains one lane runs and adds (their sum is the fold whatever lies between); a longer one is summed
+// two chunks, whose chains two lanes run and add (their sum is the fold whatever lies between); a longer one is summed
 // chunk by chunk, a lane to a chunk, like the row.
-template <int NW, bool TAIL>
-__global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, NW == 1 ? 4 : 1) void relbias_bwd_kernel(
+template <int Q, int NW, bool TAIL>
+__global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbias_bwd_kernel(
     RelBiasArgs a, int64_t blocks, int64_t per_head, const uint16_t* __restrict__ probs,
     const float* __restrict__ dprobs, uint16_t* __restrict__ dscores, float* __restrict__ rowsum) {
   constexpr int kRows = NW == 1 ? 4 : 1;
-  __shared__ __attribute__((aligned(16))) RegStage st[NW == 1 ? 4 : NW];
+  __shared__ __attribute__((aligned(16))) RowStage<Q> st[NW == 1 ? 4 : NW];
   __shared__ float slot[2][NW];
   __shared__ float part[2][NW];
   __shared__ int lo_[2 * kRelStarts], hi_[2 * kRelStarts];  // the keys of a bucket, less the query's position: lo <= . < hi
   const int w = wave_id(), lane = threadIdx.x & 63;
-  const int seg = NW == 1 ? 0 : w * (int)kRegCols;
-  const int n = (int)a.k_len - seg < (int)kRegCols ? (int)a.k_len - seg : (int)kRegCols;
+  const int seg = NW == 1 ? 0 : w * 256 * Q;
+  const int n = (int)a.k_len - seg < 256 * Q ? (int)a.k_len - seg : 256 * Q;
+  const int parts = ((int)a.k_len + 256 * Q - 1) / (256 * Q);
   const int nb = a.n_side * (a.bidirectional ? 2 : 1);
   int turn = 0;  // as above
-  if (rowsum) {
-    for (int k = threadIdx.x; k < nb; k += blockDim.x) {
-      const int side = k < a.n_side ? k : k - a.n_side;
-      const int d0 = a.start[side], d1 = side + 1 < a.n_side ? a.start[side + 1] : 2 * (int)kFarPos;
-      if (k < a.n_side) {
-        lo_[k] = 1 - d1;
-        hi_[k] = d0 == d1 ? 1 - d1 : d0 == 0 && !a.bidirectional ? 2 * (int)kFarPos : 1 - d0;
-      } else {
-        lo_[k] = d0 > 0 ? d0 : 1;
-        hi_[k] = d1;
-      }
-    }
-    __syncthreads();
-  }
   for (int64_t blk = blockIdx.x; blk < blocks; blk += gridDim.x) {
     const int64_t bh = blk / per_head, b = bh / a.heads, h = bh - b * a.heads;
-    const int64_t i0 = (blk - bh * per_head) * (kRows * kQueries);
-    for (int it = 0; it < kQueries; ++it) {
-      const int64_t i = i0 + it * kRows + (NW == 1 ? w : 0);
-      if (i >= a.q_len) break;
-      const Query qy = query_of(a, b, i);
-      const int j0 = qy.j0 - seg, span = qy.j1 - qy.j0;
-      const int64_t at = (bh * a.q_len + i) * a.ld + seg;
-      const uint16_t* pr = probs + at;
-      const float* dr = dprobs + at;
-      const int upto = n < j0 + span ? n : j0 + span + 3 < n ? j0 + span + 3 : n;  // whole vectors of what is seen
-      float p[kRegQ][4], dp[kRegQ][4], e[kRegQ][4];
-      part_load<TAIL>(upto, p,
-                      [&](int j, float(&v)[4]) {
-                        if (j + 3 >= j0) ldb_wide(pr + j, v);
-                        else v[0] = v[1] = v[2] = v[3] = 0.0f;
-                      },
-                      [&](int j) { return bf16_wide(pr[j]); });
-      part_load<TAIL>(upto, dp,
-                      [&](int j, float(&v)[4]) {
-                        if (j + 3 >= j0) ldf<4>(dr + j, v);
-                        else v[0] = v[1] = v[2] = v[3] = 0.0f;
-                      },
-                      [&](int j) { return dr[j]; });
-      auto seen = [&](int q, int t, int first) { return (unsigned)(256 * q + 4 * lane + t - first) < (unsigned)span; };
-#pragma unroll
-      for (int q = 0; q < kRegQ; ++q)
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const float x = p[q][t] * dp[q][t];
-          e[q][t] = seen(q, t, j0) ? x : 0.0f;
+    const int64_t i = (blk - bh * per_head) * kRows + (NW == 1 ? w : 0);
+    const Query qy = query_of(a, b, i);
+    const Part pt = part_of(qy, seg, n);
+    const int64_t row = (bh * a.q_len + i) * a.ld + seg;
+    const uint16_t* pr = probs + row;
+    const float* dr = dprobs + row;
+    uint16_t* sr = dscores + row;
+    float p[Q][4], dp[Q][4];
+    part_load<TAIL>(pt.from, pt.upto, p, [&](int j, float(&v)[4]) { ldb_wide(pr + j, v); },
+                    [&](int j) { return bf16_wide(pr[j]); });
+    part_load<TAIL>(pt.from, pt.upto, dp, [&](int j, float(&v)[4]) { ldf<4>(dr + j, v); }, [&](int j) { return dr[j]; });
+    if (rowsum && blk == (int64_t)blockIdx.x) {
+      for (int k = threadIdx.x; k < nb; k += blockDim.x) {
+        const int side = k < a.n_side ? k : k - a.n_side;
+        const int d0 = a.start[side], d1 = side + 1 < a.n_side ? a.start[side + 1] : 2 * (int)kFarPos;
+        if (k < a.n_side) {
+          lo_[k] = 1 - d1;
+          hi_[k] = d0 == d1 ? 1 - d1 : d0 == 0 && !a.bidirectional ? 2 * (int)kFarPos : 1 - d0;
+        } else {
+          lo_[k] = d0 > 0 ? d0 : 1;
+          hi_[k] = d1;
         }
-      turn ^= 1;
-      const float D = wide_row_sum<NW>(st[w], e, (int)a.k_len, slot[turn]);
-      const int first = again(j0);
-#pragma unroll
-      for (int q = 0; q < kRegQ; ++q)
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const float d = dp[q][t] - D;
-          const float x = p[q][t] * d;
-          e[q][t] = seen(q, t, first) ? x : 0.0f;
-        }
-      uint16_t* sr = dscores + at;
-      part_store<TAIL>(n,
-                       [&](int q, float(&o)[4]) {
-#pragma unroll
-                         for (int t = 0; t < 4; ++t) o[t] = e[q][t] * a.scale;
-                       },
-                       [&](int j, const float(&o)[4]) { stb_arith(sr + j, o); },
-                       [&](int j, float o) { sr[j] = bf16_arith(o); });
-      if (!rowsum) continue;
-      float* out = rowsum + ((b * a.q_len + i) * a.heads + h) * nb;
-      // the row's ds, a chunk to a row of LDS (a wavefront's own, its LDS operations in order)
-#pragma unroll
-      for (int q = 0; q < kRegQ; ++q) {
-        const int local = 256 * q + 4 * lane;
-        *reinterpret_cast<float4*>(&st[w].t[local >> 5][local & 31]) = make_float4(e[q][0], e[q][1], e[q][2], e[q][3]);
       }
-      if constexpr (NW > 1) __syncthreads();
-      else __builtin_amdgcn_wave_barrier();
-      for (int k = NW == 1 ? lane : (int)threadIdx.x; k < nb; k += NW == 1 ? 64 : 64 * NW) {
-        const int lo = lo_[k], hi = hi_[k];
-        if (hi - lo > kRelShort) continue;
-        const int b0 = qy.pos + lo > qy.j0 ? qy.pos + lo : qy.j0, b1 = qy.pos + hi < qy.j1 ? qy.pos + hi : qy.j1;
-        const int mid = (b0 | 31) + 1;  // the next chunk's first key
-        float s0 = 0.0f, s1 = 0.0f;
-        for (int j = b0; j < b1; j += 4) {
-          float v[4];
-#pragma unroll
-          for (int t = 0; t < 4; ++t) {
-            const int u = j + t < b1 ? j + t : b0;
-            v[t] = st[NW == 1 ? w : u >> 11].t[(u >> 5) & 63][u & 31];
-          }
-#pragma unroll
-          for (int t = 0; t < 4; ++t) {
-            s0 = s0 + (j + t < b1 && j + t < mid ? v[t] : 0.0f);
-            s1 = s1 + (j + t < b1 && j + t >= mid ? v[t] : 0.0f);
-          }
-        }
-        out[k] = s0 + s1;
-      }
-      for (int l = 0; l < a.n_long; ++l) {
-        const int k = a.longs[l];
-        const int lo = lo_[k], hi = hi_[k];
-        const int b0 = (qy.pos + lo > qy.j0 ? qy.pos + lo : qy.j0) - seg, b1 = (qy.pos + hi < qy.j1 ? qy.pos + hi : qy.j1) - seg;
-        float sum = 0.0f;
-        if (b0 < b1 && b0 < (int)kRegCols && b1 > 0) {  // the same for the whole wavefront
-          const int c0 = b0 - 32 * lane, len = b1 - b0;
-#pragma unroll
-          for (int t = 0; t < kChunk; t += 4) {
-            const float4 v = *reinterpret_cast<const float4*>(&st[w].t[lane][t]);
-            sum = sum + ((unsigned)(t - c0) < (unsigned)len ? v.x : 0.0f);
-            sum = sum + ((unsigned)(t + 1 - c0) < (unsigned)len ? v.y : 0.0f);
-            sum = sum + ((unsigned)(t + 2 - c0) < (unsigned)len ? v.z : 0.0f);
-            sum = sum + ((unsigned)(t + 3 - c0) < (unsigned)len ? v.w : 0.0f);
-          }
-          sum = wave_total(sum);
-        }
-        if constexpr (NW > 1) {
-          if (lane == 0) part[l & 1][w] = sum;
-          __syncthreads();
-          const int parts = ((int)a.k_len + (int)kRegCols - 1) / (int)kRegCols;
-          sum = wave_total(lane < parts ? part[l & 1][lane] : 0.0f);
-        }
-        if (lane == 0 && (NW == 1 || w == 0)) out[k] = sum;
-      }
-      if constexpr (NW > 1) __syncthreads();  // the row's ds are read
+      __syncthreads();
     }
+    if (i >= a.q_len) continue;  // NW = 1: a wavefront without a row
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      if (q < pt.q0 || q >= pt.q1) continue;
+      float e[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const float x = p[q][t] * dp[q][t];
+        e[t] = pt.sees(256 * q + 4 * lane + t) ? x : 0.0f;
+      }
+      st[w].put(q, lane, e);
+    }
+    turn ^= 1;
+    const float D = wide_join<NW>(st[w].span_sum(pt.q0, pt.q1), parts, slot[turn]);
+    Part pu = pt;
+    pu.from = again(pt.from);
+    part_store<TAIL, Q>(n,
+                     [&](int q, float(&o)[4]) {
+                       if (q >= pt.q0 && q < pt.q1) {
+                         float ds[4];
+#pragma unroll
+                         for (int t = 0; t < 4; ++t) {
+                           const float d = dp[q][t] - D;
+                           const float x = p[q][t] * d;
+                           ds[t] = pu.sees(256 * q + 4 * lane + t) ? x : 0.0f;
+                           o[t] = ds[t] * a.scale;
+                         }
+                         st[w].put(q, lane, ds);  // for the buckets' sums
+                       } else {
+                         o[0] = o[1] = o[2] = o[3] = 0.0f;
+                       }
+                     },
+                     [&](int j, const float(&o)[4]) { stb_arith(sr + j, o); },
+                     [&](int j, float o) { sr[j] = bf16_arith(o); });
+    if (!rowsum) continue;
+    float* out = rowsum + ((b * a.q_len + i) * a.heads + h) * nb;
+    if constexpr (NW > 1) __syncthreads();
+    else __builtin_amdgcn_wave_barrier();
+    for (int k2 = NW == 1 ? lane : (int)threadIdx.x; k2 < 2 * nb; k2 += NW == 1 ? 64 : 64 * NW) {
+      const int k = k2 >> 1, lo = lo_[k], hi = hi_[k];
+      const int b0 = qy.pos + lo > qy.j0 ? qy.pos + lo : qy.j0, b1 = qy.pos + hi < qy.j1 ? qy.pos + hi : qy.j1;
+      const int mid = (b0 | 31) + 1;  // the next chunk's first key
+      const int c0 = k2 & 1 ? mid : b0, c1 = k2 & 1 || b1 < mid ? b1 : mid;
+      float sum = 0.0f;
+      if (c0 < c1 && hi - lo <= kRelShort) {
+        const float* t = &st[NW == 1 ? w : c0 / (256 * Q)].t[(c0 >> 5) & (8 * Q - 1)][c0 & 31];
+        for (int j = 0; j < c1 - c0; j += 4) {  // up to three places behind the chunk's end: its row's padding
+#pragma unroll
+          for (int u = 0; u < 4; ++u) sum = sum + (j + u < c1 - c0 ? t[j + u] : 0.0f);
+        }
+      }
+      sum = sum + __uint_as_float(lane_move<0xB1>(__float_as_uint(sum)));  // the bucket's two chunks
+      if (!(k2 & 1) && hi - lo <= kRelShort) out[k] = sum;
+    }
+    for (int l = 0; l < a.n_long; ++l) {
+      const int k = a.longs[l];
+      const int lo = lo_[k], hi = hi_[k];
+      const int b0 = (qy.pos + lo > qy.j0 ? qy.pos + lo : qy.j0) - seg, b1 = (qy.pos + hi < qy.j1 ? qy.pos + hi : qy.j1) - seg;
+      float sum = 0.0f;
+      if (b0 < b1 && b0 < 256 * Q && b1 > 0) {  // the same for the whole wavefront
+        const int c0 = b0 - 32 * lane, len = b1 - b0;
+#pragma unroll
+        for (int t = 0; t < kChunk; t += 4) {
+          const float4 v = st[w].vec(lane, t / 4);
+          sum = sum + ((unsigned)(t - c0) < (unsigned)len ? v.x : 0.0f);
+          sum = sum + ((unsigned)(t + 1 - c0) < (unsigned)len ? v.y : 0.0f);
+          sum = sum + ((unsigned)(t + 2 - c0) < (unsigned)len ? v.z : 0.0f);
+          sum = sum + ((unsigned)(t + 3 - c0) < (unsigned)len ? v.w : 0.0f);
+        }
+        sum = wave_total(sum);
+      }
+      if constexpr (NW > 1) {
+        if (lane == 0) part[l & 1][w] = sum;
+        __syncthreads();
+        sum = wave_total(lane < parts ? part[l & 1][lane] : 0.0f);
+      }
+      if (lane == 0 && (NW == 1 || w == 0)) out[k] = sum;
+    }
+    if constexpr (NW > 1) __syncthreads();  // the row's ds are read
   }
 }
 
@@ -320,40 +316,36 @@ __global__ __launch_bounds__(256) void column_chain_kernel(int64_t rows, int64_t
   }
 }
 
-int key_waves(int64_t k_len) {
-  int nw = 1;
-  while (nw * kRegCols < k_len) nw <<= 1;
-  return nw;
-}
-
 }  // namespace
 
-#define CANON_REL_WAVES(K, nw)  \
-  switch (nw) {                 \
-    case 1: K(1); break;        \
-    case 2: K(2); break;        \
-    case 4: K(4); break;        \
-    case 8: K(8); break;        \
-    default: K(16); break;      \
+#define CANON_REL_ROWS(K)          \
+  switch (row_shape(a.k_len)) {     \
+    case 2: K(2, 1); break;         \
+    case 4: K(4, 1); break;         \
+    case 8: K(8, 1); break;         \
+    case 16: K(8, 2); break;        \
+    case 32: K(8, 4); break;        \
+    case 64: K(8, 8); break;        \
+    default: K(8, 16); break;       \
   }
 
 hipError_t relbias_fwd_launch(const RelBiasArgs& a, const float* scores, uint16_t* probs, hipStream_t s) {
-  const int nw = key_waves(a.k_len);
-  const int64_t per_head = (a.q_len + (nw == 1 ? 4 : 1) * kQueries - 1) / ((nw == 1 ? 4 : 1) * kQueries);
+  const int nw = row_waves(a.k_len);
+  const int64_t per_head = (a.q_len + (nw == 1 ? 3 : 0)) / (nw == 1 ? 4 : 1);
   const int64_t blocks = a.batch * a.heads * per_head;
   if (blocks == 0 || a.k_len == 0) return hipSuccess;
   const dim3 grid((unsigned)(blocks < kMaxBlocks ? blocks : kMaxBlocks)), wg(nw == 1 ? 256 : 64 * nw);
   const bool tail = a.k_len % 4 != 0;
   const int far = a.start[a.n_side - 1];
-  const size_t lds = sizeof(float) * (size_t)(far + 1 + (a.bidirectional ? far : 0));
-#define CANON_REL(NW)                                                                                                   \
+  const size_t lds = sizeof(float) * (size_t)(far + 1 + (a.bidirectional ? far : 0) + 2 * kEdge);
+#define CANON_REL(Q, NW)                                                                                                \
   do {                                                                                                                  \
     if (tail)                                                                                                           \
-      hipLaunchKernelGGL((relbias_fwd_kernel<NW, true>), grid, wg, lds, s, a, blocks, per_head, scores, probs);         \
+      hipLaunchKernelGGL((relbias_fwd_kernel<Q, NW, true>), grid, wg, lds, s, a, blocks, per_head, scores, probs);         \
     else                                                                                                                \
-      hipLaunchKernelGGL((relbias_fwd_kernel<NW, false>), grid, wg, lds, s, a, blocks, per_head, scores, probs);        \
+      hipLaunchKernelGGL((relbias_fwd_kernel<Q, NW, false>), grid, wg, lds, s, a, blocks, per_head, scores, probs);        \
   } while (0)
-  CANON_REL_WAVES(CANON_REL, nw)
+  CANON_REL_ROWS(CANON_REL)
 #undef CANON_REL
   return hipGetLastError();
 }
@@ -364,24 +356,24 @@ int64_t relbias_scratch_floats(int64_t rows, int64_t heads, int64_t buckets) {
 
 hipError_t relbias_bwd_launch(const RelBiasArgs& a, const uint16_t* probs, const float* dprobs, uint16_t* dscores,
                               float* dtable, float* rowsum, hipStream_t s) {
-  const int nw = key_waves(a.k_len);
-  const int64_t per_head = (a.q_len + (nw == 1 ? 4 : 1) * kQueries - 1) / ((nw == 1 ? 4 : 1) * kQueries);
+  const int nw = row_waves(a.k_len);
+  const int64_t per_head = (a.q_len + (nw == 1 ? 3 : 0)) / (nw == 1 ? 4 : 1);
   const int64_t blocks = a.batch * a.heads * per_head;
   const bool empty = blocks == 0 || a.k_len == 0;
   if (!empty) {
     const dim3 grid((unsigned)(blocks < kMaxBlocks ? blocks : kMaxBlocks)), wg(nw == 1 ? 256 : 64 * nw);
     const bool tail = a.k_len % 4 != 0;
     float* rs = dtable ? rowsum : nullptr;
-#define CANON_REL(NW)                                                                                                   \
+#define CANON_REL(Q, NW)                                                                                                \
   do {                                                                                                                  \
     if (tail)                                                                                                           \
-      hipLaunchKernelGGL((relbias_bwd_kernel<NW, true>), grid, wg, 0, s, a, blocks, per_head, probs, dprobs, dscores,   \
+      hipLaunchKernelGGL((relbias_bwd_kernel<Q, NW, true>), grid, wg, 0, s, a, blocks, per_head, probs, dprobs, dscores,   \
                          rs);                                                                                           \
     else                                                                                                                \
-      hipLaunchKernelGGL((relbias_bwd_kernel<NW, false>), grid, wg, 0, s, a, blocks, per_head, probs, dprobs, dscores,  \
+      hipLaunchKernelGGL((relbias_bwd_kernel<Q, NW, false>), grid, wg, 0, s, a, blocks, per_head, probs, dprobs, dscores,  \
                          rs);                                                                                           \
   } while (0)
-    CANON_REL_WAVES(CANON_REL, nw)
+    CANON_REL_ROWS(CANON_REL)
 #undef CANON_REL
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

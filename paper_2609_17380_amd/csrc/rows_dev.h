@@ -145,22 +145,58 @@ __device__ __forceinline__ float wave_most(float m) {
 }
 
 // Register-resident rows (cols <= 2048, or the part H of 2048 terms of a longer one): lane l holds terms
-// 4l + 256q .. +3 of its row, read from memory once.  The chunk chains still run one per lane over an LDS transpose
-// (rows of 36 floats: 16-byte stores and reads without bank conflicts; a wavefront's LDS operations complete in order).
+// 4l + 256q .. +3 of its row, read from memory once.  The chunk chains still run one per lane over an LDS transpose (rows
+// of 36 floats: 16-byte stores and reads without bank conflicts; a wavefront's LDS operations complete in order).
 constexpr int kRegQ = 8;  // 64 x 4 x 8 = 2048 terms
 constexpr int64_t kRegCols = 64 * 4 * kRegQ;
-struct RegStage {
-  float t[64][36];
+template <int Q>
+struct RowStage {  // of a row of up to 256 Q terms
+  float t[8 * Q][36];
+  __device__ __forceinline__ float4& vec(int chunk, int k) { return *reinterpret_cast<float4*>(&t[chunk][4 * k]); }
+  __device__ __forceinline__ float chain(int chunk) {
+    float p = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kChunk / 4; ++k) {
+      const float4 v = vec(chunk, k);
+      p = p + v.x; p = p + v.y; p = p + v.z; p = p + v.w;
+    }
+    return p;
+  }
+  // vector `q` of lane `lane` of a part: terms 256 q + 4 lane .. +3
+  __device__ __forceinline__ void put(int q, int lane, const float (&v)[4]) {
+    vec(8 * q + (lane >> 3), lane & 7) = make_float4(v[0], v[1], v[2], v[3]);
+  }
+  // the sum of the n terms put into it
+  __device__ __forceinline__ float sum(int n) {
+    const int lane = threadIdx.x & 63, k1 = n - lane * kChunk;
+    __builtin_amdgcn_wave_barrier();
+    float p = 0.0f;
+    if ((n & (kChunk - 1)) == 0) {
+      if (k1 > 0) p = chain(lane);
+    } else if (k1 > 0) {  // the row's last chunk is cut: what lies behind its end is left out by a select, a lane to a
+      // chunk as before (a loop up to its end waited for LDS at every term)
+#pragma unroll
+      for (int k = 0; k < kChunk / 4; ++k) {
+        const float4 v = vec(lane, k);
+        p = p + (4 * k < k1 ? v.x : 0.0f); p = p + (4 * k + 1 < k1 ? v.y : 0.0f);
+        p = p + (4 * k + 2 < k1 ? v.z : 0.0f); p = p + (4 * k + 3 < k1 ? v.w : 0.0f);
+      }
+    }
+    return wave_total(p);
+  }
+  // the same of a row whose terms outside vectors q0 .. q1 - 1 are +0, like their chunks' partials, and have not been put
+  __device__ __forceinline__ float span_sum(int q0, int q1) {
+    const int lane = threadIdx.x & 63;
+    __builtin_amdgcn_wave_barrier();
+    return wave_total(lane >= 8 * q0 && lane < 8 * q1 ? chain(lane) : 0.0f);
+  }
 };
+using RegStage = RowStage<kRegQ>;
 
 template <int H = 0, int Q>
 __device__ __forceinline__ float reg_row_sum(RegStage& st, const float (&e)[Q][4], int64_t n) {
   const int lane = threadIdx.x & 63;
-  auto stage = [&](int q) __attribute__((always_inline)) {
-    const int local = 256 * q + 4 * lane;
-    const float(&v)[4] = e[H * kRegQ + q];
-    *reinterpret_cast<float4*>(&st.t[local >> 5][local & 31]) = make_float4(v[0], v[1], v[2], v[3]);
-  };
+  auto stage = [&](int q) __attribute__((always_inline)) { st.put(q, lane, e[H * kRegQ + q]); };
   // short rows leave out the vectors past their end (norm forward of 20000 rows of 16 terms 11.2 -> 9.9 us); with the
   // test in front of every vector the softmax of 2048 keys took 66 us instead of 59
   if (n > 256 * (kRegQ - 1)) {
@@ -173,60 +209,47 @@ __device__ __forceinline__ float reg_row_sum(RegStage& st, const float (&e)[Q][4
       stage(q);
     }
   }
-  __builtin_amdgcn_wave_barrier();
-  float p = 0.0f;
-  const int k1 = (int)n - lane * kChunk;
-  if (k1 >= kChunk) {
-#pragma unroll
-    for (int i = 0; i < kChunk; i += 4) {
-      const float4 v = *reinterpret_cast<const float4*>(&st.t[lane][i]);
-      p = p + v.x; p = p + v.y; p = p + v.z; p = p + v.w;
-    }
-  } else {
-    for (int i = 0; i < k1; ++i) p = p + st.t[lane][i];
-  }
-  return wave_total(p);
+  return st.sum((int)n);
 }
 
-// ---- a part of a row in a wavefront's registers: n <= 2048 elements, lane l holding 256 q + 4 l .. +3 -----------------
-// Vectors that lie inside the part are moved whole; the one that its end cuts (TAIL: n is no multiple of 4) belongs to one
-// lane of one q and is moved by element beside the loop, so that the loop has a single condition per vector (with the
-// cut vector's branches in every iteration the masks spilled: padded rows of 1001 keys 109 us, now 72).
-template <bool TAIL, class Load4, class Load1>
-__device__ __forceinline__ void part_load(int n, float (&v)[kRegQ][4], Load4 load4, Load1 load1) {
-  const int at = 4 * (threadIdx.x & 63);
+// ---- a part of a row in a wavefront's registers: up to 256 Q elements, lane l holding 256 q + 4 l .. +3 -----------------
+// Elements from .. upto - 1 (and what shares a vector with the first of them) are loaded, +0 stands elsewhere.  Vectors that
+// end at or before `upto` are moved whole; the one that it cuts (TAIL: it need not be a multiple of 4) belongs to one lane
+// of one q and is moved by element beside the loop, so that the loop has a single condition per vector (with the cut
+// vector's branches in every iteration the masks spilled: padded rows of 1001 keys 109 us, then 53).
+template <bool TAIL, int Q, class Load4, class Load1>
+__device__ __forceinline__ void part_load(int from, int upto, float (&v)[Q][4], Load4 load4, Load1 load1) {
+  const int at = 4 * (threadIdx.x & 63), first = from - 3;
+  const unsigned whole = upto - 3 > first ? (unsigned)(upto - 3 - first) : 0u;  // places where a vector may begin
 #pragma unroll
-  for (int q = 0; q < kRegQ; ++q) {
-    if (256 * q + at + 4 <= n) {
-      load4(256 * q + at, v[q]);
-    } else {
+  for (int q = 0; q < Q; ++q) {
 #pragma unroll
-      for (int t = 0; t < 4; ++t) v[q][t] = 0.0f;
-    }
+    for (int t = 0; t < 4; ++t) v[q][t] = 0.0f;
+    if ((unsigned)(256 * q + at - first) < whole) load4(256 * q + at, v[q]);
   }
-  if (TAIL && n > 0 && (n & 3)) {
-    const int base = n & ~3;
+  if (TAIL && upto > from && (upto & 3)) {
+    const int base = upto & ~3;
     float c[3] = {0.0f, 0.0f, 0.0f};
     const int mine = at == (base & 255) ? base >> 8 : -1;  // the cut vector's q, in its lane
     if (mine >= 0) {
 #pragma unroll
       for (int t = 0; t < 3; ++t)
-        if (base + t < n) c[t] = load1(base + t);
+        if (base + t < upto) c[t] = load1(base + t);
     }
 #pragma unroll
-    for (int q = 0; q < kRegQ; ++q)
+    for (int q = 0; q < Q; ++q)
 #pragma unroll
       for (int t = 0; t < 3; ++t) v[q][t] = q == mine ? c[t] : v[q][t];
   }
 }
 // value(q, o) makes vector q, store4(j, o) moves the one at element j, store1(j, o) an element
-template <bool TAIL, class Value, class Store4, class Store1>
+template <bool TAIL, int Q, class Value, class Store4, class Store1>
 __device__ __forceinline__ void part_store(int n, Value value, Store4 store4, Store1 store1) {
   const int at = 4 * (threadIdx.x & 63);
   const int mine = TAIL && (n & 3) && n > 0 && at == (n & 252) ? n >> 8 : -1;
   float c[3] = {0.0f, 0.0f, 0.0f};
 #pragma unroll
-  for (int q = 0; q < kRegQ; ++q) {
+  for (int q = 0; q < Q; ++q) {
     if (256 * q >= n) break;
     float o[4];
     value(q, o);
@@ -270,20 +293,37 @@ __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane
 // chunks, a complete subtree of Algorithm 2 wherever a later part follows, so the parts' sums are folded by the same rule.
 // slot: NW floats of LDS, not written again before every wavefront has passed another barrier (NW = 1: one wavefront per
 // row, no barrier).
+// join: every wavefront's own part's sum p into the row's
 template <int NW>
-__device__ __forceinline__ float wide_row_sum(RegStage& st, const float (&e)[kRegQ][4], int n, float* slot) {
+__device__ __forceinline__ float wide_join(float p, int parts, float* slot) {
   if constexpr (NW == 1) {
-    return reg_row_sum(st, e, n);
+    return p;
   } else {
-    const int w = wave_id(), lane = threadIdx.x & 63;
-    const int left = n - w * (int)kRegCols;
-    float p = 0.0f;
-    if (left > 0) p = reg_row_sum(st, e, left < (int)kRegCols ? left : (int)kRegCols);
-    if (lane == 0) slot[w] = p;
+    const int lane = threadIdx.x & 63;
+    if (lane == 0) slot[wave_id()] = p;
     __syncthreads();
-    const int parts = (n + (int)kRegCols - 1) / (int)kRegCols;
     return wave_total(lane < parts ? slot[lane] : 0.0f);
   }
 }
+template <int NW, int Q>
+__device__ __forceinline__ float wide_row_sum(RowStage<Q>& st, const float (&e)[Q][4], int n, float* slot) {
+  const int lane = threadIdx.x & 63, left = NW == 1 ? n : n - wave_id() * 256 * Q;
+#pragma unroll
+  for (int q = 0; q < Q; ++q) {
+    if (256 * q >= left) break;
+    st.put(q, lane, e[q]);
+  }
+  const float p = left > 0 ? st.sum(left < 256 * Q ? left : 256 * Q) : 0.0f;
+  return wide_join<NW>(p, (n + 256 * Q - 1) / (256 * Q), slot);
+}
+
+// How rows of n terms are held: vectors of 256 to a wavefront times wavefronts.  Rows of up to 512 and 1024 terms take
+// fewer registers and less LDS, so that more of them are on the chip at once.
+inline int row_shape(int64_t n) {
+  int s = 2;
+  while (256 * (int64_t)s < n) s <<= 1;
+  return s;
+}
+inline int row_waves(int64_t n) { return n <= kRegCols ? 1 : row_shape(n) / kRegQ; }
 
 }  // namespace canon
