@@ -393,26 +393,39 @@ def devmath(op: str, n, a, b=None, c=None, out=None, stream=None):
 # device than the call needs raises ValueError and enqueues nothing.
 
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
+_T32, _T16, _TF, _TI8, _TI32 = (torch.float32,), (torch.bfloat16,), (torch.float32, torch.bfloat16), (torch.int8,), (torch.int32,)
 
 
-def _arg(t, what, numel, *dtypes):
+def _device() -> int:
+    """The current device; without one, a number that no tensor's is."""
+    try:
+        return torch._C._cuda_getDevice()
+    except RuntimeError:
+        return -2
+
+
+def _arg(t, what, numel, dtypes, dev):
     """The device address of an argument of `numel` elements (None: no pointer)."""
-    if t is None:
+    if t is None and dtypes is not _TF:  # where two types may stand the call needs one
         return None
+    if isinstance(t, torch.Tensor) and t.dtype in dtypes and t.get_device() == dev and t.numel() == numel and t.is_contiguous():
+        return t.data_ptr()
     if not isinstance(t, torch.Tensor) or t.dtype not in dtypes:
         raise ValueError(f"{what}: a tensor of {' or '.join(map(str, dtypes))} is needed")
-    if t.get_device() < 0 or t.get_device() != torch._C._cuda_getDevice():
+    if t.get_device() != dev:
         raise ValueError(f"{what}: a tensor on the current device is needed, not on {t.device}")
-    if t.numel() != numel or not t.is_contiguous():
-        raise ValueError(f"{what}: {numel} elements are needed, contiguous, not {tuple(t.shape)} of strides {t.stride()}")
-    return t.data_ptr()
+    raise ValueError(f"{what}: {numel} elements are needed, contiguous, not {tuple(t.shape)} of strides {t.stride()}")
 
 
-def _scratch(ws):
+def _scratch(ws, dev):
     """(address, bytes) of a workspace; without one, none."""
     if ws is None:
         return None, 0
-    return _arg(ws, "workspace", ws.numel(), ws.dtype), ws.numel() * ws.element_size()
+    return _arg(ws, "workspace", ws.numel(), (ws.dtype,), dev), ws.numel() * ws.element_size()
+
+
+def _stream_on(stream, dev):
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream)
 
 
 class Act8(ctypes.Structure):
@@ -420,16 +433,16 @@ class Act8(ctypes.Structure):
     _fields_ = [("group", ctypes.c_int32), ("codes", ctypes.c_void_p), ("steps", ctypes.c_void_p)]
 
     def __init__(self, group, codes, steps):
-        super().__init__(group, codes.data_ptr(), steps.data_ptr())
         self.tensors = codes, steps
+        super().__init__(group, codes.data_ptr(), steps.data_ptr())
 
-    def _of(self, rows, cols):
+    def _of(self, rows, cols, dev):
         """The record's address, once its tensors are those of [rows][cols]."""
         groups = act8_groups(cols, self.group)
         if not groups and cols:
             raise ValueError("group: 32, 64, 128 or 256 is needed")
-        _arg(self.tensors[0], "codes", rows * cols, torch.int8)
-        _arg(self.tensors[1], "steps", rows * groups, torch.float32)
+        _arg(self.tensors[0], "codes", rows * cols, _TI8, dev)
+        _arg(self.tensors[1], "steps", rows * groups, _T32, dev)
         return ctypes.byref(self)
 
 
@@ -438,41 +451,46 @@ def act8_groups(cols, group) -> int:
 
 
 def act8_pack(rows, cols, x, kept: Act8, stream=None):
-    px = _arg(x, "x", rows * cols, torch.float32, torch.bfloat16)
-    _check(_lib().canon_act8_pack(rows, cols, _DTYPES[x.dtype], px, kept._of(rows, cols), _stream(stream)),
+    dev = _device()
+    px = _arg(x, "x", rows * cols, _TF, dev)
+    _check(_lib().canon_act8_pack(rows, cols, _DTYPES[x.dtype], px, kept._of(rows, cols, dev), _stream_on(stream, dev)),
            "canon_act8_pack")
 
 
 def act8_unpack(rows, cols, kept: Act8, out, stream=None):
-    po = _arg(out, "out", rows * cols, torch.float32, torch.bfloat16)
-    _check(_lib().canon_act8_unpack(rows, cols, kept._of(rows, cols), _DTYPES[out.dtype], po, _stream(stream)),
+    dev = _device()
+    po = _arg(out, "out", rows * cols, _TF, dev)
+    _check(_lib().canon_act8_unpack(rows, cols, kept._of(rows, cols, dev), _DTYPES[out.dtype], po, _stream_on(stream, dev)),
            "canon_act8_unpack")
 
 
 def swiglu(T, F, gu, a, keep: Act8 | None = None, stream=None):
     """a = silu(gate) up from gu [T, 2F]; keep: also keeps gu in 8 bits, as the matrix [2T][F]."""
-    pg = _arg(gu, "gu", 2 * T * F, torch.float32, torch.bfloat16)
-    _check(_lib().canon_swiglu(T, F, _DTYPES[gu.dtype], pg, _arg(a, "a", T * F, torch.bfloat16),
-                               None if keep is None else keep._of(2 * T, F), _stream(stream)), "canon_swiglu")
+    dev = _device()
+    pg = _arg(gu, "gu", 2 * T * F, _TF, dev)
+    _check(_lib().canon_swiglu(T, F, _DTYPES[gu.dtype], pg, _arg(a, "a", T * F, _T16, dev),
+                               None if keep is None else keep._of(2 * T, F, dev), _stream_on(stream, dev)), "canon_swiglu")
 
 
 def swiglu_bwd(T, F, gu, da, dgu, a=None, stream=None):
     """gu: the forward's input, or the Act8 that it was kept as."""
-    kept = gu._of(2 * T, F) if isinstance(gu, Act8) else None
-    pg = None if kept else _arg(gu, "gu", 2 * T * F, torch.float32, torch.bfloat16)
+    dev = _device()
+    kept = gu._of(2 * T, F, dev) if isinstance(gu, Act8) else None
+    pg = None if kept else _arg(gu, "gu", 2 * T * F, _TF, dev)
     _check(_lib().canon_swiglu_bwd(T, F, F32 if kept else _DTYPES[gu.dtype], pg, kept,
-                                   _arg(da, "da", T * F, torch.float32), _arg(dgu, "dgu", 2 * T * F, torch.bfloat16),
-                                   _arg(a, "a", T * F, torch.bfloat16), _stream(stream)), "canon_swiglu_bwd")
+                                   _arg(da, "da", T * F, _T32, dev), _arg(dgu, "dgu", 2 * T * F, _T16, dev),
+                                   _arg(a, "a", T * F, _T16, dev), _stream_on(stream, dev)), "canon_swiglu_bwd")
 
 
 def layernorm(rows, cols, x, gain, bias, eps, y, mean, rstd, keep: Act8 | None = None, order=ORDER_V1, stream=None):
-    px = _arg(x, "x", rows * cols, torch.float32, torch.bfloat16)
-    py = _arg(y, "y", rows * cols, torch.float32, torch.bfloat16)
+    dev = _device()
+    px = _arg(x, "x", rows * cols, _TF, dev)
+    py = _arg(y, "y", rows * cols, _TF, dev)
     _check(_lib().canon_layernorm(ctypes.byref(order), rows, cols, _DTYPES[x.dtype], px,
-                                  _arg(gain, "gain", cols, torch.bfloat16), _arg(bias, "bias", cols, torch.bfloat16), eps,
-                                  _DTYPES[y.dtype], py, _arg(mean, "mean", rows, torch.float32),
-                                  _arg(rstd, "rstd", rows, torch.float32),
-                                  None if keep is None else keep._of(rows, cols), _stream(stream)), "canon_layernorm")
+                                  _arg(gain, "gain", cols, _T16, dev), _arg(bias, "bias", cols, _T16, dev), eps,
+                                  _DTYPES[y.dtype], py, _arg(mean, "mean", rows, _T32, dev),
+                                  _arg(rstd, "rstd", rows, _T32, dev),
+                                  None if keep is None else keep._of(rows, cols, dev), _stream_on(stream, dev)), "canon_layernorm")
 
 
 def layernorm_bwd_workspace_bytes(rows, cols) -> int:
@@ -482,16 +500,17 @@ def layernorm_bwd_workspace_bytes(rows, cols) -> int:
 def layernorm_bwd(rows, cols, x, gain, mean, rstd, dy, dx, workspace=None, dgain=None, dbias=None, order=ORDER_V1,
                   stream=None):
     """x: the forward's input, or the Act8 that it was kept as.  workspace: needed for dgain and dbias."""
-    kept = x._of(rows, cols) if isinstance(x, Act8) else None
-    px = None if kept else _arg(x, "x", rows * cols, torch.float32, torch.bfloat16)
-    ws, ws_bytes = _scratch(workspace)
+    dev = _device()
+    kept = x._of(rows, cols, dev) if isinstance(x, Act8) else None
+    px = None if kept else _arg(x, "x", rows * cols, _TF, dev)
+    ws, ws_bytes = _scratch(workspace, dev)
     _check(_lib().canon_layernorm_bwd(ctypes.byref(order), rows, cols, F32 if kept else _DTYPES[x.dtype], px, kept,
-                                      _arg(gain, "gain", cols, torch.bfloat16), _arg(mean, "mean", rows, torch.float32),
-                                      _arg(rstd, "rstd", rows, torch.float32),
-                                      _arg(dy, "dy", rows * cols, torch.float32),
-                                      _arg(dx, "dx", rows * cols, torch.float32),
-                                      _arg(dgain, "dgain", cols, torch.float32),
-                                      _arg(dbias, "dbias", cols, torch.float32), ws, ws_bytes, _stream(stream)),
+                                      _arg(gain, "gain", cols, _T16, dev), _arg(mean, "mean", rows, _T32, dev),
+                                      _arg(rstd, "rstd", rows, _T32, dev),
+                                      _arg(dy, "dy", rows * cols, _T32, dev),
+                                      _arg(dx, "dx", rows * cols, _T32, dev),
+                                      _arg(dgain, "dgain", cols, _T32, dev),
+                                      _arg(dbias, "dbias", cols, _T32, dev), ws, ws_bytes, _stream_on(stream, dev)),
            "canon_layernorm_bwd")
 
 
@@ -530,20 +549,22 @@ class AttnRows(ctypes.Structure):
     def __init__(self, batch, n_heads, q_len, k_len, causal=True, window=0, scale=1.0, ld=0, q_start=0, q_starts=None,
                  q_lens=None, k_lens=None):
         self.tensors = q_starts, q_lens, k_lens
+        dev = _device()
         super().__init__(batch, n_heads, q_len, k_len, ld, q_start, window, int(causal), scale,
-                         *(_arg(t, w, batch, torch.int32) for t, w in zip(self.tensors, ("q_starts", "q_lens", "k_lens"))))
+                         *(_arg(t, w, batch, _TI32, dev) for t, w in zip(self.tensors, ("q_starts", "q_lens", "k_lens"))))
 
-    def _matrix(self, t, what, dtype):
+    def _matrix(self, t, what, dtypes, dev):
         """A matrix of these rows: all of them, `ld` apart."""
-        return _arg(t, what, self.batch * self.n_heads * self.q_len * (self.ld or self.k_len), dtype)
+        return _arg(t, what, self.batch * self.n_heads * self.q_len * (self.ld or self.k_len), dtypes, dev)
 
 
 def softmax_relbias(rows: AttnRows, bias: RelBias, table, scores, probs, order=ORDER_V1, stream=None):
     """probs (bf16) of the raw scores (fp32), with table (bf16 [buckets, n_heads]) added by distance."""
+    dev = _device()
     _check(_lib().canon_softmax_relbias(ctypes.byref(order), ctypes.byref(rows), ctypes.byref(bias),
-                                        _arg(table, "table", bias.buckets * rows.n_heads, torch.bfloat16),
-                                        rows._matrix(scores, "scores", torch.float32),
-                                        rows._matrix(probs, "probs", torch.bfloat16), _stream(stream)),
+                                        _arg(table, "table", bias.buckets * rows.n_heads, _T16, dev),
+                                        rows._matrix(scores, "scores", _T32, dev),
+                                        rows._matrix(probs, "probs", _T16, dev), _stream_on(stream, dev)),
            "canon_softmax_relbias")
 
 
@@ -554,13 +575,14 @@ def softmax_relbias_bwd_workspace_bytes(rows: AttnRows, bias: RelBias) -> int:
 def softmax_relbias_bwd(rows: AttnRows, bias: RelBias, probs, dprobs, dscores, workspace=None, dtable=None,
                         order=ORDER_V1, stream=None):
     """dscores (bf16) and dtable (fp32 [buckets, n_heads]); workspace: needed for dtable."""
-    ws, ws_bytes = _scratch(workspace)
+    dev = _device()
+    ws, ws_bytes = _scratch(workspace, dev)
     _check(_lib().canon_softmax_relbias_bwd(ctypes.byref(order), ctypes.byref(rows), ctypes.byref(bias),
-                                            rows._matrix(probs, "probs", torch.bfloat16),
-                                            rows._matrix(dprobs, "dprobs", torch.float32),
-                                            rows._matrix(dscores, "dscores", torch.bfloat16),
-                                            _arg(dtable, "dtable", bias.buckets * rows.n_heads, torch.float32), ws, ws_bytes,
-                                            _stream(stream)), "canon_softmax_relbias_bwd")
+                                            rows._matrix(probs, "probs", _T16, dev),
+                                            rows._matrix(dprobs, "dprobs", _T32, dev),
+                                            rows._matrix(dscores, "dscores", _T16, dev),
+                                            _arg(dtable, "dtable", bias.buckets * rows.n_heads, _T32, dev), ws, ws_bytes,
+                                            _stream_on(stream, dev)), "canon_softmax_relbias_bwd")
 
 
 def version() -> int:

@@ -28,12 +28,14 @@ __device__ __forceinline__ float step4(const float (&v)[4], int lg) {
   m = lanes_join(m, 1 << (lg - 2), [](uint32_t a, uint32_t b) { return a > b ? a : b; });
   return __uint_as_float(m) * __uint_as_float(kInv127Bits);
 }
+// The reciprocal of a step of keep4's (|v / s| <= 127 (1 + 2^-23)), for quant_pack's rule: v_rcp_f32 is within 2^-23 of 1/s,
+// so t = RN(v rs) within 127 (2^-23 + 2^-24) (1 + 2^-22) < 2.28e-5 of v / s, and RN(v / s) within 2^-18: together below the
+// 2^-15 that t has to be away from every half-integer.  The correctly rounded quotient took 12 instructions.
+__device__ __forceinline__ float step_rcp(float s) { return recip_step_ok(s) ? __builtin_amdgcn_rcpf(s) : 0.0f; }
 __device__ __forceinline__ uint32_t codes4(const float (&v)[4], int lg, float& s) {
   s = step4(v, lg);
-  const bool recip = recip_step_ok(s);
-  const float rs = recip ? 1.0f / s : 0.0f;
   uint32_t w[1];
-  quant_pack<4>(v, s, rs, recip, w);
+  quant_pack<4>(v, s, step_rcp(s), recip_step_ok(s), w);
   return w[0];
 }
 template <bool TAIL>
@@ -55,6 +57,7 @@ __device__ __forceinline__ void keep4(const float (&v)[4], int64_t j, int64_t n,
 // branch instead of one per vector, whose masks spilled.
 template <bool TAIL, int Q>
 __device__ __forceinline__ void part_keep(const float (&v)[Q][4], int n, int lg, int8_t* codes, float* steps) {
+  n = again(n);
   const int at = 4 * (threadIdx.x & 63);
   uint32_t w[Q], undecided = 0;
   float s[Q];
@@ -62,28 +65,33 @@ __device__ __forceinline__ void part_keep(const float (&v)[Q][4], int n, int lg,
   for (int q = 0; q < Q; ++q) {
     if (256 * q >= n) break;
     s[q] = step4(v[q], lg);
-    const bool recip = recip_step_ok(s[q]);
-    const float rs = recip ? 1.0f / s[q] : 0.0f;
-    bool sure = recip;
+    const float rs = step_rcp(s[q]);
+    float off = 0.0f;  // how far the furthest is from its integer
     uint32_t x = 0;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       const float y = v[q][t] * rs, k = __builtin_rintf(y);
-      sure &= fabsf(y - k) < 0.5f - 0x1p-15f;
+      off = fmaxf(off, fabsf(y - k));
       x = __builtin_amdgcn_cvt_pk_u8_f32(k + 128.0f, t, x);
     }
     w[q] = x ^ 0x80808080u;
-    undecided |= sure ? 0u : 1u << q;
+    undecided |= rs > 0.0f && off < 0.5f - 0x1p-15f ? 0u : 1u << q;
   }
-  if (undecided) {
+  while (undecided) {  // one vector of each lane that has any
+    const int k = __builtin_ctz(undecided);
+    undecided &= undecided - 1;
+    float x[4] = {0.0f, 0.0f, 0.0f, 0.0f}, sx = 0.0f;
 #pragma unroll
-    for (int q = 0; q < Q; ++q)
-      if (undecided & (1u << q)) {
-        uint32_t x = 0;
+    for (int q = 0; q < Q; ++q) {
 #pragma unroll
-        for (int t = 0; t < 4; ++t) x |= (uint32_t)(uint8_t)quant1(v[q][t], s[q]) << (8 * t);
-        w[q] = x;
-      }
+      for (int t = 0; t < 4; ++t) x[t] = q == k ? v[q][t] : x[t];
+      sx = q == k ? s[q] : sx;
+    }
+    uint32_t c = 0;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) c |= (uint32_t)(uint8_t)quant1(x[t], sx) << (8 * t);
+#pragma unroll
+    for (int q = 0; q < Q; ++q) w[q] = q == k ? c : w[q];
   }
   const int mine = TAIL && (n & 3) && n > 0 && at == (n & 252) ? n >> 8 : -1;
   uint32_t cut = 0;

@@ -258,6 +258,7 @@ struct RelBiasArgs {
   const uint16_t* table;  // [buckets][heads]
   float scale;
   int32_t causal, n_side, bidirectional, n_long;
+  int32_t far_only, short_most;   // whether those are the last bucket(s) alone; the most distances of the others
   int32_t start[kRelStarts];
   uint8_t longs[2 * kRelStarts];  // the buckets of more than kRelShort distances
   uint8_t bucket[kRelFar + 1];    // of the distances up to the last bucket's first, on one side

@@ -149,54 +149,81 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void layer
   }
 }
 
-// The chains of 32 rows of dgain[k] = R1 over rows of RN(dy xh) and dbias[k] = R1 over rows of dy: V columns per thread,
-// B rows in flight.  part: [2][chunks][cols].
-template <int SRC, int V, int B>
-__global__ __launch_bounds__(256 / V) void layernorm_part_kernel(int64_t rows, int64_t cols, ActIn x,
-                                                                 const float* __restrict__ mean,
-                                                                 const float* __restrict__ rstd,
-                                                                 const float* __restrict__ dy,
-                                                                 float* __restrict__ part) {
-  const int64_t col = (int64_t)blockIdx.x * 256 + threadIdx.x * V;
-  if (col >= cols) return;
-  const int64_t nc = (rows + kChunk - 1) / kChunk;
-  for (int64_t c = blockIdx.y; c < nc; c += gridDim.y) {
-    const int64_t t0 = c * kChunk, t1 = t0 + kChunk < rows ? t0 + kChunk : rows;
-    float sg[V] = {}, sb[V] = {};
-    auto steps = [&](int64_t t, auto n) __attribute__((always_inline)) {
-      constexpr int N = decltype(n)::value;
-      float xv[N][V], dv[N][V];
+// Four columns of a row from column j on, n of them there (none: n <= 0), x as it is stored; 0 where there are none.
+template <int SRC, bool TAIL>
+__device__ __forceinline__ void load_columns(const ActIn& x, const float* dy, int64_t rows, int64_t row, int cols, int j,
+                                             int n, typename PartIn<SRC>::Raw& xr, float (&dv)[4]) {
+  xr = typename PartIn<SRC>::Raw{};
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
+  for (int t = 0; t < 4; ++t) dv[t] = 0.0f;
+  if (row >= rows) return;
+  const PartIn<SRC> in(x, row, cols, 0);
+  const float* dr = dy + row * cols;
+  if (n == 4) {
+    in.load4(j, xr);
+    ldf<4>(dr + j, dv);
+  } else if (TAIL) {
+#pragma unroll
+    for (int t = 0; t < 3; ++t)
+      if (t < n) {
+        in.load1(j, t, xr);
+        dv[t] = dr[j + t];
+      }
+  }
+}
+
+// The chains of 32 rows of dgain[k] = R1 over rows of RN(dy xh) and dbias[k] = R1 over rows of dy, V = 4 columns or one per
+// thread, B rows in flight.  part: [2][chunks][cols].
+template <int SRC, int V, int B, bool TAIL>
+__global__ __launch_bounds__(64) void layernorm_part_kernel(int64_t rows, int cols, ActIn x, const float* __restrict__ mean,
+                                                            const float* __restrict__ rstd, const float* __restrict__ dy,
+                                                            float* __restrict__ part) {
+  const int j = (blockIdx.x * 64 + threadIdx.x) * V, n = cols - j < V ? cols - j : V;
+  const int64_t nc = (rows + kChunk - 1) / kChunk;
+  if (n <= 0) return;
+  for (int64_t c = blockIdx.y; c < nc; c += gridDim.y) {
+    float sg[V], sb[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) sg[k] = sb[k] = 0.0f;
+    auto steps = [&](int64_t t, auto count) __attribute__((always_inline)) {  // all loads, then the chains' steps
+      constexpr int N = decltype(count)::value;
+      typename PartIn<SRC>::Raw xr[N];
+      float dv[N][4];
+#pragma unroll
+      for (int r = 0; r < N; ++r) {
         if constexpr (V == 4) {
-          act4<SRC, false>(x, t + i, col, cols, xv[i]);
+          load_columns<SRC, TAIL>(x, dy, rows, t + r, cols, j, n, xr[r], dv[r]);
         } else {
-          const int64_t at = (t + i) * cols + col;
-          if constexpr (SRC == ACT_F32) xv[i][0] = ((const float*)x.x)[at];
-          else if constexpr (SRC == ACT_BF16) xv[i][0] = bf16_to_f32(((const uint16_t*)x.x)[at]);
-          else xv[i][0] = (float)((const int8_t*)x.x)[at] *
-                          x.steps[(t + i) * ((cols + (1 << x.lg) - 1) >> x.lg) + (col >> x.lg)];
+          xr[r] = typename PartIn<SRC>::Raw{};
+          PartIn<SRC>(x, t + r, cols, 0).load1(j, 0, xr[r]);
+          dv[r][0] = dy[(t + r) * cols + j];
         }
-        ldf<V>(dy + (t + i) * cols + col, dv[i]);
       }
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float mu = mean[t + i], r = rstd[t + i];
+      for (int r = 0; r < N; ++r) {
+        const float mu = mean[t + r], rs = rstd[t + r];
+        float xv[4];
+        PartIn<SRC>::wide(xr[r], xv);
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-          const float d = xv[i][k] - mu;
-          const float xh = d * r;
-          const float pr = dv[i][k] * xh;
+          const float d = xv[k] - mu;
+          const float xh = d * rs;
+          const float pr = dv[r][k] * xh;
           sg[k] = sg[k] + pr;
-          sb[k] = sb[k] + dv[i][k];
+          sb[k] = sb[k] + dv[r][k];
         }
       }
     };
-    int64_t t = t0;
+    const int64_t t1 = (c + 1) * kChunk < rows ? (c + 1) * kChunk : rows;
+    int64_t t = c * kChunk;
     for (; t + B <= t1; t += B) steps(t, std::integral_constant<int, B>{});
     for (; t < t1; ++t) steps(t, std::integral_constant<int, 1>{});
-    stf<V>(part + c * cols + col, sg);
-    stf<V>(part + (nc + c) * cols + col, sb);
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+      if (k < n) {
+        part[c * cols + j + k] = sg[k];
+        part[(nc + c) * cols + j + k] = sb[k];
+      }
   }
 }
 
@@ -219,26 +246,9 @@ __global__ __launch_bounds__(64 * NW) void layernorm_pass_kernel(int64_t rows, i
   const int j = 256 * w + 4 * lane;  // this lane's first column
   const int n = cols - j < 4 ? cols - j : 4;  // and how many of its four there are
   const int64_t nc = (rows + kChunk - 1) / kChunk;
-  // this lane's columns of a row, x as it is stored; 0 where there are none
   using In = PartIn<SRC>;
   auto load = [&](int64_t row, typename In::Raw& xr, float(&dv)[4]) __attribute__((always_inline)) {
-    xr = typename In::Raw{};
-#pragma unroll
-    for (int t = 0; t < 4; ++t) dv[t] = 0.0f;
-    if (row >= rows) return;
-    const In in(x, row, cols, 0);
-    const float* dr = dy + row * cols;
-    if (n == 4) {
-      in.load4(j, xr);
-      ldf<4>(dr + j, dv);
-    } else if (TAIL) {
-#pragma unroll
-      for (int t = 0; t < 3; ++t)
-        if (t < n) {
-          in.load1(j, t, xr);
-          dv[t] = dr[j + t];
-        }
-    }
+    load_columns<SRC, TAIL>(x, dy, rows, row, cols, j, n, xr, dv);
   };
   float gv[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -403,27 +413,20 @@ hipError_t column_fold_launch(int64_t rows, int64_t cols, int64_t inner, const f
   return hipGetLastError();
 }
 
-#define CANON_LN_ROWS(K, SRC)                 \
-  switch (row_shape(cols)) {                  \
-    case 2: K(SRC, 2, 1); break;              \
-    case 4: K(SRC, 4, 1); break;              \
-    case 8: K(SRC, 8, 1); break;              \
-    case 16: K(SRC, 8, 2); break;             \
-    case 32: K(SRC, 8, 4); break;             \
-    case 64: K(SRC, 8, 8); break;             \
-    default: K(SRC, 8, 16); break;            \
-  }
+#define CANON_LN_ACT_F32(Q, NW) CANON_LN(ACT_F32, Q, NW)
+#define CANON_LN_ACT_BF16(Q, NW) CANON_LN(ACT_BF16, Q, NW)
+#define CANON_LN_ACT_Q8(Q, NW) CANON_LN(ACT_Q8, Q, NW)
 
 hipError_t layernorm_fwd_launch(int64_t rows, int64_t cols, const ActIn& x, const uint16_t* gain, const uint16_t* bias,
                                 float eps, int y_bf16, void* y, float* mean, float* rstd, const ActKeep& k,
                                 hipStream_t s) {
   if (rows == 0) return hipSuccess;
   const float inv_d = (float)(1.0 / (double)cols);  // RN32(1/cols), correctly rounded
-  const int nw = row_waves(cols);
-  const int64_t blocks = nw == 1 ? (rows + 3) / 4 : rows;
+  const RowShape shape = row_shape(rows, cols, 8);
+  const int64_t blocks = shape.groups(rows);
   // rows that are loaded ahead: no more workgroups than are on the chip at once (16 wavefronts to a CU)
-  const int64_t most = layernorm_ahead(k.codes) ? device_cus() * (nw == 1 ? 4 : 16 / nw) : kMaxBlocks;
-  const dim3 grid((unsigned)(blocks < most ? blocks : most)), wg(nw == 1 ? 256 : 64 * nw);
+  const int64_t most = layernorm_ahead(k.codes) ? device_cus() * (16 * 64 / shape.threads()) : kMaxBlocks;
+  const dim3 grid((unsigned)(blocks < most ? blocks : most)), wg(shape.threads());
 #define CANON_LN_K(SRC, Q, NW, TAIL, KEEP)                                                                               \
   hipLaunchKernelGGL((layernorm_fwd_kernel<SRC, Q, NW, TAIL, KEEP>), grid, wg, 0, s, rows, (int)cols, x, gain, bias, eps, \
                      inv_d, y_bf16, y, mean, rstd, k)
@@ -438,9 +441,9 @@ hipError_t layernorm_fwd_launch(int64_t rows, int64_t cols, const ActIn& x, cons
     }                                              \
   } while (0)
   if (x.src == ACT_F32) {
-    CANON_LN_ROWS(CANON_LN, ACT_F32)
+    CANON_ROW_SHAPES(CANON_LN_ACT_F32, shape);
   } else {
-    CANON_LN_ROWS(CANON_LN, ACT_BF16)
+    CANON_ROW_SHAPES(CANON_LN_ACT_BF16, shape);
   }
 #undef CANON_LN
 #undef CANON_LN_K
@@ -485,20 +488,23 @@ hipError_t layernorm_bwd_launch(int64_t rows, int64_t cols, const ActIn& x, cons
     return column_fold_launch(rows, cols, 0, part, dgain, dbias, s);
   }
   if ((dgain || dbias) && rows > 0) {
-    const dim3 grid((unsigned)((cols + 255) / 256), (unsigned)(nc < 65535 ? nc : 65535));
-#define CANON_LN_PART(SRC)                                                                                            \
-  do {                                                                                                                \
-    if (cols % 4 == 0)                                                                                                \
-      hipLaunchKernelGGL((layernorm_part_kernel<SRC, 4, 4>), grid, dim3(64), 0, s, rows, cols, x, mean, rstd, dy,     \
-                         part);                                                                                       \
-    else                                                                                                              \
-      hipLaunchKernelGGL((layernorm_part_kernel<SRC, 1, 8>), grid, dim3(256), 0, s, rows, cols, x, mean, rstd, dy,    \
-                         part);                                                                                       \
+    // four columns to a thread once that makes eight wavefronts to a CU; below, one
+    const int v = nc * ((cols + 255) / 256) >= 8 * device_cus() ? 4 : 1;
+    const dim3 grid((unsigned)((cols + 64 * v - 1) / (64 * v)), (unsigned)(nc < 65535 ? nc : 65535));
+#define CANON_LN_PART_K(SRC, V, B, TAIL)                                                                                \
+  hipLaunchKernelGGL((layernorm_part_kernel<SRC, V, B, TAIL>), grid, dim3(64), 0, s, rows, (int)cols, x, mean, rstd,    \
+                     dy, part)
+#define CANON_LN_PART(SRC)                                        \
+  do {                                                            \
+    if (v == 1) CANON_LN_PART_K(SRC, 1, 16, false);               \
+    else if (cols % 4 == 0) CANON_LN_PART_K(SRC, 4, 4, false);    \
+    else CANON_LN_PART_K(SRC, 4, 4, true);                        \
   } while (0)
     if (x.src == ACT_F32) CANON_LN_PART(ACT_F32);
     else if (x.src == ACT_BF16) CANON_LN_PART(ACT_BF16);
     else CANON_LN_PART(ACT_Q8);
 #undef CANON_LN_PART
+#undef CANON_LN_PART_K
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -507,9 +513,9 @@ hipError_t layernorm_bwd_launch(int64_t rows, int64_t cols, const ActIn& x, cons
     if (e != hipSuccess) return e;
   }
   if (rows == 0) return hipSuccess;
-  const int nw = row_waves(cols);
-  const int64_t blocks = nw == 1 ? (rows + 3) / 4 : rows;
-  const dim3 grid((unsigned)(blocks < kMaxBlocks ? blocks : kMaxBlocks)), wg(nw == 1 ? 256 : 64 * nw);
+  const RowShape shape = row_shape(rows, cols, 8);
+  const int64_t blocks = shape.groups(rows);
+  const dim3 grid((unsigned)(blocks < kMaxBlocks ? blocks : kMaxBlocks)), wg(shape.threads());
 #define CANON_LN(SRC, Q, NW)                                                                                             \
   do {                                                                                                                 \
     if (cols % 4 == 0)                                                                                                 \
@@ -520,11 +526,11 @@ hipError_t layernorm_bwd_launch(int64_t rows, int64_t cols, const ActIn& x, cons
                          dy, inv_d, dx);                                                                                   \
   } while (0)
   if (x.src == ACT_F32) {
-    CANON_LN_ROWS(CANON_LN, ACT_F32)
+    CANON_ROW_SHAPES(CANON_LN_ACT_F32, shape);
   } else if (x.src == ACT_BF16) {
-    CANON_LN_ROWS(CANON_LN, ACT_BF16)
+    CANON_ROW_SHAPES(CANON_LN_ACT_BF16, shape);
   } else {
-    CANON_LN_ROWS(CANON_LN, ACT_Q8)
+    CANON_ROW_SHAPES(CANON_LN_ACT_Q8, shape);
   }
 #undef CANON_LN
   return hipGetLastError();

@@ -15,7 +15,6 @@ namespace canon {
 
 namespace {
 
-constexpr int kEdge = 256;              // entries of either end of the bias table again, for the keys of a vector across it
 constexpr int kQueries = 4;             // queries that a wavefront (or, of longer rows, a workgroup) takes in turn
 constexpr int64_t kFarPos = 1 << 20;    // beyond every key's distance and the last bucket
 constexpr int64_t kMaxBlocks = 1 << 20;  // of up to 1024 threads: 2^30 of 2^32
@@ -59,6 +58,7 @@ __device__ __forceinline__ Query query_of(const RelBiasArgs& a, int64_t b, int64
 struct Part {
   int from, end, upto, q0, q1;
   __device__ __forceinline__ bool sees(int j) const { return (unsigned)(j - from) < (unsigned)(end - from); }
+  __device__ __forceinline__ bool sees_all(int q) const { return from <= 256 * q && 256 * q + 256 <= end; }
 };
 __device__ __forceinline__ Part part_of(const Query& q, int seg, int n) {
   Part p;
@@ -74,20 +74,23 @@ __device__ __forceinline__ Part part_of(const Query& q, int seg, int n) {
 
 template <int Q, int NW, bool TAIL>
 __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbias_fwd_kernel(
-    RelBiasArgs a, int64_t blocks, int64_t per_head, const float* __restrict__ scores, uint16_t* __restrict__ probs) {
+    RelBiasArgs a, uint32_t heads, uint32_t matrices, uint32_t per_head, const float* __restrict__ scores, uint16_t* __restrict__ probs) {
   constexpr int kRows = NW == 1 ? 4 : 1;
   __shared__ __attribute__((aligned(16))) RowStage<Q> st[NW == 1 ? 4 : NW];
   __shared__ float slot[2][NW], top[NW];
-  extern __shared__ float near_[];  // bias by place: key less query, from -far to `right`, and kEdge more on either side
+  extern __shared__ float near_[];  // bias by place: key less query, from -far to `right`
   const int w = wave_id(), lane = threadIdx.x & 63;
   const int far = a.start[a.n_side - 1], right = a.bidirectional ? far : 0;
   const int seg = NW == 1 ? 0 : w * 256 * Q;  // this wavefront's part of the row
   const int n = (int)a.k_len - seg < 256 * Q ? (int)a.k_len - seg : 256 * Q;
   const int parts = ((int)a.k_len + 256 * Q - 1) / (256 * Q);
   int turn = 0;  // rows in turn take one of two slots, so that a barrier lies between a slot's reads and its next writes
-  for (int64_t blk = blockIdx.x; blk < blocks; blk += gridDim.x) {
-    const int64_t bh = blk / per_head, b = bh / a.heads, h = bh - b * a.heads;
-    const int64_t i = (blk - bh * per_head) * kRows + (NW == 1 ? w : 0);
+  // a matrix's rows along x, the matrices (batch and head) along y; each further on by the grid where that ends first
+  bool once = true;  // this workgroup's first rows
+  for (uint32_t m = blockIdx.y; m < matrices; m += gridDim.y)
+  for (uint32_t blk = blockIdx.x; blk < per_head; blk += gridDim.x) {
+    const int64_t bh = m, b = m / heads, h = m % heads;
+    const int64_t i = (int64_t)blk * kRows + (NW == 1 ? w : 0);
     const Query qy = query_of(a, b, i);
     const Part pt = part_of(qy, seg, n);
     const int64_t row = (bh * a.q_len + i) * a.ld + seg;
@@ -95,16 +98,16 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
     uint16_t* pr = probs + row;
     float e[Q][4];
     part_load<TAIL>(pt.from, pt.upto, e, [&](int j, float(&v)[4]) { ldf<4>(rr + j, v); }, [&](int j) { return rr[j]; });
-    if (blk != (int64_t)blockIdx.x) __syncthreads();  // the last row's biases are read
-    for (int k = threadIdx.x; k <= far + right + 2 * kEdge; k += blockDim.x) {
-      int d = far + kEdge - k;  // query less key
-      d = d > far ? far : d < -right ? -right : d;
+    if (!once) __syncthreads();  // the last row's biases are read
+    once = false;
+    for (int k = threadIdx.x; k <= far + right; k += blockDim.x) {
+      const int d = far - k;  // query less key
       near_[k] = bf16_to_f32(a.table[(d >= 0 ? a.bucket[d] : a.n_side + a.bucket[-d]) * a.heads + h]);
     }
     __syncthreads();
     if (i >= a.q_len) continue;  // NW = 1: a wavefront without a row
-    const int first = far + seg - qy.pos;  // the part's first key in near_, behind its edge
-    float m = -__builtin_inff();
+    const int first = far + seg - qy.pos;  // the part's first key in near_
+    float most = -__builtin_inff();
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
       if (q < pt.q0 || q >= pt.q1) continue;
@@ -113,32 +116,39 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
       if (first + 256 * q <= -255) {
         bias[0] = bias[1] = bias[2] = bias[3] = near_[0];
       } else if (first + 256 * q >= far + right) {
-        bias[0] = bias[1] = bias[2] = bias[3] = near_[far + right + kEdge];
+        bias[0] = bias[1] = bias[2] = bias[3] = near_[far + right];
       } else {
 #pragma unroll
-        for (int t = 0; t < 4; ++t) bias[t] = near_[first + kEdge + j + t];
+        for (int t = 0; t < 4; ++t) {
+          const int k = first + j + t;
+          bias[t] = near_[k < 0 ? 0 : k > far + right ? far + right : k];
+        }
       }
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         const float x = e[q][t] * a.scale;
-        const float z = x + bias[t];
-        e[q][t] = pt.sees(j + t) ? z : -__builtin_inff();  // unseen: an e of +0
-        m = fmaxf(m, e[q][t]);
+        e[q][t] = x + bias[t];
       }
+      if (!pt.sees_all(q)) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) e[q][t] = pt.sees(j + t) ? e[q][t] : -__builtin_inff();  // unseen: an e of +0
+      }
+#pragma unroll
+      for (int t = 0; t < 4; ++t) most = fmaxf(most, e[q][t]);
     }
-    m = wave_most(m);
+    most = wave_most(most);
     if constexpr (NW > 1) {
-      if (lane == 0) top[w] = m;
+      if (lane == 0) top[w] = most;
       __syncthreads();
-      m = wave_most(lane < NW ? top[lane] : -__builtin_inff());
+      most = wave_most(lane < parts ? top[lane] : -__builtin_inff());
     }
     // a row whose seen scores are all -inf has e = cexp(-inf) = +0, not cexp(-inf - -inf)
-    m = m == -__builtin_inff() ? 0.0f : m;
+    most = most == -__builtin_inff() ? 0.0f : most;
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
       if (q < pt.q0 || q >= pt.q1) continue;
 #pragma unroll
-      for (int t = 0; t < 4; ++t) e[q][t] = cexp_neg(e[q][t] - m);
+      for (int t = 0; t < 4; ++t) e[q][t] = cexp_neg(e[q][t] - most);
       st[w].put(q, lane, e[q]);
     }
     turn ^= 1;
@@ -168,7 +178,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
 // chunk by chunk, a lane to a chunk, like the row.
 template <int Q, int NW, bool TAIL>
 __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbias_bwd_kernel(
-    RelBiasArgs a, int64_t blocks, int64_t per_head, const uint16_t* __restrict__ probs,
+    RelBiasArgs a, uint32_t heads, uint32_t matrices, uint32_t per_head, const uint16_t* __restrict__ probs,
     const float* __restrict__ dprobs, uint16_t* __restrict__ dscores, float* __restrict__ rowsum) {
   constexpr int kRows = NW == 1 ? 4 : 1;
   __shared__ __attribute__((aligned(16))) RowStage<Q> st[NW == 1 ? 4 : NW];
@@ -181,9 +191,12 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
   const int parts = ((int)a.k_len + 256 * Q - 1) / (256 * Q);
   const int nb = a.n_side * (a.bidirectional ? 2 : 1);
   int turn = 0;  // as above
-  for (int64_t blk = blockIdx.x; blk < blocks; blk += gridDim.x) {
-    const int64_t bh = blk / per_head, b = bh / a.heads, h = bh - b * a.heads;
-    const int64_t i = (blk - bh * per_head) * kRows + (NW == 1 ? w : 0);
+  // a matrix's rows along x, the matrices (batch and head) along y; each further on by the grid where that ends first
+  bool once = true;  // this workgroup's first rows
+  for (uint32_t m = blockIdx.y; m < matrices; m += gridDim.y)
+  for (uint32_t blk = blockIdx.x; blk < per_head; blk += gridDim.x) {
+    const int64_t bh = m, b = m / heads, h = m % heads;
+    const int64_t i = (int64_t)blk * kRows + (NW == 1 ? w : 0);
     const Query qy = query_of(a, b, i);
     const Part pt = part_of(qy, seg, n);
     const int64_t row = (bh * a.q_len + i) * a.ld + seg;
@@ -194,13 +207,13 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
     part_load<TAIL>(pt.from, pt.upto, p, [&](int j, float(&v)[4]) { ldb_wide(pr + j, v); },
                     [&](int j) { return bf16_wide(pr[j]); });
     part_load<TAIL>(pt.from, pt.upto, dp, [&](int j, float(&v)[4]) { ldf<4>(dr + j, v); }, [&](int j) { return dr[j]; });
-    if (rowsum && blk == (int64_t)blockIdx.x) {
+    if (rowsum && once) {
       for (int k = threadIdx.x; k < nb; k += blockDim.x) {
         const int side = k < a.n_side ? k : k - a.n_side;
         const int d0 = a.start[side], d1 = side + 1 < a.n_side ? a.start[side + 1] : 2 * (int)kFarPos;
         if (k < a.n_side) {
           lo_[k] = 1 - d1;
-          hi_[k] = d0 == d1 ? 1 - d1 : d0 == 0 && !a.bidirectional ? 2 * (int)kFarPos : 1 - d0;
+          hi_[k] = d0 == d1 ? 1 - d1 : d0 == 0 && !a.bidirectional && !a.causal ? 2 * (int)kFarPos : 1 - d0;
         } else {
           lo_[k] = d0 > 0 ? d0 : 1;
           hi_[k] = d1;
@@ -208,15 +221,17 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
       }
       __syncthreads();
     }
+    once = false;
     if (i >= a.q_len) continue;  // NW = 1: a wavefront without a row
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
       if (q < pt.q0 || q >= pt.q1) continue;
       float e[4];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const float x = p[q][t] * dp[q][t];
-        e[t] = pt.sees(256 * q + 4 * lane + t) ? x : 0.0f;
+      for (int t = 0; t < 4; ++t) e[t] = p[q][t] * dp[q][t];
+      if (!pt.sees_all(q)) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) e[t] = pt.sees(256 * q + 4 * lane + t) ? e[t] : 0.0f;
       }
       st[w].put(q, lane, e);
     }
@@ -231,10 +246,14 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
 #pragma unroll
                          for (int t = 0; t < 4; ++t) {
                            const float d = dp[q][t] - D;
-                           const float x = p[q][t] * d;
-                           ds[t] = pu.sees(256 * q + 4 * lane + t) ? x : 0.0f;
-                           o[t] = ds[t] * a.scale;
+                           ds[t] = p[q][t] * d;
                          }
+                         if (!pu.sees_all(q)) {
+#pragma unroll
+                           for (int t = 0; t < 4; ++t) ds[t] = pu.sees(256 * q + 4 * lane + t) ? ds[t] : 0.0f;
+                         }
+#pragma unroll
+                         for (int t = 0; t < 4; ++t) o[t] = ds[t] * a.scale;
                          st[w].put(q, lane, ds);  // for the buckets' sums
                        } else {
                          o[0] = o[1] = o[2] = o[3] = 0.0f;
@@ -246,7 +265,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
     float* out = rowsum + ((b * a.q_len + i) * a.heads + h) * nb;
     if constexpr (NW > 1) __syncthreads();
     else __builtin_amdgcn_wave_barrier();
-    for (int k2 = NW == 1 ? lane : (int)threadIdx.x; k2 < 2 * nb; k2 += NW == 1 ? 64 : 64 * NW) {
+    for (int k2 = NW == 1 ? lane : (int)threadIdx.x; k2 < 2 * nb; k2 += NW == 1 ? 64 : (int)blockDim.x) {
       const int k = k2 >> 1, lo = lo_[k], hi = hi_[k];
       const int b0 = qy.pos + lo > qy.j0 ? qy.pos + lo : qy.j0, b1 = qy.pos + hi < qy.j1 ? qy.pos + hi : qy.j1;
       const int mid = (b0 | 31) + 1;  // the next chunk's first key
@@ -254,46 +273,80 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
       float sum = 0.0f;
       if (c0 < c1 && hi - lo <= kRelShort) {
         const float* t = &st[NW == 1 ? w : c0 / (256 * Q)].t[(c0 >> 5) & (8 * Q - 1)][c0 & 31];
-        for (int j = 0; j < c1 - c0; j += 4) {  // up to three places behind the chunk's end: its row's padding
+        const uint32_t mine = 0xFFFFFFFFu >> (32 - (c1 - c0));  // a bit for each of its keys
+        for (int j = 0; j < a.short_most && j < c1 - c0; j += 4) {  // up to three places behind the chunk's end: its row's padding
 #pragma unroll
-          for (int u = 0; u < 4; ++u) sum = sum + (j + u < c1 - c0 ? t[j + u] : 0.0f);
+          for (int u = 0; u < 4; ++u) {
+            const int take = __builtin_amdgcn_sbfe((int)mine, j + u, 1);  // all ones or none
+            sum = sum + __uint_as_float(__float_as_uint(t[j + u]) & (uint32_t)take);
+          }
         }
       }
       sum = sum + __uint_as_float(lane_move<0xB1>(__float_as_uint(sum)));  // the bucket's two chunks
       if (!(k2 & 1) && hi - lo <= kRelShort) out[k] = sum;
     }
-    for (int l = 0; l < a.n_long; ++l) {
-      const int k = a.longs[l];
-      const int lo = lo_[k], hi = hi_[k];
-      const int b0 = (qy.pos + lo > qy.j0 ? qy.pos + lo : qy.j0) - seg, b1 = (qy.pos + hi < qy.j1 ? qy.pos + hi : qy.j1) - seg;
-      float sum = 0.0f;
-      if (b0 < b1 && b0 < 256 * Q && b1 > 0) {  // the same for the whole wavefront
-        const int c0 = b0 - 32 * lane, len = b1 - b0;
-#pragma unroll
-        for (int t = 0; t < kChunk; t += 4) {
-          const float4 v = st[w].vec(lane, t / 4);
-          sum = sum + ((unsigned)(t - c0) < (unsigned)len ? v.x : 0.0f);
-          sum = sum + ((unsigned)(t + 1 - c0) < (unsigned)len ? v.y : 0.0f);
-          sum = sum + ((unsigned)(t + 2 - c0) < (unsigned)len ? v.z : 0.0f);
-          sum = sum + ((unsigned)(t + 3 - c0) < (unsigned)len ? v.w : 0.0f);
-        }
-        sum = wave_total(sum);
-      }
+    if (a.far_only) {
+      // the last bucket(s) alone are long: the keys nearer than them give way to +0, and a lane's chunk is one bucket's
+      if constexpr (NW > 1) __syncthreads();  // the short buckets' keys are read
+      else __builtin_amdgcn_wave_barrier();
+      const int far = a.start[a.n_side - 1];
+      const int z0 = (qy.pos - far + 1 > qy.j0 ? qy.pos - far + 1 : qy.j0) - seg;
+      const int z1 = (a.bidirectional && qy.pos + far < qy.j1 ? qy.pos + far : qy.j1) - seg;
+      for (int z = (z0 > 0 ? z0 : 0) + lane; z < z1 && z < 256 * Q; z += 64) st[w].t[z >> 5][z & 31] = 0.0f;
+      __builtin_amdgcn_wave_barrier();
+      const float c = lane >= 8 * pt.q0 && lane < 8 * pt.q1 ? st[w].chain(lane) : 0.0f;
+      const bool before = !a.bidirectional || seg + 32 * lane <= qy.pos - far;
+      float left = wave_total(before ? c : 0.0f);
+      float right = a.bidirectional ? wave_total(before ? 0.0f : c) : 0.0f;
       if constexpr (NW > 1) {
-        if (lane == 0) part[l & 1][w] = sum;
+        if (lane == 0) {
+          part[0][w] = left;
+          part[1][w] = right;
+        }
         __syncthreads();
-        sum = wave_total(lane < parts ? part[l & 1][lane] : 0.0f);
+        left = wave_total(lane < parts ? part[0][lane] : 0.0f);
+        right = wave_total(lane < parts ? part[1][lane] : 0.0f);
       }
-      if (lane == 0 && (NW == 1 || w == 0)) out[k] = sum;
+      if (lane == 0 && (NW == 1 || w == 0)) {
+        out[a.n_side - 1] = left;
+        if (a.bidirectional) out[nb - 1] = right;
+      }
+    } else {
+      for (int l = 0; l < a.n_long; ++l) {
+        const int k = a.longs[l];
+        const int lo = lo_[k], hi = hi_[k];
+        const int b0 = (qy.pos + lo > qy.j0 ? qy.pos + lo : qy.j0) - seg, b1 = (qy.pos + hi < qy.j1 ? qy.pos + hi : qy.j1) - seg;
+        float sum = 0.0f;
+        if (b0 < b1 && b0 < 256 * Q && b1 > 0) {  // the same for the whole wavefront
+          if (lane < 8 * Q) {
+            const int c0 = b0 - 32 * lane, len = b1 - b0;
+  #pragma unroll
+            for (int t = 0; t < kChunk; t += 4) {
+              const float4 v = st[w].vec(lane, t / 4);
+              sum = sum + ((unsigned)(t - c0) < (unsigned)len ? v.x : 0.0f);
+              sum = sum + ((unsigned)(t + 1 - c0) < (unsigned)len ? v.y : 0.0f);
+              sum = sum + ((unsigned)(t + 2 - c0) < (unsigned)len ? v.z : 0.0f);
+              sum = sum + ((unsigned)(t + 3 - c0) < (unsigned)len ? v.w : 0.0f);
+            }
+          }
+          sum = wave_total(sum);
+        }
+        if constexpr (NW > 1) {
+          if (lane == 0) part[l & 1][w] = sum;
+          __syncthreads();
+          sum = wave_total(lane < parts ? part[l & 1][lane] : 0.0f);
+        }
+        if (lane == 0 && (NW == 1 || w == 0)) out[k] = sum;
+      }
     }
     if constexpr (NW > 1) __syncthreads();  // the row's ds are read
   }
 }
 
-// chains of 32 rows of a [rows][cols] matrix's columns
-__global__ __launch_bounds__(256) void column_chain_kernel(int64_t rows, int64_t cols, const float* __restrict__ x,
-                                                           float* __restrict__ part) {
-  const int64_t col = (int64_t)blockIdx.x * 256 + threadIdx.x;
+// chains of 32 rows of a [rows][cols] matrix's columns, a wavefront to 64 columns of one, 16 rows in flight
+__global__ __launch_bounds__(64) void column_chain_kernel(int64_t rows, int64_t cols, const float* __restrict__ x,
+                                                          float* __restrict__ part) {
+  const int64_t col = (int64_t)blockIdx.x * 64 + threadIdx.x;
   if (col >= cols) return;
   const int64_t nc = (rows + kChunk - 1) / kChunk;
   for (int64_t c = blockIdx.y; c < nc; c += gridDim.y) {
@@ -302,12 +355,12 @@ __global__ __launch_bounds__(256) void column_chain_kernel(int64_t rows, int64_t
     float s = 0.0f;
     if (n == kChunk) {
 #pragma unroll
-      for (int k = 0; k < kChunk; k += 8) {
-        float v[8];
+      for (int k = 0; k < kChunk; k += 16) {
+        float v[16];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = x[(t0 + k + i) * cols + col];
+        for (int i = 0; i < 16; ++i) v[i] = x[(t0 + k + i) * cols + col];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s = s + v[i];
+        for (int i = 0; i < 16; ++i) s = s + v[i];
       }
     } else {
       for (int k = 0; k < n; ++k) s = s + x[(t0 + k) * cols + col];
@@ -318,35 +371,31 @@ __global__ __launch_bounds__(256) void column_chain_kernel(int64_t rows, int64_t
 
 }  // namespace
 
-#define CANON_REL_ROWS(K)          \
-  switch (row_shape(a.k_len)) {     \
-    case 2: K(2, 1); break;         \
-    case 4: K(4, 1); break;         \
-    case 8: K(8, 1); break;         \
-    case 16: K(8, 2); break;        \
-    case 32: K(8, 4); break;        \
-    case 64: K(8, 8); break;        \
-    default: K(8, 16); break;       \
-  }
+// Rows along x, matrices along y, within 2^32 threads of x and 65535 of y.
+static dim3 relbias_grid(const RowShape& shape, int64_t matrices, int64_t per_head) {
+  const int64_t x = per_head < kMaxBlocks ? per_head : kMaxBlocks;
+  return dim3((unsigned)x, (unsigned)(matrices < 65535 ? matrices : 65535));
+}
 
 hipError_t relbias_fwd_launch(const RelBiasArgs& a, const float* scores, uint16_t* probs, hipStream_t s) {
-  const int nw = row_waves(a.k_len);
-  const int64_t per_head = (a.q_len + (nw == 1 ? 3 : 0)) / (nw == 1 ? 4 : 1);
-  const int64_t blocks = a.batch * a.heads * per_head;
-  if (blocks == 0 || a.k_len == 0) return hipSuccess;
-  const dim3 grid((unsigned)(blocks < kMaxBlocks ? blocks : kMaxBlocks)), wg(nw == 1 ? 256 : 64 * nw);
+  const RowShape shape = row_shape(a.batch * a.heads * a.q_len, a.k_len, 6);
+  const int64_t matrices = a.batch * a.heads, per_head = shape.groups(a.q_len);
+  if (matrices * per_head == 0 || a.k_len == 0) return hipSuccess;
+  const dim3 grid = relbias_grid(shape, matrices, per_head), wg(shape.threads());
   const bool tail = a.k_len % 4 != 0;
   const int far = a.start[a.n_side - 1];
-  const size_t lds = sizeof(float) * (size_t)(far + 1 + (a.bidirectional ? far : 0) + 2 * kEdge);
-#define CANON_REL(Q, NW)                                                                                                \
-  do {                                                                                                                  \
-    if (tail)                                                                                                           \
-      hipLaunchKernelGGL((relbias_fwd_kernel<Q, NW, true>), grid, wg, lds, s, a, blocks, per_head, scores, probs);         \
-    else                                                                                                                \
-      hipLaunchKernelGGL((relbias_fwd_kernel<Q, NW, false>), grid, wg, lds, s, a, blocks, per_head, scores, probs);        \
+  const size_t lds = sizeof(float) * (size_t)(far + 1 + (a.bidirectional ? far : 0));
+#define CANON_REL_K(Q, NW, TAIL)                                                                                    \
+  hipLaunchKernelGGL((relbias_fwd_kernel<Q, NW, TAIL>), grid, wg, lds, s, a, (uint32_t)a.heads, (uint32_t)matrices, \
+                     (uint32_t)per_head, scores, probs)
+#define CANON_REL(Q, NW)                   \
+  do {                                     \
+    if (tail) CANON_REL_K(Q, NW, true);    \
+    else CANON_REL_K(Q, NW, false);        \
   } while (0)
-  CANON_REL_ROWS(CANON_REL)
+  CANON_ROW_SHAPES(CANON_REL, shape);
 #undef CANON_REL
+#undef CANON_REL_K
   return hipGetLastError();
 }
 
@@ -356,25 +405,24 @@ int64_t relbias_scratch_floats(int64_t rows, int64_t heads, int64_t buckets) {
 
 hipError_t relbias_bwd_launch(const RelBiasArgs& a, const uint16_t* probs, const float* dprobs, uint16_t* dscores,
                               float* dtable, float* rowsum, hipStream_t s) {
-  const int nw = row_waves(a.k_len);
-  const int64_t per_head = (a.q_len + (nw == 1 ? 3 : 0)) / (nw == 1 ? 4 : 1);
-  const int64_t blocks = a.batch * a.heads * per_head;
-  const bool empty = blocks == 0 || a.k_len == 0;
+  const RowShape shape = row_shape(a.batch * a.heads * a.q_len, a.k_len, 6);
+  const int64_t matrices = a.batch * a.heads, per_head = shape.groups(a.q_len);
+  const bool empty = matrices * per_head == 0 || a.k_len == 0;
   if (!empty) {
-    const dim3 grid((unsigned)(blocks < kMaxBlocks ? blocks : kMaxBlocks)), wg(nw == 1 ? 256 : 64 * nw);
+    const dim3 grid = relbias_grid(shape, matrices, per_head), wg(shape.threads());
     const bool tail = a.k_len % 4 != 0;
     float* rs = dtable ? rowsum : nullptr;
-#define CANON_REL(Q, NW)                                                                                                \
-  do {                                                                                                                  \
-    if (tail)                                                                                                           \
-      hipLaunchKernelGGL((relbias_bwd_kernel<Q, NW, true>), grid, wg, 0, s, a, blocks, per_head, probs, dprobs, dscores,   \
-                         rs);                                                                                           \
-    else                                                                                                                \
-      hipLaunchKernelGGL((relbias_bwd_kernel<Q, NW, false>), grid, wg, 0, s, a, blocks, per_head, probs, dprobs, dscores,  \
-                         rs);                                                                                           \
+#define CANON_REL_K(Q, NW, TAIL)                                                                                  \
+  hipLaunchKernelGGL((relbias_bwd_kernel<Q, NW, TAIL>), grid, wg, 0, s, a, (uint32_t)a.heads, (uint32_t)matrices, \
+                     (uint32_t)per_head, probs, dprobs, dscores, rs)
+#define CANON_REL(Q, NW)                   \
+  do {                                     \
+    if (tail) CANON_REL_K(Q, NW, true);    \
+    else CANON_REL_K(Q, NW, false);        \
   } while (0)
-    CANON_REL_ROWS(CANON_REL)
+    CANON_ROW_SHAPES(CANON_REL, shape);
 #undef CANON_REL
+#undef CANON_REL_K
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -383,8 +431,8 @@ hipError_t relbias_bwd_launch(const RelBiasArgs& a, const uint16_t* probs, const
   const int64_t rows = empty ? 0 : a.batch * a.q_len, nc = (rows + kChunk - 1) / kChunk;
   float* part = rowsum + rows * cols;
   if (rows > 0) {
-    hipLaunchKernelGGL(column_chain_kernel, dim3((unsigned)((cols + 255) / 256), (unsigned)(nc < 65535 ? nc : 65535)),
-                       dim3(256), 0, s, rows, cols, rowsum, part);
+    hipLaunchKernelGGL(column_chain_kernel, dim3((unsigned)((cols + 63) / 64), (unsigned)(nc < 65535 ? nc : 65535)),
+                       dim3(64), 0, s, rows, cols, rowsum, part);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

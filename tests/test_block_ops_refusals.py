@@ -177,6 +177,7 @@ def test_the_binding_refuses_other_tensors():
                  lambda: C.layernorm(4, 100, f.half(), h, None, 1e-5, f, f, f),
                  lambda: C.layernorm_bwd(4, 100, kept, h, f, f, f, f),
                  lambda: C.swiglu(4, 50, f, h), lambda: C.swiglu_bwd(4, 50, kept, f, h),
+                 lambda: C.act8_pack(4, 100, None, kept), lambda: C.layernorm(4, 100, None, h, None, 1e-5, f, f, f),
                  lambda: C.AttnRows(4, 1, 1, 1, k_lens=torch.zeros(4, dtype=torch.int32)),
                  lambda: C.AttnRows(4, 1, 1, 1, k_lens=[1, 2, 3, 4]),
                  lambda: C.softmax_relbias(C.AttnRows(1, 1, 20, 20), C.RelBias([0]), h, f, h)):
