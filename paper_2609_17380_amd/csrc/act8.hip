@@ -36,9 +36,11 @@ __global__ __launch_bounds__(256) void act8_pack_kernel(int64_t rows, int64_t co
       for (int t = 0; t < 4; ++t) v[q][t] = 0.0f;
       if (j < cols) act4<SRC, TAIL>(x, row, j, cols, v[q]);
     }
+    float s[kTileQ];
+    steps4(v, k.lg, s);
 #pragma unroll
     for (int q = 0; q < kTileQ; ++q)
-      keep4<TAIL>(v[q], j0 + 256 * q, cols, k.lg, k.codes + row * cols, k.steps + row * groups);
+      keep4<TAIL>(v[q], s[q], j0 + 256 * q, cols, k.lg, k.codes + row * cols, k.steps + row * groups);
   }
 }
 
@@ -89,12 +91,17 @@ __global__ __launch_bounds__(256) void swiglu_keep_kernel(int64_t T, int64_t F, 
         act4<SRC, TAIL>(gu, 2 * t + 1, j, F, u[q]);
       }
     }
+    float sg[kGluQ], su[kGluQ];
+    if (KEEP) {
+      steps4(g, k.lg, sg);
+      steps4(u, k.lg, su);
+    }
 #pragma unroll
     for (int q = 0; q < kGluQ; ++q) {
       const int64_t j = j0 + 256 * q;
       if (KEEP) {
-        keep4<TAIL>(g[q], j, F, k.lg, k.codes + 2 * t * F, k.steps + 2 * t * groups);
-        keep4<TAIL>(u[q], j, F, k.lg, k.codes + (2 * t + 1) * F, k.steps + (2 * t + 1) * groups);
+        keep4<TAIL>(g[q], sg[q], j, F, k.lg, k.codes + 2 * t * F, k.steps + 2 * t * groups);
+        keep4<TAIL>(u[q], su[q], j, F, k.lg, k.codes + (2 * t + 1) * F, k.steps + (2 * t + 1) * groups);
       }
       if (j >= F) continue;
       float h[4];

@@ -18,38 +18,40 @@ struct __attribute__((packed, aligned(1))) B4 {
 // Elements j .. j + 3 of a row of n (j a multiple of 4 whose lanes run through whole groups; v holds 0 beyond n) into
 // codes and their group's step.  Every lane of the wavefront takes part.  The magnitudes are compared as bit patterns,
 // so that a NaN ranks above every number.
-__device__ __forceinline__ float step4(const float (&v)[4], int lg) {
-  uint32_t m = 0;
+template <int Q>
+__device__ __forceinline__ void steps4(const float (&v)[Q][4], int lg, float (&s)[Q]) {  // of Q vectors
+  uint32_t m[Q];
 #pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    const uint32_t a = __float_as_uint(v[t]) & 0x7FFFFFFFu;
-    m = a > m ? a : m;
+  for (int q = 0; q < Q; ++q) {
+    m[q] = 0;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const uint32_t a = __float_as_uint(v[q][t]) & 0x7FFFFFFFu;
+      m[q] = a > m[q] ? a : m[q];
+    }
   }
-  m = lanes_join(m, 1 << (lg - 2), [](uint32_t a, uint32_t b) { return a > b ? a : b; });
-  return __uint_as_float(m) * __uint_as_float(kInv127Bits);
+  lanes_join(m, 1 << (lg - 2), [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+#pragma unroll
+  for (int q = 0; q < Q; ++q) s[q] = __uint_as_float(m[q]) * __uint_as_float(kInv127Bits);
 }
 // The reciprocal of a step of keep4's (|v / s| <= 127 (1 + 2^-23)), for quant_pack's rule: v_rcp_f32 is within 2^-23 of 1/s,
 // so t = RN(v rs) within 127 (2^-23 + 2^-24) (1 + 2^-22) < 2.28e-5 of v / s, and RN(v / s) within 2^-18: together below the
 // 2^-15 that t has to be away from every half-integer.  The correctly rounded quotient took 12 instructions.
 __device__ __forceinline__ float step_rcp(float s) { return recip_step_ok(s) ? __builtin_amdgcn_rcpf(s) : 0.0f; }
-__device__ __forceinline__ uint32_t codes4(const float (&v)[4], int lg, float& s) {
-  s = step4(v, lg);
+// vector v of elements j .. j + 3, whose group has step s
+template <bool TAIL>
+__device__ __forceinline__ void keep4(const float (&v)[4], float s, int64_t j, int64_t n, int lg, int8_t* codes,
+                                      float* steps) {
   uint32_t w[1];
   quant_pack<4>(v, s, step_rcp(s), recip_step_ok(s), w);
-  return w[0];
-}
-template <bool TAIL>
-__device__ __forceinline__ void keep4(const float (&v)[4], int64_t j, int64_t n, int lg, int8_t* codes, float* steps) {
-  float s;
-  const uint32_t w = codes4(v, lg, s);
   if (j >= n) return;
   if ((j & ((1 << lg) - 1)) == 0) steps[j >> lg] = s;
   if (!TAIL || j + 4 <= n) {
-    reinterpret_cast<B4*>(codes + j)->x = w;
+    reinterpret_cast<B4*>(codes + j)->x = w[0];
   } else {
 #pragma unroll
     for (int t = 0; t < 4; ++t)
-      if (j + t < n) codes[j + t] = (int8_t)(w >> (8 * t));
+      if (j + t < n) codes[j + t] = (int8_t)(w[0] >> (8 * t));
   }
 }
 // The same of a part of a row (part_load): v holds 0 beyond n.  Every code is taken through the reciprocal first; the few
@@ -61,10 +63,9 @@ __device__ __forceinline__ void part_keep(const float (&v)[Q][4], int n, int lg,
   const int at = 4 * (threadIdx.x & 63);
   uint32_t w[Q], undecided = 0;
   float s[Q];
+  steps4(v, lg, s);
 #pragma unroll
   for (int q = 0; q < Q; ++q) {
-    if (256 * q >= n) break;
-    s[q] = step4(v[q], lg);
     const float rs = step_rcp(s[q]);
     float off = 0.0f;  // how far the furthest is from its integer
     uint32_t x = 0;

@@ -115,21 +115,38 @@ template <int CTRL>
 __device__ __forceinline__ uint32_t lane_move(uint32_t x) {
   return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true);
 }
-template <class Join>
-__device__ __forceinline__ uint32_t lanes_join(uint32_t x, int lanes, Join join) {
-  x = join(x, lane_move<0xB1>(x));   // lanes 1 0 3 2 of each four
-  x = join(x, lane_move<0x4E>(x));   // lanes 2 3 0 1
-  x = join(x, lane_move<0x141>(x));  // each eight mirrored
-  if (lanes > 8) x = join(x, lane_move<0x140>(x));  // each sixteen mirrored
+template <int N, class Join>
+__device__ __forceinline__ void lanes_join(uint32_t (&x)[N], int lanes, Join join) {  // N values, a step of all at a time
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = join(x[i], lane_move<0xB1>(x[i]));   // lanes 1 0 3 2 of each four
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = join(x[i], lane_move<0x4E>(x[i]));   // lanes 2 3 0 1
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = join(x[i], lane_move<0x141>(x[i]));  // each eight mirrored
+  if (lanes > 8) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = join(x[i], lane_move<0x140>(x[i]));  // each sixteen mirrored
+  }
   if (lanes > 16) {
-    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-    x = join(r[0], r[1]);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const auto r = __builtin_amdgcn_permlane16_swap(x[i], x[i], false, false);
+      x[i] = join(r[0], r[1]);
+    }
   }
   if (lanes > 32) {
-    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
-    x = join(r[0], r[1]);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const auto r = __builtin_amdgcn_permlane32_swap(x[i], x[i], false, false);
+      x[i] = join(r[0], r[1]);
+    }
   }
-  return x;
+}
+template <class Join>
+__device__ __forceinline__ uint32_t lanes_join(uint32_t x, int lanes, Join join) {
+  uint32_t v[1] = {x};
+  lanes_join(v, lanes, join);
+  return v[0];
 }
 // Algorithm 2 over 64 chunk partials, one per lane, of which those past the last chunk are +0: adding them is the
 // pass-through rule (no partial is -0).  The sum in every lane.
@@ -309,7 +326,7 @@ __device__ __forceinline__ float wide_join(float p, int parts, float* slot) {
 }
 template <int NW, int Q>
 __device__ __forceinline__ float wide_row_sum(RowStage<Q>& st, const float (&e)[Q][4], int n, float* slot) {
-  const int lane = threadIdx.x & 63, left = NW == 1 ? n : n - wave_id() * 256 * Q;
+  const int lane = threadIdx.x & 63, left = again(NW == 1 ? n : n - wave_id() * 256 * Q);
 #pragma unroll
   for (int q = 0; q < Q; ++q) {
     if (256 * q >= left) break;
