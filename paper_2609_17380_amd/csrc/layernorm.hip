@@ -175,10 +175,10 @@ __device__ __forceinline__ void load_columns(const ActIn& x, const float* dy, in
 // The chains of 32 rows of dgain[k] = R1 over rows of RN(dy xh) and dbias[k] = R1 over rows of dy, V = 4 columns or one per
 // thread, B rows in flight.  part: [2][chunks][cols].
 template <int SRC, int V, int B, bool TAIL>
-__global__ __launch_bounds__(64) void layernorm_part_kernel(int64_t rows, int cols, ActIn x, const float* __restrict__ mean,
+__global__ __launch_bounds__(256 / V) void layernorm_part_kernel(int64_t rows, int cols, ActIn x, const float* __restrict__ mean,
                                                             const float* __restrict__ rstd, const float* __restrict__ dy,
                                                             float* __restrict__ part) {
-  const int j = (blockIdx.x * 64 + threadIdx.x) * V, n = cols - j < V ? cols - j : V;
+  const int j = blockIdx.x * 256 + threadIdx.x * V, n = cols - j < V ? cols - j : V;
   const int64_t nc = (rows + kChunk - 1) / kChunk;
   if (n <= 0) return;
   for (int64_t c = blockIdx.y; c < nc; c += gridDim.y) {
@@ -227,125 +227,133 @@ __global__ __launch_bounds__(64) void layernorm_part_kernel(int64_t rows, int co
   }
 }
 
-// The whole backward in one pass over x and dy: a workgroup takes a chain of 32 rows, wavefront w the columns 256 w .. +255
-// of them, four rows at a time.  A lane's four columns run through the 32 rows in order, so it holds their chains of dgain
-// and dbias; a row's own sums, two to a row, are cut into 8 chunks to a wavefront, 64 chains in all, a lane to a chain over
-// an LDS transpose, folded over the wavefront's 8 chunks and then over the wavefronts.  The next four rows are loaded
+// The whole backward in one pass over x and dy: a workgroup takes a chain of 32 rows, wavefront w the 256 VQ columns from
+// 256 VQ w on, R = 4 / VQ rows at a time.  A lane's columns run through the 32 rows in order, so it holds their chains of
+// dgain and dbias; a row's own sums, two to a row, are cut into 8 VQ chunks to a wavefront, 64 chains in all, a lane to a
+// chain over an LDS transpose, folded over the wavefront's chunks and then over the wavefronts.  The next rows are loaded
 // before the barrier that the sums wait at.
-constexpr int kPassRows = 4;
-template <int SRC, int NW, bool TAIL>
+template <int SRC, int VQ, int NW, bool TAIL>
 __global__ __launch_bounds__(64 * NW) void layernorm_pass_kernel(int64_t rows, int cols, ActIn x,
                                                                  const uint16_t* __restrict__ gain,
                                                                  const float* __restrict__ mean,
                                                                  const float* __restrict__ rstd,
                                                                  const float* __restrict__ dy, float inv_d,
                                                                  float* __restrict__ dx, float* __restrict__ part) {
-  __shared__ __attribute__((aligned(16))) RegStage st[NW];
-  __shared__ float slot[2][2 * kPassRows][NW];
-  const int w = wave_id(), lane = threadIdx.x & 63;
-  const int j = 256 * w + 4 * lane;  // this lane's first column
-  const int n = cols - j < 4 ? cols - j : 4;  // and how many of its four there are
-  const int64_t nc = (rows + kChunk - 1) / kChunk;
+  constexpr int R = 4 / VQ, kSums = 2 * R, kLanes = 8 * VQ;  // lanes to a sum's chunks
   using In = PartIn<SRC>;
-  auto load = [&](int64_t row, typename In::Raw& xr, float(&dv)[4]) __attribute__((always_inline)) {
-    load_columns<SRC, TAIL>(x, dy, rows, row, cols, j, n, xr, dv);
-  };
-  float gv[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  __shared__ __attribute__((aligned(16))) RegStage st[NW];
+  __shared__ float slot[2][kSums][NW];
+  const int w = wave_id(), lane = threadIdx.x & 63;
+  int j[VQ], n[VQ];  // this lane's first columns, and how many of each four there are
 #pragma unroll
-  for (int t = 0; t < 4; ++t)
-    if (t < n) gv[t] = bf16_wide(gain[j + t]);
+  for (int v = 0; v < VQ; ++v) {
+    j[v] = 256 * (VQ * w + v) + 4 * lane;
+    n[v] = cols - j[v] < 4 ? cols - j[v] : 4;
+  }
+  const int64_t nc = (rows + kChunk - 1) / kChunk;
+  auto load = [&](int64_t row, typename In::Raw(&xr)[VQ], float(&dv)[VQ][4]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int v = 0; v < VQ; ++v) load_columns<SRC, TAIL>(x, dy, rows, row, cols, j[v], n[v], xr[v], dv[v]);
+  };
+  auto add = [](uint32_t a, uint32_t b) {
+    const float s = __uint_as_float(a) + __uint_as_float(b);
+    return __float_as_uint(s);
+  };
+  float gv[VQ][4];
+#pragma unroll
+  for (int v = 0; v < VQ; ++v)
+#pragma unroll
+    for (int t = 0; t < 4; ++t) gv[v][t] = t < n[v] ? bf16_wide(gain[j[v] + t]) : 0.0f;
   for (int64_t c = blockIdx.x; c < nc; c += gridDim.x) {
     const int64_t t0 = c * kChunk;
-    typename In::Raw xr[kPassRows];
-    float dv[kPassRows][4], sg[4] = {0.0f, 0.0f, 0.0f, 0.0f}, sb[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    typename In::Raw xr[R][VQ];
+    float dv[R][VQ][4], sg[VQ][4], sb[VQ][4];
 #pragma unroll
-    for (int r = 0; r < kPassRows; ++r) load(t0 + r, xr[r], dv[r]);
-    for (int k = 0; k < kChunk / kPassRows; ++k) {
-      const int64_t t = t0 + kPassRows * k;
+    for (int v = 0; v < VQ; ++v)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sg[v][i] = sb[v][i] = 0.0f;
+#pragma unroll
+    for (int r = 0; r < R; ++r) load(t0 + r, xr[r], dv[r]);
+    for (int k = 0; k < kChunk / R; ++k) {
+      const int64_t t = t0 + R * k;
       if (t >= rows) break;
-      float xh[kPassRows][4], gy[kPassRows][4], rs[kPassRows];
+      float xh[R][VQ][4], gy[R][VQ][4], rs[R];
 #pragma unroll
-      for (int r = 0; r < kPassRows; ++r) {
+      for (int r = 0; r < R; ++r) {
         const int64_t row = t + r < rows ? t + r : rows - 1;
         const float mu = mean[row];
         rs[r] = rstd[row];
-        float tm[4], xv[4];
-        In::wide(xr[r], xv);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float d = xv[i] - mu;
-          xh[r][i] = d * rs[r];
-          gy[r][i] = dv[r][i] * gv[i];
-          tm[i] = gy[r][i] * xh[r][i];
-          if (i >= n) gy[r][i] = tm[i] = 0.0f;  // no column: a term of +0
-          const float pr = dv[r][i] * xh[r][i];
-          if (t + r < rows) {
-            sg[i] = sg[i] + pr;
-            sb[i] = sb[i] + dv[r][i];
+        for (int v = 0; v < VQ; ++v) {
+          float tm[4], xv[4];
+          In::wide(xr[r][v], xv);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float d = xv[i] - mu;
+            xh[r][v][i] = d * rs[r];
+            gy[r][v][i] = dv[r][v][i] * gv[v][i];
+            tm[i] = gy[r][v][i] * xh[r][v][i];
+            if (i >= n[v]) gy[r][v][i] = tm[i] = 0.0f;  // no column: a term of +0
+            const float pr = dv[r][v][i] * xh[r][v][i];
+            if (t + r < rows) {
+              sg[v][i] = sg[v][i] + pr;
+              sb[v][i] = sb[v][i] + dv[r][v][i];
+            }
           }
+          st[w].put((2 * r) * VQ + v, lane, gy[r][v]);
+          st[w].put((2 * r + 1) * VQ + v, lane, tm);
         }
-        st[w].put(2 * r, lane, gy[r]);
-        st[w].put(2 * r + 1, lane, tm);
       }
       __builtin_amdgcn_wave_barrier();
 #pragma unroll
-      for (int r = 0; r < kPassRows; ++r) load(t + kPassRows + r < t0 + kChunk ? t + kPassRows + r : rows, xr[r], dv[r]);
-      float p = 0.0f;  // the chain of chunk lane % 8 of sum lane / 8
-#pragma unroll
-      for (int i = 0; i < kChunk / 4; ++i) {
-        const float4 v = st[w].vec(lane, i);
-        p = p + v.x; p = p + v.y; p = p + v.z; p = p + v.w;
-      }
-      auto add = [](uint32_t a, uint32_t b) {
-        const float s = __uint_as_float(a) + __uint_as_float(b);
-        return __float_as_uint(s);
-      };
-      p = __uint_as_float(lanes_join(__float_as_uint(p), 8, add));
-      if ((lane & 7) == 0) slot[k & 1][lane >> 3][w] = p;
+      for (int r = 0; r < R; ++r) load(t + R + r < t0 + kChunk ? t + R + r : rows, xr[r], dv[r]);
+      // the chain of chunk lane % kLanes of sum lane / kLanes
+      const float p = __uint_as_float(lanes_join(__float_as_uint(st[w].chain(lane)), kLanes, add));
+      if ((lane & (kLanes - 1)) == 0) slot[k & 1][lane / kLanes][w] = p;
       __syncthreads();
-      float m[2 * kPassRows];
-      if constexpr (NW <= 8) {
-        float s = (lane & 7) < NW ? slot[k & 1][lane >> 3][lane & 7] : 0.0f;
-        s = __uint_as_float(lanes_join(__float_as_uint(s), 8, add)) * inv_d;
+      float m[kSums];
+      constexpr int kWide = NW <= 8 ? 8 : 16, kOnce = 64 / kWide;  // lanes to a sum's wavefronts, and sums at a time
 #pragma unroll
-        for (int i = 0; i < 2 * kPassRows; ++i) m[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(s), 8 * i));
-      } else {
+      for (int i0 = 0; i0 < kSums; i0 += kOnce) {
+        const int sum = i0 + lane / kWide, of = lane & (kWide - 1);
+        float s = sum < kSums && of < NW ? slot[k & 1][sum < kSums ? sum : 0][of < NW ? of : 0] : 0.0f;
+        s = __uint_as_float(lanes_join(__float_as_uint(s), kWide, add)) * inv_d;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          float s = slot[k & 1][4 * half + (lane >> 4)][lane & 15];
-          s = __uint_as_float(lanes_join(__float_as_uint(s), 16, add)) * inv_d;
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            m[4 * half + i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(s), 16 * i));
-        }
+        for (int i = 0; i < kOnce; ++i)
+          if (i0 + i < kSums) m[i0 + i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(s), kWide * i));
       }
 #pragma unroll
-      for (int r = 0; r < kPassRows; ++r) {
+      for (int r = 0; r < R; ++r) {
         if (t + r >= rows) break;
-        float o[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float a = gy[r][i] - m[2 * r];
-          const float b = xh[r][i] * m[2 * r + 1];
-          const float d = a - b;
-          o[i] = rs[r] * d;
-        }
-        float* out = dx + (t + r) * cols + j;
-        if (n == 4) {
-          stf<4>(out, o);
-        } else if (TAIL) {
+        for (int v = 0; v < VQ; ++v) {
+          float o[4];
 #pragma unroll
-          for (int i = 0; i < 3; ++i)
-            if (i < n) out[i] = o[i];
+          for (int i = 0; i < 4; ++i) {
+            const float a = gy[r][v][i] - m[2 * r];
+            const float b = xh[r][v][i] * m[2 * r + 1];
+            const float d = a - b;
+            o[i] = rs[r] * d;
+          }
+          float* out = dx + (t + r) * cols + j[v];
+          if (n[v] == 4) {
+            stf<4>(out, o);
+          } else if (TAIL) {
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+              if (i < n[v]) out[i] = o[i];
+          }
         }
       }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (i < n) {
-        part[c * cols + j + i] = sg[i];
-        part[(nc + c) * cols + j + i] = sb[i];
-      }
+    for (int v = 0; v < VQ; ++v)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i < n[v]) {
+          part[c * cols + j[v] + i] = sg[v][i];
+          part[(nc + c) * cols + j[v] + i] = sb[v][i];
+        }
   }
 }
 
@@ -401,7 +409,7 @@ __global__ __launch_bounds__(64 * kFoldBlocks) void column_fold_kernel(int64_t n
 }
 
 constexpr int64_t kMaxBlocks = 1 << 20;
-constexpr int64_t kPassCols = 4096;  // 16 wavefronts of 256 columns
+constexpr int64_t kPassCols = 8192;  // 16 wavefronts of 512 columns
 
 }  // namespace
 
@@ -457,26 +465,27 @@ hipError_t layernorm_bwd_launch(int64_t rows, int64_t cols, const ActIn& x, cons
                                 hipStream_t s) {
   const float inv_d = (float)(1.0 / (double)cols);
   const int64_t nc = (rows + kChunk - 1) / kChunk;
-  // One pass over x and dy where its workgroups, one to 32 rows, are enough to fill the chip: 8192 x 2048 in 45 us against
-  // 66 in two passes, 2048 x 2048 (64 workgroups) in 29 against 21.
-  const bool once = (dgain || dbias) && cols <= kPassCols && nc >= device_cus();
+  // One pass over x and dy where its workgroups, one to 32 rows, are half as many as the CUs or more (with the forward:
+  // 4096 x 2048 in 39 us, in two passes 45; 4096 x 8192 in 151 and 178; of 2048 rows 31 and 28, 110 and 90).
+  const bool once = (dgain || dbias) && cols <= kPassCols && 2 * nc >= device_cus();
   if (once) {
     const dim3 grid((unsigned)(nc < kMaxBlocks ? nc : kMaxBlocks));
-#define CANON_LN_PASS(SRC, NW)                                                                                          \
+#define CANON_LN_PASS(SRC, VQ, NW)                                                                                         \
   do {                                                                                                                  \
     if (cols % 4 == 0)                                                                                                  \
-      hipLaunchKernelGGL((layernorm_pass_kernel<SRC, NW, false>), grid, dim3(64 * NW), 0, s, rows, (int)cols, x, gain,  \
+      hipLaunchKernelGGL((layernorm_pass_kernel<SRC, VQ, NW, false>), grid, dim3(64 * NW), 0, s, rows, (int)cols, x, gain,  \
                          mean, rstd, dy, inv_d, dx, part);                                                              \
     else                                                                                                                \
-      hipLaunchKernelGGL((layernorm_pass_kernel<SRC, NW, true>), grid, dim3(64 * NW), 0, s, rows, (int)cols, x, gain,   \
+      hipLaunchKernelGGL((layernorm_pass_kernel<SRC, VQ, NW, true>), grid, dim3(64 * NW), 0, s, rows, (int)cols, x, gain,   \
                          mean, rstd, dy, inv_d, dx, part);                                                              \
   } while (0)
-#define CANON_LN_PASS_WAVES(SRC)                   \
-  do {                                             \
-    if (cols <= 512) CANON_LN_PASS(SRC, 2);        \
-    else if (cols <= 1024) CANON_LN_PASS(SRC, 4);  \
-    else if (cols <= 2048) CANON_LN_PASS(SRC, 8);  \
-    else CANON_LN_PASS(SRC, 16);                   \
+#define CANON_LN_PASS_WAVES(SRC)                      \
+  do {                                                \
+    if (cols <= 512) CANON_LN_PASS(SRC, 1, 2);        \
+    else if (cols <= 1024) CANON_LN_PASS(SRC, 1, 4);  \
+    else if (cols <= 2048) CANON_LN_PASS(SRC, 1, 8);  \
+    else if (cols <= 4096) CANON_LN_PASS(SRC, 1, 16); \
+    else CANON_LN_PASS(SRC, 2, 16);                   \
   } while (0)
     if (x.src == ACT_F32) CANON_LN_PASS_WAVES(ACT_F32);
     else if (x.src == ACT_BF16) CANON_LN_PASS_WAVES(ACT_BF16);
@@ -490,13 +499,13 @@ hipError_t layernorm_bwd_launch(int64_t rows, int64_t cols, const ActIn& x, cons
   if ((dgain || dbias) && rows > 0) {
     // four columns to a thread once that makes eight wavefronts to a CU; below, one
     const int v = nc * ((cols + 255) / 256) >= 8 * device_cus() ? 4 : 1;
-    const dim3 grid((unsigned)((cols + 64 * v - 1) / (64 * v)), (unsigned)(nc < 65535 ? nc : 65535));
+    const dim3 grid((unsigned)((cols + 255) / 256), (unsigned)(nc < 65535 ? nc : 65535));
 #define CANON_LN_PART_K(SRC, V, B, TAIL)                                                                                \
-  hipLaunchKernelGGL((layernorm_part_kernel<SRC, V, B, TAIL>), grid, dim3(64), 0, s, rows, (int)cols, x, mean, rstd,    \
+  hipLaunchKernelGGL((layernorm_part_kernel<SRC, V, B, TAIL>), grid, dim3(256 / V), 0, s, rows, (int)cols, x, mean, rstd,    \
                      dy, part)
 #define CANON_LN_PART(SRC)                                        \
   do {                                                            \
-    if (v == 1) CANON_LN_PART_K(SRC, 1, 16, false);               \
+    if (v == 1) CANON_LN_PART_K(SRC, 1, 8, false);               \
     else if (cols % 4 == 0) CANON_LN_PART_K(SRC, 4, 4, false);    \
     else CANON_LN_PART_K(SRC, 4, 4, true);                        \
   } while (0)

@@ -116,6 +116,25 @@ def test_reductions_over_rows(rows):
     same(run(x, g, b, dy, torch.float32, torch.float32), wanted(x, g, b, dy, torch.float32))
 
 
+@pytest.mark.parametrize("cols", [3, 512, 516, 1021, 1024, 1500, 2048, 2050, 4093, 4096, 4099, 5000, 8189, 8192, 8200])
+@pytest.mark.parametrize("rows,dtype,group", [(4096, torch.float32, None), (4101, torch.bfloat16, None), (4127, torch.float32, 128)])
+def test_one_pass_over_many_rows(rows, cols, dtype, group):
+    # from 4096 rows on the backward is one pass (up to 8192 columns); a whole and a cut last chain, rows that four at a time
+    # do not divide
+    print(f"layer norm {rows}x{cols} {dtype} group {group}", flush=True)
+    x, g, b, dy = inputs(rows, cols, dtype, seed=9)
+    same(run(x, g, b, dy, dtype, torch.bfloat16, group), wanted(x, g, b, dy, torch.bfloat16, group))
+
+
+@pytest.mark.parametrize("rows,cols", [(256, 2048), (512, 2047), (513, 2048), (1023, 2048), (2048, 1030), (2050, 1025), (300, 8191),
+                                       (600, 8190)])
+def test_row_counts_around_the_shapes(rows, cols):
+    # rows spread over more wavefronts up to eight to a CU of 2048 columns each
+    print(f"layer norm {rows}x{cols}", flush=True)
+    x, g, b, dy = inputs(rows, cols, torch.float32, seed=10)
+    same(run(x, g, b, dy, torch.float32, torch.float32, 64), wanted(x, g, b, dy, torch.float32, 64))
+
+
 def test_no_rows():
     cols = 50
     z = torch.empty(0, dtype=torch.float32, device=DEV)

@@ -104,6 +104,13 @@ def test_long_rows(q, k, starts, bidirectional):
     check(1, 1, q, k, starts, bidirectional, causal=False, q_starts=[k // 2], window=k // 3)
 
 
+@pytest.mark.parametrize("b,h,q,k", [(2, 8, 100, 1100), (3, 5, 103, 1030), (8, 16, 12, 2050), (2, 16, 25, 4097), (1, 3, 64, 8190)])
+def test_row_counts_around_the_shapes(b, h, q, k):
+    # rows spread over more wavefronts up to six to a CU of 2048 keys each
+    check(b, h, q, k, LOG32, False, causal=True, q_starts=[k - q] * b)
+    check(b, h, q, k, LOG16, True, causal=False, q_starts=[k // 2] * b, window=900)
+
+
 def test_padded_batch_with_empty_sequences():
     lens = [70, 0, 1, 33]
     for starts, bidirectional in ((LOG32, False), (LOG16, True)):
