@@ -164,7 +164,7 @@ int cref_relbias_bwd(const int64_t* cfg, int64_t n_starts, int32_t bidirectional
     for (int64_t j = 0; j < K; ++j) {
       ds[j] = sees(cfg, q_starts, q_lens, k_lens, b, i, j)
                   ? cref_mul(wide16(probs[r * K + j]), cref_sub(dprobs[r * K + j], D)) : 0.0f;
-      dscores[r * K + j] = cref_bf16(cref_mul(ds[j], scale));
+      dscores[r * K + j] = sees(cfg, q_starts, q_lens, k_lens, b, i, j) ? cref_bf16(cref_mul(ds[j], scale)) : 0;
     }
     for (int64_t n = 0; n < N; ++n) {
       for (int64_t j = 0; j < K; ++j)

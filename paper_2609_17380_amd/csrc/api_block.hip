@@ -273,7 +273,8 @@ canon_status check_rows(const canon_attn_rows* r, const canon_relbias* bias) {
   if (bias->start[bias->n_starts - 1] > kRelFar) return CANON_EUNSUPPORTED;
   if (r->k_len > 32768 || r->ld > kMaxLd) return CANON_EUNSUPPORTED;
   if (!product_ok(r->batch, r->n_heads, kMaxAttnRows) || !product_ok(r->batch * r->n_heads, r->q_len, kMaxAttnRows) ||
-      r->batch > kMaxAttnRows || r->n_heads > kMaxRows || r->q_len > kMaxAttnRows)
+      r->batch > kMaxAttnRows || r->n_heads > kMaxRows || r->q_len > kMaxAttnRows ||
+      !product_ok(r->batch * r->n_heads * r->q_len, r->ld ? r->ld : r->k_len, kMaxElements))
     return CANON_EUNSUPPORTED;
   if (!aligned(r->q_starts, 4) || !aligned(r->q_lens, 4) || !aligned(r->k_lens, 4)) return CANON_EINVAL;
   return CANON_OK;

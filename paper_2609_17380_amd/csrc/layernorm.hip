@@ -389,7 +389,7 @@ __global__ __launch_bounds__(64 * kFoldBlocks) void column_fold_kernel(int64_t n
     if (G <= kFoldUnit) {
       r = unit(c0);
     } else {
-      LocalFoldN<18> f;
+      LocalFoldN<20> f;
       for (int64_t c = c0; c < c1; c += kFoldUnit) f.push(unit(c));
       r = f.result();
     }

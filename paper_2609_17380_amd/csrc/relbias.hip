@@ -30,6 +30,12 @@ __device__ __forceinline__ int bucket_of(const int32_t* start, int n, int d) {
   return lo;
 }
 
+// distances after the query that the bias table holds: up to the last bucket's, one at least
+__host__ __device__ inline int relbias_right(const RelBiasArgs& a) {
+  const int far = a.start[a.n_side - 1];
+  return a.bidirectional ? (far > 0 ? far : 1) : 0;
+}
+
 // The keys j0 <= j < j1 that query i of sequence b sees (none behind the last query), and its position (cut to +-kFarPos, which leaves every bucket as
 // it is).
 struct Query {
@@ -80,7 +86,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
   __shared__ float slot[2][NW], top[NW];
   extern __shared__ float near_[];  // bias by place: key less query, from -far to `right`
   const int w = wave_id(), lane = threadIdx.x & 63;
-  const int far = a.start[a.n_side - 1], right = a.bidirectional ? far : 0;
+  const int far = a.start[a.n_side - 1], right = relbias_right(a);
   const int seg = NW == 1 ? 0 : w * 256 * Q;  // this wavefront's part of the row
   const int n = (int)a.k_len - seg < 256 * Q ? (int)a.k_len - seg : 256 * Q;
   const int parts = ((int)a.k_len + 256 * Q - 1) / (256 * Q);
@@ -102,7 +108,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
     once = false;
     for (int k = threadIdx.x; k <= far + right; k += blockDim.x) {
       const int d = far - k;  // query less key
-      near_[k] = bf16_to_f32(a.table[(d >= 0 ? a.bucket[d] : a.n_side + a.bucket[-d]) * a.heads + h]);
+      near_[k] = bf16_to_f32(a.table[(d >= 0 ? a.bucket[d] : a.n_side + a.bucket[-d < far ? -d : far]) * a.heads + h]);
     }
     __syncthreads();
     if (i >= a.q_len) continue;  // NW = 1: a wavefront without a row
@@ -248,12 +254,16 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
                            const float d = dp[q][t] - D;
                            ds[t] = p[q][t] * d;
                          }
-                         if (!pu.sees_all(q)) {
-#pragma unroll
-                           for (int t = 0; t < 4; ++t) ds[t] = pu.sees(256 * q + 4 * lane + t) ? ds[t] : 0.0f;
-                         }
 #pragma unroll
                          for (int t = 0; t < 4; ++t) o[t] = ds[t] * a.scale;
+                         if (!pu.sees_all(q)) {
+#pragma unroll
+                           for (int t = 0; t < 4; ++t) {
+                             const bool sees = pu.sees(256 * q + 4 * lane + t);
+                             ds[t] = sees ? ds[t] : 0.0f;
+                             o[t] = sees ? o[t] : 0.0f;  // +0 whatever the scale's sign
+                           }
+                         }
                          st[w].put(q, lane, ds);  // for the buckets' sums
                        } else {
                          o[0] = o[1] = o[2] = o[3] = 0.0f;
@@ -292,7 +302,8 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
       const int far = a.start[a.n_side - 1];
       const int z0 = (qy.pos - far + 1 > qy.j0 ? qy.pos - far + 1 : qy.j0) - seg;
       const int z1 = (a.bidirectional && qy.pos + far < qy.j1 ? qy.pos + far : qy.j1) - seg;
-      for (int z = (z0 > 0 ? z0 : 0) + lane; z < z1 && z < 256 * Q; z += 64) st[w].t[z >> 5][z & 31] = 0.0f;
+      if (far > 0)  // one bucket alone: no key is nearer
+        for (int z = (z0 > 0 ? z0 : 0) + lane; z < z1 && z < 256 * Q; z += 64) st[w].t[z >> 5][z & 31] = 0.0f;
       __builtin_amdgcn_wave_barrier();
       const float c = lane >= 8 * pt.q0 && lane < 8 * pt.q1 ? st[w].chain(lane) : 0.0f;
       const bool before = !a.bidirectional || seg + 32 * lane <= qy.pos - far;
@@ -383,8 +394,7 @@ hipError_t relbias_fwd_launch(const RelBiasArgs& a, const float* scores, uint16_
   if (matrices * per_head == 0 || a.k_len == 0) return hipSuccess;
   const dim3 grid = relbias_grid(shape, matrices, per_head), wg(shape.threads());
   const bool tail = a.k_len % 4 != 0;
-  const int far = a.start[a.n_side - 1];
-  const size_t lds = sizeof(float) * (size_t)(far + 1 + (a.bidirectional ? far : 0));
+  const size_t lds = sizeof(float) * (size_t)(a.start[a.n_side - 1] + 1 + relbias_right(a));
 #define CANON_REL_K(Q, NW, TAIL)                                                                                    \
   hipLaunchKernelGGL((relbias_fwd_kernel<Q, NW, TAIL>), grid, wg, lds, s, a, (uint32_t)a.heads, (uint32_t)matrices, \
                      (uint32_t)per_head, scores, probs)

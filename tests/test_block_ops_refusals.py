@@ -142,7 +142,8 @@ def test_relbias():
                     dict(bias=starts(0, n=-1)), dict(bias=starts(0, 1, bidirectional=2))):
             assert call(**bad) == C.EINVAL, bad
         for bad in (dict(k=32769), dict(ld=(1 << 31) + 1), dict(batch=1 << 16, heads=1 << 10, q=1 << 6),
-                    dict(batch=1 << 40, heads=1 << 40, q=1 << 40), dict(bias=starts(0, 1025))):
+                    dict(batch=1 << 40, heads=1 << 40, q=1 << 40),
+                    dict(q=1 << 20, ld=1 << 31), dict(bias=starts(0, 1025))):
             assert call(**bad) == C.EUNSUPPORTED, bad
     for bad in (dict(table=None), dict(x=None), dict(y=None), dict(table=p(0) + 1), dict(x=p(1) + 2), dict(y=p(2) + 1),
                 dict(y=p(1) + 2398), dict(y=p(0)), dict(k_lens=p(2) + 4), dict(q_starts=p(2))):

@@ -68,11 +68,11 @@ def run(B, H, Q, K, starts, bidirectional, scores, table, dprobs, probs=None, ld
     return np.ascontiguousarray(got_p[..., :K]), np.ascontiguousarray(got_ds[..., :K]), host_f32(dt)
 
 
-def check(B, H, Q, K, starts, bidirectional, seed=0, ld=0, **masks):
+def check(B, H, Q, K, starts, bidirectional, seed=0, ld=0, scale=0.125, **masks):
     print(f"relbias {B}x{H}x{Q}x{K} {len(starts)} starts bidirectional={bidirectional} ld={ld} {masks}", flush=True)
     scores, table, dprobs = case_inputs(B, H, Q, K, starts, bidirectional, seed)
-    want_p = oracle.relbias_fwd(scores, table, starts, bidirectional, scale=0.125, **masks)
-    want_ds, want_dt = oracle.relbias_bwd(want_p, dprobs, starts, bidirectional, scale=0.125, **masks)
+    want_p = oracle.relbias_fwd(scores, table, starts, bidirectional, scale=scale, **masks)
+    want_ds, want_dt = oracle.relbias_bwd(want_p, dprobs, starts, bidirectional, scale=scale, **masks)
     # junk where nothing is seen: none of it may show
     hidden = ~np.broadcast_to(seen_mask(B, Q, K, masks.get("causal", True), masks.get("window", 0), masks.get("q_starts"),
                                         masks.get("q_lens"), masks.get("k_lens")), scores.shape)
@@ -80,18 +80,19 @@ def check(B, H, Q, K, starts, bidirectional, seed=0, ld=0, **masks):
     scores = np.where(hidden, junk[np.arange(scores.size).reshape(scores.shape) % 4], scores)
     dprobs = np.where(hidden, junk[np.arange(scores.size).reshape(scores.shape) % 3], dprobs)
     probs = np.where(hidden, np.uint16(0x7FC0), want_p)
-    p, ds, dt = run(B, H, Q, K, starts, bidirectional, scores, table, dprobs, probs=probs, ld=ld, **masks)
+    p, ds, dt = run(B, H, Q, K, starts, bidirectional, scores, table, dprobs, probs=probs, ld=ld, scale=scale, **masks)
     assert_bits(p, want_p, "probs")
     assert_bits(ds, want_ds, "dscores")
     assert_bits(dt, want_dt, "dtable")
-    assert not p[hidden].any() and not (ds[hidden] & 0x7FFF).any()
+    assert not p[hidden].any() and not ds[hidden].any()
 
 
 @pytest.mark.parametrize("s", [1, 2, 3, 31, 33, 64, 255, 257, 300])
 @pytest.mark.parametrize("starts,bidirectional,causal,window",
                          [(LOG32, False, True, 0), (LOG16, True, False, 0), (LOG16, True, False, 20), (LOG32, False, True, 40),
                           (LOG32, False, False, 0), (LOG16, True, True, 0), (WIDE, True, False, 0), (EQUAL, True, False, 0),
-                          (EQUAL, False, False, 0), ([0], False, True, 0), ([0, 0], True, False, 1)])
+                          (EQUAL, False, False, 0), ([0], False, True, 0), ([0], False, False, 0), ([0], True, False, 0),
+                          ([0, 0], True, False, 1), ([0, 31], True, False, 0), ([0, 32], True, False, 0)])
 def test_square_rows(s, starts, bidirectional, causal, window):
     check(2, 3, s, s, starts, bidirectional, causal=causal, window=window)
 
@@ -130,6 +131,11 @@ def test_the_next_token(k):
     lens = np.array([k, max(1, k // 2), 1, max(1, k - 1)])
     check(4, 4, 1, k, LOG32, False, causal=True, q_starts=lens - 1, k_lens=lens)
     check(4, 4, 1, k, LOG32, False, causal=True, window=17, q_starts=lens - 1, k_lens=lens)
+
+
+@pytest.mark.parametrize("scale", [-0.25, 0.0, 3.0])
+def test_scales(scale):
+    check(1, 2, 40, 300, LOG16, True, causal=False, q_starts=[100], window=150, scale=scale)
 
 
 @pytest.mark.parametrize("ld", [301, 304, 512])
