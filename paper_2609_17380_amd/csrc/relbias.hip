@@ -184,7 +184,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
 // chunk by chunk, a lane to a chunk, like the row.
 template <int Q, int NW, bool TAIL>
 __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbias_bwd_kernel(
-    RelBiasArgs a, uint32_t heads, uint32_t matrices, uint32_t per_head, const uint16_t* __restrict__ probs,
+    RelBiasArgs a, uint32_t heads, uint32_t units, uint32_t per_head, const uint16_t* __restrict__ probs,
     const float* __restrict__ dprobs, uint16_t* __restrict__ dscores, float* __restrict__ rowsum) {
   constexpr int kRows = NW == 1 ? 4 : 1;
   __shared__ __attribute__((aligned(16))) RowStage<Q> st[NW == 1 ? 4 : NW];
@@ -197,44 +197,66 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
   const int parts = ((int)a.k_len + 256 * Q - 1) / (256 * Q);
   const int nb = a.n_side * (a.bidirectional ? 2 : 1);
   int turn = 0;  // as above
-  // a matrix's rows along x, the matrices (batch and head) along y; each further on by the grid where that ends first
-  bool once = true;  // this workgroup's first rows
-  for (uint32_t m = blockIdx.y; m < matrices; m += gridDim.y)
-  for (uint32_t blk = blockIdx.x; blk < per_head; blk += gridDim.x) {
-    const int64_t bh = m, b = m / heads, h = m % heads;
-    const int64_t i = (int64_t)blk * kRows + (NW == 1 ? w : 0);
-    const Query qy = query_of(a, b, i);
-    const Part pt = part_of(qy, seg, n);
-    const int64_t row = (bh * a.q_len + i) * a.ld + seg;
-    const uint16_t* pr = probs + row;
-    const float* dr = dprobs + row;
-    uint16_t* sr = dscores + row;
-    float p[Q][4], dp[Q][4];
-    part_load<TAIL>(pt.from, pt.upto, p, [&](int j, float(&v)[4]) { ldb_wide(pr + j, v); },
-                    [&](int j) { return bf16_wide(pr[j]); });
-    part_load<TAIL>(pt.from, pt.upto, dp, [&](int j, float(&v)[4]) { ldf<4>(dr + j, v); }, [&](int j) { return dr[j]; });
-    if (rowsum && once) {
-      for (int k = threadIdx.x; k < nb; k += blockDim.x) {
-        const int side = k < a.n_side ? k : k - a.n_side;
-        const int d0 = a.start[side], d1 = side + 1 < a.n_side ? a.start[side + 1] : 2 * (int)kFarPos;
-        if (k < a.n_side) {
-          lo_[k] = 1 - d1;
-          hi_[k] = d0 == d1 ? 1 - d1 : d0 == 0 && !a.bidirectional && !a.causal ? 2 * (int)kFarPos : 1 - d0;
-        } else {
-          lo_[k] = d0 > 0 ? d0 : 1;
-          hi_[k] = d1;
-        }
+  uint32_t pw[Q][2];
+  float dp[Q][4];
+  // A unit is kRows queries of a matrix (batch and head); a wavefront loads its row of the next one before it sums this
+  // one's buckets, when this one's values are no longer needed.
+  struct At {
+    Query qy;
+    Part pt;
+    int64_t i, b, h, row;
+  };
+  auto load = [&](uint32_t unit) __attribute__((always_inline)) {  // of no key behind the last one
+    const uint32_t u = unit < units ? unit : units - 1, m = u / per_head;
+    At t;
+    t.b = m / heads;
+    t.h = m % heads;
+    t.i = unit < units ? (int64_t)(u - m * per_head) * kRows + (NW == 1 ? w : 0) : a.q_len;
+    t.qy = query_of(a, t.b, t.i);
+    t.pt = part_of(t.qy, seg, n);
+    t.row = ((int64_t)m * a.q_len + t.i) * a.ld + seg;
+    const uint16_t* pr = probs + t.row;
+    const float* dr = dprobs + t.row;
+    part_load_bf16<TAIL>(t.pt.from, t.pt.upto, pw, pr);
+    part_load<TAIL>(t.pt.from, t.pt.upto, dp, [&](int j, float(&v)[4]) { ldf<4>(dr + j, v); }, [&](int j) { return dr[j]; });
+    return t;
+  };
+  // Units are dealt out forth and back, so that a workgroup's causal rows are long and short in turn.
+  auto dealt = [&](uint32_t round) {
+    return round * gridDim.x + (round & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+  };
+  const uint32_t rounds = (units + gridDim.x - 1) / gridDim.x;
+  At at = load(dealt(0));
+  if (rowsum) {
+    for (int k = threadIdx.x; k < nb; k += blockDim.x) {
+      const int side = k < a.n_side ? k : k - a.n_side;
+      const int d0 = a.start[side], d1 = side + 1 < a.n_side ? a.start[side + 1] : 2 * (int)kFarPos;
+      if (k < a.n_side) {
+        lo_[k] = 1 - d1;
+        hi_[k] = d0 == d1 ? 1 - d1 : d0 == 0 && !a.bidirectional && !a.causal ? 2 * (int)kFarPos : 1 - d0;
+      } else {
+        lo_[k] = d0 > 0 ? d0 : 1;
+        hi_[k] = d1;
       }
-      __syncthreads();
     }
-    once = false;
-    if (i >= a.q_len) continue;  // NW = 1: a wavefront without a row
+    __syncthreads();
+  }
+  for (uint32_t round = 0; round < rounds; ++round) {
+    const At now = at;
+    const Query qy = now.qy;
+    const Part pt = now.pt;
+    if (now.i >= a.q_len) {  // a wavefront, or in the last round a workgroup, without a row
+      at = load(round + 1 < rounds ? dealt(round + 1) : units);
+      continue;
+    }
+    uint16_t* sr = dscores + now.row;
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
       if (q < pt.q0 || q >= pt.q1) continue;
       float e[4];
+      wide4(pw[q], e);
 #pragma unroll
-      for (int t = 0; t < 4; ++t) e[t] = p[q][t] * dp[q][t];
+      for (int t = 0; t < 4; ++t) e[t] = e[t] * dp[q][t];
       if (!pt.sees_all(q)) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) e[t] = pt.sees(256 * q + 4 * lane + t) ? e[t] : 0.0f;
@@ -249,10 +271,11 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
                      [&](int q, float(&o)[4]) {
                        if (q >= pt.q0 && q < pt.q1) {
                          float ds[4];
+                         wide4(pw[q], ds);
 #pragma unroll
                          for (int t = 0; t < 4; ++t) {
                            const float d = dp[q][t] - D;
-                           ds[t] = p[q][t] * d;
+                           ds[t] = ds[t] * d;
                          }
 #pragma unroll
                          for (int t = 0; t < 4; ++t) o[t] = ds[t] * a.scale;
@@ -271,8 +294,9 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
                      },
                      [&](int j, const float(&o)[4]) { stb_arith(sr + j, o); },
                      [&](int j, float o) { sr[j] = bf16_arith(o); });
+    at = load(round + 1 < rounds ? dealt(round + 1) : units);
     if (!rowsum) continue;
-    float* out = rowsum + ((b * a.q_len + i) * a.heads + h) * nb;
+    float* out = rowsum + ((now.b * a.q_len + now.i) * a.heads + now.h) * nb;
     if constexpr (NW > 1) __syncthreads();
     else __builtin_amdgcn_wave_barrier();
     for (int k2 = NW == 1 ? lane : (int)threadIdx.x; k2 < 2 * nb; k2 += NW == 1 ? 64 : (int)blockDim.x) {
@@ -419,11 +443,13 @@ hipError_t relbias_bwd_launch(const RelBiasArgs& a, const uint16_t* probs, const
   const int64_t matrices = a.batch * a.heads, per_head = shape.groups(a.q_len);
   const bool empty = matrices * per_head == 0 || a.k_len == 0;
   if (!empty) {
-    const dim3 grid = relbias_grid(shape, matrices, per_head), wg(shape.threads());
+    // no more workgroups than are on the chip at once (16 wavefronts to a CU of 8 vectors, 32 of fewer)
+    const int64_t units = matrices * per_head, most = device_cus() * ((shape.q == 8 ? 16 : 32) * 64 / shape.threads());
+    const dim3 grid((unsigned)(units < most ? units : most)), wg(shape.threads());
     const bool tail = a.k_len % 4 != 0;
     float* rs = dtable ? rowsum : nullptr;
 #define CANON_REL_K(Q, NW, TAIL)                                                                                  \
-  hipLaunchKernelGGL((relbias_bwd_kernel<Q, NW, TAIL>), grid, wg, 0, s, a, (uint32_t)a.heads, (uint32_t)matrices, \
+  hipLaunchKernelGGL((relbias_bwd_kernel<Q, NW, TAIL>), grid, wg, 0, s, a, (uint32_t)a.heads, (uint32_t)units, \
                      (uint32_t)per_head, probs, dprobs, dscores, rs)
 #define CANON_REL(Q, NW)                   \
   do {                                     \

@@ -267,6 +267,39 @@ __device__ __forceinline__ void part_load(int from, int upto, float (&v)[Q][4], 
       for (int t = 0; t < 3; ++t) v[q][t] = q == mine ? c[t] : v[q][t];
   }
 }
+// The same of bf16 elements, kept as they are stored, two to a word: half the registers while they wait.
+template <bool TAIL, int Q>
+__device__ __forceinline__ void part_load_bf16(int from, int upto, uint32_t (&v)[Q][2], const uint16_t* p) {
+  const int at = 4 * (threadIdx.x & 63), first = from - 3;
+  const unsigned whole = upto - 3 > first ? (unsigned)(upto - 3 - first) : 0u;
+#pragma unroll
+  for (int q = 0; q < Q; ++q) {
+    v[q][0] = v[q][1] = 0u;
+    if ((unsigned)(256 * q + at - first) < whole) {
+      const H4 h = *reinterpret_cast<const H4*>(p + 256 * q + at);
+      v[q][0] = h.x; v[q][1] = h.y;
+    }
+  }
+  if (TAIL && upto > from && (upto & 3)) {
+    const int base = upto & ~3;
+    uint32_t c[2] = {0u, 0u};
+    const int mine = at == (base & 255) ? base >> 8 : -1;
+    if (mine >= 0) {
+#pragma unroll
+      for (int t = 0; t < 3; ++t)
+        if (base + t < upto) c[t >> 1] |= (uint32_t)p[base + t] << (16 * (t & 1));
+    }
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      v[q][0] = q == mine ? c[0] : v[q][0];
+      v[q][1] = q == mine ? c[1] : v[q][1];
+    }
+  }
+}
+__device__ __forceinline__ void wide4(const uint32_t (&w)[2], float (&f)[4]) {
+  f[0] = __uint_as_float(w[0] << 16); f[1] = __uint_as_float(w[0] & 0xFFFF0000u);
+  f[2] = __uint_as_float(w[1] << 16); f[3] = __uint_as_float(w[1] & 0xFFFF0000u);
+}
 // value(q, o) makes vector q, store4(j, o) moves the one at element j, store1(j, o) an element
 template <bool TAIL, int Q, class Value, class Store4, class Store1>
 __device__ __forceinline__ void part_store(int n, Value value, Store4 store4, Store1 store1) {
