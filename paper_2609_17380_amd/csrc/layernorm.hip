@@ -16,7 +16,11 @@ namespace canon {
 
 namespace {
 
-constexpr bool layernorm_ahead(bool keep) { return !keep; }
+// Whether a wavefront loads its next row while it sums and writes one: rows of 1025 to 2048 columns that are not kept in 8
+// bits (8192 x 2048 24.0 -> 22.1 us, 4096 x 2048 13.8 -> 13.7).  Of shorter rows and of
+// those that several wavefronts share enough are on the chip at once (8192 x 1024 13.2 us ahead, 12.6 not; 8192 x 5001 91
+// and 68), and the codes take the registers.
+constexpr bool layernorm_ahead(bool keep, int q, int waves) { return !keep && q == 8 && waves == 1; }
 
 template <int SRC, int Q, int NW, bool TAIL, bool KEEP>
 __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void layernorm_fwd_kernel(
@@ -34,7 +38,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void layer
   };
   const int64_t step = (int64_t)gridDim.x * kRows;
   // the next row is on its way while one is summed and written, where the registers allow it
-  constexpr bool kAhead = layernorm_ahead(KEEP);
+  constexpr bool kAhead = layernorm_ahead(KEEP, Q, NW);
   float next[Q][4];
   int64_t row = (int64_t)blockIdx.x * kRows + (NW == 1 ? w : 0);
   if (kAhead) load(row, next);
@@ -432,8 +436,8 @@ hipError_t layernorm_fwd_launch(int64_t rows, int64_t cols, const ActIn& x, cons
   const float inv_d = (float)(1.0 / (double)cols);  // RN32(1/cols), correctly rounded
   const RowShape shape = row_shape(rows, cols, 8);
   const int64_t blocks = shape.groups(rows);
-  // rows that are loaded ahead: no more workgroups than are on the chip at once (16 wavefronts to a CU)
-  const int64_t most = layernorm_ahead(k.codes) ? device_cus() * (16 * 64 / shape.threads()) : kMaxBlocks;
+  // rows that are loaded ahead: no more workgroups than are on the chip at once
+  const int64_t most = layernorm_ahead(k.codes, shape.q, shape.waves) ? device_cus() * 4 : kMaxBlocks;
   const dim3 grid((unsigned)(blocks < most ? blocks : most)), wg(shape.threads());
 #define CANON_LN_K(SRC, Q, NW, TAIL, KEEP)                                                                               \
   hipLaunchKernelGGL((layernorm_fwd_kernel<SRC, Q, NW, TAIL, KEEP>), grid, wg, 0, s, rows, (int)cols, x, gain, bias, eps, \
