@@ -498,8 +498,8 @@ size_t canon_layernorm_bwd_workspace_bytes(int64_t rows, int64_t cols);
    dscores (bf16) = bf16(RN(ds scale)), +0 for keys that are not seen; dtable (fp32 [buckets][n_heads], may be NULL) = R1
    over the rows (b, i) of [R1 over the keys of ds, those of other buckets as +0 terms].  Whatever stands in places that are
    not seen (infinities, NaN) is not used.
-   k_len up to 32768, batch * n_heads * q_len up to 2^31 and that times ld up to 2^40 (else CANON_EUNSUPPORTED); window >= 0;
-   |q_start| up to 2^30.
+   k_len up to 32768, batch * n_heads * q_len up to 2^31, that times ld up to 2^40, n_heads times the buckets up to 2^24 (else
+   CANON_EUNSUPPORTED); window >= 0; |q_start| up to 2^30.
    workspace: device memory of canon_softmax_relbias_bwd_workspace_bytes(rows, bias) bytes, 256-byte aligned (the rows' sums
    per bucket; not needed where dtable is NULL). */
 #define CANON_RELBIAS_MAX_STARTS 128

@@ -421,6 +421,8 @@ def _scratch(ws, dev):
     """(address, bytes) of a workspace; without one, none."""
     if ws is None:
         return None, 0
+    if not isinstance(ws, torch.Tensor):
+        raise ValueError("workspace: a tensor is needed")
     return _arg(ws, "workspace", ws.numel(), (ws.dtype,), dev), ws.numel() * ws.element_size()
 
 
@@ -433,16 +435,18 @@ class Act8(ctypes.Structure):
     _fields_ = [("group", ctypes.c_int32), ("codes", ctypes.c_void_p), ("steps", ctypes.c_void_p)]
 
     def __init__(self, group, codes, steps):
+        if not isinstance(codes, torch.Tensor) or not isinstance(steps, torch.Tensor):
+            raise ValueError("codes and steps: tensors are needed")
         self.tensors = codes, steps
         super().__init__(group, codes.data_ptr(), steps.data_ptr())
 
     def _of(self, rows, cols, dev):
-        """The record's address, once its tensors are those of [rows][cols]."""
+        """The record's address, once its tensors are those of [rows][cols] on the current device."""
         groups = act8_groups(cols, self.group)
         if not groups and cols:
             raise ValueError("group: 32, 64, 128 or 256 is needed")
-        _arg(self.tensors[0], "codes", rows * cols, _TI8, dev)
-        _arg(self.tensors[1], "steps", rows * groups, _T32, dev)
+        self.codes = _arg(self.tensors[0], "codes", rows * cols, _TI8, dev)
+        self.steps = _arg(self.tensors[1], "steps", rows * groups, _T32, dev)
         return ctypes.byref(self)
 
 
@@ -549,9 +553,17 @@ class AttnRows(ctypes.Structure):
     def __init__(self, batch, n_heads, q_len, k_len, causal=True, window=0, scale=1.0, ld=0, q_start=0, q_starts=None,
                  q_lens=None, k_lens=None):
         self.tensors = q_starts, q_lens, k_lens
-        dev = _device()
-        super().__init__(batch, n_heads, q_len, k_len, ld, q_start, window, int(causal), scale,
-                         *(_arg(t, w, batch, _TI32, dev) for t, w in zip(self.tensors, ("q_starts", "q_lens", "k_lens"))))
+        super().__init__(batch, n_heads, q_len, k_len, ld, q_start, window, int(causal), scale)
+        self._of(_device())
+
+    def _of(self, dev):
+        """The record's address, once its tensors are a batch's on the current device."""
+        starts, queries, keys = self.tensors
+        if starts is not None or queries is not None or keys is not None:
+            self.q_starts = _arg(starts, "q_starts", self.batch, _TI32, dev)
+            self.q_lens = _arg(queries, "q_lens", self.batch, _TI32, dev)
+            self.k_lens = _arg(keys, "k_lens", self.batch, _TI32, dev)
+        return ctypes.byref(self)
 
     def _matrix(self, t, what, dtypes, dev):
         """A matrix of these rows: all of them, `ld` apart."""
@@ -561,7 +573,7 @@ class AttnRows(ctypes.Structure):
 def softmax_relbias(rows: AttnRows, bias: RelBias, table, scores, probs, order=ORDER_V1, stream=None):
     """probs (bf16) of the raw scores (fp32), with table (bf16 [buckets, n_heads]) added by distance."""
     dev = _device()
-    _check(_lib().canon_softmax_relbias(ctypes.byref(order), ctypes.byref(rows), ctypes.byref(bias),
+    _check(_lib().canon_softmax_relbias(ctypes.byref(order), rows._of(dev), ctypes.byref(bias),
                                         _arg(table, "table", bias.buckets * rows.n_heads, _T16, dev),
                                         rows._matrix(scores, "scores", _T32, dev),
                                         rows._matrix(probs, "probs", _T16, dev), _stream_on(stream, dev)),
@@ -577,7 +589,7 @@ def softmax_relbias_bwd(rows: AttnRows, bias: RelBias, probs, dprobs, dscores, w
     """dscores (bf16) and dtable (fp32 [buckets, n_heads]); workspace: needed for dtable."""
     dev = _device()
     ws, ws_bytes = _scratch(workspace, dev)
-    _check(_lib().canon_softmax_relbias_bwd(ctypes.byref(order), ctypes.byref(rows), ctypes.byref(bias),
+    _check(_lib().canon_softmax_relbias_bwd(ctypes.byref(order), rows._of(dev), ctypes.byref(bias),
                                             rows._matrix(probs, "probs", _T16, dev),
                                             rows._matrix(dprobs, "dprobs", _T32, dev),
                                             rows._matrix(dscores, "dscores", _T16, dev),

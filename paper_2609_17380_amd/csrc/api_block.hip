@@ -260,9 +260,12 @@ bool bias_ok(const canon_relbias* r) {
   return true;
 }
 
+int64_t buckets_of(const canon_relbias* b) { return (int64_t)b->n_starts * (b->bidirectional ? 2 : 1); }
+
 constexpr int64_t kMaxStart = int64_t(1) << 30;
 constexpr int64_t kMaxAttnRows = int64_t(1) << 31;
 constexpr int64_t kMaxLd = int64_t(1) << 31;
+constexpr int64_t kMaxTable = int64_t(1) << 24;  // columns of the rows' sums: a launch folds 16 threads to each
 
 canon_status check_rows(const canon_attn_rows* r, const canon_relbias* bias) {
   if (!r || r->batch < 0 || r->n_heads < 0 || r->q_len < 0 || r->k_len < 0 || r->window < 0 ||
@@ -273,7 +276,7 @@ canon_status check_rows(const canon_attn_rows* r, const canon_relbias* bias) {
   if (bias->start[bias->n_starts - 1] > kRelFar) return CANON_EUNSUPPORTED;
   if (r->k_len > 32768 || r->ld > kMaxLd) return CANON_EUNSUPPORTED;
   if (!product_ok(r->batch, r->n_heads, kMaxAttnRows) || !product_ok(r->batch * r->n_heads, r->q_len, kMaxAttnRows) ||
-      r->batch > kMaxAttnRows || r->n_heads > kMaxRows || r->q_len > kMaxAttnRows ||
+      r->batch > kMaxAttnRows || r->q_len > kMaxAttnRows || !product_ok(r->n_heads, buckets_of(bias), kMaxTable) ||
       !product_ok(r->batch * r->n_heads * r->q_len, r->ld ? r->ld : r->k_len, kMaxElements))
     return CANON_EUNSUPPORTED;
   if (!aligned(r->q_starts, 4) || !aligned(r->q_lens, 4) || !aligned(r->k_lens, 4)) return CANON_EINVAL;
@@ -310,8 +313,6 @@ RelBiasArgs args_of(const canon_attn_rows* r, const canon_relbias* bias, const u
     }
   return a;
 }
-
-int64_t buckets_of(const canon_relbias* b) { return (int64_t)b->n_starts * (b->bidirectional ? 2 : 1); }
 
 // bytes from the first to behind the last key of the rows
 int64_t row_bytes(const canon_attn_rows* r, int64_t size) {

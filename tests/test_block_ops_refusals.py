@@ -184,3 +184,52 @@ def test_the_binding_refuses_other_tensors():
                  lambda: C.softmax_relbias(C.AttnRows(1, 1, 20, 20), C.RelBias([0]), h, f, h)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_relbias_table_is_bounded():
+    # the sums of the rows have a column to a head's bucket, and one launch folds at most 2^24 of them
+    lib, bias = C.lib(), C.RelBias(range(128), bidirectional=True)
+    for heads, refused in ((1 << 16, False), ((1 << 16) + 1, True), (1 << 26, True)):
+        r = rows(batch=1, heads=heads, q=1, k=1)
+        st = lib.canon_softmax_relbias(ORDER, ctypes.byref(r), ctypes.byref(bias), None, p(1), p(2), None)
+        assert st == (C.EUNSUPPORTED if refused else C.EINVAL), heads  # EINVAL: no table
+        assert (C.softmax_relbias_bwd_workspace_bytes(r, bias) == 0) == refused
+
+
+def test_a_record_is_checked_where_it_is_used(monkeypatch):
+    lens = torch.tensor([1, 2], dtype=torch.int32)
+    with monkeypatch.context() as m:
+        m.setattr(C, "_device", lambda: -1)  # where the record's tensors are
+        r = C.AttnRows(2, 1, 1, 4, k_lens=lens)
+        other = C.AttnRows(2, 1, 1, 4, k_lens=lens)
+        other.batch = 3  # more sequences than lengths
+        t, x, y = torch.zeros(1, dtype=torch.bfloat16), torch.zeros(12), torch.zeros(12, dtype=torch.bfloat16)
+        with pytest.raises(ValueError, match="k_lens"):
+            C.softmax_relbias(other, C.RelBias([0]), t, x, y)
+        with pytest.raises(ValueError, match="k_lens"):
+            C.softmax_relbias_bwd(other, C.RelBias([0]), y, x, y)
+    with pytest.raises(ValueError, match="k_lens"):  # the current device is another
+        C.softmax_relbias(r, C.RelBias([0]), t, x[:8], y[:8])
+    with pytest.raises(ValueError, match="k_lens"):
+        C.softmax_relbias_bwd(r, C.RelBias([0]), y[:8], x[:8], y[:8])
+
+
+def test_records_follow_their_tensors(monkeypatch):
+    monkeypatch.setattr(C, "_device", lambda: -1)
+    codes, steps, lens = torch.zeros(64, dtype=torch.int8), torch.zeros(1), torch.zeros(2, dtype=torch.int32)
+    kept, r = C.Act8(64, codes, steps), C.AttnRows(2, 1, 1, 4, k_lens=lens)
+    codes.set_(torch.zeros(128, dtype=torch.int8)[64:])  # other memory under the same tensors
+    lens.set_(torch.zeros(4, dtype=torch.int32)[2:])
+    kept._of(1, 64, -1)
+    r._of(-1)
+    assert kept.codes == codes.data_ptr() and r.k_lens == lens.data_ptr()
+
+
+def test_the_binding_refuses_what_is_no_tensor():
+    f, h = torch.zeros(400), torch.zeros(400, dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        C.layernorm_bwd(4, 100, f, h, f, f, f, f, workspace=1 << 20)
+    with pytest.raises(ValueError, match="workspace"):
+        C._scratch(1 << 20, 0)
+    with pytest.raises(ValueError):
+        C.act8_pack(4, 100, f, C.Act8(64, None, None))
