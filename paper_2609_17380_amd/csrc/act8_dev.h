@@ -42,9 +42,9 @@ __device__ __forceinline__ float step_rcp(float s) { return recip_step_ok(s) ? _
 template <bool TAIL>
 __device__ __forceinline__ void keep4(const float (&v)[4], float s, int64_t j, int64_t n, int lg, int8_t* codes,
                                       float* steps) {
+  if (j >= n) return;
   uint32_t w[1];
   quant_pack<4>(v, s, step_rcp(s), recip_step_ok(s), w);
-  if (j >= n) return;
   if ((j & ((1 << lg) - 1)) == 0) steps[j >> lg] = s;
   if (!TAIL || j + 4 <= n) {
     reinterpret_cast<B4*>(codes + j)->x = w[0];
@@ -78,6 +78,9 @@ __device__ __forceinline__ void part_keep(const float (&v)[Q][4], int n, int lg,
     w[q] = x ^ 0x80808080u;
     undecided |= rs > 0.0f && off < 0.5f - 0x1p-15f ? 0u : 1u << q;
   }
+  // of the vectors that the row has in this lane (groups behind its end have the step 0, which nothing is decided by)
+  const int have = n > at ? (n - at + 255) >> 8 : 0;
+  undecided &= (1u << (have < Q ? have : Q)) - 1;
   while (undecided) {  // one vector of each lane that has any
     const int k = __builtin_ctz(undecided);
     undecided &= undecided - 1;

@@ -40,6 +40,14 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void layer
   // the next row is on its way while one is summed and written, where the registers allow it
   constexpr bool kAhead = layernorm_ahead(KEEP, Q, NW);
   float next[Q][4];
+  // Gain and bias, all vectors at once: with a load and its wait per vector 1023 x 5116 took 10.5 us instead of 9.4, 4096 x
+  // 16384 92 instead of 78, kept rows of 2048 27.8 instead of 26.6; beside a next row the registers spill (22.7, so 23.5).
+  constexpr bool kEach = kAhead && !TAIL;
+  uint32_t gw[Q][2], bw[Q][2];
+  auto load_gain = [&]() __attribute__((always_inline)) {
+    part_load_bf16<TAIL>(0, n, gw, gain + seg);
+    part_load_bf16<TAIL>(0, bias ? n : 0, bw, bias + seg);
+  };
   int64_t row = (int64_t)blockIdx.x * kRows + (NW == 1 ? w : 0);
   if (kAhead) load(row, next);
   for (; row < rows; row += step) {
@@ -63,6 +71,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void layer
         const float d = xv[q][t] - mu;
         sq[q][t] = d * d;
       }
+    if (!KEEP && !kAhead) load_gain();  // on its way while the squares are summed, where the registers allow it
     const float ss = wide_row_sum<NW>(st[w], sq, cols, slot[1]);
     const float var = ss * inv_d;
     const float v = var + eps;
@@ -74,32 +83,34 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void layer
     if (KEEP)
       part_keep<TAIL>(xv, n, k.lg, k.codes + row * cols + seg,
                       k.steps + row * ((cols + (1 << k.lg) - 1) >> k.lg) + (seg >> k.lg));
+    if (KEEP || (kAhead && !kEach)) load_gain();
     uint16_t* yh = (uint16_t*)y + row * cols + seg;
     float* yf = (float*)y + row * cols + seg;
     part_store<TAIL, Q>(n,
                      [&](int q, float(&o)[4]) {
+                       float gv[4], bv[4];
+                       if constexpr (kEach) {
+                         if (256 * q + 4 * lane < n) {
+                           ldb_wide(gain + seg + 256 * q + 4 * lane, gv);
+                           if (bias) ldb_wide(bias + seg + 256 * q + 4 * lane, bv);
+                         }
+                       } else {
+                         wide4(gw[q], gv);
+                         wide4(bw[q], bv);
+                       }
 #pragma unroll
                        for (int t = 0; t < 4; ++t) {
                          const float d = xv[q][t] - mu;
-                         o[t] = d * r;
+                         const float xh = d * r;
+                         o[t] = xh * gv[t];
+                         if (bias) o[t] = o[t] + bv[t];
                        }
                      },
-                     [&](int j, float(&o)[4]) {
-                       float gv[4];
-                       ldb_wide(gain + seg + j, gv);
-#pragma unroll
-                       for (int t = 0; t < 4; ++t) o[t] = o[t] * gv[t];
-                       if (bias) {
-                         ldb_wide(bias + seg + j, gv);
-#pragma unroll
-                         for (int t = 0; t < 4; ++t) o[t] = o[t] + gv[t];
-                       }
+                     [&](int j, const float(&o)[4]) {
                        if (y_bf16) stb_arith(yh + j, o);
                        else stf<4>(yf + j, o);
                      },
-                     [&](int j, float xh) {
-                       float o = xh * bf16_wide(gain[seg + j]);
-                       if (bias) o = o + bf16_wide(bias[seg + j]);
+                     [&](int j, float o) {
                        if (y_bf16) yh[j] = bf16_arith(o);
                        else yf[j] = o;
                      });
