@@ -32,14 +32,14 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void layer
   const int w = wave_id(), lane = threadIdx.x & 63;
   const int seg = NW == 1 ? 0 : w * 256 * Q;  // this wavefront's part of the row
   const int n = cols - seg < 256 * Q ? cols - seg : 256 * Q;
-  auto load = [&](int64_t row, float(&v)[Q][4]) __attribute__((always_inline)) {
-    const PartIn<SRC> in(x, row, cols, seg);
-    part_load<TAIL>(0, row < rows ? n : 0, v, [&](int j, float(&f)[4]) { in.load4(j, f); }, [&](int j) { return in.load1(j); });
+  using In = PartIn<SRC>;
+  auto load = [&](int64_t row, typename In::Raw(&v)[Q]) __attribute__((always_inline)) {
+    In(x, row, cols, seg).template part<TAIL>(row < rows ? n : 0, v);
   };
   const int64_t step = (int64_t)gridDim.x * kRows;
   // the next row is on its way while one is summed and written, where the registers allow it
   constexpr bool kAhead = layernorm_ahead(KEEP, Q, NW);
-  float next[Q][4];
+  typename In::Raw next[Q];
   // Gain and bias, all vectors at once: with a load and its wait per vector 1023 x 5116 took 10.5 us instead of 9.4, 4096 x
   // 16384 92 instead of 78, kept rows of 2048 27.8 instead of 26.6; beside a next row the registers spill (22.7, so 23.5).
   constexpr bool kEach = kAhead && !TAIL;
@@ -52,15 +52,10 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void layer
   if (kAhead) load(row, next);
   for (; row < rows; row += step) {
     float xv[Q][4];
-    if (kAhead) {
+    if (!kAhead) load(row, next);
 #pragma unroll
-      for (int q = 0; q < Q; ++q)
-#pragma unroll
-        for (int t = 0; t < 4; ++t) xv[q][t] = next[q][t];
-      load(row + step, next);
-    } else {
-      load(row, xv);
-    }
+    for (int q = 0; q < Q; ++q) In::wide(next[q], xv[q]);
+    if (kAhead) load(row + step, next);
     const float sum = wide_row_sum<NW>(st[w], xv, cols, slot[0]);
     const float mu = sum * inv_d;
     float sq[Q][4];  // what lies behind the row's end is not read by the chains
@@ -124,21 +119,24 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void layer
     const float* __restrict__ rstd, const float* __restrict__ dy, float inv_d, float* __restrict__ dx) {
   constexpr int kRows = NW == 1 ? 4 : 1;
   __shared__ __attribute__((aligned(16))) RowStage<Q> st[NW == 1 ? 4 : NW];
+  using In = PartIn<SRC>;
   __shared__ float slot[2][NW];
   const int w = wave_id();
   const int seg = NW == 1 ? 0 : w * 256 * Q;
   const int n = cols - seg < 256 * Q ? cols - seg : 256 * Q;
   for (int64_t row = (int64_t)blockIdx.x * kRows + (NW == 1 ? w : 0); row < rows; row += (int64_t)gridDim.x * kRows) {
     const float mu = mean[row], r = rstd[row];
-    const PartIn<SRC> in(x, row, cols, seg);
     const float* dr = dy + row * cols + seg;
+    typename In::Raw xr[Q];
+    uint32_t gw[Q][2];
     float xh[Q][4], gy[Q][4], tm[Q][4];
-    part_load<TAIL>(0, n, xh, [&](int j, float(&v)[4]) { in.load4(j, v); }, [&](int j) { return in.load1(j); });
-    part_load<TAIL>(0, n, gy, [&](int j, float(&v)[4]) { ldf<4>(dr + j, v); }, [&](int j) { return dr[j]; });
-    part_load<TAIL>(0, n, tm, [&](int j, float(&v)[4]) { ldb_wide(gain + seg + j, v); },
-                    [&](int j) { return bf16_wide(gain[seg + j]); });
+    In(x, row, cols, seg).template part<TAIL>(n, xr);
+    part_load<TAIL>(0, n, gy, dr);
+    part_load_bf16<TAIL>(0, n, gw, gain + seg);
 #pragma unroll
-    for (int q = 0; q < Q; ++q)
+    for (int q = 0; q < Q; ++q) {
+      In::wide(xr[q], xh[q]);
+      wide4(gw[q], tm[q]);
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         const float d = xh[q][t] - mu;
@@ -146,6 +144,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void layer
         gy[q][t] = gy[q][t] * tm[q][t];
         tm[q][t] = gy[q][t] * xh[q][t];
       }
+    }
     const float s1 = wide_row_sum<NW>(st[w], gy, cols, slot[0]);
     const float s2 = wide_row_sum<NW>(st[w], tm, cols, slot[1]);
     const float m1 = s1 * inv_d, m2 = s2 * inv_d;

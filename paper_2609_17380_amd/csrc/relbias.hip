@@ -107,7 +107,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
     const float* rr = scores + row;
     uint16_t* pr = probs + row;
     float e[Q][4];
-    part_load<TAIL>(pt.from, pt.upto, e, [&](int j, float(&v)[4]) { ldf<4>(rr + j, v); }, [&](int j) { return rr[j]; });
+    part_load<TAIL>(pt.from, pt.upto, e, rr);
     if (!once) __syncthreads();  // the last row's biases are read
     once = false;
     for (int k = threadIdx.x; k <= far + right; k += blockDim.x) {
@@ -224,7 +224,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
     const uint16_t* pr = probs + t.row;
     const float* dr = dprobs + t.row;
     part_load_bf16<TAIL>(t.pt.from, t.pt.upto, pw, pr);
-    part_load<TAIL>(t.pt.from, t.pt.upto, dp, [&](int j, float(&v)[4]) { ldf<4>(dr + j, v); }, [&](int j) { return dr[j]; });
+    part_load<TAIL>(t.pt.from, t.pt.upto, dp, dr);
     return t;
   };
   // Units are dealt out forth and back, so that a workgroup's causal rows are long and short in turn.

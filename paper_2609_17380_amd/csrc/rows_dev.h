@@ -242,15 +242,15 @@ __device__ __forceinline__ int again(int x) {
 // end at or before `upto` are moved whole; the one that it cuts (TAIL: it need not be a multiple of 4) belongs to one lane
 // of one q and is moved by element beside the loop, so that the loop has a single condition per vector (with the cut
 // vector's branches in every iteration the masks spilled: padded rows of 1001 keys 109 us, then 53).
-template <bool TAIL, int Q, class Load4, class Load1>
-__device__ __forceinline__ void part_load(int from, int upto, float (&v)[Q][4], Load4 load4, Load1 load1) {
+template <bool TAIL, int Q>
+__device__ __forceinline__ void part_load(int from, int upto, float (&v)[Q][4], const float* p) {
   const int at = 4 * (threadIdx.x & 63), first = from - 3;
   const unsigned whole = upto - 3 > first ? (unsigned)(upto - 3 - first) : 0u;  // places where a vector may begin
 #pragma unroll
   for (int q = 0; q < Q; ++q) {
 #pragma unroll
     for (int t = 0; t < 4; ++t) v[q][t] = 0.0f;
-    if ((unsigned)(256 * q + at - first) < whole) load4(256 * q + at, v[q]);
+    if ((unsigned)(256 * q + at - first) < whole) ldf<4>(p + 256 * q + at, v[q]);
   }
   if (TAIL && upto > from && (upto & 3)) {
     const int base = upto & ~3;
@@ -259,7 +259,7 @@ __device__ __forceinline__ void part_load(int from, int upto, float (&v)[Q][4], 
     if (mine >= 0) {
 #pragma unroll
       for (int t = 0; t < 3; ++t)
-        if (base + t < upto) c[t] = load1(base + t);
+        if (base + t < upto) c[t] = p[base + t];
     }
 #pragma unroll
     for (int q = 0; q < Q; ++q)
@@ -270,6 +270,7 @@ __device__ __forceinline__ void part_load(int from, int upto, float (&v)[Q][4], 
 // The same of bf16 elements, kept as they are stored, two to a word: half the registers while they wait.
 template <bool TAIL, int Q>
 __device__ __forceinline__ void part_load_bf16(int from, int upto, uint32_t (&v)[Q][2], const uint16_t* p) {
+  upto = again(upto);
   const int at = 4 * (threadIdx.x & 63), first = from - 3;
   const unsigned whole = upto - 3 > first ? (unsigned)(upto - 3 - first) : 0u;
 #pragma unroll
