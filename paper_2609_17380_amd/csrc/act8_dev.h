@@ -181,15 +181,26 @@ struct PartIn {
     float f[SRC == ACT_F32 ? 4 : 1];  // fp32; in 8 bits the step
     uint32_t w[SRC == ACT_BF16 ? 2 : 1];
   };
-  __device__ __forceinline__ void load4(int j, Raw& r) const {
+  __device__ __forceinline__ void load4(int j, Raw& r) const { load4(j, j, r); }
+  __device__ __forceinline__ void load4(int j, int group, Raw& r) const {  // with the step of element `group`
     if constexpr (SRC == ACT_F32) {
       ldf<4>((const float*)p + j, r.f);
     } else if constexpr (SRC == ACT_BF16) {
       const H4 h = *reinterpret_cast<const H4*>((const uint16_t*)p + j);
       r.w[0] = h.x; r.w[1] = h.y;
     } else {
-      r.f[0] = steps[j >> lg];
+      r.f[0] = steps[group >> lg];
       r.w[0] = reinterpret_cast<const B4*>((const int8_t*)p + j)->x;
+    }
+  }
+  // bf16 or 8 bits: four elements of which the last n are wanted (n > 3: all) to the first n places, 0 behind them
+  static __device__ __forceinline__ void ends(Raw& r, int n) {
+    const int away = n > 0 && n < 4 ? 4 - n : 0;
+    if constexpr (SRC == ACT_BF16) {
+      const uint64_t w = (((uint64_t)r.w[1] << 32) | r.w[0]) >> (16 * away);
+      r.w[0] = (uint32_t)w; r.w[1] = (uint32_t)(w >> 32);
+    } else {
+      r.w[0] >>= 8 * away;
     }
   }
   // element j + t into place t

@@ -167,8 +167,10 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void layer
   }
 }
 
-// Four columns of a row from column j on, n of them there (none: n <= 0), x as it is stored; 0 where there are none.
-template <int SRC, bool TAIL>
+// Four columns of a row of 4 or more from column j on, n of them there (none: n <= 0), x as it is stored; 0 where there are
+// none.  The vector that the row's end cuts is loaded element by element, or (ENDS, bf16 and 8 bits) as the row's last four,
+// which `ends` puts in place when they are needed.
+template <int SRC, bool TAIL, bool ENDS>
 __device__ __forceinline__ void load_columns(const ActIn& x, const float* dy, int64_t rows, int64_t row, int cols, int j,
                                              int n, typename PartIn<SRC>::Raw& xr, float (&dv)[4]) {
   xr = typename PartIn<SRC>::Raw{};
@@ -177,72 +179,60 @@ __device__ __forceinline__ void load_columns(const ActIn& x, const float* dy, in
   if (row >= rows) return;
   const PartIn<SRC> in(x, row, cols, 0);
   const float* dr = dy + row * cols;
+  if (ENDS && n > 0) in.load4(TAIL && n < 4 ? cols - 4 : j, j, xr);
   if (n == 4) {
-    in.load4(j, xr);
+    if (!ENDS) in.load4(j, xr);
     ldf<4>(dr + j, dv);
   } else if (TAIL) {
 #pragma unroll
     for (int t = 0; t < 3; ++t)
       if (t < n) {
-        in.load1(j, t, xr);
+        if (!ENDS) in.load1(j, t, xr);
         dv[t] = dr[j + t];
       }
   }
 }
 
-// The chains of 32 rows of dgain[k] = R1 over rows of RN(dy xh) and dbias[k] = R1 over rows of dy, V = 4 columns or one per
-// thread, B rows in flight.  part: [2][chunks][cols].  1023 x 5001 from 8 bits 9 us: 32 dependent steps to a chain, 32 chains
-// to a column.
-template <int SRC, int V, int B, bool TAIL>
-__global__ __launch_bounds__(256 / V) void layernorm_part_kernel(int64_t rows, int cols, ActIn x, const float* __restrict__ mean,
-                                                            const float* __restrict__ rstd, const float* __restrict__ dy,
-                                                            float* __restrict__ part) {
-  const int j = blockIdx.x * 256 + threadIdx.x * V, n = cols - j < V ? cols - j : V;
+// The chains of 32 rows of dgain[k] = R1 over rows of RN(dy xh) and dbias[k] = R1 over rows of dy, a column to a thread, B
+// rows in flight.  part: [2][chunks][cols].  1023 x 5001 from 8 bits 9 us: 32 dependent steps to a chain, 32 chains to a
+// column.  (Four columns to a thread are fewer, wider loads and were never faster: 8192 x 2048 with dx 69 us, so 64.5; 1023 x
+// 5001 bf16 32 and 23.)
+template <int SRC, int B>
+__global__ __launch_bounds__(256) void layernorm_part_kernel(int64_t rows, int cols, ActIn x, const float* __restrict__ mean,
+                                                             const float* __restrict__ rstd, const float* __restrict__ dy,
+                                                             float* __restrict__ part) {
+  const int j = blockIdx.x * 256 + threadIdx.x;
   const int64_t nc = (rows + kChunk - 1) / kChunk;
-  if (n <= 0) return;
+  if (j >= cols) return;
   for (int64_t c = blockIdx.y; c < nc; c += gridDim.y) {
-    float sg[V], sb[V];
-#pragma unroll
-    for (int k = 0; k < V; ++k) sg[k] = sb[k] = 0.0f;
+    float sg = 0.0f, sb = 0.0f;
     auto steps = [&](int64_t t, auto count) __attribute__((always_inline)) {  // all loads, then the chains' steps
       constexpr int N = decltype(count)::value;
       typename PartIn<SRC>::Raw xr[N];
-      float dv[N][4];
+      float dv[N];
 #pragma unroll
       for (int r = 0; r < N; ++r) {
-        if constexpr (V == 4) {
-          load_columns<SRC, TAIL>(x, dy, rows, t + r, cols, j, n, xr[r], dv[r]);
-        } else {
-          xr[r] = typename PartIn<SRC>::Raw{};
-          PartIn<SRC>(x, t + r, cols, 0).load1(j, 0, xr[r]);
-          dv[r][0] = dy[(t + r) * cols + j];
-        }
+        xr[r] = typename PartIn<SRC>::Raw{};
+        PartIn<SRC>(x, t + r, cols, 0).load1(j, 0, xr[r]);
+        dv[r] = dy[(t + r) * cols + j];
       }
 #pragma unroll
       for (int r = 0; r < N; ++r) {
-        const float mu = mean[t + r], rs = rstd[t + r];
         float xv[4];
         PartIn<SRC>::wide(xr[r], xv);
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-          const float d = xv[k] - mu;
-          const float xh = d * rs;
-          const float pr = dv[r][k] * xh;
-          sg[k] = sg[k] + pr;
-          sb[k] = sb[k] + dv[r][k];
-        }
+        const float d = xv[0] - mean[t + r];
+        const float xh = d * rstd[t + r];
+        const float pr = dv[r] * xh;
+        sg = sg + pr;
+        sb = sb + dv[r];
       }
     };
     const int64_t t1 = (c + 1) * kChunk < rows ? (c + 1) * kChunk : rows;
     int64_t t = c * kChunk;
     for (; t + B <= t1; t += B) steps(t, std::integral_constant<int, B>{});
     for (; t < t1; ++t) steps(t, std::integral_constant<int, 1>{});
-#pragma unroll
-    for (int k = 0; k < V; ++k)
-      if (k < n) {
-        part[c * cols + j + k] = sg[k];
-        part[(nc + c) * cols + j + k] = sb[k];
-      }
+    part[c * cols + j] = sg;
+    part[(nc + c) * cols + j] = sb;
   }
 }
 
@@ -259,6 +249,9 @@ __global__ __launch_bounds__(64 * NW) void layernorm_pass_kernel(int64_t rows, i
                                                                  const float* __restrict__ dy, float inv_d,
                                                                  float* __restrict__ dx, float* __restrict__ part) {
   constexpr int R = 4 / VQ, kSums = 2 * R, kLanes = 8 * VQ;  // lanes to a sum's chunks
+  // bf16 and 8-bit elements one by one are waited for (4096 x 2047 bf16 38 us, so 27), but two vectors to a lane leave no
+  // registers (4096 x 7001 from 8 bits 109 us, one by one 76), and fp32 ones need no wait
+  constexpr bool kEnds = SRC != ACT_F32 && VQ == 1;
   using In = PartIn<SRC>;
   __shared__ __attribute__((aligned(16))) RegStage st[NW];
   __shared__ float slot[2][kSums][NW];
@@ -272,7 +265,7 @@ __global__ __launch_bounds__(64 * NW) void layernorm_pass_kernel(int64_t rows, i
   const int64_t nc = (rows + kChunk - 1) / kChunk;
   auto load = [&](int64_t row, typename In::Raw(&xr)[VQ], float(&dv)[VQ][4]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int v = 0; v < VQ; ++v) load_columns<SRC, TAIL>(x, dy, rows, row, cols, j[v], n[v], xr[v], dv[v]);
+    for (int v = 0; v < VQ; ++v) load_columns<SRC, TAIL, kEnds>(x, dy, rows, row, cols, j[v], n[v], xr[v], dv[v]);
   };
   auto add = [](uint32_t a, uint32_t b) {
     const float s = __uint_as_float(a) + __uint_as_float(b);
@@ -305,6 +298,7 @@ __global__ __launch_bounds__(64 * NW) void layernorm_pass_kernel(int64_t rows, i
 #pragma unroll
         for (int v = 0; v < VQ; ++v) {
           float tm[4], xv[4];
+          if constexpr (kEnds && TAIL) In::ends(xr[r][v], n[v]);
           In::wide(xr[r][v], xv);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
@@ -484,9 +478,11 @@ hipError_t layernorm_bwd_launch(int64_t rows, int64_t cols, const ActIn& x, cons
                                 hipStream_t s) {
   const float inv_d = (float)(1.0 / (double)cols);
   const int64_t nc = (rows + kChunk - 1) / kChunk;
-  // One pass over x and dy where its workgroups, one to 32 rows, are half as many as the CUs or more (with the forward:
-  // 4096 x 2048 in 39 us, in two passes 45; 4096 x 8192 in 151 and 178; of 2048 rows 31 and 28, 110 and 90).
-  const bool once = (dgain || dbias) && cols <= kPassCols && 2 * nc >= device_cus();
+  // One pass over x and dy where its workgroups, one to 32 rows, are half as many as the CUs or more, and its wavefronts four
+  // to a CU (4096 x 8192 in 103 us, in two passes 128; 8192 x 2048 48 and 64.5; 4096 x 2048 31 and 32; of 2048 x 8192 86 and
+  // 63.5, 4096 x 1001 29 and 21, 8192 x 512 20 and 19.5).
+  const bool once = (dgain || dbias) && cols >= 4 && cols <= kPassCols && 2 * nc >= device_cus() &&
+                    nc * ((cols + 255) / 256 < 16 ? (cols + 255) / 256 : 16) >= 4 * device_cus();
   if (once) {
     const dim3 grid((unsigned)(nc < kMaxBlocks ? nc : kMaxBlocks));
 #define CANON_LN_PASS(SRC, VQ, NW)                                                                                         \
@@ -516,23 +512,13 @@ hipError_t layernorm_bwd_launch(int64_t rows, int64_t cols, const ActIn& x, cons
     return column_fold_launch(rows, cols, 0, part, dgain, dbias, s);
   }
   if ((dgain || dbias) && rows > 0) {
-    // four columns to a thread once that makes eight wavefronts to a CU; below, one
-    const int v = nc * ((cols + 255) / 256) >= 8 * device_cus() ? 4 : 1;
     const dim3 grid((unsigned)((cols + 255) / 256), (unsigned)(nc < 65535 ? nc : 65535));
-#define CANON_LN_PART_K(SRC, V, B, TAIL)                                                                                \
-  hipLaunchKernelGGL((layernorm_part_kernel<SRC, V, B, TAIL>), grid, dim3(256 / V), 0, s, rows, (int)cols, x, mean, rstd,    \
-                     dy, part)
-#define CANON_LN_PART(SRC)                                        \
-  do {                                                            \
-    if (v == 1) CANON_LN_PART_K(SRC, 1, 8, false);               \
-    else if (cols % 4 == 0) CANON_LN_PART_K(SRC, 4, 4, false);    \
-    else CANON_LN_PART_K(SRC, 4, 4, true);                        \
-  } while (0)
+#define CANON_LN_PART(SRC) \
+  hipLaunchKernelGGL((layernorm_part_kernel<SRC, 8>), grid, dim3(256), 0, s, rows, (int)cols, x, mean, rstd, dy, part)
     if (x.src == ACT_F32) CANON_LN_PART(ACT_F32);
     else if (x.src == ACT_BF16) CANON_LN_PART(ACT_BF16);
     else CANON_LN_PART(ACT_Q8);
 #undef CANON_LN_PART
-#undef CANON_LN_PART_K
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

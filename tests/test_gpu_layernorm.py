@@ -126,6 +126,17 @@ def test_one_pass_over_many_rows(rows, cols, dtype, group):
     same(run(x, g, b, dy, dtype, torch.bfloat16, group), wanted(x, g, b, dy, torch.bfloat16, group))
 
 
+@pytest.mark.parametrize("rows,cols", [(8193, 1021), (8200, 1024), (16390, 510), (16384, 511), (32769, 4), (32800, 5), (32771, 6),
+                                       (32800, 7), (32800, 3), (32770, 254)])
+@pytest.mark.parametrize("dtype,group", [(torch.float32, None), (torch.bfloat16, None), (torch.float32, 32), (torch.bfloat16, 64)])
+def test_one_pass_over_narrow_rows(rows, cols, dtype, group):
+    # narrower rows are one pass from more of them on, and every cut of the last vector, rows of one vector among them; of
+    # rows of three columns there is no whole vector
+    print(f"layer norm {rows}x{cols} {dtype} group {group}", flush=True)
+    x, g, b, dy = inputs(rows, cols, dtype, seed=10)
+    same(run(x, g, b, dy, dtype, torch.bfloat16, group), wanted(x, g, b, dy, torch.bfloat16, group))
+
+
 @pytest.mark.parametrize("rows,cols", [(256, 2048), (512, 2047), (513, 2048), (1023, 2048), (2048, 1030), (2050, 1025), (300, 8191),
                                        (600, 8190)])
 def test_row_counts_around_the_shapes(rows, cols):
