@@ -116,7 +116,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void layer
 }
 
 // dx = RN(r RN(RN(gy - m1) - RN(xh m2))): gy = RN(dy g), m1 and m2 the row's means of gy and of RN(gy xh).  1023 x 5001 from
-// 8 bits 13 us: all its rows are on the chip at once, so that a row's latency (loads, two sums, stores) is the kernel's.
+// 8 bits 11 us: all its rows are on the chip at once, so that a row's latency (loads, two sums, stores) is the kernel's.
 template <int SRC, int Q, int NW, bool TAIL>
 __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void layernorm_dx_kernel(
     int64_t rows, int cols, ActIn x, const uint16_t* __restrict__ gain, const float* __restrict__ mean,
@@ -194,7 +194,7 @@ __device__ __forceinline__ void load_columns(const ActIn& x, const float* dy, in
 }
 
 // The chains of 32 rows of dgain[k] = R1 over rows of RN(dy xh) and dbias[k] = R1 over rows of dy, a column to a thread, B
-// rows in flight.  part: [2][chunks][cols].  1023 x 5001 from 8 bits 9 us: 32 dependent steps to a chain, 32 chains to a
+// rows in flight.  part: [2][chunks][cols].  1023 x 5001 from 8 bits 10 us: 32 dependent steps to a chain, 32 chains to a
 // column.  (Four columns to a thread are fewer, wider loads and were never faster: 8192 x 2048 with dx 69 us, so 64.5; 1023 x
 // 5001 bf16 32 and 23.)
 template <int SRC, int B>
@@ -240,7 +240,8 @@ __global__ __launch_bounds__(256) void layernorm_part_kernel(int64_t rows, int c
 // 256 VQ w on, R = 4 / VQ rows at a time.  A lane's columns run through the 32 rows in order, so it holds their chains of
 // dgain and dbias; a row's own sums, two to a row, are cut into 8 VQ chunks to a wavefront, 64 chains in all, a lane to a
 // chain over an LDS transpose, folded over the wavefront's chunks and then over the wavefronts.  The next rows are loaded
-// before the barrier that the sums wait at.
+// before the barrier that the sums wait at.  8192 x 2048 fp32 36 us behind the forward, which leaves part of x and dy in the
+// last-level cache (201 MB: 42 from memory); from 8 bits 29.
 template <int SRC, int VQ, int NW, bool TAIL>
 __global__ __launch_bounds__(64 * NW) void layernorm_pass_kernel(int64_t rows, int cols, ActIn x,
                                                                  const uint16_t* __restrict__ gain,
@@ -373,7 +374,7 @@ __global__ __launch_bounds__(64 * NW) void layernorm_pass_kernel(int64_t rows, i
 // Algorithm 2 over the chunk partials of a column: 16 wavefronts take 64 columns, wavefront g folds the aligned
 // power-of-two block of chunks [g G, g G + G), and the block results are folded with the pass-through rule.  Within a block
 // 16 partials at a time are loaded and folded as a tree, those past the last chunk as +0 (no partial is -0); only blocks of
-// more need Algorithm 2's stack (whose levels are indexed in scratch memory).
+// more need Algorithm 2's stack (whose levels are indexed in scratch memory).  256 partials of 2048 columns, twice, 4.6 us.
 constexpr int kFoldBlocks = 16;
 constexpr int kFoldUnit = 16;
 __global__ __launch_bounds__(64 * kFoldBlocks) void column_fold_kernel(int64_t nc, int64_t cols, int64_t inner,
