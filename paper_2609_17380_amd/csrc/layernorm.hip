@@ -48,8 +48,8 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void layer
   constexpr bool kEach = kAhead && !TAIL;
   uint32_t gw[Q][2], bw[Q][2];
   auto load_gain = [&]() __attribute__((always_inline)) {
-    part_load_bf16<TAIL>(0, n, gw, gain + seg);
-    part_load_bf16<TAIL>(0, bias ? n : 0, bw, bias + seg);
+    part_load_bf16<TAIL>(0, again(n), gw, gain + seg);
+    part_load_bf16<TAIL>(0, again(bias ? n : 0), bw, bias + seg);
   };
   int64_t row = (int64_t)blockIdx.x * kRows + (NW == 1 ? w : 0);
   if (kAhead) load(row, next);
@@ -136,7 +136,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void layer
     float xh[Q][4], gy[Q][4], tm[Q][4];
     In(x, row, cols, seg).template part<TAIL>(n, xr);
     part_load<TAIL>(0, n, gy, dr);
-    part_load_bf16<TAIL>(0, n, gw, gain + seg);
+    part_load_bf16<TAIL>(0, again(n), gw, gain + seg);
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
       In::wide(xr[q], xh[q]);

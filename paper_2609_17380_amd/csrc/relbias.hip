@@ -187,7 +187,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
 // two chunks, whose chains two lanes run and add (their sum is the fold whatever lies between); a longer one is summed
 // chunk by chunk, a lane to a chunk, like the row.
 // 16 x 2048 x 2048 causal 68 us, and 10 for the sums over the rows (336 MB: 70.5), without the table's gradient 70; 16 x 16 x
-// 512 127 (71), without 94: there the buckets' sums, about 180 vector instructions to a row of at most 512 keys, bound it.
+// 512 115 (71), without 83: there the buckets' sums, about 180 vector instructions to a row of at most 512 keys, bound it.
 template <int Q, int NW, bool TAIL>
 __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbias_bwd_kernel(
     RelBiasArgs a, uint32_t heads, uint32_t units, uint32_t per_head, const uint16_t* __restrict__ probs,

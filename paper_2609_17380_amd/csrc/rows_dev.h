@@ -270,7 +270,6 @@ __device__ __forceinline__ void part_load(int from, int upto, float (&v)[Q][4], 
 // The same of bf16 elements, kept as they are stored, two to a word: half the registers while they wait.
 template <bool TAIL, int Q>
 __device__ __forceinline__ void part_load_bf16(int from, int upto, uint32_t (&v)[Q][2], const uint16_t* p) {
-  upto = again(upto);
   const int at = 4 * (threadIdx.x & 63), first = from - 3;
   const unsigned whole = upto - 3 > first ? (unsigned)(upto - 3 - first) : 0u;
 #pragma unroll
