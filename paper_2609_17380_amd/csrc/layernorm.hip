@@ -36,8 +36,12 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void layer
   const int seg = NW == 1 ? 0 : w * 256 * Q;  // this wavefront's part of the row
   const int n = cols - seg < 256 * Q ? cols - seg : 256 * Q;
   using In = PartIn<SRC>;
+  // beside the codes of 8 vectors the places of the last four spill (8192 x 5001 kept 101 us, with them 123)
+  constexpr bool kEnds = TAIL && SRC == ACT_BF16 && !(KEEP && Q == 8);
   auto load = [&](int64_t row, typename In::Raw(&v)[Q]) __attribute__((always_inline)) {
-    In(x, row, cols, seg).template part<TAIL>(row < rows ? n : 0, v);
+    const In in(x, row, cols, seg);
+    if constexpr (kEnds) in.part_ends(row < rows ? n : 0, cols, v);
+    else in.template part<TAIL>(row < rows ? n : 0, v);
   };
   const int64_t step = (int64_t)gridDim.x * kRows;
   // the next row is on its way while one is summed and written, where the registers allow it
@@ -57,7 +61,10 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void layer
     float xv[Q][4];
     if (!kAhead) load(row, next);
 #pragma unroll
-    for (int q = 0; q < Q; ++q) In::wide(next[q], xv[q]);
+    for (int q = 0; q < Q; ++q) {
+      if constexpr (kEnds) In::ends(next[q], again(n) - (256 * q + 4 * (int)(threadIdx.x & 63)));
+      In::wide(next[q], xv[q]);
+    }
     if (kAhead) load(row + step, next);
     const float sum = wide_row_sum<NW>(st[w], xv, cols, slot[0]);
     const float mu = sum * inv_d;
