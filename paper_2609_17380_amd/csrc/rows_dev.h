@@ -148,8 +148,11 @@ __device__ __forceinline__ uint32_t lanes_join(uint32_t x, int lanes, Join join)
   lanes_join(v, lanes, join);
   return v[0];
 }
-// Algorithm 2 over 64 chunk partials, one per lane, of which those past the last chunk are +0: adding them is the
-// pass-through rule (no partial is -0).  The sum in every lane.
+// What a sum's padding adds: x + -0 is x for every x, +0 and -0 among them.  +0 would turn a -0 (a result below 2^-126 is
+// flushed to the zero of its sign) into +0.
+constexpr float kNoTerm = -0.0f;
+// Algorithm 2 over 64 chunk partials, one per lane, of which those past the last chunk are kNoTerm: adding them is the
+// pass-through rule.  The sum in every lane.
 __device__ __forceinline__ float wave_total(float p) {
   return __uint_as_float(lanes_join(__float_as_uint(p), 64, [](uint32_t a, uint32_t b) {
     const float s = __uint_as_float(a) + __uint_as_float(b);
@@ -184,23 +187,18 @@ struct RowStage {  // of a row of up to 256 Q terms
   __device__ __forceinline__ void put(int q, int lane, const float (&v)[4]) {
     vec(8 * q + (lane >> 3), lane & 7) = make_float4(v[0], v[1], v[2], v[3]);
   }
+  // the places behind n terms in their last chunk hold no term
+  __device__ __forceinline__ void end(int n) {
+    __builtin_amdgcn_wave_barrier();
+    const int at = n + (threadIdx.x & 63);
+    if ((n & (kChunk - 1)) != 0 && at < ((n + kChunk - 1) & ~(kChunk - 1))) t[at >> 5][at & 31] = kNoTerm;
+  }
   // the sum of the n terms put into it
   __device__ __forceinline__ float sum(int n) {
-    const int lane = threadIdx.x & 63, k1 = n - lane * kChunk;
+    const int lane = threadIdx.x & 63;
+    end(n);
     __builtin_amdgcn_wave_barrier();
-    float p = 0.0f;
-    if ((n & (kChunk - 1)) == 0) {
-      if (k1 > 0) p = chain(lane);
-    } else if (k1 > 0) {  // the row's last chunk is cut: what lies behind its end is left out by a select, a lane to a
-      // chunk as before (a loop up to its end waited for LDS at every term)
-#pragma unroll
-      for (int k = 0; k < kChunk / 4; ++k) {
-        const float4 v = vec(lane, k);
-        p = p + (4 * k < k1 ? v.x : 0.0f); p = p + (4 * k + 1 < k1 ? v.y : 0.0f);
-        p = p + (4 * k + 2 < k1 ? v.z : 0.0f); p = p + (4 * k + 3 < k1 ? v.w : 0.0f);
-      }
-    }
-    return wave_total(p);
+    return wave_total(lane * kChunk < n ? chain(lane) : kNoTerm);
   }
   // the same of a row whose terms outside vectors q0 .. q1 - 1 are +0, like their chunks' partials, and have not been put
   __device__ __forceinline__ float span_sum(int q0, int q1) {
@@ -354,7 +352,7 @@ __device__ __forceinline__ float wide_join(float p, int parts, float* slot) {
     const int lane = threadIdx.x & 63;
     if (lane == 0) slot[wave_id()] = p;
     __syncthreads();
-    return wave_total(lane < parts ? slot[lane] : 0.0f);
+    return wave_total(lane < parts ? slot[lane] : kNoTerm);
   }
 }
 template <int NW, int Q>
@@ -365,7 +363,7 @@ __device__ __forceinline__ float wide_row_sum(RowStage<Q>& st, const float (&e)[
     if (256 * q >= left) break;
     st.put(q, lane, e[q]);
   }
-  const float p = left > 0 ? st.sum(left < 256 * Q ? left : 256 * Q) : 0.0f;
+  const float p = left > 0 ? st.sum(left < 256 * Q ? left : 256 * Q) : kNoTerm;
   return wide_join<NW>(p, (n + 256 * Q - 1) / (256 * Q), slot);
 }
 

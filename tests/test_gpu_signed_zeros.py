@@ -1,0 +1,131 @@
+"""Row and column sums that end at -0.  A result below 2^-126 is flushed to the zero of its own sign, so a chain, a fold or a
+whole sum can be -0; what the order does not add (chunks, columns and rows that are not there) leaves it -0, and a term of +0
+does not.  Bit-identical to the oracle, in which absent terms are not there at all."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import paper_2609_17380_amd.canon as C
+import paper_2609_17380_amd.inputs as I
+from gpu_util import DEV, assert_bits, dev_bf16, dev_f32, host_f32, host_u16, poisoned_workspace
+from test_gpu_layernorm import host_bf16
+
+pytestmark = pytest.mark.gpu
+
+ONE = 0x3F80
+TINY = np.float32(2.0 ** -126)  # the least magnitude that is not flushed
+
+
+def last_split(n):
+    """The term at which the last addition of a sum of n terms in chunks of 32 splits them (of one chunk: none, 0)."""
+    chunks = (n + 31) // 32
+    return 32 << ((chunks - 1).bit_length() - 1) if chunks > 1 else 0
+
+
+def tiny_rows(rows, n, seed, kinds=(0, 1, 2)):
+    """Rows of -0 with a few terms of 1 to 1.75 times 2^-126 of either sign, many of whose sums are flushed: a third of the rows
+    with the terms anywhere, a third with them near the row's end, both with a +0 now and then; a third with 1 and -1.5 on
+    the two sides of the sum's last addition (or of its last chunk's), which ends at -0."""
+    rng = np.random.default_rng(seed)
+    x = np.full((rows, n), -0.0, np.float32)
+    kind, r, k = rng.choice(kinds, rows) if n > 1 else np.zeros(rows, int), np.arange(rows), 6
+    near = n - 1 - rng.integers(0, min(n, 40), (rows, k))
+    at = np.where(kind[:, None] == 1, near, rng.integers(0, n, (rows, k)))
+    v = (rng.choice([1, 1.25, 1.5, 1.75], (rows, k)) * rng.choice([-1, 1], (rows, k))).astype(np.float32) * TINY
+    live = np.where(kind == 2, 0, rng.integers(2, k + 1, rows))
+    for i in range(k):
+        m = i < live
+        x[r[m], at[m, i]] = v[m, i]
+    z = (rng.random(rows) < 0.2) & (kind < 2)
+    x[r[z], rng.integers(0, n, rows)[z]] = 0.0
+    m = r[kind == 2]
+    cut = last_split(n) or n - 1
+    x[m, rng.integers(0, cut, len(m))] = TINY
+    x[m, rng.integers(cut, n, len(m))] = -1.5 * TINY
+    return x
+
+
+def minus_zeros(x):
+    return int((np.ascontiguousarray(x).view(np.uint32) == 0x80000000).sum())
+
+
+def rms_backward(x, g, rstd, dy):
+    rows, cols = x.shape
+    dx = torch.full((rows, cols), float("nan"), device=DEV)
+    C.rownorm(C.BWD, rows, cols, dev_f32(x), dev_bf16(g), np.float32(1e-5), rstd=dev_f32(rstd), dy=dev_f32(dy), dx=dx)
+    torch.cuda.synchronize()
+    return host_f32(dx)
+
+
+def test_the_norm_gradient_of_a_dot_of_minus_zero():
+    # the dot is flushed from -2^-127 to -0, so that dx[2] = RN(-0 - -0) = +0; of a dot of +0 it is -0
+    x, g, rstd = np.ones((1, 3), np.float32), np.full(3, ONE, np.uint16), np.ones(1, np.float32)
+    dy = np.array([[TINY, -1.5 * TINY, -0.0]], np.float32)
+    got = rms_backward(x, g, rstd, dy)
+    assert got.view(np.uint32)[0, 2] == 0
+    assert_bits(got, oracle.rownorm_bwd(x, g, rstd, dy)[0], "dx")
+
+
+LENGTHS = [1, 2, 3, 31, 32, 33, 63, 64, 65, 100, 255, 257, 511, 513, 700, 1024, 1025, 1500, 2047, 2048]
+
+
+@pytest.mark.parametrize("cols", LENGTHS + [2049, 4100])
+def test_norm_rows(cols):
+    print(f"norm 96x{cols}", flush=True)
+    rows = 96
+    dy, g = tiny_rows(rows, cols, 1), np.full(cols, ONE, np.uint16)
+    x = np.where(np.arange(rows)[:, None] % 2, I.normal_f32((rows, cols), 1, 3), np.float32(1)).astype(np.float32)
+    rstd = np.ones(rows, np.float32)
+    assert_bits(rms_backward(x, g, rstd, dy), oracle.rownorm_bwd(x, g, rstd, dy)[0], "dx")
+    y, r = torch.empty((rows, cols), dtype=torch.bfloat16, device=DEV), torch.empty(rows, device=DEV)
+    C.rownorm(C.FWD, rows, cols, dev_f32(dy), dev_bf16(g), np.float32(1e-5), y=y, rstd=r)
+    torch.cuda.synchronize()
+    want_y, want_r = oracle.rownorm_fwd(dy, g, np.float32(1e-5))
+    assert_bits(host_u16(y), want_y, "y")
+    assert_bits(host_f32(r), want_r, "rstd")
+
+
+@pytest.mark.parametrize("cols", LENGTHS + [2049, 4096, 4100, 5001, 8192, 8195, 16390, 32767])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_layer_norm_rows(cols, dtype):
+    # few rows (spread over wavefronts from 1025 columns on) and many
+    for rows in (64, 3000) if cols in (1500, 2047) else (64,):
+        print(f"layer norm {rows}x{cols} {dtype}", flush=True)
+        x, g, b = tiny_rows(rows, cols, 2), np.full(cols, ONE, np.uint16), np.full(cols, 0x8000, np.uint16)
+        want_y, want_m, want_r = oracle.layernorm_fwd(x, g, b, 1e-5)
+        assert cols == 1 or minus_zeros(want_m) > rows // 5
+        on = dev_f32 if dtype == torch.float32 else lambda v: dev_bf16(host_bf16(v))  # their values have 3 bits
+        y, m, r = torch.empty((rows, cols), device=DEV), torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+        C.layernorm(rows, cols, on(x), dev_bf16(g), dev_bf16(b), 1e-5, y, m, r)
+        torch.cuda.synchronize()
+        assert_bits(host_f32(m), want_m, "mean")
+        assert_bits(host_f32(r), want_r, "rstd")
+        assert_bits(host_f32(y), want_y, "y")
+
+
+def layer_norm_backward(x, dy, group=None):
+    """dx, dgain and dbias of rows whose mean is taken as 0 and whose rstd as 1 (arguments of the call), and the oracle's."""
+    rows, cols = x.shape
+    g, m, r = np.full(cols, ONE, np.uint16), np.zeros(rows, np.float32), np.ones(rows, np.float32)
+    xd = dev_f32(x)
+    if group:
+        codes, steps = oracle.act8_pack(x, group)
+        xd = C.Act8(group, torch.from_numpy(codes).to(DEV), dev_f32(steps))
+        x = oracle.act8_unpack(codes, steps, group)
+    dx, dg, db = torch.empty((rows, cols), device=DEV), torch.empty(cols, device=DEV), torch.empty(cols, device=DEV)
+    ws = poisoned_workspace(C.layernorm_bwd_workspace_bytes(rows, cols))
+    C.layernorm_bwd(rows, cols, xd, dev_bf16(g), dev_f32(m), dev_f32(r), dev_f32(dy), dx, ws, dgain=dg, dbias=db)
+    torch.cuda.synchronize()
+    return [host_f32(t) for t in (dx, dg, db)], oracle.layernorm_bwd(x, g, m, r, dy)
+
+
+@pytest.mark.parametrize("cols", LENGTHS + [2049, 4096, 4100, 5001, 8195, 16390])
+def test_layer_norm_gradient_rows(cols):
+    print(f"layer norm backward 64x{cols}", flush=True)
+    rows = 64
+    dy = tiny_rows(rows, cols, 3)
+    x = np.where(np.arange(rows)[:, None] % 2, I.normal_f32((rows, cols), 1, 3), np.float32(1)).astype(np.float32)
+    for group in (None, 64):
+        got, want = layer_norm_backward(x, dy, group)
+        assert_bits(got[0], want[0], "dx")
