@@ -380,8 +380,9 @@ __global__ __launch_bounds__(64 * NW) void layernorm_pass_kernel(int64_t rows, i
 
 // Algorithm 2 over the chunk partials of a column: 16 wavefronts take 64 columns, wavefront g folds the aligned
 // power-of-two block of chunks [g G, g G + G), and the block results are folded with the pass-through rule.  Within a block
-// 16 partials at a time are loaded and folded as a tree, those past the last chunk as +0 (no partial is -0); only blocks of
-// more need Algorithm 2's stack (whose levels are indexed in scratch memory).  256 partials of 2048 columns, twice, 4.6 us.
+// 16 partials at a time are loaded and folded as a tree, those past the last chunk as kNoTerm (of no chunk at all the sum is
+// +0); only blocks of more need Algorithm 2's stack (whose levels are indexed in scratch memory).  256 partials of 2048
+// columns, twice, 4.6 us.
 constexpr int kFoldBlocks = 16;
 constexpr int kFoldUnit = 16;
 __global__ __launch_bounds__(64 * kFoldBlocks) void column_fold_kernel(int64_t nc, int64_t cols, int64_t inner,
@@ -398,14 +399,14 @@ __global__ __launch_bounds__(64 * kFoldBlocks) void column_fold_kernel(int64_t n
   auto unit = [&](int64_t c) __attribute__((always_inline)) {
     float p[kFoldUnit];
 #pragma unroll
-    for (int i = 0; i < kFoldUnit; ++i) p[i] = c + i < c1 ? part[(c + i) * cols + col] : 0.0f;
+    for (int i = 0; i < kFoldUnit; ++i) p[i] = c + i < c1 ? part[(c + i) * cols + col] : kNoTerm;
 #pragma unroll
     for (int d = 1; d < kFoldUnit; d <<= 1)
 #pragma unroll
       for (int i = 0; i + d < kFoldUnit; i += 2 * d) p[i] = p[i] + p[i + d];
     return p[0];
   };
-  float r = 0.0f;
+  float r = nc > 0 ? kNoTerm : 0.0f;
   if (col < cols && c0 < c1) {
     if (G <= kFoldUnit) {
       r = unit(c0);

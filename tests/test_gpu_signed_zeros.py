@@ -129,3 +129,15 @@ def test_layer_norm_gradient_rows(cols):
     for group in (None, 64):
         got, want = layer_norm_backward(x, dy, group)
         assert_bits(got[0], want[0], "dx")
+
+
+@pytest.mark.parametrize("rows", [1, 2, 31, 32, 33, 64, 65, 100, 512, 513, 1000, 1057, 5000, 16500])
+def test_sums_over_rows(rows):
+    # chains of 32 rows, blocks of chunks and folds of 16, some of each absent
+    cols = 200
+    print(f"rows {rows}", flush=True)
+    dy = np.ascontiguousarray(tiny_rows(cols, rows, 4).T)
+    got, want = layer_norm_backward(np.ones((rows, cols), np.float32), dy)
+    assert rows == 1 or minus_zeros(want[2]) > cols // 5
+    assert_bits(got[2], want[2], "dbias")
+    assert_bits(got[1], want[1], "dgain")
