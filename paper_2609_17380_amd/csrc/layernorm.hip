@@ -174,7 +174,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void layer
   }
 }
 
-// Four columns of a row of 4 or more from column j on, n of them there (none: n <= 0), x as it is stored; 0 where there are
+// Four columns of a row of 4 or more from column j on, n of them there (none: n <= 0), x as it is stored; +0 where there are
 // none.  The vector that the row's end cuts is loaded element by element, or (ENDS, bf16 and 8 bits) as the row's last four,
 // which `ends` puts in place when they are needed.
 template <int SRC, bool TAIL, bool ENDS>
@@ -279,11 +279,11 @@ __global__ __launch_bounds__(64 * NW) void layernorm_pass_kernel(int64_t rows, i
     const float s = __uint_as_float(a) + __uint_as_float(b);
     return __float_as_uint(s);
   };
-  float gv[VQ][4];
+  float gv[VQ][4];  // kNoTerm where there is no column: times the dy of +0 there, kNoTerm again
 #pragma unroll
   for (int v = 0; v < VQ; ++v)
 #pragma unroll
-    for (int t = 0; t < 4; ++t) gv[v][t] = t < n[v] ? bf16_wide(gain[j[v] + t]) : 0.0f;
+    for (int t = 0; t < 4; ++t) gv[v][t] = t < n[v] ? bf16_wide(gain[j[v] + t]) : kNoTerm;
   for (int64_t c = blockIdx.x; c < nc; c += gridDim.x) {
     const int64_t t0 = c * kChunk;
     typename In::Raw xr[R][VQ];
@@ -314,7 +314,7 @@ __global__ __launch_bounds__(64 * NW) void layernorm_pass_kernel(int64_t rows, i
             xh[r][v][i] = d * rs[r];
             gy[r][v][i] = dv[r][v][i] * gv[v][i];
             tm[i] = gy[r][v][i] * xh[r][v][i];
-            if (i >= n[v]) gy[r][v][i] = tm[i] = 0.0f;  // no column: a term of +0
+            if (i >= n[v]) tm[i] = gy[r][v][i];  // no column: both kNoTerm
             const float pr = dv[r][v][i] * xh[r][v][i];
             if (t + r < rows) {
               sg[v][i] = sg[v][i] + pr;
@@ -328,8 +328,10 @@ __global__ __launch_bounds__(64 * NW) void layernorm_pass_kernel(int64_t rows, i
       __builtin_amdgcn_wave_barrier();
 #pragma unroll
       for (int r = 0; r < R; ++r) load(t + R + r < t0 + kChunk ? t + R + r : rows, xr[r], dv[r]);
-      // the chain of chunk lane % kLanes of sum lane / kLanes
-      const float p = __uint_as_float(lanes_join(__float_as_uint(st[w].chain(lane)), kLanes, add));
+      // the chain of chunk lane % kLanes of sum lane / kLanes; of a chunk that the row does not have +0, and -c0 is kNoTerm
+      const float c0 = st[w].chain(lane);
+      const float c = kChunk * (kLanes * w + (lane & (kLanes - 1))) < cols ? c0 : -c0;
+      const float p = __uint_as_float(lanes_join(__float_as_uint(c), kLanes, add));
       if ((lane & (kLanes - 1)) == 0) slot[k & 1][lane / kLanes][w] = p;
       __syncthreads();
       float m[kSums];
@@ -337,7 +339,7 @@ __global__ __launch_bounds__(64 * NW) void layernorm_pass_kernel(int64_t rows, i
 #pragma unroll
       for (int i0 = 0; i0 < kSums; i0 += kOnce) {
         const int sum = i0 + lane / kWide, of = lane & (kWide - 1);
-        float s = sum < kSums && of < NW ? slot[k & 1][sum < kSums ? sum : 0][of < NW ? of : 0] : 0.0f;
+        float s = sum < kSums && of < NW ? slot[k & 1][sum < kSums ? sum : 0][of < NW ? of : 0] : kNoTerm;
         s = __uint_as_float(lanes_join(__float_as_uint(s), kWide, add)) * inv_d;
 #pragma unroll
         for (int i = 0; i < kOnce; ++i)

@@ -141,3 +141,19 @@ def test_sums_over_rows(rows):
     assert rows == 1 or minus_zeros(want[2]) > cols // 5
     assert_bits(got[2], want[2], "dbias")
     assert_bits(got[1], want[1], "dgain")
+
+
+@pytest.mark.parametrize("rows,cols", [(4096, 2048), (4099, 2050), (4097, 4095), (4100, 4097), (4096, 8190), (8200, 1021), (16400, 257),
+                                       (32769, 4), (32800, 5), (32770, 33), (32771, 255), (32800, 31), (32768 + 40, 64), (32800, 100)])
+@pytest.mark.parametrize("group", [None, 32])
+def test_one_pass_over_many_rows(rows, cols, group):
+    # the backward of enough rows is one pass, with columns and whole wavefronts that the row does not have
+    print(f"layer norm backward {rows}x{cols} group {group}", flush=True)
+    dy = tiny_rows(rows, cols, 5)
+    dy[:, ::3] = tiny_rows(cols, rows, 6, (2,))[::3].T  # so that sums over the rows are -0 as well
+    x = np.where(np.arange(rows)[:, None] % 2, np.float32(-1), np.float32(1)) * np.ones((1, cols), np.float32)
+    got, want = layer_norm_backward(np.ascontiguousarray(x), dy, group)
+    assert minus_zeros(want[2]) > cols // 5
+    assert_bits(got[0], want[0], "dx")
+    assert_bits(got[1], want[1], "dgain")
+    assert_bits(got[2], want[2], "dbias")
