@@ -203,6 +203,10 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
   const int parts = ((int)a.k_len + 256 * Q - 1) / (256 * Q);
   const int nb = a.n_side * (a.bidirectional ? 2 : 1);
   int turn = 0;  // as above
+  // What is made of a size: held, or beside 8 vectors, which leave no register, made again where it is used (4096 rows of 4096
+  // keys 354 us, held 387).
+  auto use = [](int size) __attribute__((always_inline)) { return Q == 8 ? again(size) : size; };
+  auto none = [&]() __attribute__((always_inline)) { return kChunk * lane < use(n) ? 0.0f : kNoTerm; };  // a chunk without a term
   uint32_t pw[Q][2];
   float dp[Q][4];
   // A unit is kRows queries of a matrix (batch and head); a wavefront loads its row of the next one before it sums this
@@ -270,7 +274,9 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
       st[w].put(q, lane, e);
     }
     turn ^= 1;
-    const float D = wide_join<NW>(st[w].span_sum(pt.q0, pt.q1), parts, slot[turn]);
+    st[w].end(use(n));
+    __builtin_amdgcn_wave_barrier();
+    const float D = wide_join<NW>(wave_total(st[w].span_chain(pt.q0, pt.q1, use(n), none())), parts, slot[turn]);
     Part pu = pt;
     pu.from = again(pt.from);
     part_store<TAIL, Q>(n,
@@ -302,9 +308,11 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
                      [&](int j, float o) { sr[j] = bf16_arith(o); });
     at = load(round + 1 < rounds ? dealt(round + 1) : units);
     if (!rowsum) continue;
+    st[w].end(use(n));
     float* out = rowsum + ((now.b * a.q_len + now.i) * a.heads + now.h) * nb;
     if constexpr (NW > 1) __syncthreads();
     else __builtin_amdgcn_wave_barrier();
+    const int keys = use((int)a.k_len);
     for (int k2 = NW == 1 ? lane : (int)threadIdx.x; k2 < 2 * nb; k2 += NW == 1 ? 64 : (int)blockDim.x) {
       const int k = k2 >> 1, lo = lo_[k], hi = hi_[k];
       const int b0 = qy.pos + lo > qy.j0 ? qy.pos + lo : qy.j0, b1 = qy.pos + hi < qy.j1 ? qy.pos + hi : qy.j1;
@@ -317,12 +325,25 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
         for (int j = 0; j < a.short_most && j < c1 - c0; j += 4) {  // up to three places behind the chunk's end: its row's padding
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
-            const int take = __builtin_amdgcn_sbfe((int)mine, j + u, 1);  // all ones or none
-            sum = sum + __uint_as_float(__float_as_uint(t[j + u]) & (uint32_t)take);
+            const uint32_t take = (uint32_t)__builtin_amdgcn_sbfe((int)mine, j + u, 1);  // all ones or none
+            sum = sum + __uint_as_float((__float_as_uint(t[j + u]) & take) | (__float_as_uint(kNoTerm) & ~take));
           }
         }
       }
-      sum = sum + __uint_as_float(lane_move<0xB1>(__float_as_uint(sum)));  // the bucket's two chunks
+      // The bucket's two chunks, of which a -0 is left as it is only where nothing is added to it: no term of +0 behind the
+      // bucket in the chunk, no partial of +0 but theirs, and none after their sum.
+      if (keys > 2 * kChunk) {
+        sum = sum + 0.0f;
+        sum = sum + __uint_as_float(lane_move<0xB1>(__float_as_uint(sum)));
+        const float more = sum + 0.0f;
+        sum = mid == kChunk << (31 - __builtin_clz((unsigned)(keys - 1) / kChunk)) ? sum : more;
+      } else {
+        if (c0 < c1 && (c1 & (kChunk - 1)) != 0 && c1 < keys) sum = sum + 0.0f;
+        if (keys > kChunk) {
+          sum = sum + __uint_as_float(lane_move<0xB1>(__float_as_uint(sum)));
+          if (mid > kChunk) sum = sum + 0.0f;
+        }
+      }
       if (!(k2 & 1) && hi - lo <= kRelShort) out[k] = sum;
     }
     if (a.far_only) {
@@ -335,18 +356,18 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
       if (far > 0)  // one bucket alone: no key is nearer
         for (int z = (z0 > 0 ? z0 : 0) + lane; z < z1 && z < 256 * Q; z += 64) st[w].t[z >> 5][z & 31] = 0.0f;
       __builtin_amdgcn_wave_barrier();
-      const float c = lane >= 8 * pt.q0 && lane < 8 * pt.q1 ? st[w].chain(lane) : 0.0f;
+      const float no = none(), c = st[w].span_chain(pt.q0, pt.q1, use(n), no);
       const bool before = !a.bidirectional || seg + 32 * lane <= qy.pos - far;
-      float left = wave_total(before ? c : 0.0f);
-      float right = a.bidirectional ? wave_total(before ? 0.0f : c) : 0.0f;
+      float left = wave_total(before ? c : no);
+      float right = a.bidirectional ? wave_total(before ? no : c) : 0.0f;
       if constexpr (NW > 1) {
         if (lane == 0) {
           part[0][w] = left;
           part[1][w] = right;
         }
         __syncthreads();
-        left = wave_total(lane < parts ? part[0][lane] : 0.0f);
-        right = wave_total(lane < parts ? part[1][lane] : 0.0f);
+        left = wave_total(lane < parts ? part[0][lane] : kNoTerm);
+        right = wave_total(lane < parts ? part[1][lane] : kNoTerm);
       }
       if (lane == 0 && (NW == 1 || w == 0)) {
         out[a.n_side - 1] = left;
@@ -359,23 +380,26 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
         const int b0 = (qy.pos + lo > qy.j0 ? qy.pos + lo : qy.j0) - seg, b1 = (qy.pos + hi < qy.j1 ? qy.pos + hi : qy.j1) - seg;
         float sum = 0.0f;
         if (b0 < b1 && b0 < 256 * Q && b1 > 0) {  // the same for the whole wavefront
-          if (lane < 8 * Q) {
-            const int c0 = b0 - 32 * lane, len = b1 - b0;
+          float p = 0.0f;
+          if (32 * lane < n) {  // up to the row's end what ends it is added as well
+            const int c0 = b0 - 32 * lane, len = (b1 < n ? b1 : 256 * Q) - b0;
 #pragma unroll
             for (int t = 0; t < kChunk; t += 4) {
               const float4 v = st[w].vec(lane, t / 4);
-              sum = sum + ((unsigned)(t - c0) < (unsigned)len ? v.x : 0.0f);
-              sum = sum + ((unsigned)(t + 1 - c0) < (unsigned)len ? v.y : 0.0f);
-              sum = sum + ((unsigned)(t + 2 - c0) < (unsigned)len ? v.z : 0.0f);
-              sum = sum + ((unsigned)(t + 3 - c0) < (unsigned)len ? v.w : 0.0f);
+              p = p + ((unsigned)(t - c0) < (unsigned)len ? v.x : 0.0f);
+              p = p + ((unsigned)(t + 1 - c0) < (unsigned)len ? v.y : 0.0f);
+              p = p + ((unsigned)(t + 2 - c0) < (unsigned)len ? v.z : 0.0f);
+              p = p + ((unsigned)(t + 3 - c0) < (unsigned)len ? v.w : 0.0f);
             }
+          } else {
+            p = kNoTerm;
           }
-          sum = wave_total(sum);
+          sum = wave_total(p);
         }
         if constexpr (NW > 1) {
           if (lane == 0) part[l & 1][w] = sum;
           __syncthreads();
-          sum = wave_total(lane < parts ? part[l & 1][lane] : 0.0f);
+          sum = wave_total(lane < parts ? part[l & 1][lane] : kNoTerm);
         }
         if (lane == 0 && (NW == 1 || w == 0)) out[k] = sum;
       }

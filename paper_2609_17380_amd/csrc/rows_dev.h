@@ -190,8 +190,10 @@ struct RowStage {  // of a row of up to 256 Q terms
   // the places behind n terms in their last chunk hold no term
   __device__ __forceinline__ void end(int n) {
     __builtin_amdgcn_wave_barrier();
-    const int at = n + (threadIdx.x & 63);
-    if ((n & (kChunk - 1)) != 0 && at < ((n + kChunk - 1) & ~(kChunk - 1))) t[at >> 5][at & 31] = kNoTerm;
+    if ((n & (kChunk - 1)) != 0) {
+      const int at = n + (threadIdx.x & 63);
+      if (at < ((n + kChunk - 1) & ~(kChunk - 1))) t[at >> 5][at & 31] = kNoTerm;
+    }
   }
   // the sum of the n terms put into it
   __device__ __forceinline__ float sum(int n) {
@@ -200,11 +202,18 @@ struct RowStage {  // of a row of up to 256 Q terms
     __builtin_amdgcn_wave_barrier();
     return wave_total(lane * kChunk < n ? chain(lane) : kNoTerm);
   }
-  // the same of a row whose terms outside vectors q0 .. q1 - 1 are +0, like their chunks' partials, and have not been put
+  // the sum of a row whose terms outside vectors q0 .. q1 - 1 are +0, like their chunks' partials, and have not been put;
+  // of terms that are not below +0 (no sum of them is -0)
   __device__ __forceinline__ float span_sum(int q0, int q1) {
     const int lane = threadIdx.x & 63;
     __builtin_amdgcn_wave_barrier();
     return wave_total(lane >= 8 * q0 && lane < 8 * q1 ? chain(lane) : 0.0f);
+  }
+  // The partial of this lane's chunk of such a row of n terms of any sign, ended; none: +0, or kNoTerm behind the row's last
+  // chunk.
+  __device__ __forceinline__ float span_chain(int q0, int q1, int n, float none) {
+    const int lane = threadIdx.x & 63, upto = (n + kChunk - 1) / kChunk;
+    return lane >= 8 * q0 && lane < (8 * q1 < upto ? 8 * q1 : upto) ? chain(lane) : none;
   }
 };
 using RegStage = RowStage<kRegQ>;

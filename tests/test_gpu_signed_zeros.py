@@ -8,7 +8,7 @@ import torch
 import oracle
 import paper_2609_17380_amd.canon as C
 import paper_2609_17380_amd.inputs as I
-from gpu_util import DEV, assert_bits, dev_bf16, dev_f32, host_f32, host_u16, poisoned_workspace
+from gpu_util import DEV, assert_bits, dev_bf16, dev_f32, dev_i32, host_f32, host_u16, poisoned_workspace
 from test_gpu_layernorm import host_bf16
 
 pytestmark = pytest.mark.gpu
@@ -157,3 +157,78 @@ def test_one_pass_over_many_rows(rows, cols, group):
     assert_bits(got[0], want[0], "dx")
     assert_bits(got[1], want[1], "dgain")
     assert_bits(got[2], want[2], "dbias")
+
+
+LOG32 = list(C.relbias_log(32, 128).start)[:32]
+LOG16 = list(C.relbias_log(32, 128, True).start)[:16]
+WIDE = [0, 1, 34, 70, 200]
+
+
+KEYS = [1, 2, 5, 31, 32, 33, 63, 64, 65, 96, 97, 128, 129, 200, 255, 256, 300, 511, 512, 700, 1024, 1100, 2047, 2500, 5000]
+BUCKETS = [(LOG32, False), (LOG16, True), (WIDE, False), (WIDE, True), ([0], False), ([0], True), ([0, 32], True),
+           ([0, 1, 2, 3], True)]
+
+
+def relative_bias_backward(p, dp, starts, bidirectional, pos, causal=False, window=0, k_len=None):
+    """dscores and dtable of queries from position pos on, and the oracle's."""
+    B, H, Q, k = p.shape
+    lens = None if k_len is None else [k_len] * B
+    rows = C.AttnRows(B, H, Q, k, scale=1.0, causal=causal, q_start=pos, window=window, k_lens=None if lens is None else dev_i32(lens))
+    bias = C.RelBias(starts, bidirectional)
+    ds, dt = torch.empty(p.shape, dtype=torch.bfloat16, device=DEV), torch.empty((bias.buckets, H), device=DEV)
+    ws = poisoned_workspace(C.softmax_relbias_bwd_workspace_bytes(rows, bias))
+    C.softmax_relbias_bwd(rows, bias, dev_bf16(p), dev_f32(dp), ds, ws, dtable=dt)
+    torch.cuda.synchronize()
+    return (host_u16(ds), host_f32(dt)), oracle.relbias_bwd(p, dp, starts, bidirectional, scale=1.0, causal=causal, window=window,
+                                                            q_starts=[pos] * B, k_lens=lens)
+
+
+@pytest.mark.parametrize("k", KEYS)
+@pytest.mark.parametrize("starts,bidirectional", BUCKETS)
+def test_relative_bias_gradient(k, starts, bidirectional):
+    print(f"relbias backward {k} keys {len(starts)} starts bidirectional={bidirectional}", flush=True)
+    rng = np.random.default_rng(6)
+    dp = tiny_rows(64, k, 7).reshape(1, 16, 4, k)
+    p = np.where((rng.random(dp.shape) < 0.5) & (dp == 0), 0, ONE).astype(np.uint16)
+    got, want = relative_bias_backward(p, dp, starts, bidirectional, k // 2)
+    assert_bits(got[0], want[0], "dscores")
+    assert_bits(got[1], want[1], "dtable")
+
+
+@pytest.mark.parametrize("k", KEYS[1:])
+@pytest.mark.parametrize("starts,bidirectional", BUCKETS)
+def test_relative_bias_table_gradient(k, starts, bidirectional):
+    # Every head is a trial: its first two rows leave the chain of one bucket at -0 (ds of 1 and -1.5 times 2^-126 in one key of
+    # it, and zeros), and the third row's sum of that bucket, of two keys with ds of 1.19 and -1.31, decides whether it stays.
+    print(f"relbias table gradient {k} keys {len(starts)} starts bidirectional={bidirectional}", flush=True)
+    H, cut, rng = 48, last_split(k), np.random.default_rng(8)
+    for pos in sorted({max(0, v) for v in (0, cut - 3, cut, cut + 5, cut + 37, cut + 190, k // 2, k - 1)}):
+        p, dp = np.zeros((1, H, 3, k), np.uint16), np.full((1, H, 3, k), -0.0, np.float32)
+        for h in range(H):
+            if cut and h % 2:   # the last addition's two sides
+                a, b = max(0, cut - 1 - rng.integers(0, 4)), min(k - 1, cut + rng.integers(0, 4))
+            else:               # the row's end
+                b = k - 1 - rng.integers(0, min(3, k - 1))
+                a = max(0, b - 1 - rng.integers(0, 3))
+            p[0, h, :2, a], dp[0, h, :2, a] = 0x3F00, (4 * TINY, -6 * TINY)
+            p[0, h, 2, [a, b]], dp[0, h, 2, [a, b]] = 0x3E80, (3 * TINY, -7 * TINY)
+        got, want = relative_bias_backward(p, dp, starts, bidirectional, pos)
+        if starts == [0] and (not bidirectional or pos == 0):
+            assert minus_zeros(want[1]) > H // 8
+        assert_bits(got[0], want[0], "dscores")
+        assert_bits(got[1], want[1], "dtable")
+
+
+@pytest.mark.parametrize("k", [2, 31, 32, 33, 64, 65, 97, 256, 300, 700, 1100, 2500])
+@pytest.mark.parametrize("starts,bidirectional", BUCKETS)
+def test_relative_bias_gradient_of_unseen_keys(k, starts, bidirectional):
+    # keys that are not seen are terms of +0, unlike those that are not there: a -0 before them does not stay
+    print(f"relbias masked {k} keys {len(starts)} starts bidirectional={bidirectional}", flush=True)
+    rng = np.random.default_rng(9)
+    for masks in (dict(causal=True), dict(window=max(1, k // 3)), dict(k_len=k - 1), dict(causal=True, window=20, k_len=k // 2 + 1)):
+        dp = tiny_rows(64, k, 10).reshape(1, 8, 8, k)
+        p = np.where((rng.random(dp.shape) < 0.5) & (dp == 0), 0, ONE).astype(np.uint16)
+        for pos in sorted({0, k // 2, k - 1}):
+            got, want = relative_bias_backward(p, dp, starts, bidirectional, pos, **masks)
+            assert_bits(got[0], want[0], "dscores")
+            assert_bits(got[1], want[1], "dtable")
