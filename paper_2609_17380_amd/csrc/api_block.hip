@@ -296,21 +296,17 @@ RelBiasArgs args_of(const canon_attn_rows* r, const canon_relbias* bias, const u
   memcpy(a.start, bias->start, sizeof(int32_t) * (size_t)bias->n_starts);
   for (int n = 0, d = 0; n < a.n_side; ++n)
     for (const int end = n + 1 < a.n_side ? a.start[n + 1] : a.start[n] + 1; d < end; ++d) a.bucket[d] = (uint8_t)n;
-  // buckets without an end, or of more than kRelShort distances
   const int far = a.start[a.n_side - 1];
   a.far_only = !a.bidirectional || far >= 32;  // 32: no chunk of 32 keys has keys of both last buckets
-  for (int side = 0; side < (bias->bidirectional ? 2 : 1); ++side)
-    for (int n = 0; n < a.n_side; ++n) {
-      const bool last = n == a.n_side - 1;
-      const int many = last ? 0 : a.start[n + 1] - a.start[n];
-      const bool open = last || (!bias->bidirectional && a.start[n] == 0 && a.start[n + 1] > 0 && !a.causal);
-      if (open || many > kRelShort) {
-        a.longs[a.n_long++] = (uint8_t)(side * a.n_side + n);
-        if (!last) a.far_only = 0;
-      } else if (many > a.short_most) {
-        a.short_most = many;
-      }
+  for (int k = 0; k < a.n_side * (a.bidirectional ? 2 : 1); ++k) {
+    const RelKeys keys = relbias_keys(a, k);
+    if (keys.short_one()) {
+      a.short_most = keys.hi - keys.lo > a.short_most ? keys.hi - keys.lo : a.short_most;
+    } else {
+      a.longs[a.n_long++] = (uint8_t)k;
+      if (k % a.n_side != a.n_side - 1) a.far_only = 0;
     }
+  }
   return a;
 }
 

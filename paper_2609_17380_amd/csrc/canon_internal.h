@@ -251,18 +251,31 @@ hipError_t column_fold_launch(int64_t rows, int64_t cols, int64_t inner, const f
 // relbias.hip: attention rows with a learned relative position bias (R22)
 constexpr int kRelStarts = 128;     // buckets on one side
 constexpr int kRelFar = 1024;       // the last bucket's first distance
-constexpr int kRelShort = 32;       // a bucket of up to this many distances is summed by one lane
+constexpr int kRelShort = 32;       // a bucket of up to this many keys is summed by a pair of lanes
+constexpr int kRelFarPos = 1 << 20; // beyond every key's distance and the last bucket
 struct RelBiasArgs {
   int64_t batch, heads, q_len, k_len, ld, q_start, window;
   const int32_t *q_starts, *q_lens, *k_lens;
   const uint16_t* table;  // [buckets][heads]
   float scale;
   int32_t causal, n_side, bidirectional, n_long;
-  int32_t far_only, short_most;   // whether those are the last bucket(s) alone; the most distances of the others
+  int32_t far_only, short_most;   // whether those are the last bucket(s) alone; the most keys of the others
   int32_t start[kRelStarts];
-  uint8_t longs[2 * kRelStarts];  // the buckets of more than kRelShort distances
+  uint8_t longs[2 * kRelStarts];  // the buckets of more than kRelShort keys
   uint8_t bucket[kRelFar + 1];    // of the distances up to the last bucket's first, on one side
 };
+// The keys of bucket k, less the query's position: lo <= . < hi.  Host and kernel both tell by it which buckets are short.
+struct RelKeys {
+  int lo, hi;
+  __host__ __device__ bool short_one() const { return hi - lo <= kRelShort; }
+};
+__host__ __device__ inline RelKeys relbias_keys(const RelBiasArgs& a, int k) {
+  const int side = k < a.n_side ? k : k - a.n_side;
+  const int d0 = a.start[side], d1 = side + 1 < a.n_side ? a.start[side + 1] : 2 * kRelFarPos;
+  if (k >= a.n_side) return RelKeys{d0 > 0 ? d0 : 1, d1};  // after the query: distance 0 is before it
+  // a key after the query counts as distance 0 where the buckets have one side
+  return RelKeys{1 - d1, d0 == d1 ? 1 - d1 : d0 == 0 && !a.bidirectional && !a.causal ? 2 * kRelFarPos : 1 - d0};
+}
 hipError_t relbias_fwd_launch(const RelBiasArgs& a, const float* scores, uint16_t* probs, hipStream_t s);
 // rowsum: scratch of relbias_scratch_floats floats, unused where dtable is null
 int64_t relbias_scratch_floats(int64_t rows, int64_t heads, int64_t buckets);

@@ -15,7 +15,6 @@ namespace canon {
 
 namespace {
 
-constexpr int64_t kFarPos = 1 << 20;     // beyond every key's distance and the last bucket
 constexpr int64_t kMaxBlocks = 1 << 20;  // of up to 1024 threads: 2^30 of 2^32
 
 // bucket of a distance on one side: the last one that begins at or before it
@@ -35,7 +34,7 @@ __host__ __device__ inline int relbias_right(const RelBiasArgs& a) {
   return a.bidirectional ? (far > 0 ? far : 1) : 0;
 }
 
-// The keys j0 <= j < j1 that query i of sequence b sees (none behind the last query), and its position (cut to +-kFarPos,
+// The keys j0 <= j < j1 that query i of sequence b sees (none behind the last query), and its position (cut to +-kRelFarPos,
 // which leaves every bucket as it is).
 struct Query {
   int j0, j1, pos;
@@ -54,7 +53,7 @@ __device__ __forceinline__ Query query_of(const RelBiasArgs& a, int64_t b, int64
   Query q;
   q.j0 = __builtin_amdgcn_readfirstlane((int)lo);
   q.j1 = __builtin_amdgcn_readfirstlane((int)hi);
-  q.pos = __builtin_amdgcn_readfirstlane((int)(pos < -kFarPos ? -kFarPos : pos > kFarPos ? kFarPos : pos));
+  q.pos = __builtin_amdgcn_readfirstlane((int)(pos < -kRelFarPos ? -kRelFarPos : pos > kRelFarPos ? kRelFarPos : pos));
   return q;
 }
 
@@ -239,15 +238,9 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
   At at = load(dealt(0));
   if (rowsum) {
     for (int k = threadIdx.x; k < nb; k += blockDim.x) {
-      const int side = k < a.n_side ? k : k - a.n_side;
-      const int d0 = a.start[side], d1 = side + 1 < a.n_side ? a.start[side + 1] : 2 * (int)kFarPos;
-      if (k < a.n_side) {
-        lo_[k] = 1 - d1;
-        hi_[k] = d0 == d1 ? 1 - d1 : d0 == 0 && !a.bidirectional && !a.causal ? 2 * (int)kFarPos : 1 - d0;
-      } else {
-        lo_[k] = d0 > 0 ? d0 : 1;
-        hi_[k] = d1;
-      }
+      const RelKeys keys = relbias_keys(a, k);
+      lo_[k] = keys.lo;
+      hi_[k] = keys.hi;
     }
     __syncthreads();
   }
@@ -315,11 +308,12 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
     const int keys = use((int)a.k_len);
     for (int k2 = NW == 1 ? lane : (int)threadIdx.x; k2 < 2 * nb; k2 += NW == 1 ? 64 : (int)blockDim.x) {
       const int k = k2 >> 1, lo = lo_[k], hi = hi_[k];
+      const bool pair = RelKeys{lo, hi}.short_one();
       const int b0 = qy.pos + lo > qy.j0 ? qy.pos + lo : qy.j0, b1 = qy.pos + hi < qy.j1 ? qy.pos + hi : qy.j1;
       const int mid = (b0 | 31) + 1;  // the next chunk's first key
       const int c0 = k2 & 1 ? mid : b0, c1 = k2 & 1 || b1 < mid ? b1 : mid;
       float sum = 0.0f;
-      if (c0 < c1 && hi - lo <= kRelShort) {
+      if (c0 < c1 && pair) {
         const float* t = &st[NW == 1 ? w : c0 / (256 * Q)].t[(c0 >> 5) & (8 * Q - 1)][c0 & 31];
         const uint32_t mine = 0xFFFFFFFFu >> (32 - (c1 - c0));  // a bit for each of its keys
         for (int j = 0; j < a.short_most && j < c1 - c0; j += 4) {  // up to three places behind the chunk's end: its row's padding
@@ -344,7 +338,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
           if (mid > kChunk) sum = sum + 0.0f;
         }
       }
-      if (!(k2 & 1) && hi - lo <= kRelShort) out[k] = sum;
+      if (!(k2 & 1) && pair) out[k] = sum;
     }
     if (a.far_only) {
       // the last bucket(s) alone are long: the keys nearer than them give way to +0, and a lane's chunk is one bucket's
