@@ -17,17 +17,6 @@ namespace {
 
 constexpr int64_t kMaxBlocks = 1 << 20;  // of up to 1024 threads: 2^30 of 2^32
 
-// bucket of a distance on one side: the last one that begins at or before it
-__device__ __forceinline__ int bucket_of(const int32_t* start, int n, int d) {
-  int lo = 0, hi = n;  // start[lo] <= d < start[hi]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (start[mid] <= d) lo = mid;
-    else hi = mid;
-  }
-  return lo;
-}
-
 // distances after the query that the bias table holds: up to the last bucket's, one at least
 __host__ __device__ inline int relbias_right(const RelBiasArgs& a) {
   const int far = a.start[a.n_side - 1];
