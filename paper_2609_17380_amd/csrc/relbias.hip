@@ -7,6 +7,8 @@
 // the last bucket's first, are laid out in LDS while the row is on its way.  Bound: HBM.
 #include <hip/hip_runtime.h>
 
+#include <atomic>
+
 #include "canon_dev.h"
 #include "canon_internal.h"
 #include "rows_dev.h"
@@ -175,9 +177,10 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
 // two chunks, whose chains two lanes run and add (their sum is the fold whatever lies between); a longer one is summed
 // chunk by chunk, a lane to a chunk, like the row.
 // 16 x 2048 x 2048 causal 68 us, and 10 for the sums over the rows (336 MB: 70.5), without the table's gradient 70; 16 x 16 x
-// 512 115 (71), without 83: there the buckets' sums, about 180 vector instructions to a row of at most 512 keys, bound it.
+// 512 110 (71), without 75: there the buckets' sums, about 190 vector instructions to a row of at most 512 keys, take most of the
+// difference (119 with seven workgroups to a CU, as the registers of a kernel without a bound let in, and eight launched).
 template <int Q, int NW, bool TAIL>
-__global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbias_bwd_kernel(
+__global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : Q == 2 ? 8 : 1) void relbias_bwd_kernel(
     RelBiasArgs a, uint32_t heads, uint32_t units, uint32_t per_head, const uint16_t* __restrict__ probs,
     const float* __restrict__ dprobs, uint16_t* __restrict__ dscores, float* __restrict__ rowsum) {
   constexpr int kRows = NW == 1 ? 4 : 1;
@@ -447,6 +450,28 @@ hipError_t relbias_fwd_launch(const RelBiasArgs& a, const float* scores, uint16_
   return hipGetLastError();
 }
 
+// Workgroups of the backward that are on the chip at once.  Rows are dealt to all that are launched, so one that has to wait
+// for another to end runs its share when the chip is nearly empty: with 8 to a CU where the LDS of two wavefronts' rows lets 7
+// in, 16 x 4096 x 4096 took 354 us, so 288; 4 x 16 x 1000 x 1000 88 and 82; 16 x 512 x 10000 152 and 129.  Asked of the runtime
+// once per kernel, workgroup size and device.
+template <int Q, int NW, bool TAIL>
+static hipError_t relbias_resident(int threads, int64_t& groups) {
+  static std::atomic<int> known[64][17];
+  int dev = 0, per_cu = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  const bool keep = dev >= 0 && dev < 64;
+  if (keep) per_cu = known[dev][threads / 64].load(std::memory_order_relaxed);
+  if (per_cu == 0) {
+    e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, relbias_bwd_kernel<Q, NW, TAIL>, threads, 0);
+    if (e != hipSuccess) return e;
+    if (per_cu < 1) per_cu = 1;
+    if (keep) known[dev][threads / 64].store(per_cu, std::memory_order_relaxed);
+  }
+  groups = device_cus() * per_cu;
+  return hipSuccess;
+}
+
 int64_t relbias_scratch_floats(int64_t rows, int64_t heads, int64_t buckets) {
   return (rows + (rows + kChunk - 1) / kChunk) * heads * buckets;
 }
@@ -457,14 +482,18 @@ hipError_t relbias_bwd_launch(const RelBiasArgs& a, const uint16_t* probs, const
   const int64_t matrices = a.batch * a.heads, per_head = shape.groups(a.q_len);
   const bool empty = matrices * per_head == 0 || a.k_len == 0;
   if (!empty) {
-    // no more workgroups than are on the chip at once (16 wavefronts to a CU of 8 vectors, 32 of fewer)
-    const int64_t units = matrices * per_head, most = device_cus() * ((shape.q == 8 ? 16 : 32) * 64 / shape.threads());
-    const dim3 grid((unsigned)(units < most ? units : most)), wg(shape.threads());
+    const int64_t units = matrices * per_head;
+    const dim3 wg(shape.threads());
+    int64_t most = 0;
     const bool tail = a.k_len % 4 != 0;
     float* rs = dtable ? rowsum : nullptr;
-#define CANON_REL_K(Q, NW, TAIL)                                                                                  \
-  hipLaunchKernelGGL((relbias_bwd_kernel<Q, NW, TAIL>), grid, wg, 0, s, a, (uint32_t)a.heads, (uint32_t)units, \
-                     (uint32_t)per_head, probs, dprobs, dscores, rs)
+#define CANON_REL_K(Q, NW, TAIL)                                                                                        \
+  do {                                                                                                                  \
+    hipError_t e = relbias_resident<Q, NW, TAIL>(shape.threads(), most);                                                \
+    if (e != hipSuccess) return e;                                                                                      \
+    hipLaunchKernelGGL((relbias_bwd_kernel<Q, NW, TAIL>), dim3((unsigned)(units < most ? units : most)), wg, 0, s, a,   \
+                       (uint32_t)a.heads, (uint32_t)units, (uint32_t)per_head, probs, dprobs, dscores, rs);             \
+  } while (0)
 #define CANON_REL(Q, NW)                   \
   do {                                     \
     if (tail) CANON_REL_K(Q, NW, true);    \
