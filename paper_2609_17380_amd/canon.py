@@ -545,7 +545,7 @@ def relbias_log(n_buckets, max_distance, bidirectional=False) -> RelBias:
 
 class AttnRows(ctypes.Structure):
     """The rows of attention [batch][n_heads][q_len][ld >= k_len] and the keys that each sees; q_starts, q_lens and k_lens
-    are int32 device tensors [batch] or None."""
+    are int32 device tensors [batch] or None.  A matrix of such rows may end with the last one's k_len keys."""
     _fields_ = [(n, ctypes.c_int64) for n in ("batch", "n_heads", "q_len", "k_len", "ld", "q_start", "window")] + \
                [("causal", ctypes.c_int32), ("scale", ctypes.c_float)] + \
                [(n, ctypes.c_void_p) for n in ("q_starts", "q_lens", "k_lens")]
@@ -566,8 +566,11 @@ class AttnRows(ctypes.Structure):
         return ctypes.byref(self)
 
     def _matrix(self, t, what, dtypes, dev):
-        """A matrix of these rows: all of them, `ld` apart."""
-        return _arg(t, what, self.batch * self.n_heads * self.q_len * (self.ld or self.k_len), dtypes, dev)
+        """A matrix of these rows: all of them, `ld` apart; what would follow the last one's keys may be absent."""
+        rows, ld = self.batch * self.n_heads * self.q_len, self.ld or self.k_len
+        least = (rows - 1) * ld + self.k_len if rows > 0 else 0
+        short = isinstance(t, torch.Tensor) and t.numel() == least
+        return _arg(t, what, least if short else rows * ld, dtypes, dev)
 
 
 def softmax_relbias(rows: AttnRows, bias: RelBias, table, scores, probs, order=ORDER_V1, stream=None):
