@@ -23,7 +23,7 @@ unsigned tile_blocks(int64_t tiles) {
 }
 
 // Steps and codes: a group's largest magnitude is joined over the 8 to 64 lanes that hold it, the tile's four vectors a step
-// at a time.  8192 x 8192 fp32 80 us: 337 MB moved, 4.2 TB/s; 33 x 2048 4.4 us, a launch and one load's latency.
+// at a time.  8192 x 8192 fp32 80 us: 337 MB moved, 4.2 TB/s; 33 x 2048 4.5 us, a launch and one load's latency.
 template <int SRC, bool TAIL>
 __global__ __launch_bounds__(256) void act8_pack_kernel(int64_t rows, int64_t cols, int64_t tiles, ActIn x, ActKeep k) {
   const int lane = threadIdx.x & 63;
@@ -46,7 +46,7 @@ __global__ __launch_bounds__(256) void act8_pack_kernel(int64_t rows, int64_t co
   }
 }
 
-// The values again: 66 us for the same 337 MB, 5.1 TB/s.
+// The values again: 65 us for the same 337 MB, 5.2 TB/s.
 template <bool BF16, bool TAIL>
 __global__ __launch_bounds__(256) void act8_unpack_kernel(int64_t rows, int64_t cols, int64_t tiles, ActIn k,
                                                           void* __restrict__ out) {
@@ -119,7 +119,7 @@ __global__ __launch_bounds__(256) void swiglu_keep_kernel(int64_t T, int64_t F, 
 }
 
 // its gradient: du = bf16(RN(da silu(g))), dg = bf16(RN(RN(da u) dsg)), dsg = RN(sig RN(1 + RN(g RN(1 - sig)))); with a
-// the activation again (the same values' forward).  8192 x 8192 from 8 bits with the activation: 142 us for 809 MB, 5.7 TB/s.
+// the activation again (the same values' forward).  8192 x 8192 from 8 bits with the activation: 141 us for 809 MB, 5.7 TB/s.
 template <int SRC, bool TAIL>
 __global__ __launch_bounds__(256) void swiglu_grad_kernel(int64_t T, int64_t F, int64_t tiles, ActIn gu,
                                                           const float* __restrict__ da, uint16_t* __restrict__ dgu,

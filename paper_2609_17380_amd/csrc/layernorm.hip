@@ -201,9 +201,9 @@ __device__ __forceinline__ void load_columns(const ActIn& x, const float* dy, in
 }
 
 // The chains of 32 rows of dgain[k] = R1 over rows of RN(dy xh) and dbias[k] = R1 over rows of dy, a column to a thread, B
-// rows in flight.  part: [2][chunks][cols].  1023 x 5001 from 8 bits 10 us: 32 dependent steps to a chain, 32 chains to a
-// column.  (Four columns to a thread are fewer, wider loads and were never faster: 8192 x 2048 with dx 69 us, so 64.5; 1023 x
-// 5001 bf16 32 and 23.)
+// rows in flight.  part: [2][chunks][cols].  1023 x 5001 from 8 bits 10 us: a chain's 32 rows are four batches of loads, each
+// waited for.  (Four columns to a thread are fewer, wider loads and were never faster: 8192 x 2048 with dx 69 us, so 64.5;
+// 1023 x 5001 bf16 32 and 23.)
 template <int SRC, int B>
 __global__ __launch_bounds__(256) void layernorm_part_kernel(int64_t rows, int cols, ActIn x, const float* __restrict__ mean,
                                                              const float* __restrict__ rstd, const float* __restrict__ dy,
@@ -490,8 +490,9 @@ hipError_t layernorm_bwd_launch(int64_t rows, int64_t cols, const ActIn& x, cons
   const float inv_d = (float)(1.0 / (double)cols);
   const int64_t nc = (rows + kChunk - 1) / kChunk;
   // One pass over x and dy where its workgroups, one to 32 rows, are half as many as the CUs or more, and its wavefronts four
-  // to a CU (4096 x 8192 in 103 us, in two passes 128; 8192 x 2048 48 and 64.5; 4096 x 2048 31 and 32; of 2048 x 8192 86 and
-  // 63.5, 4096 x 1001 29 and 21, 8192 x 512 20 and 19.5).
+  // to a CU (4096 x 8192 in 103 us, in two passes 128; 8192 x 2048 47 and 65; 4096 x 2048 30.5 and 32; 8192 x 1024 27 and 32; of
+  // 2048 x 8192 86 and 63.5, 4096 x 1001 29 and 21, 8192 x 512 20 and 19.5).  fp32 rows of up to 1024 columns that four does not
+  // divide lose by it, 8192 x 1001 39 and 34, 16384 x 511 44 and 41, which bf16 and 8 bits do not: 25 and 30, 29 and 36.
   const bool once = (dgain || dbias) && cols >= 4 && cols <= kPassCols && 2 * nc >= device_cus() &&
                     nc * ((cols + 255) / 256 < 16 ? (cols + 255) / 256 : 16) >= 4 * device_cus();
   if (once) {

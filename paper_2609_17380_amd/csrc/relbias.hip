@@ -68,9 +68,9 @@ __device__ __forceinline__ Part part_of(const Query& q, int seg, int n) {
 }
 
 // 16 x 2048 x 2048 causal 70 us (the 268 MB that it cannot do without take 56 at a large copy's rate), in both directions 92
-// (85); a padded batch of 4 x 8 x 1001 x 1001 37.6 (26), where vector instructions, 26 of a canonical exponential among the
-// 40 to a score, take 61% of the cycles.  With the next row loaded ahead and a matrix's biases laid out once for many rows
-// the padded batch took 40: fewer rows at a time.
+// (85); a padded batch of 4 x 8 x 1001 x 1001 37.8 (26), where vector instructions, 26 of a canonical exponential among the
+// 40 to a score, take 61% of the cycles: more than anything else, but no bound.  With the next row loaded ahead and a matrix's
+// biases laid out once for many rows the padded batch took 40: fewer rows at a time.
 template <int Q, int NW, bool TAIL>
 __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbias_fwd_kernel(
     RelBiasArgs a, uint32_t heads, uint32_t matrices, uint32_t per_head, const float* __restrict__ scores,
@@ -173,9 +173,10 @@ __global__ __launch_bounds__(NW == 1 ? 256 : 64 * NW, Q == 8 ? 4 : 1) void relbi
 }
 
 // ds = RN(P RN(dP - D)), D = R1 over the keys of RN(P dP); dS = bf16(RN(ds scale)).  rowsum [batch][q_len][heads][buckets]:
-// for every bucket R1 over the keys of ds, those outside it as +0 terms.  A bucket of up to 32 distances touches at most
-// two chunks, whose chains two lanes run and add (their sum is the fold whatever lies between); a longer one is summed
-// chunk by chunk, a lane to a chunk, like the row.
+// for every bucket R1 over the keys of ds, those outside it as +0 terms.  A bucket of up to 32 keys touches at most two
+// chunks, whose chains two lanes run and add (their sum is the fold whatever lies between); a longer one is summed chunk by
+// chunk, a lane to a chunk, like the row: 16 x 2048 x 2048 causal with 32 buckets up to 256 85 us, up to 1024 115; in both
+// directions (537 MB: 113) up to 128 113, 256 132, 1024 149.
 // 16 x 2048 x 2048 causal 68 us, and 10 for the sums over the rows (336 MB: 70.5), without the table's gradient 70; 16 x 16 x
 // 512 110 (71), without 75: there the buckets' sums, about 190 vector instructions to a row of at most 512 keys, take most of the
 // difference (119 with seven workgroups to a CU, as the registers of a kernel without a bound let in, and eight launched).

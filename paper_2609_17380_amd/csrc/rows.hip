@@ -596,8 +596,8 @@ __global__ __launch_bounds__(256) void softmax_causal_kernel(int64_t rows, int64
 
 // Rows held in registers, read from memory once (cols <= 256 Q, Q = 8 or 16).  A wavefront's vectors q are each wholly
 // outside the visible keys j0 .. i (+0 terms, no work), wholly inside (no masks) or on an edge.  Bound: the reads of
-// the visible scores and the writes of every probability, 268 MB at 16 heads x 2048: 56 us (59 with the sum folded by
-// shuffles; masks on every term 84); 4 heads x 4096: 56 us (98).
+// the visible scores and the writes of every probability, 268 MB at 16 heads x 2048: 54 us of 20 in a graph (the sum folded
+// by shuffles 56 beside it; masks on every term 84); 4 heads x 4096: 56 us (58; 98).
 template <int Q, bool TAIL>
 __global__ __launch_bounds__(256) void softmax_causal_reg_kernel(int64_t rows, int64_t cols,
                                                                  const float* __restrict__ raw, float scale,
