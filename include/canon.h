@@ -8,7 +8,7 @@
  *     with Algorithm 2 (binary-carry tree fold) across replicas, the ascending-shard reduce-scatter order
  *     and averages taken as reciprocal multiplies (appendix "Deterministic Gradient Reduction");
  *   - AdamW is widened to fp32 and rounded to bf16 once (training recipe, optimizer-state precision).
- * The order itself (rules R0-R22, "CANON-v1") is stated with each entry point below.
+ * The order itself (rules R0-R26, "CANON-v1") is stated with each entry point below.
  *
  * Conventions for every entry point:
  *   - Tensor pointers are DEVICE memory owned by the caller.  bf16 tensors are uint16_t bit patterns.
@@ -521,6 +521,132 @@ canon_status canon_softmax_relbias_bwd(const canon_order* order, const canon_att
                                        const uint16_t* probs, const float* dprobs, uint16_t* dscores, float* dtable,
                                        void* workspace, size_t workspace_bytes, void* stream);
 size_t canon_softmax_relbias_bwd_workspace_bytes(const canon_attn_rows* rows, const canon_relbias* bias);
+
+/* ------------------------------------------------------------------------------------------------ */
+/* Products in int8 with a step for every token and every channel (R23): the projections of a model trained with 8-bit
+   weights when it answers, where the activations' step is taken from each token instead of learned for the tensor.
+     canon_quant_tokens: x [rows][cols], fp32 (CANON_F32) or bf16 (CANON_BF16): steps[r] (fp32 [rows]) = RN(amax * RN(1/127)),
+       amax the row's largest |value| by bit pattern (a NaN ranks above every number), codes (int8 [rows][cols]) =
+       clamp(rne(RN(x / step)), -128, 127) as canon_quantize; so a row with an infinity or a NaN has the codes 0 and a step
+       that makes its products NaN.  rows up to 2^31, cols up to 65536 (else CANON_EUNSUPPORTED).
+     canon_gemm_i8_tokens: acc[i][j] = sum_k a[i][k] * b[j][k] exactly, a int8 [m][k] (leading dimension lda), b int8 [n][k]
+       (ldb; one channel per row, as weights [out][in]); y[i][j] = RN(RN(RN32(acc) * sa[i]) * sb[j]), fp32 or (rounded once
+       more) bf16 by y_dtype, leading dimension ldc.  sa fp32 [m], sb fp32 [n].  k in [0, 65536] keeps |acc| < 2^31;
+       m n up to 2^32.
+   Both take any alignment that the types allow and refuse outputs that overlap an input or each other (CANON_EINVAL), as
+   every entry point of the four groups here does.  The straight-through gradients of such a product are those of
+   canon_qlinear_bwd where the tensor has one step. */
+canon_status canon_quant_tokens(int64_t rows, int64_t cols, int32_t in_dtype, const void* x, int8_t* codes, float* steps,
+                                void* stream);
+canon_status canon_gemm_i8_tokens(int64_t m, int64_t n, int64_t k, const int8_t* a, int64_t lda, const float* sa,
+                                  const int8_t* b, int64_t ldb, const float* sb, int32_t y_dtype, void* y, int64_t ldc,
+                                  void* stream);
+
+/* ------------------------------------------------------------------------------------------------ */
+/* Rotary positions (R24).  A rotation turns the pairs of the first rot_dim elements of a head (even, at most head_dim; the
+   others are kept) by the angles of the token's position: element i with i + rot_dim / 2 (interleaved = 0, R8's halves) or
+   2 i with 2 i + 1 (interleaved = 1), i < rot_dim / 2.  cos and sin: device fp32 [positions][rot_dim / 2].  With
+   (a, b) = (x of the first, x of the second), forward (backward = 0): (RN(RN(a c) - RN(b s)), RN(RN(b c) + RN(a s)));
+   backward, the gradient of x from that of y: (RN(RN(a c) + RN(b s)), RN(RN(b c) - RN(a s))).  Kept elements stay as they
+   are (a subnormal reads as zero).  A position outside [0, positions) makes the turned elements NaN.
+     canon_rope: x and y [tokens][n_heads][head_dim], each token's heads together and tokens x_stride (y_stride) elements
+       apart (>= n_heads * head_dim), so that both may be parts of wider rows; fp32 or bf16 each, y rounded once.  positions:
+       device int32 [tokens], or NULL: token t is at position t.  y may be x itself (same type and stride); any other
+       overlap returns CANON_EINVAL.  head_dim up to 1024, n_heads up to 2^20, tokens * n_heads * head_dim up to 2^40.
+     canon_rope_tables (host only): fills host arrays cos and sin [positions][rot_dim / 2] for the positions first, first +
+       1, ...: pair i has the frequency w_i = theta^(-2 i / rot_dim), scaled for contexts longer than those trained on:
+         CANON_ROPE_PLAIN    w_i (scaling may be NULL)
+         CANON_ROPE_LINEAR   w_i / factor: positions squeezed into the trained range
+         CANON_ROPE_BASE     theta * factor^(rot_dim / (rot_dim - 2)) in place of theta: the lowest frequency divided by
+                             factor, the highest kept (rot_dim > 2)
+         CANON_ROPE_BANDS    by how many turns n_i = context w_i / (2 pi) a pair makes in the trained context: w_i / factor
+                             where n_i <= low, w_i where n_i >= high, between them w_i (g + (1 - g) / factor) with
+                             g = (n_i - low) / (high - low)
+       amplitude multiplies both tables (1: a rotation; 0 is taken as 1).  Evaluated in binary64 and rounded once.
+       factor >= 1, 0 <= low < high, context > 0, theta > 0, first >= 0; |first| + positions up to 2^31. */
+typedef struct {
+  int32_t rot_dim, interleaved;
+  int64_t positions;
+  const float *cos, *sin;
+} canon_rotation;
+enum { CANON_ROPE_PLAIN = 0, CANON_ROPE_LINEAR = 1, CANON_ROPE_BASE = 2, CANON_ROPE_BANDS = 3 };
+typedef struct {
+  int32_t kind;
+  double factor, low, high, context, amplitude;
+} canon_rope_scaling;
+canon_status canon_rope_tables(int32_t rot_dim, double theta, const canon_rope_scaling* scaling, int64_t first,
+                               int64_t positions, float* cos, float* sin);
+canon_status canon_rope(int32_t backward, int64_t tokens, int64_t n_heads, int64_t head_dim, const canon_rotation* rotation,
+                        const int32_t* positions, int32_t x_dtype, const void* x, int64_t x_stride, int32_t y_dtype, void* y,
+                        int64_t y_stride, void* stream);
+
+/* ------------------------------------------------------------------------------------------------ */
+/* A paged cache of keys and values in 8 bits (R25).  Its memory is n_pages pages of `page` tokens (16, 32, 64, 128 or 256);
+   token j of sequence b lies in page table[b][j / page] at slot j % page.  Each head of a token is kept as codes and a step
+   of its own, by the rule of canon_quant_tokens over head_dim elements (so that what is kept of a token depends on that token
+   alone):
+     k_codes int8 [n_pages][n_kv_heads][page][head_dim]
+     v_codes int8 [n_pages][n_kv_heads][page / 16][head_dim][16]: 16 tokens of an element together, as the product of
+             weights and values reads them
+     k_steps, v_steps fp32 [n_pages][n_kv_heads][page], not negative
+     table   device int32 [batch][table_len]
+   codes and steps 16-byte aligned.  head_dim a multiple of 32 up to 256, batch and n_kv_heads up to 65535, n_pages * n_kv_heads *
+   page * head_dim up to 2^44 (else CANON_EUNSUPPORTED).  The struct is read during the call.
+   Rows: query or new token i < q_len (up to 2^27; batch * q_len * n_kv_heads * head_dim up to 2^33) of sequence b is at position q_start + i, or q_starts[b] + i; with q_lens only the
+   first q_lens[b] exist (device int32 [batch], each may be NULL; any values).
+     canon_cache_append: k and v [batch * q_len][n_kv_heads][head_dim], tokens k_stride (v_stride) elements apart, both fp32
+       or both bf16.  rotation (may be NULL): k is turned first (R24, to fp32, kept from that value) at its token's
+       position.  A token at a position below 0 or at or behind table_len * page, or in a page that the cache does not have
+       (an entry of the table outside [0, n_pages)), is left out; every other slot stays as it was.  Two tokens of one call
+       in the same slot (sequences that share a page) leave either in it.
+     canon_cache_read: what is kept of the same rows, k and v [batch * q_len][n_kv_heads][head_dim], fp32 RN(step * code) or
+       (rounded once more) bf16, either may be NULL; rows that do not exist are +0, tokens that append would leave out NaN. */
+typedef struct {
+  int64_t n_pages, page, n_kv_heads, head_dim;
+  int8_t *k_codes, *v_codes;
+  float *k_steps, *v_steps;
+  int64_t batch, table_len;
+  const int32_t* table;
+} canon_kv_cache;
+typedef struct {
+  int64_t q_len, q_start;
+  const int32_t *q_starts, *q_lens;
+} canon_cache_rows;
+canon_status canon_cache_append(const canon_kv_cache* cache, const canon_cache_rows* rows, int32_t in_dtype, const void* k,
+                                int64_t k_stride, const void* v, int64_t v_stride, const canon_rotation* rotation,
+                                void* stream);
+canon_status canon_cache_read(const canon_kv_cache* cache, const canon_cache_rows* rows, int32_t out_dtype, void* k, void* v,
+                              void* stream);
+
+/* Attention over such a cache (R26).  rows as for canon_softmax_relbias (batch that of the cache, ld 0): query i sees the
+   keys j < k_len <= table_len * page with j < k_lens[b], j <= pos (if causal), |pos - j| < window (if window > 0), and none
+   if i >= q_lens[b].  q [batch * q_len][n_heads][head_dim], tokens q_stride elements apart, fp32 or bf16, turned already;
+   query head h reads key/value head h / (n_heads / n_kv_heads).  out (bf16 [batch * q_len][n_heads * head_dim]) = the sum of
+   the values weighted by 2^(z - max z), z = scale log2(e) q.k, over the sum of the weights.  The rule takes every long sum in
+   integers, which no order changes, and what remains by tiles of 256 keys (key j is in tile j / 256):
+     query:  sq = RN(amax * RN(1/32512)), rs = CRdiv(1, sq), Q = clamp(rne(RN(q rs)), -32512, 32512) (0 for a NaN or a step
+             that is not > 0), f = RN(RN(sq scale) * RN(log2 e))
+     scores: t_j = RN(RN(RN32(sum_d Q_d K_jd) f) kstep_j), the sum exact
+     tile:   r = ceil(max t_j), e_j = cexp2(RN(t_j - r)) (r read as 0 where it is -inf), S_b = the 16 sums of 16 consecutive
+             keys' e, each a chain from +0, joined by a perfect pairwise tree; keys that are not seen are +0 terms
+             V = the largest vstep of the keys that are seen, by bit pattern, rv = CRdiv(32512, V) (0 if V is not > 0 or rv is
+             infinite), w_j = rne(RN(e_j RN(vstep_j rv))) (0 for all where rv = 0), A_d = sum_j w_j V_jd, exact
+     row:    over the tiles with a key that is seen, ascending, from R = -inf, S = 0, O = 0: R' = max(R, r),
+             x = 2^(R - R'), y = 2^(r - R') (1 where R, or r, is -inf; 0 below 2^-126), S = fma(S_b, y, RN(S x)),
+             O_d = fma(RN32(A_d), RN(RN(V * RN(1/32512)) y), RN(O_d x))
+     out:    bf16(RN(RN(O_d + 0) CRdiv(1, S))), +0 where S = 0 (no key seen, or only scores of -inf)
+   cexp2(x) of x <= 0: n = rne(max(x, -127)), p = 1 + u (C1 + u (C2 + u (C3 + u (C4 + u C5)))) by fma with u = x - n, RN(p 2^n),
+   0 for n = -127.  A query's row is the same in a prompt and alone, whatever the batch and the other sequences are.  Queries and
+   weights enter with 16 bits (two digits of 8): a part of 2^-16 of the largest, below the last place of bf16.  What stands
+   in places that are not seen (in unused slots, pages and table entries too) is not used; a key that is seen in a page that the
+   cache does not have makes the row NaN.
+   k_len up to 2^21, batch * n_heads * q_len below 2^24 (else CANON_EUNSUPPORTED), window >= 0, |q_start| up to 2^30.
+   workspace: device memory of canon_cache_attention_workspace_bytes(cache, rows) bytes, 256-byte aligned; 0 where none is
+   needed. */
+canon_status canon_cache_attention(const canon_order* order, const canon_kv_cache* cache, const canon_attn_rows* rows,
+                                   int32_t q_dtype, const void* q, int64_t q_stride, uint16_t* out, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+size_t canon_cache_attention_workspace_bytes(const canon_kv_cache* cache, const canon_attn_rows* rows);
 
 /* Device evaluation of the R0/R4 primitives, element by element, for testing the device math against
    the oracle: op 0 add, 1 sub, 2 mul, 3 fma(a,b,c), 4 div, 5 sqrt, 6 cexp, 7 clog, 8 sigmoid, 9 silu,

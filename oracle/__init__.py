@@ -5,7 +5,7 @@ TEST INFRASTRUCTURE.  Only ``tests/``, ``__graft_entry__.smoke()`` and the
 (the GPU library and its binding) never imports it, and it never imports the
 product path; the only shared code is the seeded input generator.
 
-Thin ctypes binding over ``liboracle.so`` (plain C, ``canon_ref.c`` and ``block_ref.c``).  Arrays
+Thin ctypes binding over ``liboracle.so`` (plain C, ``canon_ref.c``, ``block_ref.c`` and ``serve_ref.c``).  Arrays
 are numpy; bf16 tensors are uint16 bit patterns.
 """
 from __future__ import annotations
@@ -17,7 +17,7 @@ import subprocess
 import numpy as np
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
-_SRCS = [os.path.join(_HERE, "canon_ref.c"), os.path.join(_HERE, "block_ref.c")]
+_SRCS = [os.path.join(_HERE, "canon_ref.c"), os.path.join(_HERE, "block_ref.c"), os.path.join(_HERE, "serve_ref.c")]
 _LIB = os.path.join(_HERE, "liboracle.so")
 _lib = None
 
@@ -106,6 +106,11 @@ def _load():
             "cref_layernorm_bwd": (ctypes.c_int, [i64, i64, vp, vp, vp, vp, vp, vp, vp, vp]),
             "cref_relbias_fwd": (ctypes.c_int, [vp, i64, i32, vp, f, vp, vp, vp, vp, vp, vp]),
             "cref_relbias_bwd": (ctypes.c_int, [vp, i64, i32, vp, f, vp, vp, vp, vp, vp, vp, vp]),
+            "cref_gemm_i8_tokens": (ctypes.c_int, [i64, i64, i64, vp, vp, vp, vp, vp]),
+            "cref_rope": (ctypes.c_int, [i32, i64, i64, i64, i64, i32, i64, vp, vp, vp, vp, vp]),
+            "cref_cache_append": (ctypes.c_int, [vp, vp, i64, vp, vp, vp, vp, i64, i32, i64, vp, vp, vp, vp, vp, vp]),
+            "cref_exp2_neg": (ctypes.c_int, [i64, vp, vp]),
+            "cref_cache_attention": (ctypes.c_int, [vp, vp, f, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]),
             "cref_num_threads": (ctypes.c_int, []),
             "cref_set_threads": (None, [ctypes.c_int]),
         }
@@ -526,3 +531,70 @@ def relbias_bwd(probs, dprobs, starts, bidirectional=False, causal=True, window=
     dt = np.empty((len(starts) * (2 if bidirectional else 1), probs.shape[1]), dtype=np.float32)
     _check(_load().cref_relbias_bwd(*args, _p(probs), _p(dprobs), _p(ds), _p(dt)))
     return ds, dt
+
+
+def gemm_i8_tokens(a: np.ndarray, sa: np.ndarray, b: np.ndarray, sb: np.ndarray) -> np.ndarray:
+    """R23: fp32 [m, n] of int8 a [m, k] with steps sa [m] and b [n, k] with steps sb [n]."""
+    a, b = np.ascontiguousarray(a, dtype=np.int8), np.ascontiguousarray(b, dtype=np.int8)
+    sa, sb = np.ascontiguousarray(sa, dtype=np.float32), np.ascontiguousarray(sb, dtype=np.float32)
+    (m, k), n = a.shape, b.shape[0]
+    y = np.empty((m, n), np.float32)
+    _check(_load().cref_gemm_i8_tokens(m, n, k, _p(a), _p(sa), _p(b), _p(sb), _p(y)))
+    return y
+
+
+def rope(x: np.ndarray, positions: np.ndarray, cos: np.ndarray, sin: np.ndarray, rot: int, interleaved=False,
+         backward=False) -> np.ndarray:
+    """R24: fp32 heads [tokens, heads, dim] turned (or, backward, their gradient)."""
+    x = np.ascontiguousarray(x, dtype=np.float32)
+    positions = np.ascontiguousarray(positions, dtype=np.int32)
+    cos, sin = np.ascontiguousarray(cos, dtype=np.float32), np.ascontiguousarray(sin, dtype=np.float32)
+    tokens, heads, dim = x.shape
+    y = np.empty_like(x)
+    _check(_load().cref_rope(int(backward), tokens, heads, dim, rot, int(interleaved), cos.shape[0], _p(cos), _p(sin),
+                             _p(positions), _p(x), _p(y)))
+    return y
+
+
+class KVCache:
+    """R25: a paged cache on the host; table int32 [batch, table_len].  Slots that nothing was written to hold what
+    `codes` and `steps` say."""
+
+    def __init__(self, n_pages, page, kv_heads, dim, table, codes=0, steps=0.0):
+        self.table = np.ascontiguousarray(table, dtype=np.int32)
+        self.dims = np.array([n_pages, page, kv_heads, dim, *self.table.shape], dtype=np.int64)
+        self.k_codes = np.full((n_pages, kv_heads, page, dim), codes, np.int8)
+        self.v_codes = np.full((n_pages, kv_heads, page // 16, dim, 16), codes, np.int8)
+        self.k_steps, self.v_steps = (np.full((n_pages, kv_heads, page), steps, np.float32) for _ in range(2))
+
+    def arrays(self):
+        return self.k_codes, self.v_codes, self.k_steps, self.v_steps
+
+    def append(self, k, v, q_starts, q_lens, cos=None, sin=None, rot=0, interleaved=False):
+        """k, v fp32 [batch, q_len, kv_heads, dim]."""
+        k, v = np.ascontiguousarray(k, dtype=np.float32), np.ascontiguousarray(v, dtype=np.float32)
+        starts, lens = np.ascontiguousarray(q_starts, dtype=np.int32), np.ascontiguousarray(q_lens, dtype=np.int32)
+        c, s = (np.ascontiguousarray(t if rot else np.zeros((1, 1)), dtype=np.float32) for t in (cos, sin))
+        _check(_load().cref_cache_append(_p(self.dims), _p(self.table), k.shape[1], _p(starts), _p(lens), _p(k), _p(v), rot,
+                                         int(interleaved), c.shape[0], _p(c), _p(s), _p(self.k_codes), _p(self.v_codes),
+                                         _p(self.k_steps), _p(self.v_steps)))
+
+    def attention(self, q, k_len, scale, q_starts, q_lens, k_lens, causal=True, window=0) -> np.ndarray:
+        """R26: bf16 bits [batch, q_len, heads, dim] of fp32 queries of that shape."""
+        q = np.ascontiguousarray(q, dtype=np.float32)
+        _, q_len, heads, _ = q.shape
+        starts, ql, kl = (np.ascontiguousarray(a, dtype=np.int32) for a in (q_starts, q_lens, k_lens))
+        cfg = np.array([heads, q_len, k_len, window, int(causal)], dtype=np.int64)
+        out = np.empty(q.shape, np.uint16)
+        _check(_load().cref_cache_attention(_p(self.dims), _p(cfg), np.float32(scale), _p(self.table), _p(starts), _p(ql),
+                                            _p(kl), _p(self.k_codes), _p(self.v_codes), _p(self.k_steps), _p(self.v_steps),
+                                            _p(q), _p(out)))
+        return out
+
+
+def exp2_neg(x: np.ndarray) -> np.ndarray:
+    """R26's cexp2 of x <= 0."""
+    x = np.ascontiguousarray(x, dtype=np.float32)
+    y = np.empty_like(x)
+    _check(_load().cref_exp2_neg(x.size, _p(x), _p(y)))
+    return y

@@ -209,6 +209,21 @@ int cref_relbias_bwd(const int64_t* cfg, int64_t n_starts, int32_t bidirectional
                      const int32_t* q_starts, const int32_t* q_lens, const int32_t* k_lens, const uint16_t* probs,
                      const float* dprobs, uint16_t* dscores, float* dtable);
 
+/* ---- products with a step per token, rotary positions, a paged cache in 8 bits and attention over it (serve_ref.c) ---- */
+int cref_gemm_i8_tokens(int64_t m, int64_t n, int64_t k, const int8_t* a, const float* sa, const int8_t* b, const float* sb,
+                        float* y);
+int cref_rope(int32_t backward, int64_t tokens, int64_t heads, int64_t dim, int64_t rot, int32_t interleaved,
+              int64_t positions, const float* c, const float* s, const int32_t* pos, const float* x, float* y);
+/* cache: n_pages, page, kv heads, dim, batch, table_len; q_starts, q_lens, k_lens [batch] */
+int cref_cache_append(const int64_t* cache, const int32_t* table, int64_t q_len, const int32_t* q_starts,
+                      const int32_t* q_lens, const float* k, const float* v, int64_t rot, int32_t interleaved,
+                      int64_t positions, const float* c, const float* s, int8_t* kc, int8_t* vc, float* ks, float* vs);
+int cref_exp2_neg(int64_t n, const float* x, float* y);
+/* cfg: heads, q_len, k_len, window, causal */
+int cref_cache_attention(const int64_t* cache, const int64_t* cfg, float scale, const int32_t* table,
+                         const int32_t* q_starts, const int32_t* q_lens, const int32_t* k_lens, const int8_t* kc,
+                         const int8_t* vc, const float* ks, const float* vs, const float* q, uint16_t* out);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,192 @@
+/*
+ * serve_ref.c - CPU oracle of what a model answers with: products of int8 codes with a step per token (R23), rotary
+ * positions (R24), a paged cache of keys and values in 8 bits (R25) and attention over it (R26).
+ *
+ * TEST INFRASTRUCTURE, as canon_ref.c, whose R0 operations it uses.  Integer sums are written in 64 bits, one term at a time.
+ */
+#include <math.h>
+#include <stdlib.h>
+#include <string.h>
+
+#include "canon_ref.h"
+
+static float of_bits(uint32_t u) { float f; memcpy(&f, &u, 4); return f; }
+static uint32_t to_bits(float f) { uint32_t u; memcpy(&u, &f, 4); return u; }
+static float flushed(float x) { return cref_mul(x, 1.0f); }
+
+int cref_gemm_i8_tokens(int64_t m, int64_t n, int64_t k, const int8_t* a, const float* sa, const int8_t* b, const float* sb,
+                        float* y) {
+#pragma omp parallel for schedule(static)
+  for (int64_t i = 0; i < m; ++i)
+    for (int64_t j = 0; j < n; ++j) {
+      int64_t acc = 0;
+      for (int64_t l = 0; l < k; ++l) acc += (int64_t)a[i * k + l] * b[j * k + l];
+      y[i * n + j] = cref_mul(cref_mul((float)acc, sa[i]), sb[j]);
+    }
+  return 0;
+}
+
+/* one head, in and out of place */
+static void turn(int64_t dim, int64_t rot, int32_t interleaved, int32_t backward, const float* c, const float* s,
+                 const float* x, float* y) {
+  for (int64_t d = rot; d < dim; ++d) y[d] = flushed(x[d]);
+  for (int64_t i = 0; i < rot / 2; ++i) {
+    const int64_t p = interleaved ? 2 * i : i, q = interleaved ? 2 * i + 1 : i + rot / 2;
+    const float a = x[p], b = x[q];
+    if (!c) {
+      y[p] = y[q] = NAN;
+    } else if (!backward) {
+      y[p] = cref_sub(cref_mul(a, c[i]), cref_mul(b, s[i]));
+      y[q] = cref_add(cref_mul(b, c[i]), cref_mul(a, s[i]));
+    } else {
+      y[p] = cref_add(cref_mul(a, c[i]), cref_mul(b, s[i]));
+      y[q] = cref_sub(cref_mul(b, c[i]), cref_mul(a, s[i]));
+    }
+  }
+}
+
+int cref_rope(int32_t backward, int64_t tokens, int64_t heads, int64_t dim, int64_t rot, int32_t interleaved,
+              int64_t positions, const float* c, const float* s, const int32_t* pos, const float* x, float* y) {
+  for (int64_t t = 0; t < tokens; ++t)
+    for (int64_t h = 0; h < heads; ++h) {
+      const int64_t at = (t * heads + h) * dim;
+      const int in = pos[t] >= 0 && pos[t] < positions;
+      turn(dim, rot, interleaved, backward, in ? c + pos[t] * (rot / 2) : NULL, in ? s + pos[t] * (rot / 2) : NULL, x + at,
+           y + at);
+    }
+  return 0;
+}
+
+/* cache: n_pages, page, kv heads, dim, batch, table_len */
+static int64_t slot_of(const int64_t* cache, const int32_t* table, int64_t b, int64_t h, int64_t j) {
+  if (j < 0 || j >= cache[5] * cache[1]) return -1;
+  const int64_t p = table[b * cache[5] + j / cache[1]];
+  return p < 0 || p >= cache[0] ? -1 : (p * cache[2] + h) * cache[1] + j % cache[1];
+}
+static int64_t v_at(const int64_t* cache, int64_t slot, int64_t d) {
+  return slot / 16 * 16 * cache[3] + d * 16 + slot % 16;
+}
+
+int cref_cache_append(const int64_t* cache, const int32_t* table, int64_t q_len, const int32_t* q_starts,
+                      const int32_t* q_lens, const float* k, const float* v, int64_t rot, int32_t interleaved,
+                      int64_t positions, const float* c, const float* s, int8_t* kc, int8_t* vc, float* ks, float* vs) {
+  const int64_t H = cache[2], D = cache[3];
+  for (int64_t b = 0; b < cache[4]; ++b)
+    for (int64_t i = 0; i < q_len && i < q_lens[b]; ++i)
+      for (int64_t h = 0; h < H; ++h) {
+        const int64_t pos = (int64_t)q_starts[b] + i, slot = slot_of(cache, table, b, h, pos);
+        if (slot < 0) continue;
+        const float *kr = k + ((b * q_len + i) * H + h) * D, *vr = v + ((b * q_len + i) * H + h) * D;
+        float turned[256];
+        int8_t code[256];
+        if (rot) {
+          const int in = pos >= 0 && pos < positions;
+          turn(D, rot, interleaved, 0, in ? c + pos * (rot / 2) : NULL, in ? s + pos * (rot / 2) : NULL, kr, turned);
+          kr = turned;
+        }
+        cref_act8_pack(1, D, (int32_t)D, kr, kc + slot * D, ks + slot);
+        cref_act8_pack(1, D, (int32_t)D, vr, code, vs + slot);
+        for (int64_t d = 0; d < D; ++d) vc[v_at(cache, slot, d)] = code[d];
+      }
+  return 0;
+}
+
+static float exp2_neg(float x) { /* R26's cexp2, x <= 0 or NaN */
+  if (x != x) return x;
+  const float at = x > -127.0f ? x : -127.0f;
+  const float n = rintf(at), u = cref_sub(at, n);
+  float p = of_bits(0x3AADDD09u);
+  p = cref_fma(p, u, of_bits(0x3C1E7544u));
+  p = cref_fma(p, u, of_bits(0x3D635BA9u));
+  p = cref_fma(p, u, of_bits(0x3E75FCDEu));
+  p = cref_fma(p, u, of_bits(0x3F317215u));
+  p = cref_fma(p, u, 1.0f);
+  return n == -127.0f ? 0.0f : cref_mul(p, ldexpf(1.0f, (int)n));
+}
+int cref_exp2_neg(int64_t n, const float* x, float* y) {
+  for (int64_t i = 0; i < n; ++i) y[i] = exp2_neg(x[i]);
+  return 0;
+}
+
+/* 2^(a - b) of whole a <= b */
+static float shift(float a, float b) {
+  if (a == -INFINITY) return 1.0f;
+  const float x = cref_sub(a, b);
+  return x != x ? x : x < -126.0f ? 0.0f : ldexpf(1.0f, (int)x);
+}
+
+/* cfg: heads, q_len, k_len, window, causal */
+int cref_cache_attention(const int64_t* cache, const int64_t* cfg, float scale, const int32_t* table,
+                         const int32_t* q_starts, const int32_t* q_lens, const int32_t* k_lens, const int8_t* kc,
+                         const int8_t* vc, const float* ks, const float* vs, const float* q, uint16_t* out) {
+  const int64_t B = cache[4], KV = cache[2], D = cache[3], H = cfg[0], QL = cfg[1], KL = cfg[2], W = cfg[3];
+  const float inv = of_bits(0x38010204u); /* RN32(1/32512) */
+#pragma omp parallel for schedule(dynamic, 4)
+  for (int64_t r = 0; r < B * QL * H; ++r) {
+    const int64_t h = r % H, i = r / H % QL, b = r / H / QL, kvh = h / (H / KV);
+    const int64_t pos = (int64_t)q_starts[b] + i;
+    const float* x = q + r * D;
+    int64_t Q[256];
+    uint32_t top = 0;
+    for (int64_t d = 0; d < D; ++d) {
+      const uint32_t u = to_bits(x[d]) & 0x7FFFFFFFu;
+      if (u > top) top = u;
+    }
+    const float sq = cref_mul(of_bits(top), inv), rs = sq > 0.0f ? cref_div(1.0f, sq) : 0.0f;
+    for (int64_t d = 0; d < D; ++d) {
+      const float v = cref_mul(x[d], rs);
+      Q[d] = !(sq > 0.0f) || v != v ? 0 : v > 32512.0f ? 32512 : v < -32512.0f ? -32512 : (int64_t)rintf(v);
+    }
+    const float f = cref_mul(cref_mul(sq, scale), of_bits(0x3FB8AA3Bu)); /* RN32(1 / ln 2) */
+    float R = -INFINITY, S = 0.0f, O[256];
+    for (int64_t d = 0; d < D; ++d) O[d] = 0.0f;
+    for (int64_t j0 = 0; j0 < KL; j0 += 256) {
+      float t[256], e[256], m = -INFINITY;
+      int8_t sees[256];
+      int64_t slot[256], any = 0;
+      uint32_t vtop = 0;
+      for (int64_t j = 0; j < 256; ++j) {
+        const int64_t key = j0 + j;
+        sees[j] = key < KL && key < k_lens[b] && i < q_lens[b] && !(cfg[4] && key > pos) &&
+                  !(W && (pos - key >= W || key - pos >= W));
+        if (!sees[j]) continue;
+        any = 1;
+        slot[j] = slot_of(cache, table, b, kvh, key);
+        int64_t acc = 0;
+        for (int64_t d = 0; slot[j] >= 0 && d < D; ++d) acc += Q[d] * kc[slot[j] * D + d];
+        t[j] = slot[j] < 0 ? NAN : cref_mul(cref_mul((float)acc, f), ks[slot[j]]);
+        if (t[j] > m) m = t[j];
+        const uint32_t u = slot[j] < 0 ? 0x7FC00000u : to_bits(vs[slot[j]]) & 0x7FFFFFFFu;
+        if (u > vtop) vtop = u;
+      }
+      if (!any) continue;
+      const float rb = ceilf(m), V = of_bits(vtop);
+      for (int64_t j = 0; j < 256; ++j) e[j] = sees[j] ? exp2_neg(cref_sub(t[j], rb == -INFINITY ? 0.0f : rb)) : 0.0f;
+      float part[16];
+      for (int c = 0; c < 16; ++c) {
+        part[c] = 0.0f;
+        for (int j = 0; j < 16; ++j) part[c] = cref_add(part[c], e[16 * c + j]);
+      }
+      for (int n = 16; n > 1; n /= 2)
+        for (int c = 0; c < n / 2; ++c) part[c] = cref_add(part[2 * c], part[2 * c + 1]);
+      float rv = V > 0.0f ? cref_div(32512.0f, V) : 0.0f;
+      if (!(rv < INFINITY)) rv = 0.0f;
+      const float Rn = R > rb ? R : rb, xo = shift(R, Rn), y = shift(rb, Rn);
+      const float scale_v = cref_mul(cref_mul(V, inv), y);
+      S = cref_fma(part[0], y, cref_mul(S, xo));
+      for (int64_t d = 0; d < D; ++d) {
+        int64_t A = 0;
+        for (int64_t j = 0; j < 256; ++j)
+          if (sees[j] && rv != 0.0f && slot[j] >= 0) {
+            const float w = cref_mul(e[j], cref_mul(vs[slot[j]], rv));
+            A += (w != w ? 0 : (int64_t)rintf(w)) * vc[v_at(cache, slot[j], d)];
+          }
+        O[d] = cref_fma((float)A, scale_v, cref_mul(O[d], xo));
+      }
+      R = Rn;
+    }
+    const float is = S == 0.0f ? 0.0f : cref_div(1.0f, S);
+    for (int64_t d = 0; d < D; ++d) out[r * D + d] = S == 0.0f ? 0 : cref_bf16(cref_mul(cref_add(O[d], 0.0f), is));
+  }
+  return 0;
+}

@@ -126,6 +126,14 @@ def _lib():
             "canon_softmax_relbias": (i32, [vp, vp, vp, vp, vp, vp, vp]),
             "canon_softmax_relbias_bwd": (i32, [vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
             "canon_softmax_relbias_bwd_workspace_bytes": (sz, [vp, vp]),
+            "canon_quant_tokens": (i32, [i64, i64, i32, vp, vp, vp, vp]),
+            "canon_gemm_i8_tokens": (i32, [i64, i64, i64, vp, i64, vp, vp, i64, vp, i32, vp, i64, vp]),
+            "canon_rope_tables": (i32, [i32, ctypes.c_double, vp, i64, i64, vp, vp]),
+            "canon_rope": (i32, [i32, i64, i64, i64, vp, vp, i32, vp, i64, i32, vp, i64, vp]),
+            "canon_cache_append": (i32, [vp, vp, i32, vp, i64, vp, i64, vp, vp]),
+            "canon_cache_read": (i32, [vp, vp, i32, vp, vp, vp]),
+            "canon_cache_attention": (i32, [vp, vp, vp, i32, vp, i64, vp, vp, sz, vp]),
+            "canon_cache_attention_workspace_bytes": (sz, [vp, vp]),
             "canon_status_str": (ctypes.c_char_p, [i32]),
             "canon_version": (i32, []),
         }
@@ -598,6 +606,199 @@ def softmax_relbias_bwd(rows: AttnRows, bias: RelBias, probs, dprobs, dscores, w
                                             rows._matrix(dscores, "dscores", _T16, dev),
                                             _arg(dtable, "dtable", bias.buckets * rows.n_heads, _T32, dev), ws, ws_bytes,
                                             _stream_on(stream, dev)), "canon_softmax_relbias_bwd")
+
+
+# ---- products in int8 with a step per token, rotary positions, a paged cache in 8 bits and attention over it ------
+#
+# As above, these calls check their arguments.  Tokens' heads may be part of wider rows: a tensor [tokens, heads * dim] (or
+# [tokens, heads, dim]) whose rows are apart, each row's elements together.
+
+
+def _rows(t, what, rows, width, dtypes, dev):
+    """(address, elements from a row to the next) of `rows` rows of `width` elements."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes:
+        raise ValueError(f"{what}: a tensor of {' or '.join(map(str, dtypes))} is needed")
+    if t.get_device() != dev:
+        raise ValueError(f"{what}: a tensor on the current device is needed, not on {t.device}")
+    if t.numel() == rows * width and t.is_contiguous():
+        return t.data_ptr(), width
+    if t.dim() >= 2 and t.shape[0] == rows and t.numel() == rows * width and (rows == 0 or t[0].is_contiguous()):
+        return t.data_ptr(), t.stride(0) if rows > 1 else width
+    raise ValueError(f"{what}: {rows} rows of {width} elements are needed, each contiguous, not {tuple(t.shape)} of strides "
+                     f"{t.stride()}")
+
+
+def _lead(ld, least, rows, t, what, dtypes, dev):
+    """The address of a matrix of `rows` rows, `ld` (at least `least`) elements apart; the last may end with its elements."""
+    if ld < least:
+        raise ValueError(f"{what}: rows of {least} elements do not fit a leading dimension of {ld}")
+    short = (rows - 1) * ld + least if rows > 0 else 0
+    if isinstance(t, torch.Tensor) and t.numel() == short:
+        return _arg(t, what, short, dtypes, dev)
+    return _arg(t, what, rows * ld, dtypes, dev)
+
+
+def quant_tokens(rows, cols, x, codes, steps, stream=None):
+    """codes (int8 [rows, cols]) and steps (fp32 [rows]) of x: a step of its own for every row."""
+    dev = _device()
+    px = _arg(x, "x", rows * cols, _TF, dev)
+    _check(_lib().canon_quant_tokens(rows, cols, _DTYPES[x.dtype], px, _arg(codes, "codes", rows * cols, _TI8, dev),
+                                     _arg(steps, "steps", rows, _T32, dev), _stream_on(stream, dev)), "canon_quant_tokens")
+
+
+def gemm_i8_tokens(m, n, k, a, lda, sa, b, ldb, sb, y, ldc=None, stream=None):
+    """y = (a . b) sa sb: a int8 [m, k] with steps sa [m], b int8 [n, k] with steps sb [n], y fp32 or bf16 [m, n]."""
+    dev = _device()
+    ldc = n if ldc is None else ldc
+    if not isinstance(y, torch.Tensor) or y.dtype not in _TF:
+        raise ValueError("y: a tensor of torch.float32 or torch.bfloat16 is needed")
+    _check(_lib().canon_gemm_i8_tokens(m, n, k, _lead(lda, k, m, a, "a", _TI8, dev), lda, _arg(sa, "sa", m, _T32, dev),
+                                       _lead(ldb, k, n, b, "b", _TI8, dev), ldb, _arg(sb, "sb", n, _T32, dev), _DTYPES[y.dtype],
+                                       _lead(ldc, n, m, y, "y", _TF, dev), ldc, _stream_on(stream, dev)), "canon_gemm_i8_tokens")
+
+
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_BANDS = 0, 1, 2, 3
+
+
+class RopeScaling(ctypes.Structure):
+    """How a rotation's frequencies are scaled for contexts longer than those trained on (canon_rope_tables)."""
+    _fields_ = [("kind", ctypes.c_int32)] + [(n, ctypes.c_double) for n in ("factor", "low", "high", "context", "amplitude")]
+
+    def __init__(self, kind=ROPE_PLAIN, factor=1.0, low=0.0, high=1.0, context=1.0, amplitude=1.0):
+        super().__init__(kind, factor, low, high, context, amplitude)
+
+
+def rope_tables(rot_dim, positions, theta=5e5, scaling: RopeScaling | None = None, first=0):
+    """(cos, sin) on the host, fp32 [positions, rot_dim / 2]."""
+    cos, sin = (torch.empty(max(positions, 0), max(rot_dim, 0) // 2, dtype=torch.float32) for _ in range(2))
+    _check(_lib().canon_rope_tables(rot_dim, theta, None if scaling is None else ctypes.byref(scaling), first, positions,
+                                    cos.data_ptr(), sin.data_ptr()), "canon_rope_tables")
+    return cos, sin
+
+
+class Rotation(ctypes.Structure):
+    """The turns of the first rot_dim elements of a head: cos and sin fp32 [positions, rot_dim / 2] on the device; halves of
+    those elements together, or (interleaved) neighbours."""
+    _fields_ = [("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("positions", ctypes.c_int64),
+                ("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p)]
+
+    def __init__(self, cos, sin, rot_dim, interleaved=False):
+        if not isinstance(cos, torch.Tensor) or not isinstance(sin, torch.Tensor):
+            raise ValueError("cos and sin: tensors are needed")
+        half = max(rot_dim // 2, 1)
+        if cos.numel() % half or cos.numel() != sin.numel():
+            raise ValueError(f"cos and sin: [positions, {rot_dim // 2}] are needed, not {tuple(cos.shape)} and {tuple(sin.shape)}")
+        self.tensors = cos, sin
+        super().__init__(rot_dim, int(interleaved), cos.numel() // half if rot_dim > 0 else 0, None, None)
+
+    def _of(self, dev):
+        """The record's address, once its tables are on the current device."""
+        n = self.tensors[0].numel()
+        self.cos = _arg(self.tensors[0], "cos", n, _T32, dev)
+        self.sin = _arg(self.tensors[1], "sin", n, _T32, dev)
+        return ctypes.byref(self)
+
+
+def rope(tokens, heads, dim, rotation: Rotation, x, y, positions=None, backward=False, stream=None):
+    """y = the heads of x [tokens, heads * dim] turned at their tokens' positions (int32 [tokens]; None: token t at t), or,
+    backward, the gradient of x from that of y.  y may be x."""
+    dev = _device()
+    px, xs = _rows(x, "x", tokens, heads * dim, _TF, dev)
+    py, ys = _rows(y, "y", tokens, heads * dim, _TF, dev)
+    _check(_lib().canon_rope(int(backward), tokens, heads, dim, rotation._of(dev), _arg(positions, "positions", tokens, _TI32, dev),
+                             _DTYPES[x.dtype], px, xs, _DTYPES[y.dtype], py, ys, _stream_on(stream, dev)), "canon_rope")
+
+
+class KVCache(ctypes.Structure):
+    """A paged cache of keys and values in 8 bits: k_codes int8 [pages, kv_heads, page, dim], v_codes int8 [pages, kv_heads,
+    page / 16, dim, 16], k_steps and v_steps fp32 [pages, kv_heads, page], table int32 [batch, table_len]."""
+    _fields_ = [(n, ctypes.c_int64) for n in ("n_pages", "page", "n_kv_heads", "head_dim")] + \
+               [(n, ctypes.c_void_p) for n in ("k_codes", "v_codes", "k_steps", "v_steps")] + \
+               [("batch", ctypes.c_int64), ("table_len", ctypes.c_int64), ("table", ctypes.c_void_p)]
+
+    def __init__(self, page, kv_heads, dim, k_codes, v_codes, k_steps, v_steps, table):
+        self.tensors = k_codes, v_codes, k_steps, v_steps
+        if not all(isinstance(t, torch.Tensor) for t in (*self.tensors, table)):
+            raise ValueError("codes, steps and table: tensors are needed")
+        one = page * kv_heads * dim
+        if page < 1 or kv_heads < 1 or dim < 1 or k_codes.numel() % one:
+            raise ValueError(f"k_codes: pages of {one} codes are needed")
+        super().__init__(k_codes.numel() // one, page, kv_heads, dim)
+        self.set_table(table)
+
+    def set_table(self, table):
+        """The pages of other sequences, or more of the same ones'."""
+        if not isinstance(table, torch.Tensor) or table.dim() != 2:
+            raise ValueError("table: a tensor [batch, table_len] is needed")
+        self.pages = table
+        self.batch, self.table_len = table.shape
+
+    def _of(self, dev):
+        """The record's address, once its tensors are a cache's on the current device."""
+        steps = self.n_pages * self.page * self.n_kv_heads
+        for name, t, n, dtypes in zip(("k_codes", "v_codes", "k_steps", "v_steps"), self.tensors,
+                                      (steps * self.head_dim,) * 2 + (steps,) * 2, (_TI8, _TI8, _T32, _T32)):
+            setattr(self, name, _arg(t, name, n, dtypes, dev))
+        self.table = _arg(self.pages, "table", self.batch * self.table_len, _TI32, dev)
+        return ctypes.byref(self)
+
+
+class CacheRows(ctypes.Structure):
+    """New tokens [batch][q_len] of a cache's sequences: token i at position q_start + i or q_starts[b] + i, the first q_lens[b]
+    of them real (int32 device tensors [batch] or None)."""
+    _fields_ = [("q_len", ctypes.c_int64), ("q_start", ctypes.c_int64), ("q_starts", ctypes.c_void_p), ("q_lens", ctypes.c_void_p)]
+
+    def __init__(self, batch, q_len, q_start=0, q_starts=None, q_lens=None):
+        self.batch = batch
+        self.tensors = q_starts, q_lens
+        super().__init__(q_len, q_start)
+
+    def _of(self, cache, dev):
+        """The record's address, once its tensors are those of the cache's sequences on the current device."""
+        if self.batch != cache.batch:
+            raise ValueError(f"rows of {self.batch} sequences, a cache's table of {cache.batch}")
+        self.q_starts = _arg(self.tensors[0], "q_starts", self.batch, _TI32, dev)
+        self.q_lens = _arg(self.tensors[1], "q_lens", self.batch, _TI32, dev)
+        return ctypes.byref(self)
+
+
+def cache_append(cache: KVCache, rows: CacheRows, k, v, rotation: Rotation | None = None, stream=None):
+    """Keys (turned first by `rotation`, if given) and values [batch * q_len, kv_heads * dim] of new tokens into their pages."""
+    dev = _device()
+    n, width = cache.batch * rows.q_len, cache.n_kv_heads * cache.head_dim
+    pk, ks = _rows(k, "k", n, width, _TF, dev)
+    pv, vs = _rows(v, "v", n, width, (k.dtype,), dev)
+    _check(_lib().canon_cache_append(cache._of(dev), rows._of(cache, dev), _DTYPES[k.dtype], pk, ks, pv, vs,
+                                     None if rotation is None else rotation._of(dev), _stream_on(stream, dev)),
+           "canon_cache_append")
+
+
+def cache_read(cache: KVCache, rows: CacheRows, k=None, v=None, stream=None):
+    """What is kept of the tokens of `rows`, into k and v [batch * q_len, kv_heads * dim] (fp32 or bf16, both alike)."""
+    dev = _device()
+    n = cache.batch * rows.q_len * cache.n_kv_heads * cache.head_dim
+    some = k if k is not None else v
+    if not isinstance(some, torch.Tensor) or some.dtype not in _TF:
+        raise ValueError("k, v: a tensor of torch.float32 or torch.bfloat16 is needed")
+    one = (some.dtype,)
+    _check(_lib().canon_cache_read(cache._of(dev), rows._of(cache, dev), _DTYPES[some.dtype], _arg(k, "k", n, one, dev),
+                                   _arg(v, "v", n, one, dev), _stream_on(stream, dev)), "canon_cache_read")
+
+
+def cache_attention_workspace_bytes(cache: KVCache, rows: AttnRows) -> int:
+    dev = _device()
+    return int(_lib().canon_cache_attention_workspace_bytes(cache._of(dev), rows._of(dev)))
+
+
+def cache_attention(cache: KVCache, rows: AttnRows, q, out, workspace=None, order=ORDER_V1, stream=None):
+    """out (bf16 [batch * q_len, heads * dim]) = attention of the queries q [batch * q_len, heads * dim] over the cache."""
+    dev = _device()
+    n, width = rows.batch * rows.q_len, rows.n_heads * cache.head_dim
+    pq, qs = _rows(q, "q", n, width, _TF, dev)
+    ws, ws_bytes = _scratch(workspace, dev)
+    _check(_lib().canon_cache_attention(ctypes.byref(order), cache._of(dev), rows._of(dev), _DTYPES[q.dtype], pq, qs,
+                                        _arg(out, "out", n * width, _T16, dev), ws, ws_bytes, _stream_on(stream, dev)),
+           "canon_cache_attention")
 
 
 def version() -> int:

@@ -60,11 +60,13 @@ struct GemmI8Args {
   const int8_t* b;
   int32_t* acc;     // may be null
   float* y;         // may be null
-  const float* sa;  // device scalar (needed when y is set)
+  const float* sa;  // device scalar, or [m] (needed when y is set)
   const float* sb;  // device [n] (needed when y is set)
   int64_t m, n, k, lda, ldb, ldc;
   int32_t sb_scalar;  // 1: sb[0] for every column
   int32_t vec;        // set by the launcher
+  int32_t sa_rows;    // 1: sa[i] for row i
+  int32_t y_bf16;     // 1: y holds bf16
 };
 hipError_t gemm_i8_launch(const GemmI8Args& g, hipStream_t s);
 
@@ -281,5 +283,49 @@ hipError_t relbias_fwd_launch(const RelBiasArgs& a, const float* scores, uint16_
 int64_t relbias_scratch_floats(int64_t rows, int64_t heads, int64_t buckets);
 hipError_t relbias_bwd_launch(const RelBiasArgs& a, const uint16_t* probs, const float* dprobs, uint16_t* dscores,
                               float* dtable, float* rowsum, hipStream_t s);
+
+// ---- products with a step per token (gemm_i8.hip, gemm_i8_rows.hip) ----
+hipError_t quant_tokens_launch(int64_t rows, int64_t cols, int32_t bf16, const void* x, int8_t* codes, float* steps,
+                               hipStream_t s);
+constexpr bool gemm_i8_few_rows(int64_t m) { return m <= 64; }
+hipError_t gemm_i8_rows_launch(const GemmI8Args& g, hipStream_t s);  // of them
+
+// ---- rotary positions, the paged cache in 8 bits (rope.hip) and attention over it (attn_cache.hip) ----
+struct Turn {  // a rotation; rot 0: none
+  const float *cos, *sin;
+  int64_t positions;
+  int32_t rot, interleaved;
+};
+hipError_t rope_launch(int32_t backward, int64_t tokens, int64_t heads, int64_t dim, const Turn& turn, const int32_t* positions,
+                       int32_t x_bf16, const void* x, int64_t x_stride, int32_t y_bf16, void* y, int64_t y_stride,
+                       hipStream_t s);
+
+struct CacheView {
+  int8_t *kc, *vc;
+  float *ks, *vs;
+  const int32_t* table;
+  int64_t n_pages, table_len, batch;
+  int32_t lg, heads, dim;  // lg: log2 of a page's tokens
+};
+struct CacheRowsArgs {
+  int64_t q_len, q_start;
+  const int32_t *q_starts, *q_lens;
+};
+hipError_t cache_append_launch(const CacheView& c, const CacheRowsArgs& r, int32_t bf16, const void* k, int64_t k_stride,
+                               const void* v, int64_t v_stride, const Turn& turn, hipStream_t s);
+hipError_t cache_read_launch(const CacheView& c, const CacheRowsArgs& r, int32_t bf16, void* k, void* v, hipStream_t s);
+
+struct CacheAttnArgs {
+  CacheView c;
+  int64_t q_len, k_len, q_start, window, q_stride;
+  const int32_t *q_starts, *q_lens, *k_lens;
+  int32_t heads, causal, q_bf16;
+  float scale;
+  const void* q;
+  uint16_t* out;
+  float* parts;  // of the tiles, where the keys are split over workgroups
+};
+size_t cache_attention_workspace(const CacheAttnArgs& a);
+hipError_t cache_attention_launch(const CacheAttnArgs& a, hipStream_t s);
 
 }  // namespace canon

@@ -5,7 +5,8 @@
 // b holding one output column per row as weights [out][in] do).  Integer products and sums are exact, and
 // |acc| < 2^31 for k <= 65536, so every summation order gives the same int32: the k loop may be split,
 // reordered and spread over matrix instructions freely.  The dequantised output is
-// y[i][j] = RN(RN(RN32(acc) * sa) * sb[j]).
+// y[i][j] = RN(RN(RN32(acc) * sa) * sb[j]), with a step sa for the tensor or one for each row i, fp32 or rounded once more to
+// bf16.
 //
 // Tiling: whole 256 x 256 tiles (m, n multiples of 256, k of 64) run on 4 wavefronts, each a 128 x 128 block of
 // 4 x 4 v_mfma_i32_32x32x32_i8 instructions, with direct-to-LDS loads three stages ahead (gemm_i8_tile_kernel).
@@ -20,6 +21,7 @@
 
 #include <type_traits>
 
+#include "canon_dev.h"
 #include "canon_internal.h"
 
 namespace canon {
@@ -27,6 +29,10 @@ namespace canon {
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef int32_t i32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+struct __attribute__((packed, aligned(1))) I8x16 {
+  uint32_t x, y, z, w;
+};
 
 // Workgroup configuration: NW wavefronts in (NW / 2) x 2, wavefront (wr, wc) owning rows [32 HB wr, 32 HB (wr + 1))
 // and columns [32 WN wc, 32 WN (wc + 1)) of a BM x (64 WN) tile (HB x WN instruction blocks); stages of KS k bytes.
@@ -46,10 +52,15 @@ struct I8Raw {
   uint4 a[Cf::AV], b[Cf::BV];
 };
 
-// 16 consecutive bytes of which the first `valid` exist (zero fill beyond)
+// 16 consecutive bytes of which the first `valid` exist (zero fill beyond); rows off 16-byte boundaries load as wide (byte by
+// byte, 1541 x 5001 x 2056 took 1280 us)
 template <bool FAST>
-__device__ __forceinline__ uint4 ld16(const int8_t* p, int64_t valid, bool vec) {
-  if (FAST || (vec && valid >= 16)) return *reinterpret_cast<const uint4*>(p);
+__device__ __forceinline__ uint4 ld16(const int8_t* p, int64_t valid) {
+  if (FAST) return *reinterpret_cast<const uint4*>(p);
+  if (valid >= 16) {
+    const I8x16 v = *reinterpret_cast<const I8x16*>(p);
+    return make_uint4(v.x, v.y, v.z, v.w);
+  }
   uint32_t w[4] = {0u, 0u, 0u, 0u};
   for (int e = 0; e < 16; ++e)
     if (e < valid) w[e >> 2] |= (uint32_t)(uint8_t)p[e] << (8 * (e & 3));
@@ -67,13 +78,13 @@ __device__ __forceinline__ I8Raw<Cf> load_stage(const GemmI8Args& g, int64_t row
   for (int it = 0; it < Cf::AV; ++it) {
     const int idx = t + Cf::NT * it;
     const int64_t k = k0 + 16 * (idx % SEG), row = row0 + idx / SEG;
-    r.a[it] = ld16<FAST>(g.a + row * g.lda + k, (row < g.m) ? g.k - k : 0, g.vec);
+    r.a[it] = ld16<FAST>(g.a + row * g.lda + k, (row < g.m) ? g.k - k : 0);
   }
 #pragma unroll
   for (int it = 0; it < Cf::BV; ++it) {
     const int idx = t + Cf::NT * it;
     const int64_t k = k0 + 16 * (idx % SEG), col = col0 + idx / SEG;
-    r.b[it] = ld16<FAST>(g.b + col * g.ldb + k, (col < g.n) ? g.k - k : 0, g.vec);
+    r.b[it] = ld16<FAST>(g.b + col * g.ldb + k, (col < g.n) ? g.k - k : 0);
   }
   return r;
 }
@@ -164,7 +175,7 @@ __global__ __launch_bounds__(64 * NW) void gemm_i8_kernel(GemmI8Args g) {
   }
 
   // result layout: register v, lane l -> row (v % 4) + 4 (l / 32) + 8 (v / 4), column l % 32 of the block
-  const float sa = g.y ? *g.sa : 0.0f;
+  const float sa = g.y && !g.sa_rows ? *g.sa : 0.0f;
 #pragma unroll
   for (int h = 0; h < HB; ++h)
 #pragma unroll
@@ -178,8 +189,10 @@ __global__ __launch_bounds__(64 * NW) void gemm_i8_kernel(GemmI8Args g) {
           if (g.acc) g.acc[i * g.ldc + j] = a;
           if (g.y) {
             const float af = (float)a;  // round to nearest even
-            const float t = af * sa;
-            g.y[i * g.ldc + j] = t * g.sb[g.sb_scalar ? 0 : j];
+            const float t = af * (g.sa_rows ? g.sa[i] : sa);
+            const float y = t * g.sb[g.sb_scalar ? 0 : j];
+            if (g.y_bf16) reinterpret_cast<uint16_t*>(g.y)[i * g.ldc + j] = f32_to_bf16(y);
+            else g.y[i * g.ldc + j] = y;
           }
         }
       }
@@ -362,7 +375,7 @@ __global__ __launch_bounds__(64 * NW, 1) void gemm_i8_tile_kernel(GemmI8Args g) 
   const int c4 = 4 * (lane % LPR), rq = lane / LPR;  // this lane's 4 columns and row offset in the read-back
   float sa = 0.0f, sb4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
   if (g.y) {
-    sa = *g.sa;
+    if (!g.sa_rows) sa = *g.sa;
 #pragma unroll
     for (int e = 0; e < 4; ++e) sb4[e] = g.sb[g.sb_scalar ? 0 : wcol + c4 + e];
   }
@@ -378,12 +391,20 @@ __global__ __launch_bounds__(64 * NW, 1) void gemm_i8_tile_kernel(GemmI8Args g) 
       const i32x4 x = *reinterpret_cast<const i32x4*>(eb + r * ELD + c4);
       const int64_t o = (wrow + 32 * h + r) * g.ldc + wcol + c4;
       if (g.y) {  // streamed out: nontemporal
+        if (g.sa_rows) sa = g.sa[wrow + 32 * h + r];
         f32x4 y;
         y[0] = ((float)x[0] * sa) * sb4[0];  // RN(RN(RN32(acc) sa) sb), one rounding per operation
         y[1] = ((float)x[1] * sa) * sb4[1];
         y[2] = ((float)x[2] * sa) * sb4[2];
         y[3] = ((float)x[3] * sa) * sb4[3];
-        __builtin_nontemporal_store(y, reinterpret_cast<f32x4*>(g.y + o));
+        if (g.y_bf16) {
+          u32x2 y16;
+          y16[0] = pack_bf16(y[0], y[1]);
+          y16[1] = pack_bf16(y[2], y[3]);
+          __builtin_nontemporal_store(y16, reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(g.y) + o));
+        } else {
+          __builtin_nontemporal_store(y, reinterpret_cast<f32x4*>(g.y + o));
+        }
       }
       if (g.acc) __builtin_nontemporal_store(x, reinterpret_cast<i32x4*>(g.acc + o));
     }
@@ -408,6 +429,7 @@ static hipError_t launch_i8(const GemmI8Args& g, hipStream_t s) {
 
 hipError_t gemm_i8_launch(const GemmI8Args& gin, hipStream_t s) {
   if (gin.m == 0 || gin.n == 0) return hipSuccess;
+  if (gin.sa_rows && gemm_i8_few_rows(gin.m)) return gemm_i8_rows_launch(gin, s);
   GemmI8Args g = gin;
   g.vec = ((uintptr_t)g.a & 15) == 0 && ((uintptr_t)g.b & 15) == 0 && g.lda % 16 == 0 && g.ldb % 16 == 0;
   // 256 x 256 tiles of 8 wavefronts (one workgroup per CU, 64-byte stages) halve the operand bytes staged per

@@ -1,0 +1,249 @@
+// gemm_i8_rows.hip - activations into 8 bits with a step per token (R23), and the int8 product of a few tokens with weights.
+#include <hip/hip_runtime.h>
+
+#include "act8_dev.h"
+#include "canon_dev.h"
+#include "canon_internal.h"
+#include "rows_dev.h"
+
+namespace canon {
+
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+struct __attribute__((packed, aligned(1))) B16 {
+  uint32_t w[4];
+};
+
+// ---- a step per token -----------------------------------------------------------------------------------------------------
+// A workgroup holds a row in registers, Q vectors of four elements a thread (Q = 0: longer rows, read a second time): one pass
+// over memory, one join of the maximum between.
+template <bool XB, int NT, int Q>
+__global__ __launch_bounds__(NT) void quant_tokens_kernel(int64_t rows, int64_t cols, const void* __restrict__ x,
+                                                          int8_t* __restrict__ codes, float* __restrict__ steps) {
+  __shared__ uint32_t tops[NT / 64];
+  const int64_t r = blockIdx.x;
+  const int n = (int)cols;
+  auto load = [&](int j, float (&v)[4]) {
+    if constexpr (XB) {
+      const uint16_t* p = (const uint16_t*)x + r * cols + j;
+      if (j + 4 <= n) {
+        ldb<4>(p, v);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = j + e < n ? bf16_to_f32(p[e]) : 0.0f;
+      }
+    } else {
+      ldf4<true>((const float*)x + r * cols, j, cols, v);
+    }
+  };
+  auto top_of = [](const float (&v)[4], uint32_t m) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t u = __float_as_uint(v[e]) & 0x7FFFFFFFu;
+      m = u > m ? u : m;
+    }
+    return m;
+  };
+  float v[Q > 0 ? Q : 1][4];
+  uint32_t m = 0;
+  if constexpr (Q > 0) {
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const int j = 4 * (threadIdx.x + NT * q);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[q][e] = 0.0f;
+      if (j < n) load(j, v[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < Q; ++q) m = top_of(v[q], m);
+  } else {
+    for (int j = 4 * threadIdx.x; j < n; j += 4 * NT) {
+      load(j, v[0]);
+      m = top_of(v[0], m);
+    }
+  }
+  m = lanes_join(m, 64, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+  if constexpr (NT > 64) {
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = m;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NT / 64; ++i) m = tops[i] > m ? tops[i] : m;
+  }
+  const float s = __uint_as_float(m) * __uint_as_float(kInv127Bits);
+  if (threadIdx.x == 0) steps[r] = s;
+  const float rs = step_rcp(s);
+  const bool recip = recip_step_ok(s);
+  int8_t* out = codes + r * cols;
+  auto keep = [&](int j, const float (&f)[4]) {
+    uint32_t w[1];
+    quant_pack<4>(f, s, rs, recip, w);
+    if (j + 4 <= n) {
+      reinterpret_cast<B4*>(out + j)->x = w[0];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 3; ++e)
+        if (j + e < n) out[j + e] = (int8_t)(w[0] >> (8 * e));
+    }
+  };
+  if constexpr (Q > 0) {
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const int j = 4 * (threadIdx.x + NT * q);
+      if (j < n) keep(j, v[q]);
+    }
+  } else {
+    for (int j = 4 * threadIdx.x; j < n; j += 4 * NT) {
+      load(j, v[0]);
+      keep(j, v[0]);
+    }
+  }
+}
+
+template <bool XB>
+static hipError_t quant_go(int64_t rows, int64_t cols, const void* x, int8_t* codes, float* steps, hipStream_t s) {
+  // workgroups of a launch: below 2^32 threads
+  const int64_t most = (int64_t)1 << 23;
+  for (int64_t r0 = 0; r0 < rows; r0 += most) {
+    const int64_t n = rows - r0 < most ? rows - r0 : most;
+    const void* xr = (const char*)x + r0 * cols * (XB ? 2 : 4);
+    int8_t* cr = codes + r0 * cols;
+    float* sr = steps + r0;
+    auto go = [&](auto nt, auto q) {
+      hipLaunchKernelGGL((quant_tokens_kernel<XB, nt.value, q.value>), dim3((unsigned)n), dim3(nt.value), 0, s, n, cols, xr, cr,
+                         sr);
+    };
+    using N64 = std::integral_constant<int, 64>;
+    using N256 = std::integral_constant<int, 256>;
+    if (cols <= 256) go(N64{}, std::integral_constant<int, 1>{});
+    else if (cols <= 512) go(N64{}, std::integral_constant<int, 2>{});
+    else if (cols <= 1024) go(N256{}, std::integral_constant<int, 1>{});
+    else if (cols <= 2048) go(N256{}, std::integral_constant<int, 2>{});
+    else if (cols <= 4096) go(N256{}, std::integral_constant<int, 4>{});
+    else if (cols <= 8192) go(N256{}, std::integral_constant<int, 8>{});
+    else if (cols <= 16384) go(N256{}, std::integral_constant<int, 16>{});
+    else go(N256{}, std::integral_constant<int, 0>{});
+  }
+  return hipGetLastError();
+}
+
+hipError_t quant_tokens_launch(int64_t rows, int64_t cols, int32_t bf16, const void* x, int8_t* codes, float* steps,
+                               hipStream_t s) {
+  return bf16 ? quant_go<true>(rows, cols, x, codes, steps, s) : quant_go<false>(rows, cols, x, codes, steps, s);
+}
+
+// ---- few tokens -----------------------------------------------------------------------------------------------------------
+// What counts is the weights' stream.  A workgroup takes CW channels over all of k, its 8 wavefronts every eighth 64 bytes of
+// them, so that a channel's row is read in runs of 512 bytes and the whole chip has loads in flight however few the channels
+// are; the partial sums are whole numbers and are joined through LDS in any order.  Channels are the rows of
+// v_mfma_i32_16x16x64_i8 and tokens its columns: lane (c, g) supplies bytes 16 g .. + 15 of channel c and of token c, and
+// receives channels 4 g .. 4 g + 3 of token c, which it stores together.  With CW = 8 half of the rows stay empty.
+
+// 16 bytes of a row of which `valid` exist, the others 0.  A cut vector is read as the row's last 16 and moved into place.
+__device__ __forceinline__ i32x4 row16(const int8_t* p, int64_t valid, bool longer) {
+  i32x4 r = {0, 0, 0, 0};
+  if (valid >= 16) {
+    const B16 v = *reinterpret_cast<const B16*>(p);
+    r = i32x4{(int32_t)v.w[0], (int32_t)v.w[1], (int32_t)v.w[2], (int32_t)v.w[3]};
+  } else if (valid > 0) {
+    if (longer) {
+      const B16 v = *reinterpret_cast<const B16*>(p + valid - 16);
+      unsigned __int128 x = ((unsigned __int128)v.w[3] << 96) | ((unsigned __int128)v.w[2] << 64) |
+                            ((unsigned __int128)v.w[1] << 32) | v.w[0];
+      x >>= 8 * (16 - (int)valid);
+      r = i32x4{(int32_t)(uint32_t)x, (int32_t)(uint32_t)(x >> 32), (int32_t)(uint32_t)(x >> 64), (int32_t)(uint32_t)(x >> 96)};
+    } else {
+      uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+      for (int e = 0; e < 15; ++e)
+        if (e < valid) w[e >> 2] |= (uint32_t)(uint8_t)p[e] << (8 * (e & 3));
+      r = i32x4{(int32_t)w[0], (int32_t)w[1], (int32_t)w[2], (int32_t)w[3]};
+    }
+  }
+  return r;
+}
+
+template <int MT, int CW>
+__global__ __launch_bounds__(512) void gemm_i8_rows_kernel(GemmI8Args g) {
+  constexpr int NW = 8, U = MT > 2 ? 2 : 4;  // 64-byte steps in flight
+  __shared__ __attribute__((aligned(16))) i32x4 part[NW][MT][64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, c = lane & 15, q = lane >> 4;
+  const int64_t col0 = (int64_t)blockIdx.x * CW;
+  const int64_t ch = col0 + c;
+  const bool has = c < CW && ch < g.n;
+  const int8_t* bp = g.b + (has ? ch : 0) * g.ldb;
+  const int8_t* ap[MT];
+  bool tok[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    tok[i] = 16 * i + c < g.m;
+    ap[i] = g.a + (tok[i] ? 16 * i + c : 0) * g.lda;
+  }
+  i32x4 acc[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) acc[i] = i32x4{0, 0, 0, 0};
+  const bool longer = g.k >= 16;
+  for (int64_t k0 = 64 * w + 16 * q; k0 - 16 * q < g.k; k0 += 64 * NW * U) {
+    i32x4 b[U], a[U][MT];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t k = k0 + 64 * NW * u, valid = g.k - k;
+      b[u] = row16(bp + k, has ? valid : 0, longer);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) a[u][i] = row16(ap[i] + k, tok[i] ? valid : 0, longer);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < MT; ++i) acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b[u], a[u][i], acc[i], 0, 0, 0);
+  }
+#pragma unroll
+  for (int i = 0; i < MT; ++i) part[w][i][lane] = acc[i];
+  __syncthreads();
+  if (w >= MT) return;  // wavefront i finishes tokens 16 i .. + 15
+  i32x4 sum = {0, 0, 0, 0};
+#pragma unroll
+  for (int o = 0; o < NW; ++o) sum = sum + part[o][w][lane];
+  const int64_t i = 16 * w + c;
+  if (i >= g.m || 4 * q >= CW) return;
+  const float sa = g.sa[i];
+  const int64_t j0 = col0 + 4 * q;
+  float y[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = j0 + e < g.n ? ((float)sum[e] * sa) * g.sb[j0 + e] : 0.0f;
+  if (g.y_bf16) {
+    uint16_t* o = reinterpret_cast<uint16_t*>(g.y) + i * g.ldc + j0;
+    if (j0 + 4 <= g.n) {
+      *reinterpret_cast<H4*>(o) = H4{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+    } else {
+#pragma unroll
+      for (int e = 0; e < 3; ++e)
+        if (j0 + e < g.n) o[e] = f32_to_bf16(y[e]);
+    }
+  } else {
+    float* o = g.y + i * g.ldc + j0;
+    if (j0 + 4 <= g.n) {
+      stf<4>(o, y);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 3; ++e)
+        if (j0 + e < g.n) o[e] = y[e];
+    }
+  }
+}
+
+hipError_t gemm_i8_rows_launch(const GemmI8Args& g, hipStream_t s) {
+  auto go = [&](auto mt, auto cw) {
+    hipLaunchKernelGGL((gemm_i8_rows_kernel<mt.value, cw.value>), dim3((unsigned)((g.n + cw.value - 1) / cw.value)), dim3(512), 0,
+                       s, g);
+    return hipGetLastError();
+  };
+  auto width = [&](auto mt) {
+    if (g.n <= 2048) return go(mt, std::integral_constant<int, 8>{});
+    return go(mt, std::integral_constant<int, 16>{});
+  };
+  if (g.m <= 16) return width(std::integral_constant<int, 1>{});
+  if (g.m <= 32) return width(std::integral_constant<int, 2>{});
+  return width(std::integral_constant<int, 4>{});
+}
+
+}  // namespace canon
