@@ -91,17 +91,16 @@ int cref_cache_append(const int64_t* cache, const int32_t* table, int64_t q_len,
   return 0;
 }
 
-static float exp2_neg(float x) { /* R26's cexp2, x <= 0 or NaN */
+static float exp2_neg(float x) { /* R26's cexp2, x <= 2^-9 or NaN */
   if (x != x) return x;
-  const float at = x > -127.0f ? x : -127.0f;
+  const float at = x > -126.4f ? x : -126.4f;
   const float n = rintf(at), u = cref_sub(at, n);
-  float p = of_bits(0x3AADDD09u);
-  p = cref_fma(p, u, of_bits(0x3C1E7544u));
-  p = cref_fma(p, u, of_bits(0x3D635BA9u));
-  p = cref_fma(p, u, of_bits(0x3E75FCDEu));
-  p = cref_fma(p, u, of_bits(0x3F317215u));
+  float p = of_bits(0x3C1D0166u);
+  p = cref_fma(p, u, of_bits(0x3D64FE23u));
+  p = cref_fma(p, u, of_bits(0x3E7601BCu));
+  p = cref_fma(p, u, of_bits(0x3F317096u));
   p = cref_fma(p, u, 1.0f);
-  return n == -127.0f ? 0.0f : cref_mul(p, ldexpf(1.0f, (int)n));
+  return cref_mul(p, ldexpf(1.0f, (int)n));
 }
 int cref_exp2_neg(int64_t n, const float* x, float* y) {
   for (int64_t i = 0; i < n; ++i) y[i] = exp2_neg(x[i]);
@@ -134,10 +133,10 @@ int cref_cache_attention(const int64_t* cache, const int64_t* cfg, float scale, 
     }
     const float sq = cref_mul(of_bits(top), inv), rs = sq > 0.0f ? cref_div(1.0f, sq) : 0.0f;
     for (int64_t d = 0; d < D; ++d) {
-      const float v = cref_mul(x[d], rs);
+      const float v = cref_mul(scale < 0.0f ? -x[d] : x[d], rs);
       Q[d] = !(sq > 0.0f) || v != v ? 0 : v > 32512.0f ? 32512 : v < -32512.0f ? -32512 : (int64_t)rintf(v);
     }
-    const float f = cref_mul(cref_mul(sq, scale), of_bits(0x3FB8AA3Bu)); /* RN32(1 / ln 2) */
+    const float f = cref_mul(cref_mul(sq, fabsf(scale)), of_bits(0x3FB8AA3Bu)); /* RN32(1 / ln 2) */
     float R = -INFINITY, S = 0.0f, O[256];
     for (int64_t d = 0; d < D; ++d) O[d] = 0.0f;
     for (int64_t j0 = 0; j0 < KL; j0 += 256) {
@@ -154,14 +153,17 @@ int cref_cache_attention(const int64_t* cache, const int64_t* cfg, float scale, 
         slot[j] = slot_of(cache, table, b, kvh, key);
         int64_t acc = 0;
         for (int64_t d = 0; slot[j] >= 0 && d < D; ++d) acc += Q[d] * kc[slot[j] * D + d];
-        t[j] = slot[j] < 0 ? NAN : cref_mul(cref_mul((float)acc, f), ks[slot[j]]);
+        t[j] = slot[j] < 0 ? NAN : cref_mul((float)acc, ks[slot[j]]);
         if (t[j] > m) m = t[j];
         const uint32_t u = slot[j] < 0 ? 0x7FC00000u : to_bits(vs[slot[j]]) & 0x7FFFFFFFu;
         if (u > vtop) vtop = u;
       }
       if (!any) continue;
-      const float rb = ceilf(m), V = of_bits(vtop);
-      for (int64_t j = 0; j < 256; ++j) e[j] = sees[j] ? exp2_neg(cref_sub(t[j], rb == -INFINITY ? 0.0f : rb)) : 0.0f;
+      const float rb = m == -INFINITY ? m : ceilf(cref_mul(m, f)), V = of_bits(vtop);
+      const float ref = rb == -INFINITY ? 0.0f : rb;
+      for (int64_t j = 0; j < 256; ++j)
+        e[j] = !sees[j] ? 0.0f
+               : fabsf(ref) <= 65536.0f ? exp2_neg(cref_fma(t[j], f, -ref)) : exp2_neg(cref_sub(cref_mul(t[j], f), ref));
       float part[16];
       for (int c = 0; c < 16; ++c) {
         part[c] = 0.0f;
@@ -178,8 +180,8 @@ int cref_cache_attention(const int64_t* cache, const int64_t* cfg, float scale, 
         int64_t A = 0;
         for (int64_t j = 0; j < 256; ++j)
           if (sees[j] && rv != 0.0f && slot[j] >= 0) {
-            const float w = cref_mul(e[j], cref_mul(vs[slot[j]], rv));
-            A += (w != w ? 0 : (int64_t)rintf(w)) * vc[v_at(cache, slot[j], d)];
+            const double w = (double)e[j] * cref_mul(vs[slot[j]], rv); /* exact */
+            A += (w != w ? 0 : (int64_t)rint(w)) * vc[v_at(cache, slot[j], d)];
           }
         O[d] = cref_fma((float)A, scale_v, cref_mul(O[d], xo));
       }

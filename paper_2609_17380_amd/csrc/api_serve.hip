@@ -258,7 +258,7 @@ canon_status check_attention(const canon_kv_cache* cache, const canon_attn_rows*
   if (st != CANON_OK) return st;
   if (!rows || rows->batch != cache->batch || rows->n_heads < 1 || rows->n_heads % cache->n_kv_heads || rows->q_len < 0 ||
       rows->k_len < 0 || rows->ld != 0 || rows->window < 0 || (rows->causal != 0 && rows->causal != 1) ||
-      rows->k_len > cache->table_len * cache->page || !aligned(rows->q_starts, 4) || !aligned(rows->q_lens, 4) ||
+      rows->k_len > cache->table_len * cache->page || (rows->k_len > 0 && cache->n_pages < 1) || !aligned(rows->q_starts, 4) || !aligned(rows->q_lens, 4) ||
       !aligned(rows->k_lens, 4))
     return CANON_EINVAL;
   if (rows->k_len > (int64_t(1) << 21) || rows->n_heads >= (1 << 24) ||

@@ -30,21 +30,30 @@ constexpr float kDigits = 32512.0f;             // largest whole number of a que
 constexpr uint32_t kInvDigits = 0x38010204u;    // RN32(1 / 32512)
 constexpr float kNegInf = -__builtin_inff();
 
-// 2^x, |x| <= 1/2: the polynomial of least relative error with the constant 1 (its coefficients rounded; 1.6e-7 in all)
-constexpr uint32_t kExp2C[5] = {0x3F317215u, 0x3E75FCDEu, 0x3D635BA9u, 0x3C1E7544u, 0x3AADDD09u};
+// 2^x, |x| <= 1/2: the polynomial of least relative error with the constant 1, its coefficients rounded: 2.9e-6 in all, a fifth of
+// what rounding the weights to 16 bits leaves.
+constexpr uint32_t kExp2C[4] = {0x3F317096u, 0x3E7601BCu, 0x3D64FE23u, 0x3C1D0166u};
 
-// cexp2 of x <= 0 or NaN.  The clamp makes n = -127 of all that lies below, whose scale's bits are zero; it passes a NaN on.
+// cexp2 of x <= 2^-9 or NaN (which the maximum passes on).  n goes to the exponent by an integer addition; -126.4, where the
+// clamp sends all that lies below, has n = -126 and p < 1, a subnormal pattern, which every use reads as zero.
 __device__ __forceinline__ float cexp2(float x) {
-  x = __builtin_elementwise_maximum(x, -127.0f);
+  x = __builtin_elementwise_maximum(x, -126.4f);
   const float u = x + 0x1.8p23f;  // rne(x), also in the low bits
   const float f = x - (u - 0x1.8p23f);
-  float p = __builtin_fmaf(__uint_as_float(kExp2C[4]), f, __uint_as_float(kExp2C[3]));
-  p = __builtin_fmaf(p, f, __uint_as_float(kExp2C[2]));
+  float p = __builtin_fmaf(__uint_as_float(kExp2C[3]), f, __uint_as_float(kExp2C[2]));
   p = __builtin_fmaf(p, f, __uint_as_float(kExp2C[1]));
   p = __builtin_fmaf(p, f, __uint_as_float(kExp2C[0]));
   p = __builtin_fmaf(p, f, 1.0f);
-  return p * __uint_as_float((__float_as_uint(u) << 23) + 0x3F800000u);
+  return __uint_as_float(__float_as_uint(p) + (__float_as_uint(u) << 23));
 }
+// the weight of a score u f against the reference: fused where r is small enough that what r's own rounding leaves above it
+// (2^-9) does not carry a weight past its digits
+__device__ __forceinline__ float weight(float u, float f, float ref, bool near) {
+  if (near) return cexp2(__builtin_fmaf(u, f, -ref));
+  const float t = u * f;
+  return cexp2(t - ref);
+}
+__device__ __forceinline__ bool near_ref(float ref) { return fabsf(ref) <= 65536.0f; }
 
 // 2^(a - b) of whole a <= b, 1 where a is -inf
 __device__ __forceinline__ float shift2(float a, float b) {
@@ -103,11 +112,12 @@ __device__ __forceinline__ Column column_of(const CacheAttnArgs& a, int64_t b, i
 }
 
 // the 16 keys from j on (a multiple of 16): their first slot in head kvh, or -1
-__device__ __forceinline__ int64_t slots16(const CacheAttnArgs& a, int64_t b, int32_t kvh, int64_t j) {
-  if (j >= a.k_len) return -1;
-  const int64_t p = a.c.table[b * a.c.table_len + (j >> a.c.lg)];
-  if (p < 0 || p >= a.c.n_pages) return -1;
-  return ((p * a.c.heads + kvh) << a.c.lg) + (j & ((1 << a.c.lg) - 1));
+__device__ __forceinline__ int64_t slot16(const CacheAttnArgs& a, int32_t kvh, int64_t j, int32_t page) {
+  if (page < 0 || page >= a.c.n_pages) return -1;
+  return (((int64_t)page * a.c.heads + kvh) << a.c.lg) + (j & ((1 << a.c.lg) - 1));
+}
+__device__ __forceinline__ int32_t page_of(const CacheAttnArgs& a, int64_t b, int64_t j) {
+  return j < a.k_len ? a.c.table[b * a.c.table_len + (j >> a.c.lg)] : -1;
 }
 
 __device__ __forceinline__ i32x4 load16(const int8_t* p) { return *reinterpret_cast<const i32x4*>(p); }
@@ -157,7 +167,7 @@ __device__ __forceinline__ void load_query(const CacheAttnArgs& a, const Column&
       uint32_t h = 0, l = 0;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        float x = v[s][4 * w + e] * rs;
+        float x = (a.scale < 0.0f ? -v[s][4 * w + e] : v[s][4 * w + e]) * rs;
         x = sq > 0.0f && x == x ? fminf(fmaxf(x, -kDigits), kDigits) : 0.0f;
         const int32_t n = (int32_t)__builtin_rintf(x), d = (n + 128) >> 8;  // n = 256 d + (n - 256 d), the rest in [-128, 127]
         h |= (uint32_t)(d & 0xFF) << (8 * e);
@@ -166,15 +176,16 @@ __device__ __forceinline__ void load_query(const CacheAttnArgs& a, const Column&
       out.hi[s][w] = (int32_t)h;
       out.lo[s][w] = (int32_t)l;
     }
-  const float sc = sq * a.scale;
+  const float sc = sq * fabsf(a.scale);
   out.f = sc * kLog2e;
 }
 
-// Four weights as whole numbers, 0 <= w <= 32512, into a dword of each digit.  Adding 1.5 2^23 + 128 rounds to a whole number
+// Four weights e ratio as whole numbers, 0 .. 32639, into a dword of each digit.  Adding 1.5 2^23 + 128 rounds to a whole number
 // and leaves w + 128 in the low bits: byte 1 is the high digit, byte 0 the low one with its sign bit inverted.
-__device__ __forceinline__ void digits4(float w0, float w1, float w2, float w3, int32_t& hi, int32_t& lo) {
-  const uint32_t a = __float_as_uint(w0 + 12583040.0f), b = __float_as_uint(w1 + 12583040.0f);
-  const uint32_t c = __float_as_uint(w2 + 12583040.0f), d = __float_as_uint(w3 + 12583040.0f);
+constexpr float kWhole = 12583040.0f;
+__device__ __forceinline__ void digits4(const float (&e)[4], const f32x4& ratio, int32_t& hi, int32_t& lo) {
+  const uint32_t a = __float_as_uint(__builtin_fmaf(e[0], ratio[0], kWhole)), b = __float_as_uint(__builtin_fmaf(e[1], ratio[1], kWhole));
+  const uint32_t c = __float_as_uint(__builtin_fmaf(e[2], ratio[2], kWhole)), d = __float_as_uint(__builtin_fmaf(e[3], ratio[3], kWhole));
   const uint32_t ab = __builtin_amdgcn_perm(b, a, 0x05010400u);  // a0 b0 a1 b1
   const uint32_t cd = __builtin_amdgcn_perm(d, c, 0x05010400u);
   lo = (int32_t)(__builtin_amdgcn_perm(cd, ab, 0x05040100u) ^ 0x80808080u);
@@ -220,14 +231,21 @@ __global__ __launch_bounds__(256) void attn_tile_kernel(CacheAttnArgs a, int64_t
   const int32_t kvh = (int32_t)(id % a.c.heads);
   const int64_t b = id / a.c.heads;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, cc = lane & 15, g = lane >> 4;
+  const int64_t t0 = tile * kTile, j0 = t0 + 64 * w;
+  const int32_t kpage = page_of(a, b, j0 + 16 * (cc >> 2));
+  int32_t vpage[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) vpage[q] = page_of(a, b, t0 + 64 * q + 16 * g);
   const Column col = column_of(a, b, kvh, cb * 16 + cc);
-  const int64_t t0 = tile * kTile;
   const bool touched = col.lo < t0 + kTile && col.hi > t0;
   if (tiles > 1 && !__any(touched)) return;  // the join passes over tiles that a row does not see
 
-  // everything from the cache first
-  const int64_t j0 = t0 + 64 * w;
-  const int64_t kslot = slots16(a, b, kvh, j0 + 16 * (cc >> 2)), gslot = slots16(a, b, kvh, j0 + 16 * g);
+  // the cache: the slots are known, everything is asked for before anything is waited for
+  const int64_t kslot = slot16(a, kvh, j0 + 16 * (cc >> 2), kpage);
+  int64_t vslot[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) vslot[q] = slot16(a, kvh, t0 + 64 * q + 16 * g, vpage[q]);
+  const int64_t gslot = w == 0 ? vslot[0] : w == 1 ? vslot[1] : w == 2 ? vslot[2] : vslot[3];
   i32x4 kx[4][NS];
 #pragma unroll
   for (int t = 0; t < 4; ++t)
@@ -249,12 +267,11 @@ __global__ __launch_bounds__(256) void attn_tile_kernel(CacheAttnArgs a, int64_t
   i32x4 vx[NW][4];
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    const int64_t vslot = slots16(a, b, kvh, t0 + 64 * q + 16 * g);
 #pragma unroll
     for (int n = 0; n < NW; ++n) {
       const int part = w + 4 * n;
       vx[n][q] = i32x4{0, 0, 0, 0};
-      if (vslot >= 0 && (ND % 4 == 0 || part < ND)) vx[n][q] = load16(a.c.vc + vslot * HD + (16 * part + cc) * 16);
+      if (vslot[q] >= 0 && (ND % 4 == 0 || part < ND)) vx[n][q] = load16(a.c.vc + vslot[q] * HD + (16 * part + cc) * 16);
     }
   }
   Query<HD> qd;
@@ -275,8 +292,7 @@ __global__ __launch_bounds__(256) void attn_tile_kernel(CacheAttnArgs a, int64_t
     for (int i = 0; i < 4; ++i) {
       const int64_t j = j0 + 16 * g + 4 * k + i;
       const bool seen = j >= col.lo && j < col.hi;
-      const float x = (float)acc[i] * qd.f;
-      t[k][i] = seen ? x * kst[k][i] : kNegInf;
+      t[k][i] = seen ? (float)acc[i] * kst[k][i] : kNegInf;
       m = __builtin_elementwise_maximum(m, t[k][i]);
       const uint32_t u = seen ? __float_as_uint(vst[k][i]) & 0x7FFFFFFFu : 0u;
       vtop = u > vtop ? u : vtop;
@@ -294,22 +310,25 @@ __global__ __launch_bounds__(256) void attn_tile_kernel(CacheAttnArgs a, int64_t
     m = __builtin_elementwise_maximum(m, ms[o][cc]);
     vtop = vs[o][cc] > vtop ? vs[o][cc] : vtop;
   }
-  const float r = __builtin_ceilf(m), ref = r == kNegInf ? 0.0f : r, rv = value_recip(vtop);
+  const float mf = m * qd.f, r = m == kNegInf ? m : __builtin_ceilf(mf), ref = r == kNegInf ? 0.0f : r, rv = value_recip(vtop);
+  const bool near = near_ref(ref);
   float sum = 0.0f;
   i32x4 wh, wl;
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    float x[4];
+    float e[4];
+    f32x4 ratio;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float e = cexp2(t[k][i] - ref);
-      sum = sum + e;
       const int64_t j = j0 + 16 * g + 4 * k + i;
-      const float ratio = vst[k][i] * rv;
-      x[i] = rv != 0.0f && j >= col.lo && j < col.hi ? e * ratio : 0.0f;
+      const bool seen = j >= col.lo && j < col.hi;
+      e[i] = seen ? weight(t[k][i], qd.f, ref, near) : 0.0f;
+      sum = sum + e[i];
+      const float x = vst[k][i] * rv;
+      ratio[i] = rv != 0.0f && seen ? x : 0.0f;
     }
     int32_t h, l;
-    digits4(x[0], x[1], x[2], x[3], h, l);
+    digits4(e, ratio, h, l);
     wh[k] = h;
     wl[k] = l;
   }
@@ -348,10 +367,12 @@ __global__ __launch_bounds__(256) void attn_tile_kernel(CacheAttnArgs a, int64_t
   }
 }
 
-// A row's tiles joined, ascending: one wavefront a row, HD / 64 (or fewer) elements a lane.
+// A row's tiles joined, ascending: one wavefront a row, HD / 64 (or fewer) elements a lane.  The references and sums of 64 tiles
+// come at once, a tile a lane, and the sums of 16 tiles before any is used (one by one, every tile's were waited for: a row of
+// 128 tiles 156 us, of 16 16).
 template <int HD>
 __global__ __launch_bounds__(64) void attn_join_kernel(CacheAttnArgs a, int64_t tiles) {
-  constexpr int E = (HD + 63) / 64;
+  constexpr int E = (HD + 63) / 64, U = E > 2 ? 8 : 16;
   const int64_t row = blockIdx.x;
   const int lane = threadIdx.x;
   const int64_t tok = row / a.heads, b = tok / a.q_len;
@@ -361,18 +382,33 @@ __global__ __launch_bounds__(64) void attn_join_kernel(CacheAttnArgs a, int64_t 
   float R = kNegInf, S = 0.0f, o[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.0f;
-  if (col.hi > col.lo)
-    for (int64_t t = col.lo / kTile; t <= (col.hi - 1) / kTile; ++t) {
-      const float* p = parts + t * (HD + 4);
-      const f32x4 d = *reinterpret_cast<const f32x4*>(p + HD);
-      const float Rn = __builtin_elementwise_maximum(R, d[0]), x = shift2(R, Rn), y = shift2(d[0], Rn);
-      S = __builtin_fmaf(d[1], y, S * x);
-      const float sc = d[2] * y;
+  const int64_t first = col.lo / kTile, end = col.hi > col.lo ? (col.hi + kTile - 1) / kTile : first;
+  for (int64_t c0 = first; c0 < end; c0 += 64) {
+    const int n = end - c0 < 64 ? (int)(end - c0) : 64;
+    f32x4 d = {kNegInf, 0.0f, 0.0f, 0.0f};
+    if (lane < n) d = *reinterpret_cast<const f32x4*>(parts + (c0 + lane) * (HD + 4) + HD);
+    for (int t0 = 0; t0 < n; t0 += U) {
+      float p[U][E];
 #pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (lane + 64 * e < HD) o[e] = __builtin_fmaf(p[lane + 64 * e], sc, o[e] * x);
-      R = Rn;
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          p[u][e] = t0 + u < n && lane + 64 * e < HD ? parts[(c0 + t0 + u) * (HD + 4) + lane + 64 * e] : 0.0f;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (t0 + u >= n) break;
+        const float r = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(d[0]), t0 + u));
+        const float s = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(d[1]), t0 + u));
+        const float v = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(d[2]), t0 + u));
+        const float Rn = __builtin_elementwise_maximum(R, r), x = shift2(R, Rn), y = shift2(r, Rn);
+        S = __builtin_fmaf(s, y, S * x);
+        const float sc = v * y;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(p[u][e], sc, o[e] * x);
+        R = Rn;
+      }
     }
+  }
   const float inv = S == 0.0f ? 0.0f : 1.0f / S;
 #pragma unroll
   for (int e = 0; e < E; ++e)
@@ -382,99 +418,255 @@ __global__ __launch_bounds__(64) void attn_join_kernel(CacheAttnArgs a, int64_t 
     }
 }
 
-// ---- all keys of a block of queries in one wavefront: prompts ------------------------------------------------------------
+// ---- all keys of a block of queries in one workgroup: prompts -------------------------------------------------------------
+//
+// Four wavefronts of 16 queries each go over the tiles together.  A tile's keys and values come straight into LDS in the order
+// in which the matrix instructions take them (each 1 KB block is one instruction's operand, lane l's bytes at 16 l, so that
+// reading has no bank conflicts and no address is computed per lane), a wavefront fetching its quarter of the tile: the next
+// tile's keys while the present one's weights are computed, its values while the next scores are.  Two workgroups a CU (heads
+// of up to 128) run out of step, one's products under the other's exponentials.
+__device__ const float kNanStep = __builtin_nanf("");
+
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+// 16 (or 4) bytes a lane from global memory to LDS, lane l's at lds + 16 l (4 l); not tracked by the compiler: vm_left waits
+__device__ __forceinline__ void dma16(const void* p, unsigned lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory", "m0");
+}
+__device__ __forceinline__ void dma4(const void* p, unsigned lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(p) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+template <int N>
+__device__ __forceinline__ void vm_left() {  // at most N vector-memory operations of this wavefront outstanding
+  static_assert(N >= 0 && N < 64, "vmcnt range");
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x70 | 0xF00);
+}
+
 template <int HD>
-__global__ __launch_bounds__(256, 1) void attn_rows_kernel(CacheAttnArgs a, int64_t blocks) {
+struct RowsLds {
+  static constexpr int NS = Query<HD>::NS, ND = HD / 16;
+  i32x4 k[16 * NS][64];  // block (4 q + t) NS + s: 64 q keys on, instruction t, elements 64 s on
+  i32x4 v[4 * ND][64];   // block q ND + n
+  float ks[2][kTile], vs[2][kTile];
+  float ratio[4][kTile];  // RN(vstep rv) where a wavefront's queries all see the whole tile
+  int32_t span[4][2];     // tiles of the wavefronts
+};
+
+template <int HD>
+__global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void attn_rows_kernel(CacheAttnArgs a, int64_t blocks) {
   constexpr int NS = Query<HD>::NS, ND = HD / 16;
-  int64_t id = blockIdx.x;
-  const int64_t cb = blocks - 1 - id % blocks;  // the longest causal rows first
-  id /= blocks;
-  const int32_t kvh = (int32_t)(id % a.c.heads);
-  const int64_t b = id / a.c.heads;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, cc = lane & 15, g = lane >> 4;
+  typedef const __attribute__((address_space(4))) int32_t* ConstInts;  // the table through the scalar cache
+  __shared__ __attribute__((aligned(1024))) RowsLds<HD> L;
+  // workgroups of one head of a sequence on one XCD where their number allows it, the longest causal rows first
+  const int64_t bh = blockIdx.x % (a.c.heads * a.c.batch), cb = blocks - 1 - blockIdx.x / (a.c.heads * a.c.batch);
+  const int32_t kvh = (int32_t)(bh % a.c.heads);
+  const int64_t b = bh / a.c.heads;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), cc = lane & 15, g = lane >> 4;
   const Column col = column_of(a, b, kvh, (cb * 4 + w) * 16 + cc);
-  if (!__any(col.real)) return;
-  int64_t lo = col.hi > col.lo ? col.lo : (int64_t)1 << 62, hi = col.hi;
+  int32_t lo = col.hi > col.lo ? (int32_t)col.lo : 0x7FFFFFFF, hi = (int32_t)col.hi;  // k_len fits
 #pragma unroll
   for (int s = 1; s < 16; s <<= 1) {
-    const int64_t l = __shfl_xor(lo, s, 64), h = __shfl_xor(hi, s, 64);
+    const int32_t l = __shfl_xor(lo, s, 64), h = __shfl_xor(hi, s, 64);
     lo = l < lo ? l : lo;
     hi = h > hi ? h : hi;
   }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  hi = __builtin_amdgcn_readfirstlane(hi);
+  if (lane == 0) {
+    L.span[w][0] = lo;
+    L.span[w][1] = hi;
+  }
   Query<HD> qd;
   load_query<HD>(a, col, qd);
+  __syncthreads();
+  int32_t all_lo = 0x7FFFFFFF, all_hi = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    all_lo = L.span[i][0] < all_lo ? L.span[i][0] : all_lo;
+    all_hi = L.span[i][1] > all_hi ? L.span[i][1] : all_hi;
+  }
+  all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+  all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+
+  const unsigned lk = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)&L.k[0][0];
+  const unsigned lv = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)&L.v[0][0];
+  const unsigned lks = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)&L.ks[0][0];
+  const unsigned lvs = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void*)&L.vs[0][0];
+  const ConstInts table = (ConstInts)(uintptr_t)(a.c.table + b * a.c.table_len);
+  // the first slots of the four groups of 16 keys of this wavefront's quarter of a tile, -1 where there is none
+  auto group_slots = [&](int32_t t0, int64_t (&s)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int32_t j = t0 + 64 * w + 16 * i;
+      s[i] = j < (int32_t)a.k_len ? slot16(a, kvh, j, table[j >> a.c.lg]) : -1;
+    }
+  };
+  auto pick = [](const int64_t (&s)[4], int i) { return i == 0 ? s[0] : i == 1 ? s[1] : i == 2 ? s[2] : s[3]; };
+  // Slots that the cache does not have: any of its codes (their weights are 0, or the step NaN), the step NaN.
+  auto fetch_keys = [&](const int64_t (&s)[4], int par) {
+    int64_t ks = pick(s, cc >> 2);
+    const int64_t gs = pick(s, g);
+    ks = ks < 0 ? 0 : ks;
+    const int8_t* p = a.c.kc + (ks + (cc & 3)) * HD;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int e = 0; e < NS; ++e)  // elements behind a head of 32 (mod 64): its first ones, which meet digits of 0
+        dma16(p + 4 * t * HD + (HD % 64 == 0 || 64 * e + 16 * g < HD ? 64 * e + 16 * g : 0), lk + 1024 * ((4 * w + t) * NS + e));
+    dma4(gs < 0 ? &kNanStep : a.c.ks + gs + cc, lks + 1024 * par + 256 * w);
+    dma4(gs < 0 ? &kNanStep : a.c.vs + gs + cc, lvs + 1024 * par + 256 * w);
+  };
+  auto fetch_values = [&](const int64_t (&s)[4]) {
+    int64_t vs = pick(s, g);
+    vs = vs < 0 ? 0 : vs;
+    const int8_t* p = a.c.vc + vs * HD + 16 * cc;
+#pragma unroll
+    for (int n = 0; n < ND; ++n) dma16(p + 256 * n, lv + 1024 * (w * ND + n));
+  };
+
   float R = kNegInf, S = 0.0f;
   f32x4 o[ND];
 #pragma unroll
   for (int n = 0; n < ND; ++n) o[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-
-  for (int64_t t0 = hi > lo ? lo / kTile * kTile : hi; t0 < hi; t0 += kTile) {
-    const bool all = __all(!col.real || (col.lo <= t0 && col.hi >= t0 + kTile));
-    float t[4][4][4];
+  int64_t slots[4];
+  int32_t t0 = all_lo < all_hi ? all_lo / kTile * kTile : all_hi;
+  int par = 0;
+  if (t0 < all_hi) {
+    group_slots(t0, slots);
+    fetch_keys(slots, 0);
+  }
+  for (; t0 < all_hi; t0 += kTile, par ^= 1) {
+    // this tile's keys have landed, and every wavefront is done with the last one's values
+    vm_left<0>();
+    __syncthreads();
+    fetch_values(slots);
+    const bool mine = lo < t0 + kTile && hi > t0;
+    const bool all = mine && __all(!col.real || (col.lo <= t0 && col.hi >= t0 + kTile));
+    // quarters of the tile that some query of this wavefront sees
+    const int q0 = lo > t0 ? (lo - t0) >> 6 : 0, q1 = !mine ? 0 : hi - t0 < kTile ? (hi - t0 + 63) >> 6 : 4;
+    float u[4][4][4];
     float m = kNegInf;
-    uint32_t vtop = 0;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const int64_t j0 = t0 + 64 * q;
-      const int64_t kslot = slots16(a, b, kvh, j0 + 16 * (cc >> 2)), gslot = slots16(a, b, kvh, j0 + 16 * g);
+      if (q >= q0 && q < q1) {
+        i32x4 acc[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        i32x4 kx[NS];
+        for (int t = 0; t < 4; ++t) acc[t] = i32x4{0, 0, 0, 0};
+        i32x4 kx[4][NS];
 #pragma unroll
-        for (int s = 0; s < NS; ++s) {
-          kx[s] = i32x4{0, 0, 0, 0};
-          if (kslot >= 0 && (HD % 64 == 0 || 64 * s + 16 * g < HD))
-            kx[s] = load16(a.c.kc + (kslot + 4 * k + (cc & 3)) * HD + 64 * s + 16 * g);
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+          for (int t = 0; t < 4; ++t) kx[t][s] = L.k[(4 * q + t) * NS + s][lane];
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+          for (int t = 0; t < 4; ++t) acc[t] = mfma(kx[t][s], qd.hi[s], acc[t]);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) acc[t] = acc[t] << 8;
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+          for (int t = 0; t < 4; ++t) acc[t] = mfma(kx[t][s], qd.lo[s], acc[t]);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const f32x4 st = *reinterpret_cast<const f32x4*>(&L.ks[par][64 * q + 16 * g + 4 * t]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            u[q][t][i] = (float)acc[t][i] * st[i];
+            if (!all) {
+              const int32_t j = t0 + 64 * q + 16 * g + 4 * t + i;
+              u[q][t][i] = j >= col.lo && j < col.hi ? u[q][t][i] : kNegInf;
+            }
+            m = __builtin_elementwise_maximum(m, u[q][t][i]);
+          }
         }
-        f32x4 kst{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")}, vst = kst;
-        if (gslot >= 0) {
-          kst = *reinterpret_cast<const f32x4*>(a.c.ks + gslot + 4 * k);
-          vst = *reinterpret_cast<const f32x4*>(a.c.vs + gslot + 4 * k);
-        }
-        i32x4 acc = {0, 0, 0, 0};
+      } else {
 #pragma unroll
-        for (int s = 0; s < NS; ++s) acc = mfma(kx[s], qd.hi[s], acc);
-        acc = acc << 8;
+        for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int s = 0; s < NS; ++s) acc = mfma(kx[s], qd.lo[s], acc);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int64_t j = j0 + 16 * g + 4 * k + i;
-          const bool seen = all || (j >= col.lo && j < col.hi);
-          const float x = (float)acc[i] * qd.f;
-          t[q][k][i] = seen ? x * kst[i] : kNegInf;
-          m = __builtin_elementwise_maximum(m, t[q][k][i]);
-          const uint32_t u = seen ? __float_as_uint(vst[i]) & 0x7FFFFFFFu : 0u;
-          vtop = u > vtop ? u : vtop;
-        }
+          for (int i = 0; i < 4; ++i) u[q][t][i] = kNegInf;
       }
     }
+    // every wavefront is done with the keys: the next tile's
+    __syncthreads();
+    const bool more = t0 + kTile < all_hi;
+    if (more) {
+      group_slots(t0 + kTile, slots);
+      fetch_keys(slots, par ^ 1);
+    }
+    // the largest step of the values that a query sees, and what each of them is to it
+    uint32_t vtop = 0;
+    if (all) {
+      const f32x4 vst = *reinterpret_cast<const f32x4*>(&L.vs[par][4 * lane]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t x = __float_as_uint(vst[i]) & 0x7FFFFFFFu;
+        vtop = x > vtop ? x : vtop;
+      }
+      vtop = lanes_join(vtop, 64, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
+      const float rv = value_recip(vtop);
+      f32x4 ratio;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = vst[i] * rv;
+        ratio[i] = rv != 0.0f ? x : 0.0f;
+      }
+      *reinterpret_cast<f32x4*>(&L.ratio[w][4 * lane]) = ratio;
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (q >= q0 && q < q1)
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int32_t at = 64 * q + 16 * g + 4 * t + i, j = t0 + at;
+              const uint32_t x = __float_as_uint(L.vs[par][at]) & 0x7FFFFFFFu;
+              vtop = j >= col.lo && j < col.hi && x > vtop ? x : vtop;
+            }
+      vtop = umax4(vtop);
+    }
     m = max4(m);
-    vtop = umax4(vtop);
-    const float r = __builtin_ceilf(m), ref = r == kNegInf ? 0.0f : r, rv = value_recip(vtop);
+    const float mf = m * qd.f, r = m == kNegInf ? m : __builtin_ceilf(mf), ref = r == kNegInf ? 0.0f : r;
+    const float rv = value_recip(vtop);
+    const bool near = near_ref(ref), near_all = __all(near);
     i32x4 wh[4], wl[4];
     float sums[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const int64_t j0 = t0 + 64 * q, gslot = slots16(a, b, kvh, j0 + 16 * g);
+      wh[q] = wl[q] = i32x4{0, 0, 0, 0};
+      wl[q] = i32x4{0, 0, 0, 0};
+      sums[q] = 0.0f;
+      if (q < q0 || q >= q1) continue;
       float sum = 0.0f;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        f32x4 vst{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
-        if (gslot >= 0) vst = *reinterpret_cast<const f32x4*>(a.c.vs + gslot + 4 * k);
-        float x[4];
+      for (int t = 0; t < 4; ++t) {
+        float e[4];
+        f32x4 ratio;
+        if (all && near_all) {
+          ratio = *reinterpret_cast<const f32x4*>(&L.ratio[w][64 * q + 16 * g + 4 * t]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float e = cexp2(t[q][k][i] - ref);
-          sum = sum + e;
-          const int64_t j = j0 + 16 * g + 4 * k + i;
-          const float ratio = vst[i] * rv;
-          x[i] = rv != 0.0f && (all || (j >= col.lo && j < col.hi)) ? e * ratio : 0.0f;
+          for (int i = 0; i < 4; ++i) {
+            e[i] = cexp2(__builtin_fmaf(u[q][t][i], qd.f, -ref));
+            sum = sum + e[i];
+          }
+        } else {
+          const f32x4 vst = *reinterpret_cast<const f32x4*>(&L.vs[par][64 * q + 16 * g + 4 * t]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int32_t j = t0 + 64 * q + 16 * g + 4 * t + i;
+            const bool seen = j >= col.lo && j < col.hi;
+            e[i] = seen ? weight(u[q][t][i], qd.f, ref, near) : 0.0f;
+            sum = sum + e[i];
+            const float x = vst[i] * rv;
+            ratio[i] = rv != 0.0f && seen ? x : 0.0f;
+          }
         }
         int32_t h, l;
-        digits4(x[0], x[1], x[2], x[3], h, l);
-        wh[q][k] = h;
-        wl[q][k] = l;
+        digits4(e, ratio, h, l);
+        wh[q][t] = h;
+        wl[q][t] = l;
       }
       sums[q] = sum4(sum);
     }
@@ -484,26 +676,38 @@ __global__ __launch_bounds__(256, 1) void attn_rows_kernel(CacheAttnArgs a, int6
     // (but for the sign of a zero, which the output's + 0 takes away).
     S = __builtin_fmaf(Sb, y, S * x);
     R = Rn;
-    const float sc = (__uint_as_float(vtop) * __uint_as_float(kInvDigits)) * y;
-    int64_t vslot[4];
+    const float vsc = __uint_as_float(vtop) * __uint_as_float(kInvDigits), sc = vsc * y;
+    const bool still = __all(x == 1.0f);
+    // the values have landed (what was asked for after them, the next keys, may not have)
+    if (more) vm_left<4 * NS + 2>();
+    else vm_left<0>();
+    __syncthreads();
+    if (mine) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) vslot[q] = slots16(a, b, kvh, t0 + 64 * q + 16 * g);
+      for (int n = 0; n < ND; n += 2) {
+        i32x4 acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}}, vx[2][4];
 #pragma unroll
-    for (int n = 0; n < ND; ++n) {
-      i32x4 vx[4];
+        for (int q = 0; q < 4; ++q)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        vx[q] = i32x4{0, 0, 0, 0};
-        if (vslot[q] >= 0) vx[q] = load16(a.c.vc + vslot[q] * HD + (16 * n + cc) * 16);
+          for (int d = 0; d < 2; ++d) vx[d][q] = L.v[q * ND + n + d][lane];
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int d = 0; d < 2; ++d) acc[d] = mfma(vx[d][q], wh[q], acc[d]);
+#pragma unroll
+        for (int d = 0; d < 2; ++d) acc[d] = acc[d] << 8;
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int d = 0; d < 2; ++d) acc[d] = mfma(vx[d][q], wl[q], acc[d]);
+#pragma unroll
+        for (int d = 0; d < 2; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float p = still ? o[n + d][i] : o[n + d][i] * x;
+            o[n + d][i] = __builtin_fmaf((float)acc[d][i], sc, p);
+          }
       }
-      i32x4 acc = {0, 0, 0, 0};
-#pragma unroll
-      for (int q = 0; q < 4; ++q) acc = mfma(vx[q], wh[q], acc);
-      acc = acc << 8;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) acc = mfma(vx[q], wl[q], acc);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) o[n][i] = __builtin_fmaf((float)acc[i], sc, o[n][i] * x);
     }
   }
   if (!col.real) return;
