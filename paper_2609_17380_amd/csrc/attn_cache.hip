@@ -367,55 +367,63 @@ __global__ __launch_bounds__(256) void attn_tile_kernel(CacheAttnArgs a, int64_t
   }
 }
 
-// A row's tiles joined, ascending: one wavefront a row, HD / 64 (or fewer) elements a lane.  The references and sums of 64 tiles
-// come at once, a tile a lane, and the sums of 16 tiles before any is used (one by one, every tile's were waited for: a row of
-// 128 tiles 156 us, of 16 16).
+// A row's tiles joined, ascending: one wavefront a row, E elements a lane.  What the references change by is worked out for 64
+// tiles at once, a tile a lane (the largest reference up to a tile is a prefix maximum), so that the chain over the tiles is two
+// operations an element; and 16 tiles' sums are on their way together.  (One tile after the other, each waited for: a row of 128
+// tiles took 156 us, of 16 16.)
 template <int HD>
 __global__ __launch_bounds__(64) void attn_join_kernel(CacheAttnArgs a, int64_t tiles) {
-  constexpr int E = (HD + 63) / 64, U = E > 2 ? 8 : 16;
+  constexpr int E = HD > 128 ? 4 : 2, U = 16;
+  typedef float Vec __attribute__((ext_vector_type(E)));
   const int64_t row = blockIdx.x;
-  const int lane = threadIdx.x;
+  const int lane = threadIdx.x, at = lane * E < HD ? lane * E : 0;
   const int64_t tok = row / a.heads, b = tok / a.q_len;
   const int32_t G = a.heads / a.c.heads, h = (int32_t)(row - tok * a.heads);
   const Column col = column_of(a, b, h / G, (tok - b * a.q_len) * G + h % G);
   const float* parts = a.parts + row * tiles * (HD + 4);
-  float R = kNegInf, S = 0.0f, o[E];
+  float R = kNegInf, S = 0.0f;
+  Vec o;
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.0f;
   const int64_t first = col.lo / kTile, end = col.hi > col.lo ? (col.hi + kTile - 1) / kTile : first;
   for (int64_t c0 = first; c0 < end; c0 += 64) {
     const int n = end - c0 < 64 ? (int)(end - c0) : 64;
-    f32x4 d = {kNegInf, 0.0f, 0.0f, 0.0f};
-    if (lane < n) d = *reinterpret_cast<const f32x4*>(parts + (c0 + lane) * (HD + 4) + HD);
+    const float* p = parts + c0 * (HD + 4);
+    const f32x4 d = *reinterpret_cast<const f32x4*>(p + (lane < n ? lane : n - 1) * (HD + 4) + HD);
+    // R of the rule before and after this lane's tile
+    float up = d[0];
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+      const float x = __shfl_up(up, s, 64);
+      up = lane >= s ? __builtin_elementwise_maximum(up, x) : up;
+    }
+    const float after = __builtin_elementwise_maximum(R, up), left = __shfl_up(after, 1, 64), before = lane == 0 ? R : left;
+    const float x = shift2(before, after), y = shift2(d[0], after), sy = d[1], sc = d[2] * y;
     for (int t0 = 0; t0 < n; t0 += U) {
-      float p[U][E];
+      Vec v[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          p[u][e] = t0 + u < n && lane + 64 * e < HD ? parts[(c0 + t0 + u) * (HD + 4) + lane + 64 * e] : 0.0f;
+      for (int u = 0; u < U; ++u) v[u] = *reinterpret_cast<const Vec*>(p + (t0 + u < n ? t0 + u : n - 1) * (HD + 4) + at);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        if (t0 + u >= n) break;
-        const float r = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(d[0]), t0 + u));
-        const float s = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(d[1]), t0 + u));
-        const float v = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(d[2]), t0 + u));
-        const float Rn = __builtin_elementwise_maximum(R, r), x = shift2(R, Rn), y = shift2(r, Rn);
-        S = __builtin_fmaf(s, y, S * x);
-        const float sc = v * y;
+        const int t = t0 + u;
+        if (t >= n) break;
+        auto of = [&](float f) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), t)); };
+        const float xt = of(x), st = of(sc);
+        S = __builtin_fmaf(of(sy), of(y), S * xt);
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(p[u][e], sc, o[e] * x);
-        R = Rn;
+        for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(v[u][e], st, o[e] * xt);
       }
     }
+    R = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(after), n - 1));
   }
+  if (lane * E >= HD) return;
   const float inv = S == 0.0f ? 0.0f : 1.0f / S;
 #pragma unroll
-  for (int e = 0; e < E; ++e)
-    if (lane + 64 * e < HD) {
-      const float x = o[e] + 0.0f;
-      a.out[row * HD + lane + 64 * e] = S == 0.0f ? 0 : f32_to_bf16(x * inv);
-    }
+  for (int e = 0; e < E; e += 2) {
+    const float f0 = o[e] + 0.0f, f1 = o[e + 1] + 0.0f;
+    struct __attribute__((packed, aligned(2))) H2 { uint32_t x; };
+    reinterpret_cast<H2*>(a.out + row * HD + at + e)->x = S == 0.0f ? 0u : pack_bf16(f0 * inv, f1 * inv);
+  }
 }
 
 // ---- all keys of a block of queries in one workgroup: prompts -------------------------------------------------------------
