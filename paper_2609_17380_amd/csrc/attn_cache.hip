@@ -30,6 +30,10 @@ constexpr float kDigits = 32512.0f;             // largest whole number of a que
 constexpr uint32_t kInvDigits = 0x38010204u;    // RN32(1 / 32512)
 constexpr float kNegInf = -__builtin_inff();
 
+#define CANON_NAN4 __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")
+__device__ const __attribute__((aligned(16))) float kNanSteps[16] = {CANON_NAN4, CANON_NAN4, CANON_NAN4, CANON_NAN4};
+#undef CANON_NAN4
+
 // 2^x, |x| <= 1/2: the polynomial of least relative error with the constant 1, its coefficients rounded: 2.9e-6 in all, a fifth of
 // what rounding the weights to 16 bits leaves.
 constexpr uint32_t kExp2C[4] = {0x3F317096u, 0x3E7601BCu, 0x3D64FE23u, 0x3C1D0166u};
@@ -49,9 +53,8 @@ __device__ __forceinline__ float cexp2(float x) {
 // the weight of a score u f against the reference: fused where r is small enough that what r's own rounding leaves above it
 // (2^-9) does not carry a weight past its digits
 __device__ __forceinline__ float weight(float u, float f, float ref, bool near) {
-  if (near) return cexp2(__builtin_fmaf(u, f, -ref));
-  const float t = u * f;
-  return cexp2(t - ref);
+  const float fused = __builtin_fmaf(u, f, -ref), t = u * f, far = t - ref;
+  return cexp2(near ? fused : far);
 }
 __device__ __forceinline__ bool near_ref(float ref) { return fabsf(ref) <= 65536.0f; }
 
@@ -90,9 +93,9 @@ struct Column {
 };
 __device__ __forceinline__ Column column_of(const CacheAttnArgs& a, int64_t b, int32_t kvh, int64_t idx) {
   Column c;
-  const int32_t G = a.heads / a.c.heads;
-  const int64_t i = idx / G;
-  c.h = kvh * G + (int32_t)(idx - i * G);
+  const uint32_t G = (uint32_t)(a.heads / a.c.heads), iq = (uint32_t)idx / G;  // rows of a call: below 2^24
+  const int64_t i = iq;
+  c.h = kvh * (int32_t)G + (int32_t)((uint32_t)idx - iq * G);
   c.real = i < a.q_len;
   c.tok = b * a.q_len + i;
   c.row = c.tok * a.heads + c.h;
@@ -110,6 +113,16 @@ __device__ __forceinline__ Column column_of(const CacheAttnArgs& a, int64_t b, i
   if (c.lo >= c.hi) c.lo = c.hi = 0;
   return c;
 }
+// which of a tile's keys a column sees: those from lo on, n of them
+struct Seen {
+  int32_t lo, n;
+  __device__ __forceinline__ bool key(int32_t at) const { return (uint32_t)(at - lo) < (uint32_t)n; }
+};
+__device__ __forceinline__ Seen seen_of(const Column& c, int64_t t0) {
+  const int64_t lo = c.lo > t0 ? c.lo - t0 : 0, hi = c.hi - t0;
+  const int32_t l = lo < kTile ? (int32_t)lo : kTile, h = hi < 0 ? 0 : hi < kTile ? (int32_t)hi : kTile;
+  return Seen{l, h > l ? h - l : 0};
+}
 
 // the 16 keys from j on (a multiple of 16): their first slot in head kvh, or -1
 __device__ __forceinline__ int64_t slot16(const CacheAttnArgs& a, int32_t kvh, int64_t j, int32_t page) {
@@ -122,7 +135,16 @@ __device__ __forceinline__ int32_t page_of(const CacheAttnArgs& a, int64_t b, in
 
 __device__ __forceinline__ i32x4 load16(const int8_t* p) { return *reinterpret_cast<const i32x4*>(p); }
 
-// The queries of a block as digits: lane (c, g) holds elements 64 s + 16 g .. + 15 of column c, and the column's f.
+// The queries of a block: lane (c, g) has elements 64 s + 16 g .. + 15 of column c, first as they are stored (asked for early),
+// then as digits with the column's f.
+struct __attribute__((packed, aligned(2))) U16x8 {
+  uint32_t w[4];
+};
+template <int HD>
+struct RawQuery {
+  static constexpr int NS = (HD + 63) / 64;
+  uint32_t w[NS][16];
+};
 template <int HD>
 struct Query {
   static constexpr int NS = (HD + 63) / 64;
@@ -130,36 +152,42 @@ struct Query {
   float f;
 };
 template <int HD>
-__device__ __forceinline__ void load_query(const CacheAttnArgs& a, const Column& c, Query<HD>& out) {
+__device__ __forceinline__ void ask_query(const CacheAttnArgs& a, const Column& c, RawQuery<HD>& r) {
+  const int g = (threadIdx.x & 63) >> 4;
+  const int64_t at = c.real ? c.tok * a.q_stride + (int64_t)c.h * HD : 0;  // an unreal column: the first row, unused
+#pragma unroll
+  for (int s = 0; s < RawQuery<HD>::NS; ++s) {
+    const int d = HD % 64 == 0 || 64 * s + 16 * g < HD ? 64 * s + 16 * g : 0;
+    const char* p = (const char*)a.q + (at + d) * (a.q_bf16 ? 2 : 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (i >= 2 && a.q_bf16) break;
+      const U16x8 x = reinterpret_cast<const U16x8*>(p)[i];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r.w[s][4 * i + e] = x.w[e];
+    }
+  }
+}
+template <int HD>
+__device__ __forceinline__ void make_query(const CacheAttnArgs& a, const Column& c, const RawQuery<HD>& r, Query<HD>& out) {
   constexpr int NS = Query<HD>::NS;
   const int g = (threadIdx.x & 63) >> 4;
   float v[NS][16];
   uint32_t top = 0;
 #pragma unroll
   for (int s = 0; s < NS; ++s) {
-    const int d = 64 * s + 16 * g;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) v[s][e] = 0.0f;
-    if (c.real && d < HD) {
-      const int64_t at = c.tok * a.q_stride + (int64_t)c.h * HD + d;
-#pragma unroll
-      for (int e = 0; e < 16; e += 4) {
-        float t[4];
-        if (a.q_bf16) ldb<4>((const uint16_t*)a.q + at + e, t);
-        else ldf<4>((const float*)a.q + at + e, t);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[s][e + i] = t[i];
-      }
-    }
+    const bool has = c.real && (HD % 64 == 0 || 64 * s + 16 * g < HD);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
+      const uint32_t half = e & 1 ? r.w[s][e >> 1] & 0xFFFF0000u : r.w[s][e >> 1] << 16;
+      v[s][e] = has ? __uint_as_float(a.q_bf16 ? half : r.w[s][e]) : 0.0f;
       const uint32_t u = __float_as_uint(v[s][e]) & 0x7FFFFFFFu;
       top = u > top ? u : top;
     }
   }
   top = umax4(top);
   const float sq = __uint_as_float(top) * __uint_as_float(kInvDigits);
-  const float rs = sq > 0.0f ? 1.0f / sq : 0.0f;
+  const float rs = sq > 0.0f ? 1.0f / sq : 0.0f, sgn = a.scale < 0.0f ? -rs : rs;  // a product's sign passes its rounding
 #pragma unroll
   for (int s = 0; s < NS; ++s)
 #pragma unroll
@@ -167,7 +195,7 @@ __device__ __forceinline__ void load_query(const CacheAttnArgs& a, const Column&
       uint32_t h = 0, l = 0;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        float x = (a.scale < 0.0f ? -v[s][4 * w + e] : v[s][4 * w + e]) * rs;
+        float x = v[s][4 * w + e] * sgn;
         x = sq > 0.0f && x == x ? fminf(fmaxf(x, -kDigits), kDigits) : 0.0f;
         const int32_t n = (int32_t)__builtin_rintf(x), d = (n + 128) >> 8;  // n = 256 d + (n - 256 d), the rest in [-128, 127]
         h |= (uint32_t)(d & 0xFF) << (8 * e);
@@ -223,59 +251,55 @@ __global__ __launch_bounds__(256) void attn_tile_kernel(CacheAttnArgs a, int64_t
   __shared__ __attribute__((aligned(16))) i32x4 wts[2][4][64];
   __shared__ float ms[4][16], ss[4][16];
   __shared__ uint32_t vs[4][16];
-  int64_t id = blockIdx.x;
-  const int64_t tile = id % tiles;
-  id /= tiles;
-  const int64_t cb = id % blocks;
-  id /= blocks;
-  const int32_t kvh = (int32_t)(id % a.c.heads);
-  const int64_t b = id / a.c.heads;
+  const uint32_t id = blockIdx.x, bt = id / (uint32_t)tiles, bk = bt / (uint32_t)blocks;
+  const int64_t tile = id - bt * (uint32_t)tiles, cb = bt - bk * (uint32_t)blocks;
+  const int64_t b = bk / (uint32_t)a.c.heads;
+  const int32_t kvh = (int32_t)(bk - (uint32_t)b * (uint32_t)a.c.heads);
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, cc = lane & 15, g = lane >> 4;
-  const int64_t t0 = tile * kTile, j0 = t0 + 64 * w;
-  const int32_t kpage = page_of(a, b, j0 + 16 * (cc >> 2));
+  const int64_t t0 = tile * kTile;
+  const int at0 = 64 * w + 16 * g;  // of this lane's 16 keys in the tile
+  // which pages, and the queries: asked for before anything is waited for
+  const int32_t kpage = page_of(a, b, t0 + 64 * w + 16 * (cc >> 2));
   int32_t vpage[4];
 #pragma unroll
   for (int q = 0; q < 4; ++q) vpage[q] = page_of(a, b, t0 + 64 * q + 16 * g);
   const Column col = column_of(a, b, kvh, cb * 16 + cc);
-  const bool touched = col.lo < t0 + kTile && col.hi > t0;
-  if (tiles > 1 && !__any(touched)) return;  // the join passes over tiles that a row does not see
+  RawQuery<HD> raw;
+  ask_query<HD>(a, col, raw);
+  const Seen sees = seen_of(col, t0);
+  if (tiles > 1 && !__any(sees.n > 0)) return;  // the join passes over tiles that a row does not see
 
-  // the cache: the slots are known, everything is asked for before anything is waited for
-  const int64_t kslot = slot16(a, kvh, j0 + 16 * (cc >> 2), kpage);
-  int64_t vslot[4];
+  // The cache, all at once.  Slots that it does not have: any of its codes (their weights are 0, or their steps NaN).
+  int64_t kslot = slot16(a, kvh, t0 + 64 * w + 16 * (cc >> 2), kpage), vslot[4];
 #pragma unroll
   for (int q = 0; q < 4; ++q) vslot[q] = slot16(a, kvh, t0 + 64 * q + 16 * g, vpage[q]);
   const int64_t gslot = w == 0 ? vslot[0] : w == 1 ? vslot[1] : w == 2 ? vslot[2] : vslot[3];
-  i32x4 kx[4][NS];
+  kslot = kslot < 0 ? 0 : kslot;
+  i32x4 kx[4][NS], vx[NW][4];
 #pragma unroll
   for (int t = 0; t < 4; ++t)
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      kx[t][s] = i32x4{0, 0, 0, 0};
-      if (kslot >= 0 && (HD % 64 == 0 || 64 * s + 16 * g < HD))
-        kx[t][s] = load16(a.c.kc + (kslot + 4 * t + (cc & 3)) * HD + 64 * s + 16 * g);
-    }
+    for (int s = 0; s < NS; ++s)  // elements behind a head of 32 (mod 64): its first ones, which meet digits of 0
+      kx[t][s] = load16(a.c.kc + (kslot + 4 * t + (cc & 3)) * HD + (HD % 64 == 0 || 64 * s + 16 * g < HD ? 64 * s + 16 * g : 0));
+  typedef const __attribute__((address_space(1))) f32x4* GlobalVec;  // or the choice between the two arrays makes flat loads
+  const GlobalVec kp = (GlobalVec)(uintptr_t)(gslot < 0 ? kNanSteps : a.c.ks + gslot);
+  const GlobalVec vp = (GlobalVec)(uintptr_t)(gslot < 0 ? kNanSteps : a.c.vs + gslot);
   f32x4 kst[4], vst[4];
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
-    kst[t] = vst[t] = f32x4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
-    if (gslot >= 0) {
-      kst[t] = *reinterpret_cast<const f32x4*>(a.c.ks + gslot + 4 * t);
-      vst[t] = *reinterpret_cast<const f32x4*>(a.c.vs + gslot + 4 * t);
-    }
+    kst[t] = kp[t];
+    vst[t] = vp[t];
   }
-  i32x4 vx[NW][4];
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
+    const int8_t* p = a.c.vc + (vslot[q] < 0 ? 0 : vslot[q]) * HD + 16 * cc;
 #pragma unroll
-    for (int n = 0; n < NW; ++n) {
-      const int part = w + 4 * n;
-      vx[n][q] = i32x4{0, 0, 0, 0};
-      if (vslot[q] >= 0 && (ND % 4 == 0 || part < ND)) vx[n][q] = load16(a.c.vc + vslot[q] * HD + (16 * part + cc) * 16);
-    }
+    for (int n = 0; n < NW; ++n) vx[n][q] = load16(p + 256 * (ND % 4 == 0 || w + 4 * n < ND ? w + 4 * n : 0));
   }
+  // the loads stay before the queries' divisions (left to itself, the compiler asked for keys and values when they were used)
+  __builtin_amdgcn_sched_barrier(0);
   Query<HD> qd;
-  load_query<HD>(a, col, qd);
+  make_query<HD>(a, col, raw, qd);
 
   float t[4][4];
   float m = kNegInf;
@@ -290,8 +314,7 @@ __global__ __launch_bounds__(256) void attn_tile_kernel(CacheAttnArgs a, int64_t
     for (int s = 0; s < NS; ++s) acc = mfma(kx[k][s], qd.lo[s], acc);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int64_t j = j0 + 16 * g + 4 * k + i;
-      const bool seen = j >= col.lo && j < col.hi;
+      const bool seen = sees.key(at0 + 4 * k + i);
       t[k][i] = seen ? (float)acc[i] * kst[k][i] : kNegInf;
       m = __builtin_elementwise_maximum(m, t[k][i]);
       const uint32_t u = seen ? __float_as_uint(vst[k][i]) & 0x7FFFFFFFu : 0u;
@@ -320,9 +343,9 @@ __global__ __launch_bounds__(256) void attn_tile_kernel(CacheAttnArgs a, int64_t
     f32x4 ratio;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int64_t j = j0 + 16 * g + 4 * k + i;
-      const bool seen = j >= col.lo && j < col.hi;
-      e[i] = seen ? weight(t[k][i], qd.f, ref, near) : 0.0f;
+      const bool seen = sees.key(at0 + 4 * k + i);
+      e[i] = weight(t[k][i], qd.f, ref, near);
+      e[i] = seen ? e[i] : 0.0f;
       sum = sum + e[i];
       const float x = vst[k][i] * rv;
       ratio[i] = rv != 0.0f && seen ? x : 0.0f;
@@ -377,7 +400,7 @@ __global__ __launch_bounds__(64) void attn_join_kernel(CacheAttnArgs a, int64_t 
   typedef float Vec __attribute__((ext_vector_type(E)));
   const int64_t row = blockIdx.x;
   const int lane = threadIdx.x, at = lane * E < HD ? lane * E : 0;
-  const int64_t tok = row / a.heads, b = tok / a.q_len;
+  const int64_t tok = (uint32_t)row / (uint32_t)a.heads, b = (uint32_t)tok / (uint32_t)a.q_len;  // rows of a call: below 2^24
   const int32_t G = a.heads / a.c.heads, h = (int32_t)(row - tok * a.heads);
   const Column col = column_of(a, b, h / G, (tok - b * a.q_len) * G + h % G);
   const float* parts = a.parts + row * tiles * (HD + 4);
@@ -405,8 +428,8 @@ __global__ __launch_bounds__(64) void attn_join_kernel(CacheAttnArgs a, int64_t 
       for (int u = 0; u < U; ++u) v[u] = *reinterpret_cast<const Vec*>(p + (t0 + u < n ? t0 + u : n - 1) * (HD + 4) + at);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int t = t0 + u;
-        if (t >= n) break;
+        const int t = t0 + u < n ? t0 + u : n - 1;
+        if (t0 + u >= n) continue;
         auto of = [&](float f) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), t)); };
         const float xt = of(x), st = of(sc);
         S = __builtin_fmaf(of(sy), of(y), S * xt);
@@ -433,8 +456,6 @@ __global__ __launch_bounds__(64) void attn_join_kernel(CacheAttnArgs a, int64_t 
 // reading has no bank conflicts and no address is computed per lane), a wavefront fetching its quarter of the tile: the next
 // tile's keys while the present one's weights are computed, its values while the next scores are.  Two workgroups a CU (heads
 // of up to 128) run out of step, one's products under the other's exponentials.
-__device__ const float kNanStep = __builtin_nanf("");
-
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
 // 16 (or 4) bytes a lane from global memory to LDS, lane l's at lds + 16 l (4 l); not tracked by the compiler: vm_left waits
@@ -467,9 +488,9 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void attn_rows_kernel(Cache
   typedef const __attribute__((address_space(4))) int32_t* ConstInts;  // the table through the scalar cache
   __shared__ __attribute__((aligned(1024))) RowsLds<HD> L;
   // workgroups of one head of a sequence on one XCD where their number allows it, the longest causal rows first
-  const int64_t bh = blockIdx.x % (a.c.heads * a.c.batch), cb = blocks - 1 - blockIdx.x / (a.c.heads * a.c.batch);
-  const int32_t kvh = (int32_t)(bh % a.c.heads);
-  const int64_t b = bh / a.c.heads;
+  const uint32_t n_bh = (uint32_t)(a.c.heads * a.c.batch), turn = blockIdx.x / n_bh, bh = blockIdx.x - turn * n_bh;
+  const int64_t cb = blocks - 1 - turn, b = bh / (uint32_t)a.c.heads;
+  const int32_t kvh = (int32_t)(bh - (uint32_t)b * (uint32_t)a.c.heads);
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), cc = lane & 15, g = lane >> 4;
   const Column col = column_of(a, b, kvh, (cb * 4 + w) * 16 + cc);
   int32_t lo = col.hi > col.lo ? (int32_t)col.lo : 0x7FFFFFFF, hi = (int32_t)col.hi;  // k_len fits
@@ -486,7 +507,11 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void attn_rows_kernel(Cache
     L.span[w][1] = hi;
   }
   Query<HD> qd;
-  load_query<HD>(a, col, qd);
+  {
+    RawQuery<HD> raw;
+    ask_query<HD>(a, col, raw);
+    make_query<HD>(a, col, raw, qd);
+  }
   __syncthreads();
   int32_t all_lo = 0x7FFFFFFF, all_hi = 0;
 #pragma unroll
@@ -522,8 +547,8 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void attn_rows_kernel(Cache
 #pragma unroll
       for (int e = 0; e < NS; ++e)  // elements behind a head of 32 (mod 64): its first ones, which meet digits of 0
         dma16(p + 4 * t * HD + (HD % 64 == 0 || 64 * e + 16 * g < HD ? 64 * e + 16 * g : 0), lk + 1024 * ((4 * w + t) * NS + e));
-    dma4(gs < 0 ? &kNanStep : a.c.ks + gs + cc, lks + 1024 * par + 256 * w);
-    dma4(gs < 0 ? &kNanStep : a.c.vs + gs + cc, lvs + 1024 * par + 256 * w);
+    dma4(gs < 0 ? kNanSteps : a.c.ks + gs + cc, lks + 1024 * par + 256 * w);
+    dma4(gs < 0 ? kNanSteps : a.c.vs + gs + cc, lvs + 1024 * par + 256 * w);
   };
   auto fetch_values = [&](const int64_t (&s)[4]) {
     int64_t vs = pick(s, g);
@@ -550,7 +575,8 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void attn_rows_kernel(Cache
     __syncthreads();
     fetch_values(slots);
     const bool mine = lo < t0 + kTile && hi > t0;
-    const bool all = mine && __all(!col.real || (col.lo <= t0 && col.hi >= t0 + kTile));
+    const Seen sees = seen_of(col, t0);
+    const bool all = mine && __all(!col.real || sees.n == kTile);
     // quarters of the tile that some query of this wavefront sees
     const int q0 = lo > t0 ? (lo - t0) >> 6 : 0, q1 = !mine ? 0 : hi - t0 < kTile ? (hi - t0 + 63) >> 6 : 4;
     float u[4][4][4];
@@ -582,10 +608,7 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void attn_rows_kernel(Cache
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             u[q][t][i] = (float)acc[t][i] * st[i];
-            if (!all) {
-              const int32_t j = t0 + 64 * q + 16 * g + 4 * t + i;
-              u[q][t][i] = j >= col.lo && j < col.hi ? u[q][t][i] : kNegInf;
-            }
+            if (!all) u[q][t][i] = sees.key(64 * q + 16 * g + 4 * t + i) ? u[q][t][i] : kNegInf;
             m = __builtin_elementwise_maximum(m, u[q][t][i]);
           }
         }
@@ -629,9 +652,9 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void attn_rows_kernel(Cache
           for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const int32_t at = 64 * q + 16 * g + 4 * t + i, j = t0 + at;
+              const int32_t at = 64 * q + 16 * g + 4 * t + i;
               const uint32_t x = __float_as_uint(L.vs[par][at]) & 0x7FFFFFFFu;
-              vtop = j >= col.lo && j < col.hi && x > vtop ? x : vtop;
+              vtop = sees.key(at) && x > vtop ? x : vtop;
             }
       vtop = umax4(vtop);
     }
@@ -663,9 +686,9 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void attn_rows_kernel(Cache
           const f32x4 vst = *reinterpret_cast<const f32x4*>(&L.vs[par][64 * q + 16 * g + 4 * t]);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int32_t j = t0 + 64 * q + 16 * g + 4 * t + i;
-            const bool seen = j >= col.lo && j < col.hi;
-            e[i] = seen ? weight(u[q][t][i], qd.f, ref, near) : 0.0f;
+            const bool seen = sees.key(64 * q + 16 * g + 4 * t + i);
+            e[i] = weight(u[q][t][i], qd.f, ref, near);
+            e[i] = seen ? e[i] : 0.0f;
             sum = sum + e[i];
             const float x = vst[i] * rv;
             ratio[i] = rv != 0.0f && seen ? x : 0.0f;
