@@ -627,17 +627,20 @@ canon_status canon_cache_read(const canon_kv_cache* cache, const canon_cache_row
      query:  sq = RN(amax * RN(1/32512)), rs = CRdiv(1, sq), Q = clamp(rne(RN(q rs)), -32512, 32512) (0 for a NaN or a step
              that is not > 0; -q in place of q for a negative scale), f = RN(RN(sq |scale|) * RN(log2 e))
      scores: u_j = RN(RN32(sum_d Q_d K_jd) kstep_j), the sum exact; they stand for u_j f
-     tile:   r = ceil(RN(max u_j f)) (-inf where the largest u_j is), e_j = cexp2(fma(u_j, f, -r)), or cexp2(RN(RN(u_j f) - r))
-             where |r| > 65536 (r read as 0 where it is -inf), S_b = the 16 sums of 16 consecutive keys' e, each a chain from
-             +0, joined by a perfect pairwise tree; keys that are not seen are +0 terms
-             V = the largest vstep of the keys that are seen, by bit pattern, rv = CRdiv(32512, V) (0 if V is not > 0 or rv is
-             infinite), w_j = rne(e_j RN(vstep_j rv)) (0 for all where rv = 0), A_d = sum_j w_j V_jd, exact
+     tile:   r = ceil(RN(max u_j f)) (-inf where the largest u_j is; read as 0 there in what follows)
+             x_j = 128 (clamp(y_j, 0, 1) - 1), y_j = fma(u_j, RN(f / 128), RN(1 - RN(r / 128))), or where |r| > 65536
+             fma(RN(RN(u_j f) - r), 1/128, 1); e_j = exp2(x_j)
+             S_b = the 16 sums of 16 consecutive keys' 4 e, each a chain from +0, joined by a perfect pairwise tree, times 1/4;
+             keys that are not seen are +0 terms; 0 where r is -inf, NaN where a u_j is NaN or r is +inf
+             V = the largest vstep of the keys that are seen, by bit pattern, rv = CRdiv(32512 / 4, V) (0 if V is not > 0 or rv
+             is infinite), w_j = rne(4 e_j RN(vstep_j rv)) (0 for all where rv = 0), A_d = sum_j w_j V_jd, exact
      row:    over the tiles with a key that is seen, ascending, from R = -inf, S = 0, O = 0: R' = max(R, r),
              x = 2^(R - R'), y = 2^(r - R') (1 where R, or r, is -inf; 0 below 2^-126), S = fma(S_b, y, RN(S x)),
              O_d = fma(RN32(A_d), RN(RN(V * RN(1/32512)) y), RN(O_d x))
      out:    bf16(RN(RN(O_d + 0) CRdiv(1, S))), +0 where S = 0 (no key seen, or only scores of -inf)
-   cexp2(x): n = rne(max(x, -126.4)), p = 1 + t (C1 + t (C2 + t (C3 + t C4))) by fma with t = max(x, -126.4) - n, RN(p 2^n); the
-   C are 0x3F317096, 0x3E7601BC, 0x3D64FE23, 0x3C1D0166: 2^t within 2.9e-6 of itself.  A query's row is the same in a prompt and alone, whatever the batch and the other sequences are.  Queries and
+   exp2(x): n = rne(x), p = 1 + t (C1 + t (C2 + t (C3 + t C4))) by fma with t = x - n, p 2^n; the C are 0x3F317096, 0x3E7601BC,
+   0x3D64FE23, 0x3C1D0166: 2^t within 2.9e-6 of itself, a fifth of what rounding the weights leaves.
+   A query's row is the same in a prompt and alone, whatever the batch and the other sequences are.  Queries and
    weights enter with 16 bits (two digits of 8): a part of 2^-16 of the largest, below the last place of bf16.  What stands
    in places that are not seen (in unused slots, pages and table entries too) is not used; a key that is seen in a page that the
    cache does not have makes the row NaN.

@@ -91,21 +91,21 @@ int cref_cache_append(const int64_t* cache, const int32_t* table, int64_t q_len,
   return 0;
 }
 
-static float exp2_neg(float x) { /* R26's cexp2, x <= 2^-9 or NaN */
-  if (x != x) return x;
-  const float at = x > -126.4f ? x : -126.4f;
-  const float n = rintf(at), u = cref_sub(at, n);
+/* R26's weight of a score: 2^(128 (y - 1)), y in [0, 1] */
+static float exp2_unit(float y) {
+  const float n = (float)nearbyint(128.0 * (double)y) - 128.0f, t = (float)(128.0 * (double)y - 128.0 - (double)n);
   float p = of_bits(0x3C1D0166u);
-  p = cref_fma(p, u, of_bits(0x3D64FE23u));
-  p = cref_fma(p, u, of_bits(0x3E7601BCu));
-  p = cref_fma(p, u, of_bits(0x3F317096u));
-  p = cref_fma(p, u, 1.0f);
-  return cref_mul(p, ldexpf(1.0f, (int)n));
+  p = cref_fma(p, t, of_bits(0x3D64FE23u));
+  p = cref_fma(p, t, of_bits(0x3E7601BCu));
+  p = cref_fma(p, t, of_bits(0x3F317096u));
+  p = cref_fma(p, t, 1.0f);
+  return ldexpf(p, (int)n + 2); /* four times it: a normal number */
 }
-int cref_exp2_neg(int64_t n, const float* x, float* y) {
-  for (int64_t i = 0; i < n; ++i) y[i] = exp2_neg(x[i]);
+int cref_exp2_unit(int64_t n, const float* y, float* e4) {
+  for (int64_t i = 0; i < n; ++i) e4[i] = exp2_unit(y[i]);
   return 0;
 }
+static float unit(float x) { return x > 0.0f ? (x < 1.0f ? x : 1.0f) : 0.0f; } /* 0 for a NaN */
 
 /* 2^(a - b) of whole a <= b */
 static float shift(float a, float b) {
@@ -137,7 +137,7 @@ int cref_cache_attention(const int64_t* cache, const int64_t* cfg, float scale, 
       Q[d] = !(sq > 0.0f) || v != v ? 0 : v > 32512.0f ? 32512 : v < -32512.0f ? -32512 : (int64_t)rintf(v);
     }
     const float f = cref_mul(cref_mul(sq, fabsf(scale)), of_bits(0x3FB8AA3Bu)); /* RN32(1 / ln 2) */
-    float R = -INFINITY, S = 0.0f, O[256];
+    float R = -INFINITY, S = 0.0f, O[256]; /* a NaN among the scores makes R and S NaN */
     for (int64_t d = 0; d < D; ++d) O[d] = 0.0f;
     for (int64_t j0 = 0; j0 < KL; j0 += 256) {
       float t[256], e[256], m = -INFINITY;
@@ -154,16 +154,20 @@ int cref_cache_attention(const int64_t* cache, const int64_t* cfg, float scale, 
         int64_t acc = 0;
         for (int64_t d = 0; slot[j] >= 0 && d < D; ++d) acc += Q[d] * kc[slot[j] * D + d];
         t[j] = slot[j] < 0 ? NAN : cref_mul((float)acc, ks[slot[j]]);
-        if (t[j] > m) m = t[j];
+        if (t[j] > m || t[j] != t[j] || m != m) m = t[j] != t[j] || m != m ? NAN : t[j];
         const uint32_t u = slot[j] < 0 ? 0x7FC00000u : to_bits(vs[slot[j]]) & 0x7FFFFFFFu;
         if (u > vtop) vtop = u;
       }
       if (!any) continue;
       const float rb = m == -INFINITY ? m : ceilf(cref_mul(m, f)), V = of_bits(vtop);
-      const float ref = rb == -INFINITY ? 0.0f : rb;
-      for (int64_t j = 0; j < 256; ++j)
-        e[j] = !sees[j] ? 0.0f
-               : fabsf(ref) <= 65536.0f ? exp2_neg(cref_fma(t[j], f, -ref)) : exp2_neg(cref_sub(cref_mul(t[j], f), ref));
+      const float ref = rb == -INFINITY ? 0.0f : rb, part7 = 0.0078125f;
+      for (int64_t j = 0; j < 256; ++j) {
+        e[j] = 0.0f;
+        if (!sees[j]) continue;
+        const float near = cref_fma(t[j], cref_mul(f, part7), cref_sub(1.0f, cref_mul(ref, part7)));
+        const float far = cref_fma(cref_sub(cref_mul(t[j], f), ref), part7, 1.0f);
+        e[j] = exp2_unit(unit(fabsf(ref) <= 65536.0f ? near : far));
+      }
       float part[16];
       for (int c = 0; c < 16; ++c) {
         part[c] = 0.0f;
@@ -171,11 +175,12 @@ int cref_cache_attention(const int64_t* cache, const int64_t* cfg, float scale, 
       }
       for (int n = 16; n > 1; n /= 2)
         for (int c = 0; c < n / 2; ++c) part[c] = cref_add(part[2 * c], part[2 * c + 1]);
-      float rv = V > 0.0f ? cref_div(32512.0f, V) : 0.0f;
+      float rv = V > 0.0f ? cref_div(8128.0f, V) : 0.0f; /* 32512 / 4 */
       if (!(rv < INFINITY)) rv = 0.0f;
-      const float Rn = R > rb ? R : rb, xo = shift(R, Rn), y = shift(rb, Rn);
+      const float Rn = R != R || rb != rb ? NAN : R > rb ? R : rb, xo = shift(R, Rn), y = shift(rb, Rn);
       const float scale_v = cref_mul(cref_mul(V, inv), y);
-      S = cref_fma(part[0], y, cref_mul(S, xo));
+      const float Sb = rb == -INFINITY ? 0.0f : rb < INFINITY ? cref_mul(part[0], 0.25f) : NAN;
+      S = cref_fma(Sb, y, cref_mul(S, xo));
       for (int64_t d = 0; d < D; ++d) {
         int64_t A = 0;
         for (int64_t j = 0; j < 256; ++j)

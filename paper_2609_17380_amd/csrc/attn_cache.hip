@@ -13,6 +13,8 @@
 // No lane ever needs another's weights, and a query's maxima and sums cross 4 lanes.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "act8_dev.h"
 #include "canon_dev.h"
 #include "canon_internal.h"
@@ -38,25 +40,46 @@ __device__ const __attribute__((aligned(16))) float kNanSteps[16] = {CANON_NAN4,
 // what rounding the weights to 16 bits leaves.
 constexpr uint32_t kExp2C[4] = {0x3F317096u, 0x3E7601BCu, 0x3D64FE23u, 0x3C1D0166u};
 
-// cexp2 of x <= 2^-9 or NaN (which the maximum passes on).  n goes to the exponent by an integer addition; -126.4, where the
-// clamp sends all that lies below, has n = -126 and p < 1, a subnormal pattern, which every use reads as zero.
-__device__ __forceinline__ float cexp2(float x) {
-  x = __builtin_elementwise_maximum(x, -126.4f);
-  const float u = x + 0x1.8p23f;  // rne(x), also in the low bits
-  const float f = x - (u - 0x1.8p23f);
+// Four times the weight 2^x of a score u f against the reference r, x = 128 (y - 1) with y = u f / 128 + 1 - r / 128 held to
+// [0, 1] (the clamp costs nothing on the multiply-add, and holds what r's own rounding leaves above it): f7 = f / 128, c = 1 - r /
+// 128.  n + 2, n = rne(x), goes to the exponent by an integer addition; for 128 <= -x the smallest normal number comes of it.
+constexpr float kExpShift = 12582786.0f;  // 1.5 2^23 - 126
+__device__ __forceinline__ float weight4(float y) {
+  const float t = __builtin_fmaf(y, 128.0f, kExpShift), g = t - kExpShift;  // n + 2 in the low bits; n + 128
+  const float f = __builtin_fmaf(y, 128.0f, -g);
   float p = __builtin_fmaf(__uint_as_float(kExp2C[3]), f, __uint_as_float(kExp2C[2]));
   p = __builtin_fmaf(p, f, __uint_as_float(kExp2C[1]));
   p = __builtin_fmaf(p, f, __uint_as_float(kExp2C[0]));
   p = __builtin_fmaf(p, f, 1.0f);
-  return __uint_as_float(__float_as_uint(p) + (__float_as_uint(u) << 23));
+  return __uint_as_float(__float_as_uint(p) + (__float_as_uint(t) << 23));
 }
-// the weight of a score u f against the reference: fused where r is small enough that what r's own rounding leaves above it
-// (2^-9) does not carry a weight past its digits
-__device__ __forceinline__ float weight(float u, float f, float ref, bool near) {
-  const float fused = __builtin_fmaf(u, f, -ref), t = u * f, far = t - ref;
-  return cexp2(near ? fused : far);
-}
-__device__ __forceinline__ bool near_ref(float ref) { return fabsf(ref) <= 65536.0f; }
+__device__ __forceinline__ float to_unit(float x) { return __builtin_amdgcn_fmed3f(x, 0.0f, 1.0f); }
+// A tile's reference for one query.  Beyond 65536 the fused form would lose the largest score itself to r's rounding: it is taken
+// apart there.
+struct Ref {
+  float r, f, f7, c, ref;
+  bool near;
+  __device__ __forceinline__ Ref(float m, float f_) : f(f_) {
+    const float mf = m * f;
+    r = m == kNegInf ? m : __builtin_ceilf(mf);
+    ref = r == kNegInf ? 0.0f : r;
+    near = fabsf(ref) <= 65536.0f;
+    f7 = f * 0.0078125f;
+    const float r7 = ref * 0.0078125f;
+    c = 1.0f - r7;
+  }
+  __device__ __forceinline__ float y_near(float u) const { return to_unit(__builtin_fmaf(u, f7, c)); }
+  __device__ __forceinline__ float y(float u) const {
+    const float t = u * f, x = t - ref;
+    const float far = to_unit(__builtin_fmaf(x, 0.0078125f, 1.0f));
+    return near ? y_near(u) : far;
+  }
+  // a tile's sum: of quarters, 0 where no score is above -inf, NaN where one is NaN or +inf
+  __device__ __forceinline__ float sum(float s4) const {
+    const float s = s4 * 0.25f;
+    return r == kNegInf ? 0.0f : r < __builtin_inff() ? s : __builtin_nanf("");
+  }
+};
 
 // 2^(a - b) of whole a <= b, 1 where a is -inf
 __device__ __forceinline__ float shift2(float a, float b) {
@@ -220,10 +243,10 @@ __device__ __forceinline__ void digits4(const float (&e)[4], const f32x4& ratio,
   hi = (int32_t)__builtin_amdgcn_perm(cd, ab, 0x07060302u);
 }
 
-// what a tile's values are scaled by: rv (0 where all weights are) and RN(V RN(1/32512))
+// what a tile's value steps are multiplied by: a quarter (the weights come times 4) of 32512 / V, 0 where all weights are
 __device__ __forceinline__ float value_recip(uint32_t vtop) {
   const float V = __uint_as_float(vtop);
-  const float rv = V > 0.0f ? kDigits / V : 0.0f;
+  const float rv = V > 0.0f ? 0.25f * kDigits / V : 0.0f;
   return rv < __builtin_inff() ? rv : 0.0f;
 }
 
@@ -333,8 +356,8 @@ __global__ __launch_bounds__(256) void attn_tile_kernel(CacheAttnArgs a, int64_t
     m = __builtin_elementwise_maximum(m, ms[o][cc]);
     vtop = vs[o][cc] > vtop ? vs[o][cc] : vtop;
   }
-  const float mf = m * qd.f, r = m == kNegInf ? m : __builtin_ceilf(mf), ref = r == kNegInf ? 0.0f : r, rv = value_recip(vtop);
-  const bool near = near_ref(ref);
+  const Ref rf(m, qd.f);
+  const float rv = value_recip(vtop);
   float sum = 0.0f;
   i32x4 wh, wl;
 #pragma unroll
@@ -344,7 +367,7 @@ __global__ __launch_bounds__(256) void attn_tile_kernel(CacheAttnArgs a, int64_t
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const bool seen = sees.key(at0 + 4 * k + i);
-      e[i] = weight(t[k][i], qd.f, ref, near);
+      e[i] = weight4(rf.y(t[k][i]));
       e[i] = seen ? e[i] : 0.0f;
       sum = sum + e[i];
       const float x = vst[k][i] * rv;
@@ -360,12 +383,12 @@ __global__ __launch_bounds__(256) void attn_tile_kernel(CacheAttnArgs a, int64_t
   sum = sum4(sum);
   if (g == 0) ss[w][cc] = sum;
   __syncthreads();
-  const float S = (ss[0][cc] + ss[1][cc]) + (ss[2][cc] + ss[3][cc]);
+  const float S = rf.sum((ss[0][cc] + ss[1][cc]) + (ss[2][cc] + ss[3][cc]));
   const float vsc = __uint_as_float(vtop) * __uint_as_float(kInvDigits);
   const float inv = S == 0.0f ? 0.0f : 1.0f / S;
   float* parts = a.parts + (col.row * tiles + tile) * (HD + 4);
   if (tiles > 1 && col.real && w == 0 && g == 0)
-    *reinterpret_cast<f32x4*>(parts + HD) = f32x4{r, S, vsc, 0.0f};
+    *reinterpret_cast<f32x4*>(parts + HD) = f32x4{rf.r, S, vsc, 0.0f};
 #pragma unroll
   for (int n = 0; n < NW; ++n) {
     const int part = w + 4 * n;
@@ -533,6 +556,7 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void attn_rows_kernel(Cache
     for (int i = 0; i < 4; ++i) {
       const int32_t j = t0 + 64 * w + 16 * i;
       s[i] = j < (int32_t)a.k_len ? slot16(a, kvh, j, table[j >> a.c.lg]) : -1;
+      asm volatile("" : "+s"(s[i]));  // in scalar registers, for the picks below to be selections
     }
   };
   auto pick = [](const int64_t (&s)[4], int i) { return i == 0 ? s[0] : i == 1 ? s[1] : i == 2 ? s[2] : s[3]; };
@@ -569,25 +593,21 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void attn_rows_kernel(Cache
     group_slots(t0, slots);
     fetch_keys(slots, 0);
   }
-  for (; t0 < all_hi; t0 += kTile, par ^= 1) {
-    // this tile's keys have landed, and every wavefront is done with the last one's values
-    vm_left<0>();
-    __syncthreads();
-    fetch_values(slots);
-    const bool mine = lo < t0 + kTile && hi > t0;
-    const Seen sees = seen_of(col, t0);
-    const bool all = mine && __all(!col.real || sees.n == kTile);
+  // One tile.  FULL: every query of the wavefront sees all of it, so that nothing is masked.
+  auto tile = [&](auto full, bool mine, const Seen& sees) {
+    constexpr bool FULL = full.value;
     // quarters of the tile that some query of this wavefront sees
-    const int q0 = lo > t0 ? (lo - t0) >> 6 : 0, q1 = !mine ? 0 : hi - t0 < kTile ? (hi - t0 + 63) >> 6 : 4;
+    const int q0 = FULL || lo <= t0 ? 0 : (lo - t0) >> 6;
+    const int q1 = FULL ? 4 : !mine ? 0 : hi - t0 < kTile ? (hi - t0 + 63) >> 6 : 4;
     float u[4][4][4];
     float m = kNegInf;
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      if (q >= q0 && q < q1) {
-        i32x4 acc[4];
+      if (FULL || (q >= q0 && q < q1)) {
+        i32x4 acc[4], kx[4][NS];
 #pragma unroll
         for (int t = 0; t < 4; ++t) acc[t] = i32x4{0, 0, 0, 0};
-        i32x4 kx[4][NS];
 #pragma unroll
         for (int s = 0; s < NS; ++s)
 #pragma unroll
@@ -608,7 +628,7 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void attn_rows_kernel(Cache
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             u[q][t][i] = (float)acc[t][i] * st[i];
-            if (!all) u[q][t][i] = sees.key(64 * q + 16 * g + 4 * t + i) ? u[q][t][i] : kNegInf;
+            if (!FULL) u[q][t][i] = sees.key(64 * q + 16 * g + 4 * t + i) ? u[q][t][i] : kNegInf;
             m = __builtin_elementwise_maximum(m, u[q][t][i]);
           }
         }
@@ -619,6 +639,7 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void attn_rows_kernel(Cache
           for (int i = 0; i < 4; ++i) u[q][t][i] = kNegInf;
       }
     }
+    __builtin_amdgcn_s_setprio(0);
     // every wavefront is done with the keys: the next tile's
     __syncthreads();
     const bool more = t0 + kTile < all_hi;
@@ -628,7 +649,7 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void attn_rows_kernel(Cache
     }
     // the largest step of the values that a query sees, and what each of them is to it
     uint32_t vtop = 0;
-    if (all) {
+    if constexpr (FULL) {
       const f32x4 vst = *reinterpret_cast<const f32x4*>(&L.vs[par][4 * lane]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -659,49 +680,62 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void attn_rows_kernel(Cache
       vtop = umax4(vtop);
     }
     m = max4(m);
-    const float mf = m * qd.f, r = m == kNegInf ? m : __builtin_ceilf(mf), ref = r == kNegInf ? 0.0f : r;
-    const float rv = value_recip(vtop);
-    const bool near = near_ref(ref), near_all = __all(near);
+    const Ref rf(m, qd.f);
+    const float r = rf.r;
     i32x4 wh[4], wl[4];
     float sums[4];
+    if (FULL && __all(rf.near)) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      wh[q] = wl[q] = i32x4{0, 0, 0, 0};
-      wl[q] = i32x4{0, 0, 0, 0};
-      sums[q] = 0.0f;
-      if (q < q0 || q >= q1) continue;
-      float sum = 0.0f;
+      for (int q = 0; q < 4; ++q) {
+        float sum = 0.0f;
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        float e[4];
-        f32x4 ratio;
-        if (all && near_all) {
-          ratio = *reinterpret_cast<const f32x4*>(&L.ratio[w][64 * q + 16 * g + 4 * t]);
+        for (int t = 0; t < 4; ++t) {
+          const f32x4 ratio = *reinterpret_cast<const f32x4*>(&L.ratio[w][64 * q + 16 * g + 4 * t]);
+          float e[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            e[i] = cexp2(__builtin_fmaf(u[q][t][i], qd.f, -ref));
+            e[i] = weight4(rf.y_near(u[q][t][i]));
             sum = sum + e[i];
           }
-        } else {
+          int32_t h, l;
+          digits4(e, ratio, h, l);
+          wh[q][t] = h;
+          wl[q][t] = l;
+        }
+        sums[q] = sum4(sum);
+      }
+    } else {
+      const float rv = value_recip(vtop);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        wh[q] = i32x4{0, 0, 0, 0};
+        wl[q] = i32x4{0, 0, 0, 0};
+        sums[q] = 0.0f;
+        if (q < q0 || q >= q1) continue;
+        float sum = 0.0f;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
           const f32x4 vst = *reinterpret_cast<const f32x4*>(&L.vs[par][64 * q + 16 * g + 4 * t]);
+          f32x4 ratio;
+          float e[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const bool seen = sees.key(64 * q + 16 * g + 4 * t + i);
-            e[i] = weight(u[q][t][i], qd.f, ref, near);
+            const bool seen = FULL || sees.key(64 * q + 16 * g + 4 * t + i);
+            e[i] = weight4(rf.y(u[q][t][i]));
             e[i] = seen ? e[i] : 0.0f;
             sum = sum + e[i];
             const float x = vst[i] * rv;
             ratio[i] = rv != 0.0f && seen ? x : 0.0f;
           }
+          int32_t h, l;
+          digits4(e, ratio, h, l);
+          wh[q][t] = h;
+          wl[q][t] = l;
         }
-        int32_t h, l;
-        digits4(e, ratio, h, l);
-        wh[q][t] = h;
-        wl[q][t] = l;
+        sums[q] = sum4(sum);
       }
-      sums[q] = sum4(sum);
     }
-    const float Sb = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+    const float Sb = rf.sum((sums[0] + sums[1]) + (sums[2] + sums[3]));
     const float Rn = __builtin_elementwise_maximum(R, r), x = shift2(R, Rn), y = shift2(r, Rn);
     // A column that sees nothing of the tile has S_b = 0, A = 0 and V = 0 and keeps R: the steps below leave its row as it is
     // (but for the sign of a zero, which the output's + 0 takes away).
@@ -713,33 +747,47 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void attn_rows_kernel(Cache
     if (more) vm_left<4 * NS + 2>();
     else vm_left<0>();
     __syncthreads();
-    if (mine) {
+    if (!FULL && !mine) return;
+    if (!still) {
 #pragma unroll
-      for (int n = 0; n < ND; n += 2) {
-        i32x4 acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}}, vx[2][4];
+      for (int n = 0; n < ND; ++n)
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-#pragma unroll
-          for (int d = 0; d < 2; ++d) vx[d][q] = L.v[q * ND + n + d][lane];
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-#pragma unroll
-          for (int d = 0; d < 2; ++d) acc[d] = mfma(vx[d][q], wh[q], acc[d]);
-#pragma unroll
-        for (int d = 0; d < 2; ++d) acc[d] = acc[d] << 8;
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-#pragma unroll
-          for (int d = 0; d < 2; ++d) acc[d] = mfma(vx[d][q], wl[q], acc[d]);
-#pragma unroll
-        for (int d = 0; d < 2; ++d)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float p = still ? o[n + d][i] : o[n + d][i] * x;
-            o[n + d][i] = __builtin_fmaf((float)acc[d][i], sc, p);
-          }
-      }
+        for (int i = 0; i < 4; ++i) o[n][i] = o[n][i] * x;
     }
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int n = 0; n < ND; n += 2) {
+      i32x4 acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}}, vx[2][4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int d = 0; d < 2; ++d) vx[d][q] = L.v[q * ND + n + d][lane];
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int d = 0; d < 2; ++d) acc[d] = mfma(vx[d][q], wh[q], acc[d]);
+#pragma unroll
+      for (int d = 0; d < 2; ++d) acc[d] = acc[d] << 8;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int d = 0; d < 2; ++d) acc[d] = mfma(vx[d][q], wl[q], acc[d]);
+#pragma unroll
+      for (int d = 0; d < 2; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[n + d][i] = __builtin_fmaf((float)acc[d][i], sc, o[n + d][i]);
+    }
+    __builtin_amdgcn_s_setprio(0);
+  };
+  for (; t0 < all_hi; t0 += kTile, par ^= 1) {
+    // this tile's keys have landed, and every wavefront is done with the last one's values
+    vm_left<0>();
+    __syncthreads();
+    fetch_values(slots);
+    const bool mine = lo < t0 + kTile && hi > t0;
+    const Seen sees = seen_of(col, t0);
+    if (mine && __all(!col.real || sees.n == kTile)) tile(std::true_type{}, mine, sees);
+    else tile(std::false_type{}, mine, sees);
   }
   if (!col.real) return;
   const float inv = S == 0.0f ? 0.0f : 1.0f / S;
@@ -776,7 +824,8 @@ static hipError_t attn_go(const CacheAttnArgs& a, hipStream_t s) {
   const int64_t cols = a.q_len * (a.heads / a.c.heads);
   if (!p.split) {
     const int64_t blocks = (cols + 63) / 64;
-    hipLaunchKernelGGL((attn_rows_kernel<HD>), dim3((unsigned)(blocks * a.c.heads * a.c.batch)), dim3(256), 0, s, a, blocks);
+    const int64_t n = blocks * a.c.heads * a.c.batch;
+    hipLaunchKernelGGL((attn_rows_kernel<HD>), dim3((unsigned)n), dim3(256), 0, s, a, blocks);
     return hipGetLastError();
   }
   const int64_t blocks = (cols + 15) / 16, tiles = p.tiles > 0 ? p.tiles : 1;
