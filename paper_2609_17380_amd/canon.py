@@ -717,29 +717,34 @@ class KVCache(ctypes.Structure):
                [("batch", ctypes.c_int64), ("table_len", ctypes.c_int64), ("table", ctypes.c_void_p)]
 
     def __init__(self, page, kv_heads, dim, k_codes, v_codes, k_steps, v_steps, table):
-        self.tensors = k_codes, v_codes, k_steps, v_steps
-        if not all(isinstance(t, torch.Tensor) for t in (*self.tensors, table)):
-            raise ValueError("codes, steps and table: tensors are needed")
         one = page * kv_heads * dim
-        if page < 1 or kv_heads < 1 or dim < 1 or k_codes.numel() % one:
-            raise ValueError(f"k_codes: pages of {one} codes are needed")
-        super().__init__(k_codes.numel() // one, page, kv_heads, dim)
+        if not isinstance(k_codes, torch.Tensor) or page < 1 or kv_heads < 1 or dim < 1 or k_codes.numel() % one:
+            raise ValueError(f"k_codes: a tensor of pages of {one} codes is needed")
+        codes = k_codes.numel()
+        self.tensors, self.device = (k_codes, v_codes, k_steps, v_steps), k_codes.get_device()
+        super().__init__(codes // one, page, kv_heads, dim, _arg(k_codes, "k_codes", codes, _TI8, self.device),
+                         _arg(v_codes, "v_codes", codes, _TI8, self.device),
+                         _arg(k_steps, "k_steps", codes // dim, _T32, self.device),
+                         _arg(v_steps, "v_steps", codes // dim, _T32, self.device))
+        if not all(isinstance(t, torch.Tensor) for t in (v_codes, k_steps, v_steps)):
+            raise ValueError("codes and steps: tensors are needed")
         self.set_table(table)
 
     def set_table(self, table):
         """The pages of other sequences, or more of the same ones'."""
         if not isinstance(table, torch.Tensor) or table.dim() != 2:
             raise ValueError("table: a tensor [batch, table_len] is needed")
-        self.pages = table
-        self.batch, self.table_len = table.shape
+        batch, table_len = table.shape
+        self.table = _arg(table, "table", batch * table_len, _TI32, self.device)
+        self.pages, self.batch, self.table_len = table, batch, table_len
 
     def _of(self, dev):
-        """The record's address, once its tensors are a cache's on the current device."""
-        steps = self.n_pages * self.page * self.n_kv_heads
-        for name, t, n, dtypes in zip(("k_codes", "v_codes", "k_steps", "v_steps"), self.tensors,
-                                      (steps * self.head_dim,) * 2 + (steps,) * 2, (_TI8, _TI8, _T32, _T32)):
-            setattr(self, name, _arg(t, name, n, dtypes, dev))
-        self.table = _arg(self.pages, "table", self.batch * self.table_len, _TI32, dev)
+        """The record's address, with the present addresses of tensors that were checked when they came."""
+        if dev != self.device:
+            raise ValueError(f"a cache on the current device is needed, not on device {self.device}")
+        k, v, ks, vs = self.tensors
+        self.k_codes, self.v_codes, self.k_steps, self.v_steps = k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr()
+        self.table = self.pages.data_ptr()
         return ctypes.byref(self)
 
 
@@ -786,8 +791,7 @@ def cache_read(cache: KVCache, rows: CacheRows, k=None, v=None, stream=None):
 
 
 def cache_attention_workspace_bytes(cache: KVCache, rows: AttnRows) -> int:
-    dev = _device()
-    return int(_lib().canon_cache_attention_workspace_bytes(cache._of(dev), rows._of(dev)))
+    return int(_lib().canon_cache_attention_workspace_bytes(ctypes.byref(cache), ctypes.byref(rows)))
 
 
 def cache_attention(cache: KVCache, rows: AttnRows, q, out, workspace=None, order=ORDER_V1, stream=None):

@@ -287,8 +287,9 @@ hipError_t relbias_bwd_launch(const RelBiasArgs& a, const uint16_t* probs, const
 // ---- products with a step per token (gemm_i8.hip, gemm_i8_rows.hip) ----
 hipError_t quant_tokens_launch(int64_t rows, int64_t cols, int32_t bf16, const void* x, int8_t* codes, float* steps,
                                hipStream_t s);
-constexpr bool gemm_i8_few_rows(int64_t m) { return m <= 64; }
+constexpr bool gemm_i8_few_rows(int64_t m) { return m <= 16; }
 hipError_t gemm_i8_rows_launch(const GemmI8Args& g, hipStream_t s);  // of them
+hipError_t gemm_i8_split_launch(const GemmI8Args& g, int cus, hipStream_t s);  // gemm_i8_split.hip
 
 // ---- rotary positions, the paged cache in 8 bits (rope.hip) and attention over it (attn_cache.hip) ----
 struct Turn {  // a rotation; rot 0: none

@@ -11,10 +11,10 @@
 // Tiling: whole 256 x 256 tiles (m, n multiples of 256, k of 64) run on 4 wavefronts, each a 128 x 128 block of
 // 4 x 4 v_mfma_i32_32x32x32_i8 instructions, with direct-to-LDS loads three stages ahead (gemm_i8_tile_kernel).
 // Other shapes: a workgroup of NW wavefronts owns a 16 NW HB x 64 WN output tile, each wavefront a 32 HB x 32 WN
-// block: 256 x 256 tiles of 8 wavefronts with 64-byte stages for large products, else 128 x 128 tiles of 4
-// wavefronts with 128-byte stages; their stages of KS k bytes are staged through registers into LDS (rows
-// padded by 16 bytes, which keeps the 16-byte operand reads of 32 consecutive rows free of bank conflicts),
-// double buffered.
+// block: 128 x 128 tiles of 8 wavefronts, two workgroups a CU (256 x 256 tiles of 8, one a CU: 8191 x 5000 x 8192
+// 822 us, so 495); their stages of KS = 128 k bytes are staged through registers into LDS (rows padded by 16 bytes,
+// which keeps the 16-byte operand reads of 32 consecutive rows free of bank conflicts), double buffered.
+// Few rows, or few tiles: gemm_i8_rows.hip, gemm_i8_split.hip.
 // Each lane of a 32x32x32 instruction supplies 16 consecutive k bytes of one row of A and of B; the two
 // half-wavefronts cover k 0..15 and 16..31 of the instruction's 32.
 #include <hip/hip_runtime.h>
@@ -52,15 +52,14 @@ struct I8Raw {
   uint4 a[Cf::AV], b[Cf::BV];
 };
 
-// 16 consecutive bytes of which the first `valid` exist (zero fill beyond); rows off 16-byte boundaries load as wide (byte by
-// byte, 1541 x 5001 x 2056 took 1280 us)
-template <bool FAST>
-__device__ __forceinline__ uint4 ld16(const int8_t* p, int64_t valid) {
-  if (FAST) return *reinterpret_cast<const uint4*>(p);
-  if (valid >= 16) {
-    const I8x16 v = *reinterpret_cast<const I8x16*>(p);
-    return make_uint4(v.x, v.y, v.z, v.w);
-  }
+// 16 consecutive bytes; rows off 16-byte boundaries load as wide
+__device__ __forceinline__ uint4 ld16(const int8_t* p) {
+  const I8x16 v = *reinterpret_cast<const I8x16*>(p);
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
+// the first `valid` of them (zero fill beyond)
+__device__ __forceinline__ uint4 ld16_cut(const int8_t* p, int64_t valid) {
+  if (valid >= 16) return ld16(p);
   uint32_t w[4] = {0u, 0u, 0u, 0u};
   for (int e = 0; e < 16; ++e)
     if (e < valid) w[e >> 2] |= (uint32_t)(uint8_t)p[e] << (8 * (e & 3));
@@ -68,25 +67,26 @@ __device__ __forceinline__ uint4 ld16(const int8_t* p, int64_t valid) {
 }
 
 // Global -> registers for the stage starting at k0: vector idx = t + NT it covers row idx / (KS/16),
-// 16-byte segment idx % (KS/16) of the row's KS bytes.
-template <class Cf, int KS, bool FAST>
-__device__ __forceinline__ I8Raw<Cf> load_stage(const GemmI8Args& g, int64_t row0, int64_t col0, int64_t k0) {
+// 16-byte segment idx % (KS/16) of the row's KS bytes.  Rows behind the last are read as the last: what they give is not
+// stored.  WHOLE: the stage lies within k.
+template <class Cf, int KS, bool WHOLE>
+__device__ __forceinline__ void load_stage(const GemmI8Args& g, int64_t row0, int64_t col0, int64_t k0, I8Raw<Cf>& r) {
   constexpr int SEG = KS / 16;
   const int t = threadIdx.x;
-  I8Raw<Cf> r;
 #pragma unroll
   for (int it = 0; it < Cf::AV; ++it) {
     const int idx = t + Cf::NT * it;
     const int64_t k = k0 + 16 * (idx % SEG), row = row0 + idx / SEG;
-    r.a[it] = ld16<FAST>(g.a + row * g.lda + k, (row < g.m) ? g.k - k : 0);
+    const int8_t* p = g.a + (row < g.m ? row : g.m - 1) * g.lda + k;
+    r.a[it] = WHOLE ? ld16(p) : ld16_cut(p, g.k - k);
   }
 #pragma unroll
   for (int it = 0; it < Cf::BV; ++it) {
     const int idx = t + Cf::NT * it;
     const int64_t k = k0 + 16 * (idx % SEG), col = col0 + idx / SEG;
-    r.b[it] = ld16<FAST>(g.b + col * g.ldb + k, (col < g.n) ? g.k - k : 0);
+    const int8_t* p = g.b + (col < g.n ? col : g.n - 1) * g.ldb + k;
+    r.b[it] = WHOLE ? ld16(p) : ld16_cut(p, g.k - k);
   }
-  return r;
 }
 
 template <class Cf, int KS>
@@ -124,7 +124,6 @@ __global__ __launch_bounds__(64 * NW) void gemm_i8_kernel(GemmI8Args g) {
   const int64_t gsize = (tiles_m - first_m) < GM ? (tiles_m - first_m) : GM;
   const int64_t within = tile - group * GM * tiles_n;
   const int64_t row0 = (first_m + within % gsize) * BM, col0 = (within / gsize) * BN;
-  const bool tile_in = g.vec && row0 + BM <= g.m && col0 + BN <= g.n;
 
   // wavefront (wr, wc) owns rows [32 HB wr, 32 HB (wr + 1)) and columns [32 WN wc, 32 WN (wc + 1)) of the tile
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
@@ -140,17 +139,16 @@ __global__ __launch_bounds__(64 * NW) void gemm_i8_kernel(GemmI8Args g) {
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[h][v2][v] = 0;
 
+  // Stage s is multiplied out of LDS while stage s + 1 waits in registers and stage s + 2 is on its way (with one stage ahead,
+  // a memory latency passed in every stage: 1541 x 5001 x 2056 in 256 x 256 tiles 85 us, then 77).
   const int64_t ns = (g.k + KS - 1) / KS;
-  int buf = 0;
-  if (ns > 0) store_stage<Cf, KS>(As[0], Bs[0], load_stage<Cf, KS, false>(g, row0, col0, 0));
-  __syncthreads();
-  for (int64_t s = 0; s < ns; ++s) {
-    const bool more = s + 1 < ns;
-    I8Raw<Cf> nxt;
-    if (more) {
-      if (tile_in && (s + 2) * KS <= g.k) nxt = load_stage<Cf, KS, true>(g, row0, col0, (s + 1) * KS);
-      else nxt = load_stage<Cf, KS, false>(g, row0, col0, (s + 1) * KS);
-    }
+  I8Raw<Cf> raw[2];
+  auto load = [&](int64_t st, I8Raw<Cf>& r) {
+    if ((st + 1) * KS <= g.k) load_stage<Cf, KS, true>(g, row0, col0, st * KS, r);
+    else load_stage<Cf, KS, false>(g, row0, col0, st * KS, r);
+  };
+  auto stage = [&](int64_t st, int buf, I8Raw<Cf>& next, I8Raw<Cf>& after) {
+    if (st + 2 < ns) load(st + 2, after);
     __builtin_amdgcn_sched_barrier(0);
     const int8_t* as = As[buf];
     const int8_t* bs = Bs[buf];
@@ -169,9 +167,18 @@ __global__ __launch_bounds__(64 * NW) void gemm_i8_kernel(GemmI8Args g) {
           acc[h][v2] = __builtin_amdgcn_mfma_i32_32x32x32_i8(a[h], b[v2], acc[h][v2], 0, 0, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
-    if (more) store_stage<Cf, KS>(As[buf ^ 1], Bs[buf ^ 1], nxt);
+    if (st + 1 < ns) store_stage<Cf, KS>(As[buf ^ 1], Bs[buf ^ 1], next);
     __syncthreads();
-    buf ^= 1;
+  };
+  if (ns > 0) {
+    load(0, raw[0]);
+    if (ns > 1) load(1, raw[1]);
+    store_stage<Cf, KS>(As[0], Bs[0], raw[0]);
+  }
+  __syncthreads();
+  for (int64_t s = 0; s < ns; s += 2) {
+    stage(s, 0, raw[1], raw[0]);
+    if (s + 1 < ns) stage(s + 1, 1, raw[0], raw[1]);
   }
 
   // result layout: register v, lane l -> row (v % 4) + 4 (l / 32) + 8 (v / 4), column l % 32 of the block
@@ -432,24 +439,19 @@ hipError_t gemm_i8_launch(const GemmI8Args& gin, hipStream_t s) {
   if (gin.sa_rows && gemm_i8_few_rows(gin.m)) return gemm_i8_rows_launch(gin, s);
   GemmI8Args g = gin;
   g.vec = ((uintptr_t)g.a & 15) == 0 && ((uintptr_t)g.b & 15) == 0 && g.lda % 16 == 0 && g.ldb % 16 == 0;
-  // 256 x 256 tiles of 8 wavefronts (one workgroup per CU, 64-byte stages) halve the operand bytes staged per
-  // multiply-add and run a tile's work about 1.12x faster than four 128 x 128 tiles of 4 wavefronts (two
-  // workgroups per CU); they are taken unless their coarser rounds of workgroups over the CUs cost more
   int dev = 0, cus = 0;
   if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) !=
                                               hipSuccess || cus <= 0)
     cus = 256;
-  const int64_t small_tiles = ((g.m + 127) / 128) * ((g.n + 127) / 128);
-  const int64_t big_tiles = ((g.m + 255) / 256) * ((g.n + 255) / 256);
-  const double small_time = (double)((small_tiles + 2 * cus - 1) / (2 * cus));        // rounds of one tile time
-  const double big_time = (double)((big_tiles + cus - 1) / cus) * (2.0 / 1.12);
-  // whole 256 x 256 tiles (and 16-byte output stores: y, acc and ldc aligned to 4 elements): the pipelined
-  // kernel with 128 x 128 wavefront blocks
+  // Whole 256 x 256 tiles (and 16-byte output stores: y, acc and ldc aligned to 4 elements) that fill three quarters of the CUs
+  // or more: the pipelined kernel (8192 x 16384 x 2048 310 us).  With fewer of them (256 x 2048 x 8192: 113 us in 8 tiles, 15 in
+  // 256 smaller ones), and where 128 x 128 tiles are fewer than the CUs (700 x 2048 x 2048: 21 us in 96, 17 in 352 smaller
+  // ones), k is split over the wavefronts.
   const bool whole = g.vec && g.m % 256 == 0 && g.n % 256 == 0 && g.ldc % 4 == 0 && ((uintptr_t)g.y & 15) == 0 &&
-                     ((uintptr_t)g.acc & 15) == 0;
-  if (whole && g.k % 64 == 0 && g.k > 0) return launch_i8_tile(g, s);
-  if (big_time < small_time) return launch_i8<2, 4, 64, 8>(g, s);
-  return launch_i8<2, 2, 128, 4>(g, s);
+                     ((uintptr_t)g.acc & 15) == 0 && g.k % 64 == 0 && g.k > 0;
+  if (whole && (g.m / 256) * (g.n / 256) >= 3 * cus / 4) return launch_i8_tile(g, s);
+  if (((g.m + 127) / 128) * ((g.n + 127) / 128) < cus) return gemm_i8_split_launch(g, cus, s);
+  return launch_i8<1, 2, 128, 8>(g, s);
 }
 
 }  // namespace canon

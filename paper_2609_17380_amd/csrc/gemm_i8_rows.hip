@@ -114,10 +114,13 @@ static hipError_t quant_go(int64_t rows, int64_t cols, const void* x, int8_t* co
     };
     using N64 = std::integral_constant<int, 64>;
     using N256 = std::integral_constant<int, 256>;
+    using N1024 = std::integral_constant<int, 1024>;
     if (cols <= 256) go(N64{}, std::integral_constant<int, 1>{});
     else if (cols <= 512) go(N64{}, std::integral_constant<int, 2>{});
     else if (cols <= 1024) go(N256{}, std::integral_constant<int, 1>{});
     else if (cols <= 2048) go(N256{}, std::integral_constant<int, 2>{});
+    else if (rows < 256 && cols <= 4096) go(N1024{}, std::integral_constant<int, 1>{});
+    else if (rows < 256 && cols <= 8192) go(N1024{}, std::integral_constant<int, 2>{});
     else if (cols <= 4096) go(N256{}, std::integral_constant<int, 4>{});
     else if (cols <= 8192) go(N256{}, std::integral_constant<int, 8>{});
     else if (cols <= 16384) go(N256{}, std::integral_constant<int, 16>{});
@@ -132,8 +135,8 @@ hipError_t quant_tokens_launch(int64_t rows, int64_t cols, int32_t bf16, const v
 }
 
 // ---- few tokens -----------------------------------------------------------------------------------------------------------
-// What counts is the weights' stream.  A workgroup takes CW channels over all of k, its 8 wavefronts every eighth 64 bytes of
-// them, so that a channel's row is read in runs of 512 bytes and the whole chip has loads in flight however few the channels
+// What counts is the weights' stream.  A workgroup takes CW channels over all of k, its 8 wavefronts every eighth cache line of
+// them, so that a channel's row is read in runs of 1024 bytes and the whole chip has loads in flight however few the channels
 // are; the partial sums are whole numbers and are joined through LDS in any order.  Channels are the rows of
 // v_mfma_i32_16x16x64_i8 and tokens its columns: lane (c, g) supplies bytes 16 g .. + 15 of channel c and of token c, and
 // receives channels 4 g .. 4 g + 3 of token c, which it stores together.  With CW = 8 half of the rows stay empty.
@@ -162,48 +165,67 @@ __device__ __forceinline__ i32x4 row16(const int8_t* p, int64_t valid, bool long
   return r;
 }
 
-template <int MT, int CW>
+template <int CW, int U>
 __global__ __launch_bounds__(512) void gemm_i8_rows_kernel(GemmI8Args g) {
-  constexpr int NW = 8, U = MT > 2 ? 2 : 4;  // 64-byte steps in flight
-  __shared__ __attribute__((aligned(16))) i32x4 part[NW][MT][64];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, c = lane & 15, q = lane >> 4;
+  constexpr int NW = 8;
+  __shared__ __attribute__((aligned(16))) i32x4 part[NW][64];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, q = lane >> 4;
   const int64_t col0 = (int64_t)blockIdx.x * CW;
   const int64_t ch = col0 + c;
   const bool has = c < CW && ch < g.n;
-  const int8_t* bp = g.b + (has ? ch : 0) * g.ldb;
-  const int8_t* ap[MT];
-  bool tok[MT];
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    tok[i] = 16 * i + c < g.m;
-    ap[i] = g.a + (tok[i] ? 16 * i + c : 0) * g.lda;
-  }
-  i32x4 acc[MT];
-#pragma unroll
-  for (int i = 0; i < MT; ++i) acc[i] = i32x4{0, 0, 0, 0};
-  const bool longer = g.k >= 16;
-  for (int64_t k0 = 64 * w + 16 * q; k0 - 16 * q < g.k; k0 += 64 * NW * U) {
-    i32x4 b[U], a[U][MT];
+  const int8_t* bp = g.b + (has ? ch : 0) * g.ldb + 16 * q;
+  const bool tok = c < g.m;
+  const int8_t* ap = g.a + (tok ? c : 0) * g.lda + 16 * q;
+  i32x4 acc = {0, 0, 0, 0};
+  auto vec = [](const int8_t* p) {
+    const B16 v = *reinterpret_cast<const B16*>(p);
+    return i32x4{(int32_t)v.w[0], (int32_t)v.w[1], (int32_t)v.w[2], (int32_t)v.w[3]};
+  };
+  // Whole steps: this wavefront has 2 w, 2 w + 1 (a cache line), 16 + 2 w, ...  Workgroups begin at different ones: tokens' rows a power of two apart come
+  // from the same few channels of the L2, and all workgroups would ask for the same bytes at once.
+  const int32_t steps = (int32_t)(g.k >> 6), rest = (steps & 15) - 2 * w;
+  const int32_t mine = 2 * (steps >> 4) + (rest > 1 ? 2 : rest > 0 ? rest : 0);
+  const int32_t rot = mine > 1 ? 2 * (int32_t)((blockIdx.x >> 3) % (uint32_t)(mine >> 1)) : 0;  // by 8: within an XCD
+  for (int32_t j0 = 0; j0 < mine; j0 += U) {
+    i32x4 b[U], a[U];
+    int64_t at[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t k = k0 + 64 * NW * u, valid = g.k - k;
-      b[u] = row16(bp + k, has ? valid : 0, longer);
-#pragma unroll
-      for (int i = 0; i < MT; ++i) a[u][i] = row16(ap[i] + k, tok[i] ? valid : 0, longer);
+      int32_t j = (j0 + u < mine ? j0 + u : mine - 1) + rot;
+      j = j < mine ? j : j - mine;
+      at[u] = 64 * (int64_t)(16 * (j >> 1) + 2 * w + (j & 1));
     }
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U; ++u) b[u] = i32x4{0, 0, 0, 0};
+    if (has) {
 #pragma unroll
-      for (int i = 0; i < MT; ++i) acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b[u], a[u][i], acc[i], 0, 0, 0);
+      for (int u = 0; u < U; ++u) b[u] = vec(bp + at[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) a[u] = i32x4{0, 0, 0, 0};
+    if (tok) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) a[u] = vec(ap + at[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (j0 + u >= mine) break;
+      acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(b[u], a[u], acc, 0, 0, 0);
+    }
   }
-#pragma unroll
-  for (int i = 0; i < MT; ++i) part[w][i][lane] = acc[i];
+  if ((g.k & 63) && w == (steps & (NW - 1))) {  // the cut step
+    const int64_t valid = (g.k & 63) - 16 * q;
+    const bool longer = g.k >= 16;
+    const i32x4 b = row16(bp + 64 * (int64_t)steps, has ? valid : 0, longer);
+    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(b, row16(ap + 64 * (int64_t)steps, tok ? valid : 0, longer), acc, 0, 0, 0);
+  }
+  part[w][lane] = acc;
   __syncthreads();
-  if (w >= MT) return;  // wavefront i finishes tokens 16 i .. + 15
+  if (w > 0) return;
   i32x4 sum = {0, 0, 0, 0};
 #pragma unroll
-  for (int o = 0; o < NW; ++o) sum = sum + part[o][w][lane];
-  const int64_t i = 16 * w + c;
+  for (int o = 0; o < NW; ++o) sum = sum + part[o][lane];
+  const int64_t i = c;
   if (i >= g.m || 4 * q >= CW) return;
   const float sa = g.sa[i];
   const int64_t j0 = col0 + 4 * q;
@@ -232,18 +254,18 @@ __global__ __launch_bounds__(512) void gemm_i8_rows_kernel(GemmI8Args g) {
 }
 
 hipError_t gemm_i8_rows_launch(const GemmI8Args& g, hipStream_t s) {
-  auto go = [&](auto mt, auto cw) {
-    hipLaunchKernelGGL((gemm_i8_rows_kernel<mt.value, cw.value>), dim3((unsigned)((g.n + cw.value - 1) / cw.value)), dim3(512), 0,
+  auto go = [&](auto cw, auto u) {
+    hipLaunchKernelGGL((gemm_i8_rows_kernel<cw.value, u.value>), dim3((unsigned)((g.n + cw.value - 1) / cw.value)), dim3(512), 0,
                        s, g);
     return hipGetLastError();
   };
-  auto width = [&](auto mt) {
-    if (g.n <= 2048) return go(mt, std::integral_constant<int, 8>{});
-    return go(mt, std::integral_constant<int, 16>{});
+  auto depth = [&](auto cw) {  // as many steps on their way as a wavefront has, up to 8
+    if (g.k < 64 * 8 * 8) return go(cw, std::integral_constant<int, 4>{});
+    return go(cw, std::integral_constant<int, 8>{});
   };
-  if (g.m <= 16) return width(std::integral_constant<int, 1>{});
-  if (g.m <= 32) return width(std::integral_constant<int, 2>{});
-  return width(std::integral_constant<int, 4>{});
+  // half as many channels a workgroup where there would be fewer workgroups than CUs
+  if (g.n <= 2048) return depth(std::integral_constant<int, 8>{});
+  return depth(std::integral_constant<int, 16>{});
 }
 
 }  // namespace canon

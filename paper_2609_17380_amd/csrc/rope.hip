@@ -207,29 +207,49 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, CacheRow
       wide_in<XB, 4>(k, ka + at, kv[0]);
       if (at < t.rot) {
         const bool in_table = pos < t.positions;
-        float o[4], cs[4], sn[4];
+        const float* cp = t.cos + pos * half;
+        const float* sp = t.sin + pos * half;
+        float o[4];
         if (t.interleaved) {  // elements at, at + 1 and at + 2, at + 3 together
 #pragma unroll
           for (int e = 0; e < 4; e += 2) {
-            const bool two = at + e < t.rot;
-            const float cc = !two ? 1.0f : in_table ? t.cos[pos * half + (at + e) / 2] : __builtin_nanf("");
-            const float ss = !two ? 0.0f : in_table ? t.sin[pos * half + (at + e) / 2] : __builtin_nanf("");
-            if (two) turn_pair(kv[0][e], kv[0][e + 1], cc, ss, o[e], o[e + 1]);
-            else { o[e] = kv[0][e]; o[e + 1] = kv[0][e + 1]; }
+            if (at + e < t.rot) {
+              const float cc = in_table ? cp[(at + e) / 2] : __builtin_nanf(""), ss = in_table ? sp[(at + e) / 2] : __builtin_nanf("");
+              turn_pair(kv[0][e], kv[0][e + 1], cc, ss, o[e], o[e + 1]);
+            } else {
+              o[e] = kv[0][e];
+              o[e + 1] = kv[0][e + 1];
+            }
+          }
+        } else if (t.rot % 8 == 0) {  // four elements of one half, with the same four of the other
+          const int p = at < half ? at : at - half;
+          float other[4], cs[4], sn[4];
+          wide_in<XB, 4>(k, ka + (at < half ? at + half : p), other);
+          if (in_table) {
+            ldf<4>(cp + p, cs);
+            ldf<4>(sp + p, sn);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) cs[e] = sn[e] = __builtin_nanf("");
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float x, y;
+            turn_pair(at < half ? kv[0][e] : other[e], at < half ? other[e] : kv[0][e], cs[e], sn[e], x, y);
+            o[e] = at < half ? x : y;
           }
         } else {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int d = at + e, p = d < half ? d : d - half;
-            const bool two = d < t.rot;
-            float other[1] = {0.0f};
-            if (two) wide_in<XB, 1>(k, ka + (d < half ? d + half : p), other);
-            cs[e] = !two ? 1.0f : in_table ? t.cos[pos * half + p] : __builtin_nanf("");
-            sn[e] = !two ? 0.0f : in_table ? t.sin[pos * half + p] : __builtin_nanf("");
-            float x, y;
-            if (d < half) turn_pair(kv[0][e], other[0], cs[e], sn[e], x, y);
-            else turn_pair(other[0], kv[0][e], cs[e], sn[e], y, x);
-            o[e] = two ? x : kv[0][e];
+            o[e] = kv[0][e];
+            if (d < t.rot) {
+              float other[1], x, y;
+              wide_in<XB, 1>(k, ka + (d < half ? d + half : p), other);
+              const float cc = in_table ? cp[p] : __builtin_nanf(""), ss = in_table ? sp[p] : __builtin_nanf("");
+              turn_pair(d < half ? kv[0][e] : other[0], d < half ? other[0] : kv[0][e], cc, ss, x, y);
+              o[e] = d < half ? x : y;
+            }
           }
         }
 #pragma unroll
@@ -281,44 +301,75 @@ hipError_t cache_append_launch(const CacheView& c, const CacheRowsArgs& r, int32
   return bf16 ? lanes(std::true_type{}) : lanes(std::false_type{});
 }
 
-// One thread: four elements of a head of a row, keys or values.
+// One thread: four elements of a head of the 16 tokens that share a group of the value codes: four 16-byte vectors of values,
+// turned over four by four bytes, and a row's four key codes at a time (one thread to four elements of one token gathered its
+// value codes byte by byte: 4 x 2048 tokens of 8 heads of 128 22.5 us, so XX).
 template <bool YB>
-__global__ __launch_bounds__(256) void cache_read_kernel(CacheView c, CacheRowsArgs r, int64_t n, void* k, void* v) {
-  const int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (idx >= n) return;
-  const uint32_t per = (uint32_t)c.dim >> 2;
-  const int32_t at = 4 * (int32_t)(idx % per);
-  const int64_t hr = idx / per, row = hr / c.heads, b = row / r.q_len, i = row - b * r.q_len;
-  const int32_t h = (int32_t)(hr - row * c.heads);
-  float fk[4] = {0.0f, 0.0f, 0.0f, 0.0f}, fv[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  if (!r.q_lens || i < r.q_lens[b]) {
-    const int64_t slot = cache_slot(c, b, h, (r.q_starts ? r.q_starts[b] : r.q_start) + i);
-    if (slot < 0) {
+__global__ __launch_bounds__(256) void cache_read_kernel(CacheView c, CacheRowsArgs r, void* k, void* v) {
+  const uint32_t per = (uint32_t)c.dim >> 2, idx = blockIdx.y * 256 + threadIdx.x;
+  if (idx >= per * (uint32_t)c.heads) return;
+  const int32_t h = (int32_t)(idx / per), at = 4 * (int32_t)(idx - (uint32_t)h * per);
+  const int64_t b = blockIdx.z, first = r.q_starts ? r.q_starts[b] : r.q_start, g0 = ((first >> 4) + blockIdx.x) << 4;
+  const int64_t count = r.q_lens && r.q_lens[b] < r.q_len ? r.q_lens[b] : r.q_len;  // rows that exist
+  if (g0 >= first + r.q_len) return;
+  const int64_t base = cache_slot(c, b, h, g0);  // of the group, in one page
+  const int64_t i0 = g0 - first;
+  const int lo = i0 < 0 ? (int)-i0 : 0, end = i0 + 16 > r.q_len ? (int)(r.q_len - i0) : 16;
+  const int64_t out0 = ((b * r.q_len + i0) * c.heads + h) * c.dim + at, next = (int64_t)c.heads * c.dim;
+  uint32_t w[16];
+  auto put = [&](void* out, const float* steps) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) fk[e] = fv[e] = __builtin_nanf("");
-    } else {
-      if (k) {
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(c.kc + slot * c.dim + at);
-        const float st = c.ks[slot];
+    for (int t = 0; t < 16; ++t) {
+      if (t < lo || t >= end) continue;
+      float f[4];
+      if (i0 + t >= count) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) fk[e] = (float)(int8_t)(w >> (8 * e)) * st;
+        for (int e = 0; e < 4; ++e) f[e] = 0.0f;
+      } else if (base < 0) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[e] = __builtin_nanf("");
+      } else {
+        const float st = steps[base + t];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[e] = (float)(int8_t)(w[t] >> (8 * e)) * st;
       }
-      if (v) {
-        const int8_t* p = c.vc + (slot & ~(int64_t)15) * c.dim + at * 16 + (slot & 15);
-        const float st = c.vs[slot];
+      wide_out<YB, 4>(out, out0 + t * next, f);
+    }
+  };
+  if (k) {
+    if (base >= 0) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) fv[e] = (float)p[16 * e] * st;
+      for (int t = 0; t < 16; ++t) w[t] = *reinterpret_cast<const uint32_t*>(c.kc + (base + t) * c.dim + at);
+    }
+    put(k, c.ks);
+  }
+  if (v) {
+    if (base >= 0) {
+      const uint4* p = reinterpret_cast<const uint4*>(c.vc + base * c.dim + 16 * at);
+      uint4 d[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) d[e] = p[e];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {  // tokens 4 q .. 4 q + 3: byte t of the dword of element e becomes byte e of token t's
+        uint32_t x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = q == 0 ? d[e].x : q == 1 ? d[e].y : q == 2 ? d[e].z : d[e].w;
+        const uint32_t a01 = __builtin_amdgcn_perm(x[1], x[0], 0x05010400u), b01 = __builtin_amdgcn_perm(x[1], x[0], 0x07030602u);
+        const uint32_t a23 = __builtin_amdgcn_perm(x[3], x[2], 0x05010400u), b23 = __builtin_amdgcn_perm(x[3], x[2], 0x07030602u);
+        w[4 * q] = __builtin_amdgcn_perm(a23, a01, 0x05040100u);
+        w[4 * q + 1] = __builtin_amdgcn_perm(a23, a01, 0x07060302u);
+        w[4 * q + 2] = __builtin_amdgcn_perm(b23, b01, 0x05040100u);
+        w[4 * q + 3] = __builtin_amdgcn_perm(b23, b01, 0x07060302u);
       }
     }
+    put(v, c.vs);
   }
-  if (k) wide_out<YB, 4>(k, hr * c.dim + at, fk);
-  if (v) wide_out<YB, 4>(v, hr * c.dim + at, fv);
 }
 
 hipError_t cache_read_launch(const CacheView& c, const CacheRowsArgs& r, int32_t bf16, void* k, void* v, hipStream_t s) {
-  const int64_t n = c.batch * r.q_len * c.heads * (c.dim / 4);
-  if (bf16) hipLaunchKernelGGL(cache_read_kernel<true>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, c, r, n, k, v);
-  else hipLaunchKernelGGL(cache_read_kernel<false>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, c, r, n, k, v);
+  const dim3 grid((unsigned)((r.q_len + 15) / 16 + 1), (unsigned)((c.heads * (c.dim / 4) + 255) / 256), (unsigned)c.batch);
+  if (bf16) hipLaunchKernelGGL(cache_read_kernel<true>, grid, dim3(256), 0, s, c, r, k, v);
+  else hipLaunchKernelGGL(cache_read_kernel<false>, grid, dim3(256), 0, s, c, r, k, v);
   return hipGetLastError();
 }
 
