@@ -619,7 +619,7 @@ canon_status canon_cache_read(const canon_kv_cache* cache, const canon_cache_row
                               void* stream);
 
 /* Attention over such a cache (R26).  rows as for canon_softmax_relbias (batch that of the cache, ld 0): query i sees the
-   keys j < k_len <= table_len * page with j < k_lens[b], j <= pos (if causal), |pos - j| < window (if window > 0), and none
+   keys j < k_len <= table_len * page (0 for a cache of no pages) with j < k_lens[b], j <= pos (if causal), |pos - j| < window (if window > 0), and none
    if i >= q_lens[b].  q [batch * q_len][n_heads][head_dim], tokens q_stride elements apart, fp32 or bf16, turned already;
    query head h reads key/value head h / (n_heads / n_kv_heads).  out (bf16 [batch * q_len][n_heads * head_dim]) = the sum of
    the values weighted by 2^(z - max z), z = scale log2(e) q.k, over the sum of the weights.  The rule takes every long sum in

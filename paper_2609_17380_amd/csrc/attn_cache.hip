@@ -268,19 +268,33 @@ __device__ __forceinline__ void store_out(const CacheAttnArgs& a, int64_t row, i
 // with the values (the weights cross through LDS, 8 KB): a workgroup has all of its 2 * 256 * head_dim bytes of the cache on
 // their way at once and waits for them once.  What a tile gives goes to `parts`, a row's tiles one after the other, to be
 // joined by attn_join_kernel; where there is one tile only, straight to the output.
+// With a window, `span` workgroups a block of queries, from the first tile that one of them sees on (of all tiles, 12 of 257
+// queries behind 2744 keys, most workgroups had nothing to do).
 template <int HD>
-__global__ __launch_bounds__(256) void attn_tile_kernel(CacheAttnArgs a, int64_t tiles, int64_t blocks) {
+__global__ __launch_bounds__(256) void attn_tile_kernel(CacheAttnArgs a, int64_t tiles, int64_t blocks, int64_t span) {
   constexpr int NS = Query<HD>::NS, ND = HD / 16, NW = (ND + 3) / 4;  // 16-element parts of a head, of a wavefront
   __shared__ __attribute__((aligned(16))) i32x4 wts[2][4][64];
   __shared__ float ms[4][16], ss[4][16];
   __shared__ uint32_t vs[4][16];
-  const uint32_t id = blockIdx.x, bt = id / (uint32_t)tiles, bk = bt / (uint32_t)blocks;
-  const int64_t tile = id - bt * (uint32_t)tiles, cb = bt - bk * (uint32_t)blocks;
+  const uint32_t id = blockIdx.x, bt = id / (uint32_t)span, bk = bt / (uint32_t)blocks;
+  int64_t tile = id - bt * (uint32_t)span;
+  const int64_t cb = bt - bk * (uint32_t)blocks;
   const int64_t b = bk / (uint32_t)a.c.heads;
   const int32_t kvh = (int32_t)(bk - (uint32_t)b * (uint32_t)a.c.heads);
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, cc = lane & 15, g = lane >> 4;
-  const int64_t t0 = tile * kTile;
   const int at0 = 64 * w + 16 * g;  // of this lane's 16 keys in the tile
+  if (span < tiles) {
+    const Column c = column_of(a, b, kvh, cb * 16 + cc);
+    int32_t lo = c.hi > c.lo ? (int32_t)c.lo : 0x7FFFFFFF;
+#pragma unroll
+    for (int s = 1; s < 16; s <<= 1) {
+      const int32_t l = __shfl_xor(lo, s, 64);
+      lo = l < lo ? l : lo;
+    }
+    tile += __builtin_amdgcn_readfirstlane(lo) / kTile;
+    if (tile >= tiles) return;
+  }
+  const int64_t t0 = tile * kTile;
   // which pages, and the queries: asked for before anything is waited for
   const int32_t kpage = page_of(a, b, t0 + 64 * w + 16 * (cc >> 2));
   int32_t vpage[4];
@@ -445,10 +459,16 @@ __global__ __launch_bounds__(64) void attn_join_kernel(CacheAttnArgs a, int64_t 
     }
     const float after = __builtin_elementwise_maximum(R, up), left = __shfl_up(after, 1, 64), before = lane == 0 ? R : left;
     const float x = shift2(before, after), y = shift2(d[0], after), sy = d[1], sc = d[2] * y;
-    for (int t0 = 0; t0 < n; t0 += U) {
-      Vec v[U];
+    Vec v[U], ahead[U];
+    auto ask = [&](int t0) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) v[u] = *reinterpret_cast<const Vec*>(p + (t0 + u < n ? t0 + u : n - 1) * (HD + 4) + at);
+      for (int u = 0; u < U; ++u) ahead[u] = *reinterpret_cast<const Vec*>(p + (t0 + u < n ? t0 + u : n - 1) * (HD + 4) + at);
+    };
+    ask(0);
+    for (int t0 = 0; t0 < n; t0 += U) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = ahead[u];
+      if (t0 + U < n) ask(t0 + U);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int t = t0 + u < n ? t0 + u : n - 1;
@@ -829,8 +849,14 @@ static hipError_t attn_go(const CacheAttnArgs& a, hipStream_t s) {
     return hipGetLastError();
   }
   const int64_t blocks = (cols + 15) / 16, tiles = p.tiles > 0 ? p.tiles : 1;
-  hipLaunchKernelGGL((attn_tile_kernel<HD>), dim3((unsigned)(tiles * blocks * a.c.heads * a.c.batch)), dim3(256), 0, s, a,
-                     tiles, blocks);
+  // tiles that the keys of a block's queries can lie in: those of one query, and the other queries' positions
+  int64_t span = tiles;
+  if (a.window > 0) {
+    const int64_t G = a.heads / a.c.heads, more = 15 / G + 1, keys = (a.causal ? a.window : 2 * a.window - 1) + more;
+    span = keys / kTile + 2 < tiles ? keys / kTile + 2 : tiles;
+  }
+  hipLaunchKernelGGL((attn_tile_kernel<HD>), dim3((unsigned)(span * blocks * a.c.heads * a.c.batch)), dim3(256), 0, s, a,
+                     tiles, blocks, span);
   if (tiles > 1)
     hipLaunchKernelGGL((attn_join_kernel<HD>), dim3((unsigned)(a.c.batch * a.q_len * a.heads)), dim3(64), 0, s, a, tiles);
   return hipGetLastError();

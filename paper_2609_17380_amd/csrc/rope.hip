@@ -303,7 +303,7 @@ hipError_t cache_append_launch(const CacheView& c, const CacheRowsArgs& r, int32
 
 // One thread: four elements of a head of the 16 tokens that share a group of the value codes: four 16-byte vectors of values,
 // turned over four by four bytes, and a row's four key codes at a time (one thread to four elements of one token gathered its
-// value codes byte by byte: 4 x 2048 tokens of 8 heads of 128 22.5 us, so XX).
+// value codes byte by byte: 4 x 2048 tokens of 8 heads of 128 22.5 us, so 16).
 template <bool YB>
 __global__ __launch_bounds__(256) void cache_read_kernel(CacheView c, CacheRowsArgs r, void* k, void* v) {
   const uint32_t per = (uint32_t)c.dim >> 2, idx = blockIdx.y * 256 + threadIdx.x;
