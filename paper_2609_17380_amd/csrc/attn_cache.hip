@@ -536,15 +536,21 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void attn_rows_kernel(Cache
   const int32_t kvh = (int32_t)(bh - (uint32_t)b * (uint32_t)a.c.heads);
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), cc = lane & 15, g = lane >> 4;
   const Column col = column_of(a, b, kvh, (cb * 4 + w) * 16 + cc);
-  int32_t lo = col.hi > col.lo ? (int32_t)col.lo : 0x7FFFFFFF, hi = (int32_t)col.hi;  // k_len fits
+  // keys that some query of the wavefront sees, and that all of them see (k_len fits 32 bits)
+  int32_t lo = col.hi > col.lo ? (int32_t)col.lo : 0x7FFFFFFF, hi = (int32_t)col.hi;
+  int32_t in_lo = col.real ? (int32_t)col.lo : 0, in_hi = col.real ? (int32_t)col.hi : 0x7FFFFFFF;
 #pragma unroll
   for (int s = 1; s < 16; s <<= 1) {
-    const int32_t l = __shfl_xor(lo, s, 64), h = __shfl_xor(hi, s, 64);
+    const int32_t l = __shfl_xor(lo, s, 64), h = __shfl_xor(hi, s, 64), il = __shfl_xor(in_lo, s, 64), ih = __shfl_xor(in_hi, s, 64);
     lo = l < lo ? l : lo;
     hi = h > hi ? h : hi;
+    in_lo = il > in_lo ? il : in_lo;
+    in_hi = ih < in_hi ? ih : in_hi;
   }
   lo = __builtin_amdgcn_readfirstlane(lo);
   hi = __builtin_amdgcn_readfirstlane(hi);
+  in_lo = __builtin_amdgcn_readfirstlane(in_lo);
+  in_hi = lo < hi ? __builtin_amdgcn_readfirstlane(in_hi) : 0;  // a wavefront without queries: no whole tiles
   if (lane == 0) {
     L.span[w][0] = lo;
     L.span[w][1] = hi;
@@ -775,39 +781,48 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void attn_rows_kernel(Cache
         for (int i = 0; i < 4; ++i) o[n][i] = o[n][i] * x;
     }
     __builtin_amdgcn_s_setprio(1);
+    constexpr int C = 2;  // chains of products side by side
 #pragma unroll
-    for (int n = 0; n < ND; n += 2) {
-      i32x4 acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}}, vx[2][4];
+    for (int n = 0; n < ND; n += C) {
+      i32x4 acc[C], vx[C][4];
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-#pragma unroll
-        for (int d = 0; d < 2; ++d) vx[d][q] = L.v[q * ND + n + d][lane];
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-#pragma unroll
-        for (int d = 0; d < 2; ++d) acc[d] = mfma(vx[d][q], wh[q], acc[d]);
-#pragma unroll
-      for (int d = 0; d < 2; ++d) acc[d] = acc[d] << 8;
+      for (int d = 0; d < C; ++d) acc[d] = i32x4{0, 0, 0, 0};
 #pragma unroll
       for (int q = 0; q < 4; ++q)
 #pragma unroll
-        for (int d = 0; d < 2; ++d) acc[d] = mfma(vx[d][q], wl[q], acc[d]);
+        for (int d = 0; d < C; ++d) vx[d][q] = L.v[q * ND + n + d][lane];
 #pragma unroll
-      for (int d = 0; d < 2; ++d)
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int d = 0; d < C; ++d) acc[d] = mfma(vx[d][q], wh[q], acc[d]);
+#pragma unroll
+      for (int d = 0; d < C; ++d) acc[d] = acc[d] << 8;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int d = 0; d < C; ++d) acc[d] = mfma(vx[d][q], wl[q], acc[d]);
+#pragma unroll
+      for (int d = 0; d < C; ++d)
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[n + d][i] = __builtin_fmaf((float)acc[d][i], sc, o[n + d][i]);
     }
     __builtin_amdgcn_s_setprio(0);
   };
-  for (; t0 < all_hi; t0 += kTile, par ^= 1) {
-    // this tile's keys have landed, and every wavefront is done with the last one's values
-    vm_left<0>();
-    __syncthreads();
-    fetch_values(slots);
-    const bool mine = lo < t0 + kTile && hi > t0;
-    const Seen sees = seen_of(col, t0);
-    if (mine && __all(!col.real || sees.n == kTile)) tile(std::true_type{}, mine, sees);
-    else tile(std::false_type{}, mine, sees);
+  // runs of whole tiles and of others in loops of their own, which keep their registers where they are from tile to tile
+  auto run = [&](auto full) {
+    while (t0 < all_hi && (t0 >= in_lo && t0 + kTile <= in_hi) == full.value) {
+      // this tile's keys have landed, and every wavefront is done with the last one's values
+      vm_left<0>();
+      __syncthreads();
+      fetch_values(slots);
+      tile(full, lo < t0 + kTile && hi > t0, seen_of(col, t0));
+      t0 += kTile;
+      par ^= 1;
+    }
+  };
+  while (t0 < all_hi) {
+    run(std::false_type{});
+    run(std::true_type{});
   }
   if (!col.real) return;
   const float inv = S == 0.0f ? 0.0f : 1.0f / S;
