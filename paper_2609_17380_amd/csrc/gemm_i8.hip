@@ -23,17 +23,13 @@
 
 #include "canon_dev.h"
 #include "canon_internal.h"
+#include "i8_dev.h"
 
 namespace canon {
 
-typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef int32_t i32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-struct __attribute__((packed, aligned(1))) I8x16 {
-  uint32_t x, y, z, w;
-};
-
 // Workgroup configuration: NW wavefronts in (NW / 2) x 2, wavefront (wr, wc) owning rows [32 HB wr, 32 HB (wr + 1))
 // and columns [32 WN wc, 32 WN (wc + 1)) of a BM x (64 WN) tile (HB x WN instruction blocks); stages of KS k bytes.
 template <int HB, int WN, int KS, int NW>
@@ -49,22 +45,8 @@ struct I8Cfg {
 
 template <class Cf>
 struct I8Raw {
-  uint4 a[Cf::AV], b[Cf::BV];
+  i32x4 a[Cf::AV], b[Cf::BV];
 };
-
-// 16 consecutive bytes; rows off 16-byte boundaries load as wide
-__device__ __forceinline__ uint4 ld16(const int8_t* p) {
-  const I8x16 v = *reinterpret_cast<const I8x16*>(p);
-  return make_uint4(v.x, v.y, v.z, v.w);
-}
-// the first `valid` of them (zero fill beyond)
-__device__ __forceinline__ uint4 ld16_cut(const int8_t* p, int64_t valid) {
-  if (valid >= 16) return ld16(p);
-  uint32_t w[4] = {0u, 0u, 0u, 0u};
-  for (int e = 0; e < 16; ++e)
-    if (e < valid) w[e >> 2] |= (uint32_t)(uint8_t)p[e] << (8 * (e & 3));
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
 
 // Global -> registers for the stage starting at k0: vector idx = t + NT it covers row idx / (KS/16),
 // 16-byte segment idx % (KS/16) of the row's KS bytes.  Rows behind the last are read as the last: what they give is not
@@ -78,14 +60,14 @@ __device__ __forceinline__ void load_stage(const GemmI8Args& g, int64_t row0, in
     const int idx = t + Cf::NT * it;
     const int64_t k = k0 + 16 * (idx % SEG), row = row0 + idx / SEG;
     const int8_t* p = g.a + (row < g.m ? row : g.m - 1) * g.lda + k;
-    r.a[it] = WHOLE ? ld16(p) : ld16_cut(p, g.k - k);
+    r.a[it] = WHOLE ? whole16(p) : cut16(p, g.k - k, g.k >= 16);
   }
 #pragma unroll
   for (int it = 0; it < Cf::BV; ++it) {
     const int idx = t + Cf::NT * it;
     const int64_t k = k0 + 16 * (idx % SEG), col = col0 + idx / SEG;
     const int8_t* p = g.b + (col < g.n ? col : g.n - 1) * g.ldb + k;
-    r.b[it] = WHOLE ? ld16(p) : ld16_cut(p, g.k - k);
+    r.b[it] = WHOLE ? whole16(p) : cut16(p, g.k - k, g.k >= 16);
   }
 }
 
@@ -96,17 +78,17 @@ __device__ __forceinline__ void store_stage(int8_t* As, int8_t* Bs, const I8Raw<
 #pragma unroll
   for (int it = 0; it < Cf::AV; ++it) {
     const int idx = t + Cf::NT * it;
-    *reinterpret_cast<uint4*>(As + (idx / SEG) * Cf::LD + 16 * (idx % SEG)) = r.a[it];
+    *reinterpret_cast<i32x4*>(As + (idx / SEG) * Cf::LD + 16 * (idx % SEG)) = r.a[it];
   }
 #pragma unroll
   for (int it = 0; it < Cf::BV; ++it) {
     const int idx = t + Cf::NT * it;
-    *reinterpret_cast<uint4*>(Bs + (idx / SEG) * Cf::LD + 16 * (idx % SEG)) = r.b[it];
+    *reinterpret_cast<i32x4*>(Bs + (idx / SEG) * Cf::LD + 16 * (idx % SEG)) = r.b[it];
   }
 }
 
 template <int HB, int WN, int KS, int NW>
-__global__ __launch_bounds__(64 * NW) void gemm_i8_kernel(GemmI8Args g) {
+__global__ __launch_bounds__(64 * NW, NW / 2) void gemm_i8_kernel(GemmI8Args g) {
   using Cf = I8Cfg<HB, WN, KS, NW>;
   constexpr int BM = Cf::BM, BN = Cf::BN, LD = Cf::LD;
   __shared__ __attribute__((aligned(16))) int8_t As[2][BM * LD];
@@ -182,27 +164,51 @@ __global__ __launch_bounds__(64 * NW) void gemm_i8_kernel(GemmI8Args g) {
   }
 
   // result layout: register v, lane l -> row (v % 4) + 4 (l / 32) + 8 (v / 4), column l % 32 of the block
-  const float sa = g.y && !g.sa_rows ? *g.sa : 0.0f;
+  // The steps are asked for and the results finished before the first store, those of rows and columns behind the last with the
+  // last's steps: a wait between two stores is one for the first of them (33 x 300 x 64 with such waits 9.3 us, so 5.8; 1541 x 5001 x 1024 33 and 29).
+  float sb[WN];
 #pragma unroll
-  for (int h = 0; h < HB; ++h)
+  for (int v2 = 0; v2 < WN; ++v2) {
+    const int64_t j = col0 + 32 * WN * wc + 32 * v2 + (lane & 31);
+    sb[v2] = g.y ? g.sb[g.sb_scalar ? 0 : j < g.n ? j : g.n - 1] : 0.0f;
+  }
+#pragma unroll
+  for (int h = 0; h < HB; ++h) {
+    const int64_t i0 = row0 + 32 * HB * wr + 32 * h + 4 * (lane >> 5);
+    if (g.acc) {
+#pragma unroll
+      for (int v2 = 0; v2 < WN; ++v2)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int64_t i = i0 + (v & 3) + 8 * (v >> 2), j = col0 + 32 * WN * wc + 32 * v2 + (lane & 31);
+          if (i < g.m && j < g.n) g.acc[i * g.ldc + j] = acc[h][v2][v];
+        }
+    }
+    if (!g.y) continue;
+    float sa[16], y[WN][16];
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const int64_t i = i0 + (v & 3) + 8 * (v >> 2);
+      sa[v] = g.sa[!g.sa_rows ? 0 : i < g.m ? i : g.m - 1];
+    }
 #pragma unroll
     for (int v2 = 0; v2 < WN; ++v2)
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
-        const int64_t i = row0 + 32 * HB * wr + 32 * h + (v & 3) + 4 * (lane >> 5) + 8 * (v >> 2);
-        const int64_t j = col0 + 32 * WN * wc + 32 * v2 + (lane & 31);
-        if (i < g.m && j < g.n) {
-          const int32_t a = acc[h][v2][v];
-          if (g.acc) g.acc[i * g.ldc + j] = a;
-          if (g.y) {
-            const float af = (float)a;  // round to nearest even
-            const float t = af * (g.sa_rows ? g.sa[i] : sa);
-            const float y = t * g.sb[g.sb_scalar ? 0 : j];
-            if (g.y_bf16) reinterpret_cast<uint16_t*>(g.y)[i * g.ldc + j] = f32_to_bf16(y);
-            else g.y[i * g.ldc + j] = y;
-          }
-        }
+        const float t = (float)acc[h][v2][v] * sa[v];
+        y[v2][v] = t * sb[v2];  // RN(RN(RN32(acc) sa) sb)
+        asm volatile("" : "+v"(y[v2][v]));
       }
+#pragma unroll
+    for (int v2 = 0; v2 < WN; ++v2)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const int64_t i = i0 + (v & 3) + 8 * (v >> 2), j = col0 + 32 * WN * wc + 32 * v2 + (lane & 31);
+        if (i >= g.m || j >= g.n) continue;
+        if (g.y_bf16) reinterpret_cast<uint16_t*>(g.y)[i * g.ldc + j] = f32_to_bf16(y[v2][v]);
+        else g.y[i * g.ldc + j] = y[v2][v];
+      }
+  }
 }
 
 // 16 bytes per lane from global memory straight into LDS: lane l of the wavefront writes lds_addr + 16 l
@@ -444,13 +450,14 @@ hipError_t gemm_i8_launch(const GemmI8Args& gin, hipStream_t s) {
                                               hipSuccess || cus <= 0)
     cus = 256;
   // Whole 256 x 256 tiles (and 16-byte output stores: y, acc and ldc aligned to 4 elements) that fill three quarters of the CUs
-  // or more: the pipelined kernel (8192 x 16384 x 2048 310 us).  With fewer of them (256 x 2048 x 8192: 113 us in 8 tiles, 15 in
-  // 256 smaller ones), and where 128 x 128 tiles are fewer than the CUs (700 x 2048 x 2048: 21 us in 96, 17 in 352 smaller
-  // ones), k is split over the wavefronts.
+  // or more: the pipelined kernel (8192 x 16384 x 2048 310 us; 256 x 2048 x 8192 in its 8 tiles 113, in 256 smaller ones 15).
   const bool whole = g.vec && g.m % 256 == 0 && g.n % 256 == 0 && g.ldc % 4 == 0 && ((uintptr_t)g.y & 15) == 0 &&
                      ((uintptr_t)g.acc & 15) == 0 && g.k % 64 == 0 && g.k > 0;
   if (whole && (g.m / 256) * (g.n / 256) >= 3 * cus / 4) return launch_i8_tile(g, s);
-  if (((g.m + 127) / 128) * ((g.n + 127) / 128) < cus) return gemm_i8_split_launch(g, cus, s);
+  // 128 x 128 tiles where they fill three quarters of the CUs (440 x 7296 x 256: 10 us, with k split over the wavefronts of
+  // smaller tiles 19), with little to split half as many (700 x 2048 x 256: 7.4 and 10; x 4096: 30 and 22).
+  const int64_t tiles = ((g.m + 127) / 128) * ((g.n + 127) / 128);
+  if (tiles < 3 * cus / 4 && !(g.k <= 512 && g.m > 64 && tiles >= 3 * cus / 8)) return gemm_i8_split_launch(g, cus, s);
   return launch_i8<1, 2, 128, 8>(g, s);
 }
 

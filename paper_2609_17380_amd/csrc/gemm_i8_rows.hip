@@ -4,15 +4,10 @@
 #include "act8_dev.h"
 #include "canon_dev.h"
 #include "canon_internal.h"
+#include "i8_dev.h"
 #include "rows_dev.h"
 
 namespace canon {
-
-typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-struct __attribute__((packed, aligned(1))) B16 {
-  uint32_t w[4];
-};
 
 // ---- a step per token -----------------------------------------------------------------------------------------------------
 // A workgroup holds a row in registers, Q vectors of four elements a thread (Q = 0: longer rows, read a second time): one pass
@@ -141,30 +136,6 @@ hipError_t quant_tokens_launch(int64_t rows, int64_t cols, int32_t bf16, const v
 // v_mfma_i32_16x16x64_i8 and tokens its columns: lane (c, g) supplies bytes 16 g .. + 15 of channel c and of token c, and
 // receives channels 4 g .. 4 g + 3 of token c, which it stores together.  With CW = 8 half of the rows stay empty.
 
-// 16 bytes of a row of which `valid` exist, the others 0.  A cut vector is read as the row's last 16 and moved into place.
-__device__ __forceinline__ i32x4 row16(const int8_t* p, int64_t valid, bool longer) {
-  i32x4 r = {0, 0, 0, 0};
-  if (valid >= 16) {
-    const B16 v = *reinterpret_cast<const B16*>(p);
-    r = i32x4{(int32_t)v.w[0], (int32_t)v.w[1], (int32_t)v.w[2], (int32_t)v.w[3]};
-  } else if (valid > 0) {
-    if (longer) {
-      const B16 v = *reinterpret_cast<const B16*>(p + valid - 16);
-      unsigned __int128 x = ((unsigned __int128)v.w[3] << 96) | ((unsigned __int128)v.w[2] << 64) |
-                            ((unsigned __int128)v.w[1] << 32) | v.w[0];
-      x >>= 8 * (16 - (int)valid);
-      r = i32x4{(int32_t)(uint32_t)x, (int32_t)(uint32_t)(x >> 32), (int32_t)(uint32_t)(x >> 64), (int32_t)(uint32_t)(x >> 96)};
-    } else {
-      uint32_t w[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-      for (int e = 0; e < 15; ++e)
-        if (e < valid) w[e >> 2] |= (uint32_t)(uint8_t)p[e] << (8 * (e & 3));
-      r = i32x4{(int32_t)w[0], (int32_t)w[1], (int32_t)w[2], (int32_t)w[3]};
-    }
-  }
-  return r;
-}
-
 template <int CW, int U>
 __global__ __launch_bounds__(512) void gemm_i8_rows_kernel(GemmI8Args g) {
   constexpr int NW = 8;
@@ -177,10 +148,6 @@ __global__ __launch_bounds__(512) void gemm_i8_rows_kernel(GemmI8Args g) {
   const bool tok = c < g.m;
   const int8_t* ap = g.a + (tok ? c : 0) * g.lda + 16 * q;
   i32x4 acc = {0, 0, 0, 0};
-  auto vec = [](const int8_t* p) {
-    const B16 v = *reinterpret_cast<const B16*>(p);
-    return i32x4{(int32_t)v.w[0], (int32_t)v.w[1], (int32_t)v.w[2], (int32_t)v.w[3]};
-  };
   // Whole steps: this wavefront has 2 w, 2 w + 1 (a cache line), 16 + 2 w, ...  Workgroups begin at different ones: tokens' rows a power of two apart come
   // from the same few channels of the L2, and all workgroups would ask for the same bytes at once.
   const int32_t steps = (int32_t)(g.k >> 6), rest = (steps & 15) - 2 * w;
@@ -199,13 +166,13 @@ __global__ __launch_bounds__(512) void gemm_i8_rows_kernel(GemmI8Args g) {
     for (int u = 0; u < U; ++u) b[u] = i32x4{0, 0, 0, 0};
     if (has) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) b[u] = vec(bp + at[u]);
+      for (int u = 0; u < U; ++u) b[u] = whole16(bp + at[u]);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) a[u] = i32x4{0, 0, 0, 0};
     if (tok) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) a[u] = vec(ap + at[u]);
+      for (int u = 0; u < U; ++u) a[u] = whole16(ap + at[u]);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -216,8 +183,8 @@ __global__ __launch_bounds__(512) void gemm_i8_rows_kernel(GemmI8Args g) {
   if ((g.k & 63) && w == (steps & (NW - 1))) {  // the cut step
     const int64_t valid = (g.k & 63) - 16 * q;
     const bool longer = g.k >= 16;
-    const i32x4 b = row16(bp + 64 * (int64_t)steps, has ? valid : 0, longer);
-    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(b, row16(ap + 64 * (int64_t)steps, tok ? valid : 0, longer), acc, 0, 0, 0);
+    const i32x4 b = cut16(bp + 64 * (int64_t)steps, has ? valid : 0, longer);
+    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(b, cut16(ap + 64 * (int64_t)steps, tok ? valid : 0, longer), acc, 0, 0, 0);
   }
   part[w][lane] = acc;
   __syncthreads();

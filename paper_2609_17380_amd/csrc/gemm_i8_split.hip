@@ -9,45 +9,11 @@
 
 #include "canon_dev.h"
 #include "canon_internal.h"
+#include "i8_dev.h"
 
 namespace canon {
 
-typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef int32_t i32x16 __attribute__((ext_vector_type(16)));
-struct __attribute__((packed, aligned(1))) S16 {
-  uint32_t w[4];
-};
-
-namespace {
-
-__device__ __forceinline__ i32x4 whole16(const int8_t* p) {
-  const S16 v = *reinterpret_cast<const S16*>(p);
-  return i32x4{(int32_t)v.w[0], (int32_t)v.w[1], (int32_t)v.w[2], (int32_t)v.w[3]};
-}
-// 16 bytes of a row of which `valid` exist, the others 0.  A cut vector is read as the row's last 16 and moved into place.
-__device__ __forceinline__ i32x4 cut16(const int8_t* p, int64_t valid, bool longer) {
-  if (valid >= 16) return whole16(p);
-  i32x4 r = {0, 0, 0, 0};
-  if (valid > 0) {
-    if (longer) {
-      const S16 v = *reinterpret_cast<const S16*>(p + valid - 16);
-      unsigned __int128 x = ((unsigned __int128)v.w[3] << 96) | ((unsigned __int128)v.w[2] << 64) |
-                            ((unsigned __int128)v.w[1] << 32) | v.w[0];
-      x >>= 8 * (16 - (int)valid);
-      r = i32x4{(int32_t)(uint32_t)x, (int32_t)(uint32_t)(x >> 32), (int32_t)(uint32_t)(x >> 64), (int32_t)(uint32_t)(x >> 96)};
-    } else {
-      uint32_t w[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-      for (int e = 0; e < 15; ++e)
-        if (e < valid) w[e >> 2] |= (uint32_t)(uint8_t)p[e] << (8 * (e & 3));
-      r = i32x4{(int32_t)w[0], (int32_t)w[1], (int32_t)w[2], (int32_t)w[3]};
-    }
-  }
-  return r;
-}
-
-}  // namespace
-
 template <int TM, int TN>
 __global__ __launch_bounds__(512) void gemm_i8_split_kernel(GemmI8Args g, int64_t tiles_m, int64_t tiles_n) {
   constexpr int NW = 8, KS = 128, LD = KS + 16;  // padded rows: 32 of them at one k offset fall on different banks
@@ -147,28 +113,43 @@ __global__ __launch_bounds__(512) void gemm_i8_split_kernel(GemmI8Args g, int64_
         *reinterpret_cast<i32x4*>(mine + 16 * (64 * (4 * (h * WN + v2) + v) + lane)) =
             i32x4{acc[h][v2][4 * v], acc[h][v2][4 * v + 1], acc[h][v2][4 * v + 2], acc[h][v2][4 * v + 3]};
   __syncthreads();
-  const float sa = g.y && !g.sa_rows ? *g.sa : 0.0f;
+  // everything is finished before the first store: a wait between two stores is one for the first of them
+  constexpr int VECS = TM * TN / 4, IT = VECS > 512 ? VECS / 512 : 1;
+  if (VECS < 512 && threadIdx.x >= VECS) return;
+  i32x4 sum[IT];
+  float y[IT][4];
 #pragma unroll
-  for (int it = 0; it < TM * TN / 4 / 512 || it == 0; ++it) {
-    const int idx = (int)threadIdx.x + 512 * it;
-    if (TM * TN / 4 < 512 && idx >= TM * TN / 4) break;
-    i32x4 sum = {0, 0, 0, 0};
+  for (int it = 0; it < IT; ++it) {
+    const int idx = (int)threadIdx.x + 512 * it, l = idx & 63, v = (idx >> 6) & 3, blk = idx >> 8;
+    const int64_t j = col0 + 32 * (blk % WN) + (l & 31), i0 = row0 + 32 * (blk / WN) + 8 * v + 4 * (l >> 5);
+    float sb = 0.0f, sa[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (g.y) {
+      sb = g.sb[g.sb_scalar ? 0 : j < g.n ? j : g.n - 1];
 #pragma unroll
-    for (int o = 0; o < NW; ++o) sum = sum + *reinterpret_cast<const i32x4*>(lds + o * PART + 16 * idx);
-    const int l = idx & 63, v = (idx >> 6) & 3, blk = idx >> 8;
+      for (int e = 0; e < 4; ++e) sa[e] = g.sa[!g.sa_rows ? 0 : i0 + e < g.m ? i0 + e : g.m - 1];
+    }
+    sum[it] = i32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int o = 0; o < NW; ++o) sum[it] = sum[it] + *reinterpret_cast<const i32x4*>(lds + o * PART + 16 * idx);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float t = (float)sum[it][e] * sa[e];
+      y[it][e] = t * sb;
+      asm volatile("" : "+v"(y[it][e]));
+    }
+  }
+#pragma unroll
+  for (int it = 0; it < IT; ++it) {
+    const int idx = (int)threadIdx.x + 512 * it, l = idx & 63, v = (idx >> 6) & 3, blk = idx >> 8;
     const int64_t j = col0 + 32 * (blk % WN) + (l & 31), i0 = row0 + 32 * (blk / WN) + 8 * v + 4 * (l >> 5);
     if (j >= g.n) continue;
-    const float sb = g.y ? g.sb[g.sb_scalar ? 0 : j] : 0.0f;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int64_t i = i0 + e;
       if (i >= g.m) break;
-      if (g.acc) g.acc[i * g.ldc + j] = sum[e];
-      if (g.y) {
-        const float t = (float)sum[e] * (g.sa_rows ? g.sa[i] : sa), y = t * sb;
-        if (g.y_bf16) reinterpret_cast<uint16_t*>(g.y)[i * g.ldc + j] = f32_to_bf16(y);
-        else g.y[i * g.ldc + j] = y;
-      }
+      if (g.acc) g.acc[i * g.ldc + j] = sum[it][e];
+      if (g.y && g.y_bf16) reinterpret_cast<uint16_t*>(g.y)[i * g.ldc + j] = f32_to_bf16(y[it][e]);
+      else if (g.y) g.y[i * g.ldc + j] = y[it][e];
     }
   }
 }

@@ -71,6 +71,7 @@ def product(a, sa, b, sb, dtype, pads=(0, 0, 0)):
                                    (17, 100, 500), (31, 64, 512), (33, 65, 1030), (64, 2056, 2048), (64, 48, 8192), (65, 130, 72),
                                    (1, 5001, 2056), (100, 300, 129), (129, 257, 640), (256, 256, 64), (256, 512, 192), (300, 200, 0),
                                    (5, 9, 0), (1, 300, 65536), (66, 70, 4000), (700, 1300, 260), (70, 2500, 140), (1290, 3300, 130),
+                                   (130, 12400, 300), (650, 1300, 12), (650, 1300, 700),
                                    (3584, 3584, 64)])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_product(m, n, k, dtype):
