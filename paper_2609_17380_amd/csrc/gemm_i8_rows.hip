@@ -1,6 +1,8 @@
 // gemm_i8_rows.hip - activations into 8 bits with a step per token (R23), and the int8 product of a few tokens with weights.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "act8_dev.h"
 #include "canon_dev.h"
 #include "canon_internal.h"

@@ -5,6 +5,8 @@
 // that every lane has a wide load of its own in flight and no lane waits for another's.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "act8_dev.h"
 #include "canon_dev.h"
 #include "canon_internal.h"
@@ -132,9 +134,8 @@ hipError_t rope_launch(int32_t backward, int64_t tokens, int64_t heads, int64_t 
   const int w = wide ? 4 : 1;
   const int32_t units = (int32_t)(t.rot / 2 / w + (dim - t.rot + 2 * w - 1) / (2 * w));
   const int32_t per_token = (int32_t)(heads * units);
-  const int64_t n = tokens * per_token, blocks = (n + 255) / 256;
   auto go = [&](auto xb, auto yb, auto width, auto pairs) {
-    // a grid of more than 2^24 workgroups of 256 would pass 2^32 threads: split by tokens
+    // launches below 2^32 threads
     const int64_t most = ((int64_t)1 << 31) / per_token > 0 ? ((int64_t)1 << 31) / per_token : 1;
     for (int64_t t0 = 0; t0 < tokens; t0 += most) {
       const int64_t nt = tokens - t0 < most ? tokens - t0 : most, nn = nt * per_token;
@@ -151,7 +152,6 @@ hipError_t rope_launch(int32_t backward, int64_t tokens, int64_t heads, int64_t 
     }
     return hipGetLastError();
   };
-  (void)blocks;
   using T = std::true_type;
   using F = std::false_type;
   using W1 = std::integral_constant<int, 1>;

@@ -111,7 +111,7 @@ def test_a_row_is_the_same_alone_and_in_a_prompt():
 
 @pytest.mark.parametrize("Q,K,D", [(1, 3000, 128), (40, 900, 64)])
 def test_near_the_formula(Q, K, D):
-    # bf16's rounding is 2^-9 of a value; the digits of 16 bits and binary32 leave less than 2^-12 of the largest value
+    # bf16's rounding is 2^-8 of a value (half a step of 8 significant bits); what the digits of 16 bits leave is reckoned below
     B, H, KV = 2, 8, 2
     c = host_cache(B, KV, D, 64, K, seed=9)
     q = queries(B, Q, H, D, seed=10)
@@ -121,7 +121,7 @@ def test_near_the_formula(Q, K, D):
     # score: |q16/2^16 error| sum |k| scale <= 2^-16 amax_q sum_d |k_d| / 8; with amax_q < 11 and |k| < 8 on D <= 128 elements
     # < 2^-16 * 11 * 8 * 128 / 8 = 0.022 at the very worst, and 4e-4 at six standard deviations of its random signs; a weight
     # is off by that part, a value by 2^-16 of the largest of its tile: 1e-3 |v|max in all
-    assert (np.abs(got - ref) <= np.abs(ref) * 2.0 ** -9 + 1e-3 * np.abs(kept_max(c))).all()
+    assert (np.abs(got - ref) <= np.abs(ref) * 2.0 ** -8 + 1e-3 * np.abs(kept_max(c))).all()
 
 
 def kept_max(c):
