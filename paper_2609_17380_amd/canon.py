@@ -620,7 +620,7 @@ def _rows(t, what, rows, width, dtypes, dev):
         raise ValueError(f"{what}: a tensor of {' or '.join(map(str, dtypes))} is needed")
     if t.get_device() != dev:
         raise ValueError(f"{what}: a tensor on the current device is needed, not on {t.device}")
-    if t.numel() == rows * width and t.is_contiguous():
+    if t.is_contiguous() and t.numel() == rows * width:
         return t.data_ptr(), width
     if t.dim() >= 2 and t.shape[0] == rows and t.numel() == rows * width and (rows == 0 or t[0].is_contiguous()):
         return t.data_ptr(), t.stride(0) if rows > 1 else width
@@ -632,10 +632,9 @@ def _lead(ld, least, rows, t, what, dtypes, dev):
     """The address of a matrix of `rows` rows, `ld` (at least `least`) elements apart; the last may end with its elements."""
     if ld < least:
         raise ValueError(f"{what}: rows of {least} elements do not fit a leading dimension of {ld}")
-    short = (rows - 1) * ld + least if rows > 0 else 0
-    if isinstance(t, torch.Tensor) and t.numel() == short:
-        return _arg(t, what, short, dtypes, dev)
-    return _arg(t, what, rows * ld, dtypes, dev)
+    full = rows * ld
+    short = full - ld + least if rows > 0 else 0
+    return _arg(t, what, short if short != full and isinstance(t, torch.Tensor) and t.numel() == short else full, dtypes, dev)
 
 
 def quant_tokens(rows, cols, x, codes, steps, stream=None):
@@ -685,17 +684,18 @@ class Rotation(ctypes.Structure):
     def __init__(self, cos, sin, rot_dim, interleaved=False):
         if not isinstance(cos, torch.Tensor) or not isinstance(sin, torch.Tensor):
             raise ValueError("cos and sin: tensors are needed")
-        half = max(rot_dim // 2, 1)
-        if cos.numel() % half or cos.numel() != sin.numel():
+        half, n = max(rot_dim // 2, 1), cos.numel()
+        if n % half or n != sin.numel():
             raise ValueError(f"cos and sin: [positions, {rot_dim // 2}] are needed, not {tuple(cos.shape)} and {tuple(sin.shape)}")
-        self.tensors = cos, sin
-        super().__init__(rot_dim, int(interleaved), cos.numel() // half if rot_dim > 0 else 0, None, None)
+        self.tensors, self.device = (cos, sin), cos.get_device()
+        super().__init__(rot_dim, int(interleaved), n // half if rot_dim > 0 else 0, _arg(cos, "cos", n, _T32, self.device),
+                         _arg(sin, "sin", n, _T32, self.device))
 
     def _of(self, dev):
-        """The record's address, once its tables are on the current device."""
-        n = self.tensors[0].numel()
-        self.cos = _arg(self.tensors[0], "cos", n, _T32, dev)
-        self.sin = _arg(self.tensors[1], "sin", n, _T32, dev)
+        """The record's address, with the present addresses of tables that were checked when they came."""
+        if dev != self.device:
+            raise ValueError(f"a rotation's tables on the current device are needed, not on device {self.device}")
+        self.cos, self.sin = self.tensors[0].data_ptr(), self.tensors[1].data_ptr()
         return ctypes.byref(self)
 
 

@@ -837,13 +837,22 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void attn_rows_kernel(Cache
 
 namespace {
 struct Plan {
-  int64_t tiles;  // 1: the rows kernel, or one tile that the tile kernel finishes
+  int64_t tiles, span;  // of all keys; that the keys of a block's queries can lie in: those of one query, and the others' positions
   bool split;
 };
 Plan plan_of(const CacheAttnArgs& a) {
-  const int64_t cols = a.q_len * (a.heads / a.c.heads), tiles = (a.k_len + kTile - 1) / kTile;
-  const int64_t rows_wg = a.c.batch * a.c.heads * ((cols + 63) / 64);
-  return Plan{tiles, tiles <= 1 || rows_wg < 256};
+  const int64_t G = a.heads / a.c.heads, cols = a.q_len * G, tiles = (a.k_len + kTile - 1) / kTile;
+  int64_t span = tiles;
+  if (a.window > 0) {
+    const int64_t keys = (a.causal ? a.window : 2 * a.window - 1) + 15 / G + 1;
+    span = keys / kTile + 2 < tiles ? keys / kTile + 2 : tiles;
+  }
+  // A workgroup for every tile where those for 64 queries would be few (2 heads of 8 over 2048 keys: 64 of them 38 us, 49 in
+  // whole rows; 128 of them 64 and 50; of one tile, 128 of them 10.8 and 13.7, 224 16 and 14), or would have at most two
+  // wavefronts with queries; launches stay below 2^32 threads.
+  const int64_t groups = a.c.batch * a.c.heads, wgs = groups * ((cols + 63) / 64);
+  const int64_t split_wgs = (span > 0 ? span : 1) * groups * ((cols + 15) / 16);
+  return Plan{tiles, span, (cols <= 32 || wgs < (tiles <= 1 ? 200 : 96)) && split_wgs < (int64_t(1) << 24)};
 }
 }  // namespace
 
@@ -864,12 +873,7 @@ static hipError_t attn_go(const CacheAttnArgs& a, hipStream_t s) {
     return hipGetLastError();
   }
   const int64_t blocks = (cols + 15) / 16, tiles = p.tiles > 0 ? p.tiles : 1;
-  // tiles that the keys of a block's queries can lie in: those of one query, and the other queries' positions
-  int64_t span = tiles;
-  if (a.window > 0) {
-    const int64_t G = a.heads / a.c.heads, more = 15 / G + 1, keys = (a.causal ? a.window : 2 * a.window - 1) + more;
-    span = keys / kTile + 2 < tiles ? keys / kTile + 2 : tiles;
-  }
+  const int64_t span = tiles < p.span ? tiles : p.span > 0 ? p.span : 1;
   hipLaunchKernelGGL((attn_tile_kernel<HD>), dim3((unsigned)(span * blocks * a.c.heads * a.c.batch)), dim3(256), 0, s, a,
                      tiles, blocks, span);
   if (tiles > 1)

@@ -69,7 +69,8 @@ def test_matches_the_oracle(B, H, KV, D, page, Q, K, mask):
           causal=mask != "both sides", window=37 if mask == "window" else 0)
 
 
-@pytest.mark.parametrize("D,KV,H", [(128, 8, 16), (64, 4, 4), (96, 16, 16), (256, 8, 8)])
+@pytest.mark.parametrize("D,KV,H", [(128, 8, 16), (64, 4, 4), (96, 16, 16), (256, 8, 8), (32, 8, 8), (160, 8, 8), (192, 8, 8),
+                                    (224, 8, 8)])
 @pytest.mark.parametrize("window,causal", [(0, True), (100, True), (300, False)])
 def test_prompts(D, KV, H, window, causal):
     # enough blocks of queries that a wavefront takes all keys of its queries
@@ -95,6 +96,23 @@ def want_row(c, q, K, b, i, k_len, q_len, causal, window):
     one.dims[4] = 1
     return one.attention(np.ascontiguousarray(q[b:b + 1, i:i + 1]), K, 0.125, [i], [1 if i < q_len else 0], [k_len], causal,
                          window)[0, 0]
+
+
+def test_many_short_prompts():
+    # one tile of keys, and enough blocks of queries for wavefronts that take all of it
+    B, H, KV, D, K = 8, 16, 8, 64, 200
+    c = host_cache(B, KV, D, 32, K, seed=30)
+    q = queries(B, K, H, D, seed=31, bf16=True)
+    lens = [K - 23 * b for b in range(B)]
+    check(c, q, K, q_lens=lens, k_lens=lens, bf16=True)
+
+
+def test_many_sequences():
+    # a batch that fills the chip with single tokens: a workgroup for every tile all the same
+    B, H, KV, D, K = 40, 8, 4, 64, 700
+    c = host_cache(B, KV, D, 64, K, seed=32)
+    lens = [1 + 17 * b for b in range(B)]
+    check(c, queries(B, 1, H, D, seed=33), K, starts=[n - 1 for n in lens], k_lens=lens)
 
 
 def test_a_row_is_the_same_alone_and_in_a_prompt():
