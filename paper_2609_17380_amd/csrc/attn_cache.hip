@@ -853,8 +853,9 @@ Plan plan_of(const CacheAttnArgs& a) {
   // whole rows; 128 of them 64 and 50; of one tile, 128 of them 10.8 and 13.7, 224 16 and 14), or would have at most two
   // wavefronts with queries; launches stay below 2^32 threads.
   const int64_t groups = a.c.batch * a.c.heads, wgs = groups * ((cols + 63) / 64);
-  const int64_t split_wgs = (span > 0 ? span : 1) * groups * ((cols + 15) / 16);
-  return Plan{tiles, span, (cols <= 32 || wgs < (tiles <= 1 ? 200 : 96)) && split_wgs < (int64_t(1) << 24)};
+  const int64_t split_wgs = span * groups * ((cols + 15) / 16);
+  // Without keys there may be no cache either (no pages, null pointers): whole rows, which load nothing of it then.
+  return Plan{tiles, span, tiles > 0 && (cols <= 32 || wgs < (tiles <= 1 ? 200 : 96)) && split_wgs < (int64_t(1) << 24)};
 }
 }  // namespace
 
@@ -874,8 +875,7 @@ static hipError_t attn_go(const CacheAttnArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((attn_rows_kernel<HD>), dim3((unsigned)n), dim3(256), 0, s, a, blocks);
     return hipGetLastError();
   }
-  const int64_t blocks = (cols + 15) / 16, tiles = p.tiles > 0 ? p.tiles : 1;
-  const int64_t span = tiles < p.span ? tiles : p.span > 0 ? p.span : 1;
+  const int64_t blocks = (cols + 15) / 16, tiles = p.tiles, span = p.span;
   hipLaunchKernelGGL((attn_tile_kernel<HD>), dim3((unsigned)(span * blocks * a.c.heads * a.c.batch)), dim3(256), 0, s, a,
                      tiles, blocks, span);
   if (tiles > 1)

@@ -1,0 +1,30 @@
+"""canon_cache_attention at the ends of its range: a cache of no pages."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2609_17380_amd.canon as C
+from gpu_util import DEV, dev_i32, host_u16, poisoned_workspace
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("D", [32, 64, 96, 128, 160, 192, 224, 256])
+@pytest.mark.parametrize("pages,table_len", [(0, 0), (0, 3), (2, 0), (2, 3)])
+def test_no_keys(D, pages, table_len):
+    # a cache of no pages has no address at all; with pages and k_len 0 nothing of it is to be read either
+    B, KV, page = 2, 2, 16
+    codes = lambda *s: torch.full(s, 77, dtype=torch.int8, device=DEV)  # noqa: E731
+    steps = lambda: torch.full((pages, KV, page), float("nan"), device=DEV)  # noqa: E731
+    table = torch.full((B, table_len), 1 << 30, dtype=torch.int32, device=DEV)
+    cache = C.KVCache(page, KV, D, codes(pages, KV, page, D), codes(pages, KV, page // 16, D, 16), steps(), steps(), table)
+    assert cache.n_pages == pages and (pages > 0 or not cache.k_codes)
+    for Q, G in ((1, 1), (3, 2), (16, 1), (17, 3), (70, 1), (400, 1)):
+        H = KV * G
+        for lens in (None, dev_i32(np.array([5, 0]))):
+            rows = C.AttnRows(B, H, Q, 0, scale=0.125, k_lens=lens)
+            q = torch.full((B * Q, H * D), 3.0, device=DEV)
+            out = torch.full((B * Q, H * D), 7.0, dtype=torch.bfloat16, device=DEV)
+            C.cache_attention(cache, rows, q, out, poisoned_workspace(C.cache_attention_workspace_bytes(cache, rows)))
+            torch.cuda.synchronize()
+            assert (host_u16(out) == 0).all(), (Q, G)
