@@ -628,21 +628,22 @@ canon_status canon_cache_read(const canon_kv_cache* cache, const canon_cache_row
              that is not > 0; -q in place of q for a negative scale), f = RN(RN(sq |scale|) * RN(log2 e))
      scores: u_j = RN(RN32(sum_d Q_d K_jd) kstep_j), the sum exact; they stand for u_j f
      tile:   r = ceil(RN(max u_j f)) (-inf where the largest u_j is; read as 0 there in what follows)
-             x_j = 128 (clamp(y_j, 0, 1) - 1), y_j = fma(u_j, RN(f / 128), RN(1 - RN(r / 128))), or where |r| > 65536
-             fma(RN(RN(u_j f) - r), 1/128, 1); e_j = exp2(x_j)
-             S_b = the 16 sums of 16 consecutive keys' 4 e, each a chain from +0, joined by a perfect pairwise tree, times 1/4;
+             x_j = fma(u_j, f, -r), or where |r| > 2^22 RN(RN(u_j f) - r), held to [-127, 0]; e_j = exp2(x_j)
+             S_b = the 16 sums of 16 consecutive keys' e, each a chain from +0, joined by a perfect pairwise tree;
              keys that are not seen are +0 terms; 0 where r is -inf, NaN where a u_j is NaN or r is +inf
-             V = the largest vstep of the keys that are seen, by bit pattern, rv = CRdiv(32512 / 4, V) (0 if V is not > 0 or rv
-             is infinite), w_j = rne(4 e_j RN(vstep_j rv)) (0 for all where rv = 0), A_d = sum_j w_j V_jd, exact
+             p_j = RN(e_j vstep_j), P = the largest of them by bit pattern, s = max(floor(log2 P) - 21, -126), w_j = rne(p_j 2^-s) =
+             256 h_j + l_j with -128 <= l_j < 128, A_d = fma(RN32(sum h_j V_jd), 256, sum l_j V_jd), both sums exact (NaN
+             where P is an infinity or a NaN)
      row:    over the tiles with a key that is seen, ascending, from R = -inf, S = 0, O = 0: R' = max(R, r),
              x = 2^(R - R'), y = 2^(r - R') (1 where R, or r, is -inf; 0 below 2^-126), S = fma(S_b, y, RN(S x)),
-             O_d = fma(RN32(A_d), RN(RN(V * RN(1/32512)) y), RN(O_d x))
+             O_d = fma(RN(A_d y), 2^s, RN(O_d x))
      out:    bf16(RN(RN(O_d + 0) CRdiv(1, S))), +0 where S = 0 (no key seen, or only scores of -inf)
-   exp2(x): n = rne(x), p = 1 + t (C1 + t (C2 + t (C3 + t C4))) by fma with t = x - n, p 2^n; the C are 0x3F317096, 0x3E7601BC,
-   0x3D64FE23, 0x3C1D0166: 2^t within 2.9e-6 of itself, a fifth of what rounding the weights leaves.
-   A query's row is the same in a prompt and alone, whatever the batch and the other sequences are.  Queries and
-   weights enter with 16 bits (two digits of 8): a part of 2^-16 of the largest, below the last place of bf16.  What stands
-   in places that are not seen (in unused slots, pages and table entries too) is not used; a key that is seen in a page that the
+   exp2(x): n = rne(x), p = 1 + t (C1 + t (C2 + t (C3 + t (C4 + t C5)))) by fma with t = x - n, p 2^n (0 below 2^-126); the C are
+   0x3F317215, 0x3E75FCE1, 0x3D635B6C, 0x3C1E7456, 0x3AADED20: 2^x within 1.6e-7 of itself.
+   A weight times its value's step is kept to 2^-22 of the largest such product of its tile, so that a key counts by what it adds
+   to the row, whatever the values of the others.
+   A query's row is the same in a prompt and alone, whatever the batch and the other sequences are.  Queries
+   enter with 16 bits (two digits of 8): a part of 2^-16 of the largest.  What stands in places that are not seen (in unused slots, pages and table entries too) is not used; a key that is seen in a page that the
    cache does not have makes the row NaN.
    k_len up to 2^21, batch * n_heads * q_len below 2^24 (else CANON_EUNSUPPORTED), window >= 0, |q_start| up to 2^30.
    workspace: device memory of canon_cache_attention_workspace_bytes(cache, rows) bytes, 256-byte aligned; 0 where none is

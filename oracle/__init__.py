@@ -109,6 +109,7 @@ def _load():
             "cref_gemm_i8_tokens": (ctypes.c_int, [i64, i64, i64, vp, vp, vp, vp, vp]),
             "cref_rope": (ctypes.c_int, [i32, i64, i64, i64, i64, i32, i64, vp, vp, vp, vp, vp]),
             "cref_cache_append": (ctypes.c_int, [vp, vp, i64, vp, vp, vp, vp, i64, i32, i64, vp, vp, vp, vp, vp, vp]),
+            "cref_exp2": (ctypes.c_int, [i64, vp, vp]),
             "cref_exp2_unit": (ctypes.c_int, [i64, vp, vp]),
             "cref_cache_attention": (ctypes.c_int, [vp, vp, f, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]),
             "cref_num_threads": (ctypes.c_int, []),
@@ -592,8 +593,16 @@ class KVCache:
         return out
 
 
+def exp2(x: np.ndarray) -> np.ndarray:
+    """R26's weights 2^x of x in [-127, 0]: 0 below 2^-126."""
+    x = np.ascontiguousarray(x, dtype=np.float32)
+    e = np.empty_like(x)
+    _check(_load().cref_exp2(x.size, _p(x), _p(e)))
+    return e
+
+
 def exp2_unit(y: np.ndarray) -> np.ndarray:
-    """R26's weights 2^(128 (y - 1)) of y in [0, 1], times 4."""
+    """The same exponential as 2^(128 (y - 1)) of y in [0, 1], times 4."""
     y = np.ascontiguousarray(y, dtype=np.float32)
     e = np.empty_like(y)
     _check(_load().cref_exp2_unit(y.size, _p(y), _p(e)))

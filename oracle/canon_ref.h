@@ -218,6 +218,7 @@ int cref_rope(int32_t backward, int64_t tokens, int64_t heads, int64_t dim, int6
 int cref_cache_append(const int64_t* cache, const int32_t* table, int64_t q_len, const int32_t* q_starts,
                       const int32_t* q_lens, const float* k, const float* v, int64_t rot, int32_t interleaved,
                       int64_t positions, const float* c, const float* s, int8_t* kc, int8_t* vc, float* ks, float* vs);
+int cref_exp2(int64_t n, const float* x, float* e);
 int cref_exp2_unit(int64_t n, const float* y, float* e4);
 /* cfg: heads, q_len, k_len, window, causal */
 int cref_cache_attention(const int64_t* cache, const int64_t* cfg, float scale, const int32_t* table,

@@ -91,21 +91,38 @@ int cref_cache_append(const int64_t* cache, const int32_t* table, int64_t q_len,
   return 0;
 }
 
-/* R26's weight of a score: 2^(128 (y - 1)), y in [0, 1] */
-static float exp2_unit(float y) {
-  const float n = (float)nearbyint(128.0 * (double)y) - 128.0f, t = (float)(128.0 * (double)y - 128.0 - (double)n);
-  float p = of_bits(0x3C1D0166u);
-  p = cref_fma(p, t, of_bits(0x3D64FE23u));
-  p = cref_fma(p, t, of_bits(0x3E7601BCu));
-  p = cref_fma(p, t, of_bits(0x3F317096u));
-  p = cref_fma(p, t, 1.0f);
-  return ldexpf(p, (int)n + 2); /* four times it: a normal number */
+/* R26's exponential: 2^x of x in [-127, 0], 0 below 2^-126.  Without the last step: p 2^n. */
+static float exp2_parts(float x, int* n) {
+  *n = (int)nearbyint(x);
+  const float t = x - (float)*n; /* exact */
+  float p = of_bits(0x3AADED20u);
+  p = cref_fma(p, t, of_bits(0x3C1E7456u));
+  p = cref_fma(p, t, of_bits(0x3D635B6Cu));
+  p = cref_fma(p, t, of_bits(0x3E75FCE1u));
+  p = cref_fma(p, t, of_bits(0x3F317215u));
+  return cref_fma(p, t, 1.0f);
 }
-int cref_exp2_unit(int64_t n, const float* y, float* e4) {
-  for (int64_t i = 0; i < n; ++i) e4[i] = exp2_unit(y[i]);
+static float exp2_neg(float x) {
+  int n;
+  const float p = exp2_parts(x, &n);
+  return flushed(ldexpf(p, n));
+}
+int cref_exp2(int64_t n, const float* x, float* e) {
+  for (int64_t i = 0; i < n; ++i) e[i] = exp2_neg(x[i]);
   return 0;
 }
-static float unit(float x) { return x > 0.0f ? (x < 1.0f ? x : 1.0f) : 0.0f; } /* 0 for a NaN */
+/* four times 2^(128 (y - 1)), y in [0, 1]: the same exponential, of a range whose ends are normal numbers */
+int cref_exp2_unit(int64_t n, const float* y, float* e4) {
+  for (int64_t i = 0; i < n; ++i) {
+    int k;
+    const double x = 128.0 * (double)y[i] - 128.0;
+    const float p = exp2_parts((float)x, &k);
+    e4[i] = ldexpf(p, k + 2);
+  }
+  return 0;
+}
+/* x held to [-127, 0] */
+static float held(float x) { return x > -127.0f ? (x < 0.0f ? x : 0.0f) : -127.0f; }
 
 /* 2^(a - b) of whole a <= b */
 static float shift(float a, float b) {
@@ -126,12 +143,12 @@ int cref_cache_attention(const int64_t* cache, const int64_t* cfg, float scale, 
     const int64_t pos = (int64_t)q_starts[b] + i;
     const float* x = q + r * D;
     int64_t Q[256];
-    uint32_t top = 0;
+    uint32_t amax = 0;
     for (int64_t d = 0; d < D; ++d) {
       const uint32_t u = to_bits(x[d]) & 0x7FFFFFFFu;
-      if (u > top) top = u;
+      if (u > amax) amax = u;
     }
-    const float sq = cref_mul(of_bits(top), inv), rs = sq > 0.0f ? cref_div(1.0f, sq) : 0.0f;
+    const float sq = cref_mul(of_bits(amax), inv), rs = sq > 0.0f ? cref_div(1.0f, sq) : 0.0f;
     for (int64_t d = 0; d < D; ++d) {
       const float v = cref_mul(scale < 0.0f ? -x[d] : x[d], rs);
       Q[d] = !(sq > 0.0f) || v != v ? 0 : v > 32512.0f ? 32512 : v < -32512.0f ? -32512 : (int64_t)rintf(v);
@@ -143,7 +160,6 @@ int cref_cache_attention(const int64_t* cache, const int64_t* cfg, float scale, 
       float t[256], e[256], m = -INFINITY;
       int8_t sees[256];
       int64_t slot[256], any = 0;
-      uint32_t vtop = 0;
       for (int64_t j = 0; j < 256; ++j) {
         const int64_t key = j0 + j;
         sees[j] = key < KL && key < k_lens[b] && i < q_lens[b] && !(cfg[4] && key > pos) &&
@@ -155,18 +171,19 @@ int cref_cache_attention(const int64_t* cache, const int64_t* cfg, float scale, 
         for (int64_t d = 0; slot[j] >= 0 && d < D; ++d) acc += Q[d] * kc[slot[j] * D + d];
         t[j] = slot[j] < 0 ? NAN : cref_mul((float)acc, ks[slot[j]]);
         if (t[j] > m || t[j] != t[j] || m != m) m = t[j] != t[j] || m != m ? NAN : t[j];
-        const uint32_t u = slot[j] < 0 ? 0x7FC00000u : to_bits(vs[slot[j]]) & 0x7FFFFFFFu;
-        if (u > vtop) vtop = u;
       }
       if (!any) continue;
-      const float rb = m == -INFINITY ? m : ceilf(cref_mul(m, f)), V = of_bits(vtop);
-      const float ref = rb == -INFINITY ? 0.0f : rb, part7 = 0.0078125f;
+      const float rb = m == -INFINITY ? m : ceilf(cref_mul(m, f));
+      const float ref = rb == -INFINITY ? 0.0f : rb;
+      float p[256];
+      uint32_t top = 0;
       for (int64_t j = 0; j < 256; ++j) {
-        e[j] = 0.0f;
+        e[j] = p[j] = 0.0f;
         if (!sees[j]) continue;
-        const float near = cref_fma(t[j], cref_mul(f, part7), cref_sub(1.0f, cref_mul(ref, part7)));
-        const float far = cref_fma(cref_sub(cref_mul(t[j], f), ref), part7, 1.0f);
-        e[j] = exp2_unit(unit(fabsf(ref) <= 65536.0f ? near : far));
+        const float near = cref_fma(t[j], f, -ref), far = cref_sub(cref_mul(t[j], f), ref);
+        e[j] = exp2_neg(held(fabsf(ref) <= 4194304.0f ? near : far));
+        p[j] = cref_mul(e[j], slot[j] < 0 ? NAN : vs[slot[j]]);
+        if ((to_bits(p[j]) & 0x7FFFFFFFu) > top) top = to_bits(p[j]) & 0x7FFFFFFFu;
       }
       float part[16];
       for (int c = 0; c < 16; ++c) {
@@ -175,20 +192,22 @@ int cref_cache_attention(const int64_t* cache, const int64_t* cfg, float scale, 
       }
       for (int n = 16; n > 1; n /= 2)
         for (int c = 0; c < n / 2; ++c) part[c] = cref_add(part[2 * c], part[2 * c + 1]);
-      float rv = V > 0.0f ? cref_div(8128.0f, V) : 0.0f; /* 32512 / 4 */
-      if (!(rv < INFINITY)) rv = 0.0f;
+      /* whole weights: multiples of 2^step of the products, 2^21 .. 2^22 of the largest */
+      const int finite = top < 0x7F800000u, exponent = (int)(top >> 23) - 127;
+      const int step = exponent - 21 > -126 ? exponent - 21 : -126;
       const float Rn = R != R || rb != rb ? NAN : R > rb ? R : rb, xo = shift(R, Rn), y = shift(rb, Rn);
-      const float scale_v = cref_mul(cref_mul(V, inv), y);
-      const float Sb = rb == -INFINITY ? 0.0f : rb < INFINITY ? cref_mul(part[0], 0.25f) : NAN;
+      const float Sb = rb == -INFINITY ? 0.0f : rb < INFINITY ? part[0] : NAN;
       S = cref_fma(Sb, y, cref_mul(S, xo));
       for (int64_t d = 0; d < D; ++d) {
-        int64_t A = 0;
+        int64_t hi = 0, lo = 0;
         for (int64_t j = 0; j < 256; ++j)
-          if (sees[j] && rv != 0.0f && slot[j] >= 0) {
-            const double w = (double)e[j] * cref_mul(vs[slot[j]], rv); /* exact */
-            A += (w != w ? 0 : (int64_t)rint(w)) * vc[v_at(cache, slot[j], d)];
+          if (sees[j] && finite && slot[j] >= 0) {
+            const int64_t w = (int64_t)rint(ldexp((double)p[j], -step)), l = (w + 128) % 256 - 128;
+            hi += (w - l) / 256 * vc[v_at(cache, slot[j], d)];
+            lo += l * vc[v_at(cache, slot[j], d)];
           }
-        O[d] = cref_fma((float)A, scale_v, cref_mul(O[d], xo));
+        const float A = finite ? cref_fma((float)hi, 256.0f, (float)lo) : NAN;
+        O[d] = cref_fma(cref_mul(A, y), ldexpf(1.0f, step), cref_mul(O[d], xo));
       }
       R = Rn;
     }

@@ -1,7 +1,8 @@
 // attn_cache.hip - attention over the paged cache of keys and values in 8 bits (R26).
 //
-// Every long sum is a sum of products of whole numbers, so it runs on the int8 matrix instructions in any order: a query (and
-// a weight) is a whole number of 16 bits, split into two digits of 8, x = 256 hi + lo, and sum x k = 256 sum hi k + sum lo k.
+// Every long sum is a sum of products of whole numbers, so it runs on the int8 matrix instructions in any order: a query is a
+// whole number of 16 bits, split into two digits of 8, x = 256 hi + lo, and sum x k = 256 sum hi k + sum lo k; a weight one of
+// 23 bits in three digits, x = 256 (256 hi + mid) + lo, the sum over its first two exact in 32 bits and the third's another.
 // Left to floating point are a maximum, a tile's 256 exponentials and their tree, and one fused multiply-add per tile and
 // element, with every change of reference a power of two.
 //
@@ -36,48 +37,55 @@ constexpr float kNegInf = -__builtin_inff();
 __device__ const __attribute__((aligned(16))) float kNanSteps[16] = {CANON_NAN4, CANON_NAN4, CANON_NAN4, CANON_NAN4};
 #undef CANON_NAN4
 
-// 2^x, |x| <= 1/2: the polynomial of least relative error with the constant 1, its coefficients rounded: 2.9e-6 in all, a fifth of
-// what rounding the weights to 16 bits leaves.
-constexpr uint32_t kExp2C[4] = {0x3F317096u, 0x3E7601BCu, 0x3D64FE23u, 0x3C1D0166u};
+// 2^x, |x| <= 1/2: the polynomial of least relative error with the constant 1, its coefficients rounded: 9.4e-8, and 1.6e-7 with
+// the roundings of its steps (with one term less 2.9e-6, which showed beside the rounding of the output).
+constexpr uint32_t kExp2C[5] = {0x3F317215u, 0x3E75FCE1u, 0x3D635B6Cu, 0x3C1E7456u, 0x3AADED20u};
 
-// Four times the weight 2^x of a score u f against the reference r, x = 128 (y - 1) with y = u f / 128 + 1 - r / 128 held to
-// [0, 1] (the clamp costs nothing on the multiply-add, and holds what r's own rounding leaves above it): f7 = f / 128, c = 1 - r /
-// 128.  n + 2, n = rne(x), goes to the exponent by an integer addition; for 128 <= -x the smallest normal number comes of it.
-constexpr float kExpShift = 12582786.0f;  // 1.5 2^23 - 126
-__device__ __forceinline__ float weight4(float y) {
-  const float t = __builtin_fmaf(y, 128.0f, kExpShift), g = t - kExpShift;  // n + 2 in the low bits; n + 128
-  const float f = __builtin_fmaf(y, 128.0f, -g);
-  float p = __builtin_fmaf(__uint_as_float(kExp2C[3]), f, __uint_as_float(kExp2C[2]));
+// The weight 2^x, x in [-127, 0].  n = rne(x) goes to the exponent by an integer addition; below 2^-126 a subnormal number comes
+// of it, which everything that reads it takes for 0 (at -127, where all that is smaller is held, 0 itself).
+constexpr float kExpShift = 12582912.0f;  // 1.5 2^23
+__device__ __forceinline__ float weight(float x) {
+  const float t = x + kExpShift, g = t - kExpShift;  // n in the low bits; n
+  const float f = x - g;
+  float p = __builtin_fmaf(__uint_as_float(kExp2C[4]), f, __uint_as_float(kExp2C[3]));
+  p = __builtin_fmaf(p, f, __uint_as_float(kExp2C[2]));
   p = __builtin_fmaf(p, f, __uint_as_float(kExp2C[1]));
   p = __builtin_fmaf(p, f, __uint_as_float(kExp2C[0]));
   p = __builtin_fmaf(p, f, 1.0f);
   return __uint_as_float(__float_as_uint(p) + (__float_as_uint(t) << 23));
 }
-__device__ __forceinline__ float to_unit(float x) { return __builtin_amdgcn_fmed3f(x, 0.0f, 1.0f); }
-// A tile's reference for one query.  Beyond 65536 the fused form would lose the largest score itself to r's rounding: it is taken
-// apart there.
+// A tile's reference for one query: x = u f - r in one rounding.  Beyond 2^22 r's own rounding would show in it: the product is
+// rounded as r's was there.
 struct Ref {
-  float r, f, f7, c, ref;
+  float r, f, ref;
   bool near;
   __device__ __forceinline__ Ref(float m, float f_) : f(f_) {
     const float mf = m * f;
     r = m == kNegInf ? m : __builtin_ceilf(mf);
     ref = r == kNegInf ? 0.0f : r;
-    near = fabsf(ref) <= 65536.0f;
-    f7 = f * 0.0078125f;
-    const float r7 = ref * 0.0078125f;
-    c = 1.0f - r7;
+    near = fabsf(ref) <= 4194304.0f;
   }
-  __device__ __forceinline__ float y_near(float u) const { return to_unit(__builtin_fmaf(u, f7, c)); }
-  __device__ __forceinline__ float y(float u) const {
-    const float t = u * f, x = t - ref;
-    const float far = to_unit(__builtin_fmaf(x, 0.0078125f, 1.0f));
-    return near ? y_near(u) : far;
+  static __device__ __forceinline__ float held(float x) { return __builtin_amdgcn_fmed3f(x, -127.0f, 0.0f); }
+  __device__ __forceinline__ float x_near(float u) const { return held(__builtin_fmaf(u, f, -ref)); }
+  __device__ __forceinline__ float x(float u) const {
+    const float t = u * f, far = t - ref;
+    return held(near ? __builtin_fmaf(u, f, -ref) : far);
   }
-  // a tile's sum: of quarters, 0 where no score is above -inf, NaN where one is NaN or +inf
-  __device__ __forceinline__ float sum(float s4) const {
-    const float s = s4 * 0.25f;
+  // a tile's sum: 0 where no score is above -inf, NaN where one is NaN or +inf
+  __device__ __forceinline__ float sum(float s) const {
     return r == kNegInf ? 0.0f : r < __builtin_inff() ? s : __builtin_nanf("");
+  }
+};
+
+// What a tile's products of weight and value step are kept to: multiples of 2^s, the largest, P, between 2^21 and 2^22 of them
+// (s >= -126: the smallest normal number).  A part of 2^-22 of the largest *product*: of the largest value step alone, one key
+// with a large value and no weight took the bits of all the others.
+struct Whole {
+  float up, down;  // 2^-s; 2^s, NaN where P is an infinity or a NaN
+  __device__ __forceinline__ explicit Whole(uint32_t top) {
+    const uint32_t field = top >> 23, up_to = field > 22u ? field : 22u;  // s + 148
+    up = __uint_as_float((275u - up_to) << 23);
+    down = field < 255u ? __uint_as_float((up_to - 21u) << 23) : __builtin_nanf("");
   }
 };
 
@@ -231,24 +239,22 @@ __device__ __forceinline__ void make_query(const CacheAttnArgs& a, const Column&
   out.f = sc * kLog2e;
 }
 
-// Four weights e ratio as whole numbers, 0 .. 32639, into a dword of each digit.  Adding 1.5 2^23 + 128 rounds to a whole number
-// and leaves w + 128 in the low bits: byte 1 is the high digit, byte 0 the low one with its sign bit inverted.
-constexpr float kWhole = 12583040.0f;
-__device__ __forceinline__ void digits4(const float (&e)[4], const f32x4& ratio, int32_t& hi, int32_t& lo) {
-  const uint32_t a = __float_as_uint(__builtin_fmaf(e[0], ratio[0], kWhole)), b = __float_as_uint(__builtin_fmaf(e[1], ratio[1], kWhole));
-  const uint32_t c = __float_as_uint(__builtin_fmaf(e[2], ratio[2], kWhole)), d = __float_as_uint(__builtin_fmaf(e[3], ratio[3], kWhole));
+// Four products as whole numbers of 2^s, 0 .. 2^22, into a dword of each digit.  Adding 2^23 + 32768 + 128 rounds to a whole
+// number and leaves w + 32896 in the low bits: byte 2 is the high digit, bytes 1 and 0 the others with their sign bits inverted.
+constexpr float kWhole = 8421504.0f;
+__device__ __forceinline__ void digits4(const float (&p)[4], float up, int32_t& hi, int32_t& mid, int32_t& lo) {
+  const uint32_t a = __float_as_uint(__builtin_fmaf(p[0], up, kWhole)), b = __float_as_uint(__builtin_fmaf(p[1], up, kWhole));
+  const uint32_t c = __float_as_uint(__builtin_fmaf(p[2], up, kWhole)), d = __float_as_uint(__builtin_fmaf(p[3], up, kWhole));
   const uint32_t ab = __builtin_amdgcn_perm(b, a, 0x05010400u);  // a0 b0 a1 b1
   const uint32_t cd = __builtin_amdgcn_perm(d, c, 0x05010400u);
   lo = (int32_t)(__builtin_amdgcn_perm(cd, ab, 0x05040100u) ^ 0x80808080u);
-  hi = (int32_t)__builtin_amdgcn_perm(cd, ab, 0x07060302u);
+  mid = (int32_t)(__builtin_amdgcn_perm(cd, ab, 0x07060302u) ^ 0x80808080u);
+  const uint32_t ab2 = __builtin_amdgcn_perm(b, a, 0x0C0C0602u), cd2 = __builtin_amdgcn_perm(d, c, 0x06020C0Cu);  // a2 b2 0 0; 0 0 c2 d2
+  hi = (int32_t)(ab2 | cd2);
 }
 
-// what a tile's value steps are multiplied by: a quarter (the weights come times 4) of 32512 / V, 0 where all weights are
-__device__ __forceinline__ float value_recip(uint32_t vtop) {
-  const float V = __uint_as_float(vtop);
-  const float rv = V > 0.0f ? 0.25f * kDigits / V : 0.0f;
-  return rv < __builtin_inff() ? rv : 0.0f;
-}
+// a tile's sum of whole weights and codes, from the sums over the first two digits and over the last
+__device__ __forceinline__ float whole_sum(int32_t hi, int32_t lo) { return __builtin_fmaf((float)hi, 256.0f, (float)lo); }
 
 __device__ __forceinline__ void store_out(const CacheAttnArgs& a, int64_t row, int d, float inv, const f32x4& o, int hd) {
   float f[4];
@@ -265,7 +271,7 @@ __device__ __forceinline__ void store_out(const CacheAttnArgs& a, int64_t row, i
 // ---- one tile of keys a workgroup: few queries, many keys ---------------------------------------------------------------
 //
 // Four wavefronts, each with 64 of the tile's 256 keys in the score product and a quarter of the head's elements in the product
-// with the values (the weights cross through LDS, 8 KB): a workgroup has all of its 2 * 256 * head_dim bytes of the cache on
+// with the values (the weights cross through LDS, 12 KB): a workgroup has all of its 2 * 256 * head_dim bytes of the cache on
 // their way at once and waits for them once.  What a tile gives goes to `parts`, a row's tiles one after the other, to be
 // joined by attn_join_kernel; where there is one tile only, straight to the output.
 // With a window, `span` workgroups a block of queries, from the first tile that one of them sees on (of all tiles, 12 of 257
@@ -275,7 +281,7 @@ __device__ __forceinline__ void store_out(const CacheAttnArgs& a, int64_t row, i
 template <int HD>
 __global__ __launch_bounds__(256) void attn_tile_kernel(CacheAttnArgs a, int64_t tiles, int64_t blocks, int64_t span) {
   constexpr int NS = Query<HD>::NS, ND = HD / 16, NW = (ND + 3) / 4;  // 16-element parts of a head, of a wavefront
-  __shared__ __attribute__((aligned(16))) i32x4 wts[2][4][64];
+  __shared__ __attribute__((aligned(16))) i32x4 wts[3][4][64];
   __shared__ float ms[4][16], ss[4][16];
   __shared__ uint32_t vs[4][16];
   const uint32_t id = blockIdx.x, bt = id / (uint32_t)span, bk = bt / (uint32_t)blocks;
@@ -342,7 +348,6 @@ __global__ __launch_bounds__(256) void attn_tile_kernel(CacheAttnArgs a, int64_t
 
   float t[4][4];
   float m = kNegInf;
-  uint32_t vtop = 0;
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     i32x4 acc = {0, 0, 0, 0};
@@ -356,55 +361,57 @@ __global__ __launch_bounds__(256) void attn_tile_kernel(CacheAttnArgs a, int64_t
       const bool seen = sees.key(at0 + 4 * k + i);
       t[k][i] = seen ? (float)acc[i] * kst[k][i] : kNegInf;
       m = __builtin_elementwise_maximum(m, t[k][i]);
-      const uint32_t u = seen ? __float_as_uint(vst[k][i]) & 0x7FFFFFFFu : 0u;
-      vtop = u > vtop ? u : vtop;
     }
   }
   m = max4(m);
-  vtop = umax4(vtop);
-  if (g == 0) {
-    ms[w][cc] = m;
-    vs[w][cc] = vtop;
-  }
+  if (g == 0) ms[w][cc] = m;
   __syncthreads();
 #pragma unroll
-  for (int o = 0; o < 4; ++o) {
-    m = __builtin_elementwise_maximum(m, ms[o][cc]);
-    vtop = vs[o][cc] > vtop ? vs[o][cc] : vtop;
-  }
+  for (int o = 0; o < 4; ++o) m = __builtin_elementwise_maximum(m, ms[o][cc]);
   const Ref rf(m, qd.f);
-  const float rv = value_recip(vtop);
   float sum = 0.0f;
-  i32x4 wh, wl;
+  uint32_t top = 0;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    float e[4];
-    f32x4 ratio;
+  for (int k = 0; k < 4; ++k)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const bool seen = sees.key(at0 + 4 * k + i);
-      e[i] = weight4(rf.y(t[k][i]));
-      e[i] = seen ? e[i] : 0.0f;
-      sum = sum + e[i];
-      const float x = vst[k][i] * rv;
-      ratio[i] = rv != 0.0f && seen ? x : 0.0f;
+      float e = weight(rf.x(t[k][i])), p = e * vst[k][i];
+      e = seen ? e : 0.0f;
+      p = seen ? p : 0.0f;
+      sum = sum + e;
+      t[k][i] = p;
+      const uint32_t u = __float_as_uint(p) & 0x7FFFFFFFu;
+      top = u > top ? u : top;
     }
-    int32_t h, l;
-    digits4(e, ratio, h, l);
+  top = umax4(top);
+  sum = sum4(sum);
+  if (g == 0) {
+    vs[w][cc] = top;
+    ss[w][cc] = sum;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int o = 0; o < 4; ++o) top = vs[o][cc] > top ? vs[o][cc] : top;
+  const Whole whole(top);
+  i32x4 wh, wm, wl;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    int32_t h, d, l;
+    digits4(t[k], whole.up, h, d, l);
     wh[k] = h;
+    wm[k] = d;
     wl[k] = l;
   }
   wts[0][w][lane] = wh;
-  wts[1][w][lane] = wl;
-  sum = sum4(sum);
-  if (g == 0) ss[w][cc] = sum;
+  wts[1][w][lane] = wm;
+  wts[2][w][lane] = wl;
   __syncthreads();
   const float S = rf.sum((ss[0][cc] + ss[1][cc]) + (ss[2][cc] + ss[3][cc]));
-  const float vsc = __uint_as_float(vtop) * __uint_as_float(kInvDigits);
   const float inv = S == 0.0f ? 0.0f : 1.0f / S;
   float* parts = a.parts + (col.row * tiles + tile) * (HD + 4);
   if (tiles > 1 && col.real && w == 0 && g == 0)
-    *reinterpret_cast<f32x4*>(parts + HD) = f32x4{rf.r, S, vsc, 0.0f};
+    *reinterpret_cast<f32x4*>(parts + HD) = f32x4{rf.r, S, whole.down, 0.0f};
 #pragma unroll
   for (int n = 0; n < NW; ++n) {
     const int part = w + 4 * n;
@@ -415,15 +422,18 @@ __global__ __launch_bounds__(256) void attn_tile_kernel(CacheAttnArgs a, int64_t
     acc = acc << 8;
 #pragma unroll
     for (int q = 0; q < 4; ++q) acc = mfma(vx[n][q], wts[1][q][lane], acc);
+    i32x4 low = {0, 0, 0, 0};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) low = mfma(vx[n][q], wts[2][q][lane], low);
     if (!col.real) continue;
     f32x4 o;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = (float)acc[i];
+    for (int i = 0; i < 4; ++i) o[i] = whole_sum(acc[i], low[i]);
     if (tiles > 1) {
       *reinterpret_cast<f32x4*>(parts + 16 * part + 4 * g) = o;
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) o[i] = S == 0.0f ? 0.0f : o[i] * vsc;
+      for (int i = 0; i < 4; ++i) o[i] = S == 0.0f ? 0.0f : o[i] * whole.down;
       store_out(a, col.row, 16 * part + 4 * g, inv, o, HD);
     }
   }
@@ -460,7 +470,7 @@ __global__ __launch_bounds__(64) void attn_join_kernel(CacheAttnArgs a, int64_t 
       up = lane >= s ? __builtin_elementwise_maximum(up, x) : up;
     }
     const float after = __builtin_elementwise_maximum(R, up), left = __shfl_up(after, 1, 64), before = lane == 0 ? R : left;
-    const float x = shift2(before, after), y = shift2(d[0], after), sy = d[1], sc = d[2] * y;
+    const float x = shift2(before, after), y = shift2(d[0], after), sy = d[1], sc = d[2];
     Vec v[U], ahead[U];
     auto ask = [&](int t0) {
 #pragma unroll
@@ -476,10 +486,10 @@ __global__ __launch_bounds__(64) void attn_join_kernel(CacheAttnArgs a, int64_t 
         const int t = t0 + u < n ? t0 + u : n - 1;
         if (t0 + u >= n) continue;
         auto of = [&](float f) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), t)); };
-        const float xt = of(x), st = of(sc);
-        S = __builtin_fmaf(of(sy), of(y), S * xt);
+        const float xt = of(x), yt = of(y), st = of(sc);
+        S = __builtin_fmaf(of(sy), yt, S * xt);
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(v[u][e], st, o[e] * xt);
+        for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(v[u][e] * yt, st, o[e] * xt);
       }
     }
     R = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(after), n - 1));
@@ -523,7 +533,6 @@ struct RowsLds {
   i32x4 k[16 * NS][64];  // block (4 q + t) NS + s: 64 q keys on, instruction t, elements 64 s on
   i32x4 v[4 * ND][64];   // block q ND + n
   float ks[2][kTile], vs[2][kTile];
-  float ratio[4][kTile];  // RN(vstep rv) where a wavefront's queries all see the whole tile
   int32_t span[4][2];     // tiles of the wavefronts
 };
 
@@ -675,102 +684,68 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void attn_rows_kernel(Cache
       group_slots(t0 + kTile, slots);
       fetch_keys(slots, par ^ 1);
     }
-    // the largest step of the values that a query sees, and what each of them is to it
-    uint32_t vtop = 0;
-    if constexpr (FULL) {
-      const f32x4 vst = *reinterpret_cast<const f32x4*>(&L.vs[par][4 * lane]);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t x = __float_as_uint(vst[i]) & 0x7FFFFFFFu;
-        vtop = x > vtop ? x : vtop;
-      }
-      vtop = lanes_join(vtop, 64, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
-      const float rv = value_recip(vtop);
-      f32x4 ratio;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float x = vst[i] * rv;
-        ratio[i] = rv != 0.0f ? x : 0.0f;
-      }
-      *reinterpret_cast<f32x4*>(&L.ratio[w][4 * lane]) = ratio;
-    } else {
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        if (q >= q0 && q < q1)
-#pragma unroll
-          for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int32_t at = 64 * q + 16 * g + 4 * t + i;
-              const uint32_t x = __float_as_uint(L.vs[par][at]) & 0x7FFFFFFFu;
-              vtop = sees.key(at) && x > vtop ? x : vtop;
-            }
-      vtop = umax4(vtop);
-    }
     m = max4(m);
     const Ref rf(m, qd.f);
     const float r = rf.r;
-    i32x4 wh[4], wl[4];
+    // weights, and their products with the values' steps in the scores' places
     float sums[4];
-    if (FULL && __all(rf.near)) {
+    uint32_t top = 0;
+    auto weigh = [&](auto is_near) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        float sum = 0.0f;
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const f32x4 ratio = *reinterpret_cast<const f32x4*>(&L.ratio[w][64 * q + 16 * g + 4 * t]);
-          float e[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            e[i] = weight4(rf.y_near(u[q][t][i]));
-            sum = sum + e[i];
-          }
-          int32_t h, l;
-          digits4(e, ratio, h, l);
-          wh[q][t] = h;
-          wl[q][t] = l;
-        }
-        sums[q] = sum4(sum);
-      }
-    } else {
-      const float rv = value_recip(vtop);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        wh[q] = i32x4{0, 0, 0, 0};
-        wl[q] = i32x4{0, 0, 0, 0};
         sums[q] = 0.0f;
-        if (q < q0 || q >= q1) continue;
+        if (!FULL && (q < q0 || q >= q1)) {
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) u[q][t][i] = 0.0f;
+          continue;
+        }
         float sum = 0.0f;
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           const f32x4 vst = *reinterpret_cast<const f32x4*>(&L.vs[par][64 * q + 16 * g + 4 * t]);
-          f32x4 ratio;
-          float e[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const bool seen = FULL || sees.key(64 * q + 16 * g + 4 * t + i);
-            e[i] = weight4(rf.y(u[q][t][i]));
-            e[i] = seen ? e[i] : 0.0f;
-            sum = sum + e[i];
-            const float x = vst[i] * rv;
-            ratio[i] = rv != 0.0f && seen ? x : 0.0f;
+            float e = weight(is_near.value ? rf.x_near(u[q][t][i]) : rf.x(u[q][t][i])), p = e * vst[i];
+            e = seen ? e : 0.0f;
+            p = seen ? p : 0.0f;
+            sum = sum + e;
+            u[q][t][i] = p;
+            const uint32_t x = __float_as_uint(p) & 0x7FFFFFFFu;
+            top = x > top ? x : top;
           }
-          int32_t h, l;
-          digits4(e, ratio, h, l);
-          wh[q][t] = h;
-          wl[q][t] = l;
         }
         sums[q] = sum4(sum);
+        // one quarter's steps in registers at a time (all four's: 45 registers spilled, 16 heads x 4096 160 us instead of 142)
+        __builtin_amdgcn_sched_barrier(0);
       }
-    }
+    };
+    if (__all(rf.near)) weigh(std::true_type{});
+    else weigh(std::false_type{});
+    const Whole whole(umax4(top));
+    i32x4 wh[4], wm[4], wl[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        int32_t h, d, l;
+        digits4(u[q][t], whole.up, h, d, l);
+        wh[q][t] = h;
+        wm[q][t] = d;
+        wl[q][t] = l;
+      }
     const float Sb = rf.sum((sums[0] + sums[1]) + (sums[2] + sums[3]));
     const float Rn = __builtin_elementwise_maximum(R, r), x = shift2(R, Rn), y = shift2(r, Rn);
-    // A column that sees nothing of the tile has S_b = 0, A = 0 and V = 0 and keeps R: the steps below leave its row as it is
-    // (but for the sign of a zero, which the output's + 0 takes away).
+    // A column that sees nothing of the tile has S_b = 0 and A = 0 and keeps R: the steps below leave its row as it is (but for
+    // the sign of a zero, which the output's + 0 takes away).
     S = __builtin_fmaf(Sb, y, S * x);
     R = Rn;
-    const float vsc = __uint_as_float(vtop) * __uint_as_float(kInvDigits), sc = vsc * y;
-    const bool still = __all(x == 1.0f);
+    // A y 2^s = A (y 2^s) but where that is subnormal
+    float sc = whole.down * y;
+    const bool tiny = __any(sc == 0.0f && y > 0.0f), still = __all(x == 1.0f);
+    if (tiny) sc = whole.down;
     // the values have landed (what was asked for after them, the next keys, may not have)
     if (more) vm_left<4 * NS + 2>();
     else vm_left<0>();
@@ -786,9 +761,9 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void attn_rows_kernel(Cache
     constexpr int C = 2;  // chains of products side by side
 #pragma unroll
     for (int n = 0; n < ND; n += C) {
-      i32x4 acc[C], vx[C][4];
+      i32x4 acc[C], low[C], vx[C][4];
 #pragma unroll
-      for (int d = 0; d < C; ++d) acc[d] = i32x4{0, 0, 0, 0};
+      for (int d = 0; d < C; ++d) acc[d] = low[d] = i32x4{0, 0, 0, 0};
 #pragma unroll
       for (int q = 0; q < 4; ++q)
 #pragma unroll
@@ -802,11 +777,19 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void attn_rows_kernel(Cache
 #pragma unroll
       for (int q = 0; q < 4; ++q)
 #pragma unroll
-        for (int d = 0; d < C; ++d) acc[d] = mfma(vx[d][q], wl[q], acc[d]);
+        for (int d = 0; d < C; ++d) low[d] = mfma(vx[d][q], wl[q], low[d]);
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int d = 0; d < C; ++d) acc[d] = mfma(vx[d][q], wm[q], acc[d]);
 #pragma unroll
       for (int d = 0; d < C; ++d)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[n + d][i] = __builtin_fmaf((float)acc[d][i], sc, o[n + d][i]);
+        for (int i = 0; i < 4; ++i) {
+          float s = whole_sum(acc[d][i], low[d][i]);
+          if (tiny) s = s * y;
+          o[n + d][i] = __builtin_fmaf(s, sc, o[n + d][i]);
+        }
     }
     __builtin_amdgcn_s_setprio(0);
   };

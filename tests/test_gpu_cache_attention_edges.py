@@ -1,10 +1,12 @@
-"""canon_cache_attention at the ends of its range: a cache of no pages."""
+"""canon_cache_attention at the ends of its range: a cache of no pages, values of very different sizes."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2609_17380_amd.canon as C
-from gpu_util import DEV, dev_i32, host_u16, poisoned_workspace
+from gpu_util import DEV, assert_bits, dev_f32, dev_i32, host_u16, poisoned_workspace
+from serve_bounds import SPREADS, attention_bound, spread_case
+from serve_util import device_cache, from_bf16
 
 pytestmark = pytest.mark.gpu
 
@@ -28,3 +30,29 @@ def test_no_keys(D, pages, table_len):
             C.cache_attention(cache, rows, q, out, poisoned_workspace(C.cache_attention_workspace_bytes(cache, rows)))
             torch.cuda.synchronize()
             assert (host_u16(out) == 0).all(), (Q, G)
+
+
+def attend(c, q, k_len, scale, starts):
+    B, Q, H, D = q.shape
+    cache = device_cache(c)
+    rows = C.AttnRows(B, H, Q, k_len, scale=scale, q_starts=dev_i32(np.asarray(starts)))
+    out = torch.full((B * Q, H * D), 7.0, dtype=torch.bfloat16, device=DEV)
+    C.cache_attention(cache, rows, dev_f32(q).view(B * Q, H * D), out,
+                      poisoned_workspace(C.cache_attention_workspace_bytes(cache, rows)))
+    torch.cuda.synchronize()
+    return host_u16(out).reshape(q.shape)
+
+
+@pytest.mark.parametrize("kind,size", SPREADS)
+@pytest.mark.parametrize("prompt", [False, True])
+def test_values_of_different_sizes(kind, size, prompt):
+    # a workgroup for a tile, and (a prompt) wavefronts that take all keys
+    K = 1024
+    c, q = spread_case(kind, size, KV=8, Q=K) if prompt else spread_case(kind, size)
+    first = K - q.shape[1]
+    got = attend(c, q, K, 0.125, [first])
+    for at in ((0, 96, 255, 500, K - 3) if prompt else (0,)):
+        few = np.ascontiguousarray(q[:, at:at + 3])
+        assert_bits(got[:, at:at + 3], c.attention(few, K, 0.125, [first + at], [3], [K]), f"rows from {at}")
+        want, bound = attention_bound(c, few, 0.125, [first + at], [3], [K])
+        assert (np.abs(from_bf16(got[:, at:at + 3]) - want) <= bound).all(), at
