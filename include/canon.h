@@ -619,32 +619,34 @@ canon_status canon_cache_read(const canon_kv_cache* cache, const canon_cache_row
                               void* stream);
 
 /* Attention over such a cache (R26).  rows as for canon_softmax_relbias (batch that of the cache, ld 0): query i sees the
-   keys j < k_len <= table_len * page (0 for a cache of no pages) with j < k_lens[b], j <= pos (if causal), |pos - j| < window (if window > 0), and none
-   if i >= q_lens[b].  q [batch * q_len][n_heads][head_dim], tokens q_stride elements apart, fp32 or bf16, turned already;
+   keys j < k_len <= table_len * page (0 for a cache of no pages) with j < k_lens[b], j <= pos (if causal), |pos - j| < window
+   (if window > 0), and none if i >= q_lens[b].  q [batch * q_len][n_heads][head_dim], tokens q_stride elements apart, fp32 or bf16, turned already;
    query head h reads key/value head h / (n_heads / n_kv_heads).  out (bf16 [batch * q_len][n_heads * head_dim]) = the sum of
    the values weighted by 2^(z - max z), z = scale log2(e) q.k, over the sum of the weights.  The rule takes every long sum in
    integers, which no order changes, and what remains by tiles of 256 keys (key j is in tile j / 256):
-     query:  sq = RN(amax * RN(1/32512)), rs = CRdiv(1, sq), Q = clamp(rne(RN(q rs)), -32512, 32512) (0 for a NaN or a step
-             that is not > 0; -q in place of q for a negative scale), f = RN(RN(sq |scale|) * RN(log2 e))
-     scores: u_j = RN(RN32(sum_d Q_d K_jd) kstep_j), the sum exact; they stand for u_j f
+     three digits: of numbers of which M is the largest magnitude, s = the least whole number with rne(M 2^-s) <= 8355711 = 127
+             (65536 + 256 + 1), n = rne(x 2^-s) = 256 h + l with -128 <= l < 128; a sum of products with codes c is fma(RN32(sum h
+             c), 256, sum l c), both sums exact
+     query:  Q = three digits of q (-q for a negative scale), f = RN(RN(|scale| RN(log2 e)) 2^s); Q = f = 0 where the largest |q|
+             is below 2^-126, f = NaN where it is an infinity or a NaN
+     scores: u_j = RN((Q . K_j) kstep_j); they stand for u_j f
      tile:   r = ceil(RN(max u_j f)) (-inf where the largest u_j is; read as 0 there in what follows)
              x_j = fma(u_j, f, -r), or where |r| > 2^22 RN(RN(u_j f) - r), held to [-127, 0]; e_j = exp2(x_j)
              S_b = the 16 sums of 16 consecutive keys' e, each a chain from +0, joined by a perfect pairwise tree;
              keys that are not seen are +0 terms; 0 where r is -inf, NaN where a u_j is NaN or r is +inf
-             p_j = RN(e_j vstep_j), P = the largest of them by bit pattern, s = max(floor(log2 P) - 21, -126), w_j = rne(p_j 2^-s) =
-             256 h_j + l_j with -128 <= l_j < 128, A_d = fma(RN32(sum h_j V_jd), 256, sum l_j V_jd), both sums exact (NaN
-             where P is an infinity or a NaN)
+             w = three digits of the p_j = RN(e_j vstep_j), s not below -126, A_d = w . V_d (NaN where a p_j is an infinity or a NaN)
      row:    over the tiles with a key that is seen, ascending, from R = -inf, S = 0, O = 0: R' = max(R, r),
              x = 2^(R - R'), y = 2^(r - R') (1 where R, or r, is -inf; 0 below 2^-126), S = fma(S_b, y, RN(S x)),
              O_d = fma(RN(A_d y), 2^s, RN(O_d x))
      out:    bf16(RN(RN(O_d + 0) CRdiv(1, S))), +0 where S = 0 (no key seen, or only scores of -inf)
    exp2(x): n = rne(x), p = 1 + t (C1 + t (C2 + t (C3 + t (C4 + t C5)))) by fma with t = x - n, p 2^n (0 below 2^-126); the C are
    0x3F317215, 0x3E75FCE1, 0x3D635B6C, 0x3C1E7456, 0x3AADED20: 2^x within 1.6e-7 of itself.
-   A weight times its value's step is kept to 2^-22 of the largest such product of its tile, so that a key counts by what it adds
-   to the row, whatever the values of the others.
-   A query's row is the same in a prompt and alone, whatever the batch and the other sequences are.  Queries
-   enter with 16 bits (two digits of 8): a part of 2^-16 of the largest.  What stands in places that are not seen (in unused slots, pages and table entries too) is not used; a key that is seen in a page that the
-   cache does not have makes the row NaN.
+   A query element is kept to 2^-22 of the query's largest (bf16 elements down to 2^-14 of it as they are), a weight times its
+   value's step to 2^-22 of the largest such product of its tile: a key counts by what it adds to the row, whatever the values
+   of the others.  Sums over 2^104 times the query's largest element overflow: a row that sees such a score is NaN.
+   A query's row is the same in a prompt and alone, whatever the batch and the other sequences are.  What stands in places
+   that are not seen (in unused slots, pages and table entries too) is not used; a key that is seen in a page that the cache
+   does not have makes the row NaN.
    k_len up to 2^21, batch * n_heads * q_len below 2^24 (else CANON_EUNSUPPORTED), window >= 0, |q_start| up to 2^30.
    workspace: device memory of canon_cache_attention_workspace_bytes(cache, rows) bytes, 256-byte aligned; 0 where none is
    needed. */

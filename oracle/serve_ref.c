@@ -121,6 +121,16 @@ int cref_exp2_unit(int64_t n, const float* y, float* e4) {
   }
   return 0;
 }
+/* what is left of a whole number to the nearest multiple of 256, -128 .. 127 */
+static int64_t low_digit(int64_t n) { return ((n + 128) % 256 + 256) % 256 - 128; }
+
+/* the least s for which x 2^-s, rounded, fits three digits of -128 .. 127: 127 (65536 + 256 + 1); x finite, not negative */
+static int step_of(float x) {
+  int s = -200;
+  while (rint(ldexp((double)x, -s)) > 8355711.0) ++s;
+  return s;
+}
+
 /* x held to [-127, 0] */
 static float held(float x) { return x > -127.0f ? (x < 0.0f ? x : 0.0f) : -127.0f; }
 
@@ -136,7 +146,6 @@ int cref_cache_attention(const int64_t* cache, const int64_t* cfg, float scale, 
                          const int32_t* q_starts, const int32_t* q_lens, const int32_t* k_lens, const int8_t* kc,
                          const int8_t* vc, const float* ks, const float* vs, const float* q, uint16_t* out) {
   const int64_t B = cache[4], KV = cache[2], D = cache[3], H = cfg[0], QL = cfg[1], KL = cfg[2], W = cfg[3];
-  const float inv = of_bits(0x38010204u); /* RN32(1/32512) */
 #pragma omp parallel for schedule(dynamic, 4)
   for (int64_t r = 0; r < B * QL * H; ++r) {
     const int64_t h = r % H, i = r / H % QL, b = r / H / QL, kvh = h / (H / KV);
@@ -148,12 +157,11 @@ int cref_cache_attention(const int64_t* cache, const int64_t* cfg, float scale, 
       const uint32_t u = to_bits(x[d]) & 0x7FFFFFFFu;
       if (u > amax) amax = u;
     }
-    const float sq = cref_mul(of_bits(amax), inv), rs = sq > 0.0f ? cref_div(1.0f, sq) : 0.0f;
-    for (int64_t d = 0; d < D; ++d) {
-      const float v = cref_mul(scale < 0.0f ? -x[d] : x[d], rs);
-      Q[d] = !(sq > 0.0f) || v != v ? 0 : v > 32512.0f ? 32512 : v < -32512.0f ? -32512 : (int64_t)rintf(v);
-    }
-    const float f = cref_mul(cref_mul(sq, fabsf(scale)), of_bits(0x3FB8AA3Bu)); /* RN32(1 / ln 2) */
+    const int zero = amax < 0x00800000u, finite_q = !zero && amax < 0x7F800000u, qs = finite_q ? step_of(of_bits(amax)) : 0;
+    for (int64_t d = 0; d < D; ++d)
+      Q[d] = finite_q ? (int64_t)rint(ldexp((double)flushed(scale < 0.0f ? -x[d] : x[d]), -qs)) : 0;
+    const double fs = ldexp((double)cref_mul(fabsf(scale), of_bits(0x3FB8AA3Bu)), qs); /* RN32(1 / ln 2) */
+    const float f = zero ? 0.0f : !finite_q ? NAN : fs >= 0x1p128 ? INFINITY : fs < 0x1p-126 ? 0.0f : (float)fs;
     float R = -INFINITY, S = 0.0f, O[256]; /* a NaN among the scores makes R and S NaN */
     for (int64_t d = 0; d < D; ++d) O[d] = 0.0f;
     for (int64_t j0 = 0; j0 < KL; j0 += 256) {
@@ -167,9 +175,13 @@ int cref_cache_attention(const int64_t* cache, const int64_t* cfg, float scale, 
         if (!sees[j]) continue;
         any = 1;
         slot[j] = slot_of(cache, table, b, kvh, key);
-        int64_t acc = 0;
-        for (int64_t d = 0; slot[j] >= 0 && d < D; ++d) acc += Q[d] * kc[slot[j] * D + d];
-        t[j] = slot[j] < 0 ? NAN : cref_mul((float)acc, ks[slot[j]]);
+        int64_t hi = 0, lo = 0;
+        for (int64_t d = 0; slot[j] >= 0 && d < D; ++d) {
+          const int64_t l = low_digit(Q[d]);
+          hi += (Q[d] - l) / 256 * kc[slot[j] * D + d];
+          lo += l * kc[slot[j] * D + d];
+        }
+        t[j] = slot[j] < 0 ? NAN : cref_mul(cref_fma((float)hi, 256.0f, (float)lo), ks[slot[j]]);
         if (t[j] > m || t[j] != t[j] || m != m) m = t[j] != t[j] || m != m ? NAN : t[j];
       }
       if (!any) continue;
@@ -192,9 +204,9 @@ int cref_cache_attention(const int64_t* cache, const int64_t* cfg, float scale, 
       }
       for (int n = 16; n > 1; n /= 2)
         for (int c = 0; c < n / 2; ++c) part[c] = cref_add(part[2 * c], part[2 * c + 1]);
-      /* whole weights: multiples of 2^step of the products, 2^21 .. 2^22 of the largest */
-      const int finite = top < 0x7F800000u, exponent = (int)(top >> 23) - 127;
-      const int step = exponent - 21 > -126 ? exponent - 21 : -126;
+      const int finite = top < 0x7F800000u;
+      int step = finite ? step_of(of_bits(top)) : 0;
+      if (step < -126) step = -126;
       const float Rn = R != R || rb != rb ? NAN : R > rb ? R : rb, xo = shift(R, Rn), y = shift(rb, Rn);
       const float Sb = rb == -INFINITY ? 0.0f : rb < INFINITY ? part[0] : NAN;
       S = cref_fma(Sb, y, cref_mul(S, xo));
@@ -202,7 +214,7 @@ int cref_cache_attention(const int64_t* cache, const int64_t* cfg, float scale, 
         int64_t hi = 0, lo = 0;
         for (int64_t j = 0; j < 256; ++j)
           if (sees[j] && finite && slot[j] >= 0) {
-            const int64_t w = (int64_t)rint(ldexp((double)p[j], -step)), l = (w + 128) % 256 - 128;
+            const int64_t w = (int64_t)rint(ldexp((double)p[j], -step)), l = low_digit(w);
             hi += (w - l) / 256 * vc[v_at(cache, slot[j], d)];
             lo += l * vc[v_at(cache, slot[j], d)];
           }

@@ -1,10 +1,9 @@
 // attn_cache.hip - attention over the paged cache of keys and values in 8 bits (R26).
 //
-// Every long sum is a sum of products of whole numbers, so it runs on the int8 matrix instructions in any order: a query is a
-// whole number of 16 bits, split into two digits of 8, x = 256 hi + lo, and sum x k = 256 sum hi k + sum lo k; a weight one of
-// 23 bits in three digits, x = 256 (256 hi + mid) + lo, the sum over its first two exact in 32 bits and the third's another.
-// Left to floating point are a maximum, a tile's 256 exponentials and their tree, and one fused multiply-add per tile and
-// element, with every change of reference a power of two.
+// Every long sum is a sum of products of whole numbers, so it runs on the int8 matrix instructions in any order: a query (and a
+// weight times its value's step) is a whole number of 23 bits in three digits of 8, x = 256 (256 hi + mid) + lo, the sum over the
+// first two of them exact in 32 bits and that over the third another.  Left to floating point are a maximum, a tile's 256
+// exponentials and their tree, and one fused multiply-add per tile and element, with every change of reference a power of two.
 //
 // v_mfma_i32_16x16x64_i8 multiplies 16 rows by 16 columns over 64 k.  Lane (c, g) = (lane % 16, lane / 16) supplies bytes 16 g
 // .. 16 g + 15 of row (column) c and receives rows 4 g .. 4 g + 3 of column c.  Keys are the rows of the score product, queries
@@ -29,8 +28,6 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 namespace {
 
 constexpr int kTile = 256;                      // keys of a tile of the rule
-constexpr float kDigits = 32512.0f;             // largest whole number of a query or a weight: its high digit is 127
-constexpr uint32_t kInvDigits = 0x38010204u;    // RN32(1 / 32512)
 constexpr float kNegInf = -__builtin_inff();
 
 #define CANON_NAN4 __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")
@@ -77,15 +74,17 @@ struct Ref {
   }
 };
 
-// What a tile's products of weight and value step are kept to: multiples of 2^s, the largest, P, between 2^21 and 2^22 of them
-// (s >= -126: the smallest normal number).  A part of 2^-22 of the largest *product*: of the largest value step alone, one key
-// with a large value and no weight took the bits of all the others.
+// Numbers are kept as multiples of 2^s, s the least that leaves the largest of them three digits, 127 (65536 + 256 + 1): its
+// exponent less 22, or 21 where its significand is above theirs.  s + 149 for the largest number's bits:
+__device__ __forceinline__ uint32_t three_digits(uint32_t top) { return (top + 65793u) >> 23; }
+// What a tile's products of weight and value step are kept to (s >= -126: the smallest normal number).  A part of the largest
+// *product*: of the largest value step alone, one key with a large value and no weight took the bits of all the others.
 struct Whole {
-  float up, down;  // 2^-s; 2^s, NaN where P is an infinity or a NaN
+  float up, down;  // 2^-s; 2^s, NaN where the largest is an infinity or a NaN
   __device__ __forceinline__ explicit Whole(uint32_t top) {
-    const uint32_t field = top >> 23, up_to = field > 22u ? field : 22u;  // s + 148
-    up = __uint_as_float((275u - up_to) << 23);
-    down = field < 255u ? __uint_as_float((up_to - 21u) << 23) : __builtin_nanf("");
+    const uint32_t at = three_digits(top), s149 = at > 23u ? at : 23u;
+    up = __uint_as_float((276u - s149) << 23);
+    down = top < 0x7F800000u ? __uint_as_float((s149 - 22u) << 23) : __builtin_nanf("");
   }
 };
 
@@ -164,6 +163,9 @@ __device__ __forceinline__ int32_t page_of(const CacheAttnArgs& a, int64_t b, in
   return j < a.k_len ? a.c.table[b * a.c.table_len + (j >> a.c.lg)] : -1;
 }
 
+// a sum of products, from the sums over the first two digits and over the last
+__device__ __forceinline__ float whole_sum(int32_t hi, int32_t lo) { return __builtin_fmaf((float)hi, 256.0f, (float)lo); }
+
 __device__ __forceinline__ i32x4 load16(const int8_t* p) { return *reinterpret_cast<const i32x4*>(p); }
 
 // The queries of a block: lane (c, g) has elements 64 s + 16 g .. + 15 of column c, first as they are stored (asked for early),
@@ -179,7 +181,7 @@ struct RawQuery {
 template <int HD>
 struct Query {
   static constexpr int NS = (HD + 63) / 64;
-  i32x4 hi[NS], lo[NS];
+  i32x4 hi[NS], mid[NS], lo[NS];
   float f;
 };
 template <int HD>
@@ -217,29 +219,35 @@ __device__ __forceinline__ void make_query(const CacheAttnArgs& a, const Column&
     }
   }
   top = umax4(top);
-  const float sq = __uint_as_float(top) * __uint_as_float(kInvDigits);
-  const float rs = sq > 0.0f ? 1.0f / sq : 0.0f, sgn = a.scale < 0.0f ? -rs : rs;  // a product's sign passes its rounding
+  // Whole numbers of three digits: bf16 elements down to 2^-14 of the largest come as they are (with 16 bits, a channel 1000
+  // times the others left these six, and outputs off by 2%).  2^-s and 2^s in two factors each, as their exponents leave the
+  // range of one; a product with them rounds at most to zero.
+  const int s = (int)three_digits(top) - 149, h = s >> 1;
+  const bool zero = top < 0x00800000u, finite = !zero && top < 0x7F800000u;
+  auto pow2 = [](int e) { return __uint_as_float((uint32_t)(e + 127) << 23); };
+  const float up = pow2(-h), up2 = a.scale < 0.0f ? -pow2(h - s) : pow2(h - s);
 #pragma unroll
-  for (int s = 0; s < NS; ++s)
+  for (int q = 0; q < NS; ++q)
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      uint32_t h = 0, l = 0;
+      uint32_t d0 = 0, d1 = 0, d2 = 0;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        float x = v[s][4 * w + e] * sgn;
-        x = sq > 0.0f && x == x ? fminf(fmaxf(x, -kDigits), kDigits) : 0.0f;
-        const int32_t n = (int32_t)__builtin_rintf(x), d = (n + 128) >> 8;  // n = 256 d + (n - 256 d), the rest in [-128, 127]
-        h |= (uint32_t)(d & 0xFF) << (8 * e);
-        l |= (uint32_t)(n & 0xFF) << (8 * e);
+        const float x = v[q][4 * w + e] * up;
+        const int32_t n = (int32_t)__builtin_rintf(finite ? x * up2 : 0.0f);
+        d0 |= (uint32_t)(n & 0xFF) << (8 * e);  // n = 65536 d2 + 256 d1 + d0, the last two in [-128, 127]
+        d1 |= (uint32_t)(((n + 128) >> 8) & 0xFF) << (8 * e);
+        d2 |= (uint32_t)(((n + 32896) >> 16) & 0xFF) << (8 * e);
       }
-      out.hi[s][w] = (int32_t)h;
-      out.lo[s][w] = (int32_t)l;
+      out.hi[q][w] = (int32_t)d2;
+      out.mid[q][w] = (int32_t)d1;
+      out.lo[q][w] = (int32_t)d0;
     }
-  const float sc = sq * fabsf(a.scale);
-  out.f = sc * kLog2e;
+  const float sc = fabsf(a.scale) * kLog2e, part = sc * pow2(h), f = part * pow2(s - h);
+  out.f = zero ? 0.0f : finite ? f : __builtin_nanf("");
 }
 
-// Four products as whole numbers of 2^s, 0 .. 2^22, into a dword of each digit.  Adding 2^23 + 32768 + 128 rounds to a whole
+// Four products as whole numbers of 2^s, 0 .. 8355711, into a dword of each digit.  Adding 2^23 + 32768 + 128 rounds to a whole
 // number and leaves w + 32896 in the low bits: byte 2 is the high digit, bytes 1 and 0 the others with their sign bits inverted.
 constexpr float kWhole = 8421504.0f;
 __device__ __forceinline__ void digits4(const float (&p)[4], float up, int32_t& hi, int32_t& mid, int32_t& lo) {
@@ -252,9 +260,6 @@ __device__ __forceinline__ void digits4(const float (&p)[4], float up, int32_t& 
   const uint32_t ab2 = __builtin_amdgcn_perm(b, a, 0x0C0C0602u), cd2 = __builtin_amdgcn_perm(d, c, 0x06020C0Cu);  // a2 b2 0 0; 0 0 c2 d2
   hi = (int32_t)(ab2 | cd2);
 }
-
-// a tile's sum of whole weights and codes, from the sums over the first two digits and over the last
-__device__ __forceinline__ float whole_sum(int32_t hi, int32_t lo) { return __builtin_fmaf((float)hi, 256.0f, (float)lo); }
 
 __device__ __forceinline__ void store_out(const CacheAttnArgs& a, int64_t row, int d, float inv, const f32x4& o, int hd) {
   float f[4];
@@ -355,11 +360,14 @@ __global__ __launch_bounds__(256) void attn_tile_kernel(CacheAttnArgs a, int64_t
     for (int s = 0; s < NS; ++s) acc = mfma(kx[k][s], qd.hi[s], acc);
     acc = acc << 8;
 #pragma unroll
-    for (int s = 0; s < NS; ++s) acc = mfma(kx[k][s], qd.lo[s], acc);
+    for (int s = 0; s < NS; ++s) acc = mfma(kx[k][s], qd.mid[s], acc);
+    i32x4 low = {0, 0, 0, 0};
+#pragma unroll
+    for (int s = 0; s < NS; ++s) low = mfma(kx[k][s], qd.lo[s], low);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const bool seen = sees.key(at0 + 4 * k + i);
-      t[k][i] = seen ? (float)acc[i] * kst[k][i] : kNegInf;
+      t[k][i] = seen ? whole_sum(acc[i], low[i]) * kst[k][i] : kNegInf;
       m = __builtin_elementwise_maximum(m, t[k][i]);
     }
   }
@@ -381,7 +389,7 @@ __global__ __launch_bounds__(256) void attn_tile_kernel(CacheAttnArgs a, int64_t
       p = seen ? p : 0.0f;
       sum = sum + e;
       t[k][i] = p;
-      const uint32_t u = __float_as_uint(p) & 0x7FFFFFFFu;
+      const uint32_t u = __float_as_uint(p);  // never negative
       top = u > top ? u : top;
     }
   top = umax4(top);
@@ -642,9 +650,9 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void attn_rows_kernel(Cache
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       if (FULL || (q >= q0 && q < q1)) {
-        i32x4 acc[4], kx[4][NS];
+        i32x4 acc[4], low[4], kx[4][NS];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) acc[t] = i32x4{0, 0, 0, 0};
+        for (int t = 0; t < 4; ++t) acc[t] = low[t] = i32x4{0, 0, 0, 0};
 #pragma unroll
         for (int s = 0; s < NS; ++s)
 #pragma unroll
@@ -658,13 +666,17 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void attn_rows_kernel(Cache
 #pragma unroll
         for (int s = 0; s < NS; ++s)
 #pragma unroll
-          for (int t = 0; t < 4; ++t) acc[t] = mfma(kx[t][s], qd.lo[s], acc[t]);
+          for (int t = 0; t < 4; ++t) low[t] = mfma(kx[t][s], qd.lo[s], low[t]);
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+          for (int t = 0; t < 4; ++t) acc[t] = mfma(kx[t][s], qd.mid[s], acc[t]);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           const f32x4 st = *reinterpret_cast<const f32x4*>(&L.ks[par][64 * q + 16 * g + 4 * t]);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            u[q][t][i] = (float)acc[t][i] * st[i];
+            u[q][t][i] = whole_sum(acc[t][i], low[t][i]) * st[i];
             if (!FULL) u[q][t][i] = sees.key(64 * q + 16 * g + 4 * t + i) ? u[q][t][i] : kNegInf;
             m = __builtin_elementwise_maximum(m, u[q][t][i]);
           }
@@ -713,7 +725,7 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void attn_rows_kernel(Cache
             p = seen ? p : 0.0f;
             sum = sum + e;
             u[q][t][i] = p;
-            const uint32_t x = __float_as_uint(p) & 0x7FFFFFFFu;
+            const uint32_t x = __float_as_uint(p);  // never negative
             top = x > top ? x : top;
           }
         }
@@ -742,10 +754,7 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void attn_rows_kernel(Cache
     // the sign of a zero, which the output's + 0 takes away).
     S = __builtin_fmaf(Sb, y, S * x);
     R = Rn;
-    // A y 2^s = A (y 2^s) but where that is subnormal
-    float sc = whole.down * y;
-    const bool tiny = __any(sc == 0.0f && y > 0.0f), still = __all(x == 1.0f);
-    if (tiny) sc = whole.down;
+    const bool still = __all(x == 1.0f);
     // the values have landed (what was asked for after them, the next keys, may not have)
     if (more) vm_left<4 * NS + 2>();
     else vm_left<0>();
@@ -786,9 +795,8 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void attn_rows_kernel(Cache
       for (int d = 0; d < C; ++d)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          float s = whole_sum(acc[d][i], low[d][i]);
-          if (tiny) s = s * y;
-          o[n + d][i] = __builtin_fmaf(s, sc, o[n + d][i]);
+          const float s = whole_sum(acc[d][i], low[d][i]) * y;  // y 2^s may be subnormal where this times 2^s is not
+          o[n + d][i] = __builtin_fmaf(s, whole.down, o[n + d][i]);
         }
     }
     __builtin_amdgcn_s_setprio(0);

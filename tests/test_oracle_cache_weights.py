@@ -1,9 +1,10 @@
-"""R26 against the formula where the tokens' values are of very different sizes: a key counts by what it adds to the row."""
+"""R26 against the formula where the tokens' values, or the channels of a query, are of very different sizes: a key counts by what
+it adds to the row."""
 import numpy as np
 import pytest
 
 import oracle
-from serve_bounds import SPREADS, attention_bound, spread_case
+from serve_bounds import OUTLIERS, SPREADS, attention_bound, outlier_case, spread_case
 from serve_util import from_bf16
 
 
@@ -17,6 +18,29 @@ def test_values_of_different_sizes(kind, size):
     if kind == "none":  # the row is one of the other keys': rounding to bf16 alone leaves 1.7e-3
         rms = np.sqrt(((got - want) ** 2).mean(-1) / (want ** 2).mean(-1))
         assert (rms <= 2.5e-3).all()
+
+
+@pytest.mark.parametrize("times,bf16", OUTLIERS)
+def test_channels_of_different_sizes(times, bf16):
+    c, q = outlier_case(times, bf16)
+    K, Q = 700, q.shape[1]
+    got = from_bf16(c.attention(q, K, 0.125, [K - Q], [Q], [K])).astype(np.float64)
+    want, bound = attention_bound(c, q, 0.125, [K - Q], [Q], [K])
+    assert (np.abs(got - want) <= bound).all(), np.max(np.abs(got - want) / bound)
+    # rounding to bf16 alone leaves 1.7e-3; at 10^4 the largest channel passes 2^15, the others come as multiples of 2^-7, and 0.29 of
+    # that on 63 channels, times a key's 1 and the scale, leaves a score off by 2.2e-3 more
+    if times <= 1e3:
+        assert (np.sqrt(((got - want) ** 2).mean(-1) / (want ** 2).mean(-1)) <= 2.5e-3).all()
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e30])
+def test_scores_are_products_of_query_and_scale(scale):
+    # a query and a scale of sizes whose product is an ordinary score's
+    c, q = spread_case("all", 1.0, K=300)
+    plain = c.attention(q, 300, 0.125, [297], [3], [300])
+    other = c.attention(q * np.float32(2.0 ** -100 if scale > 1 else 2.0 ** 100), 300,
+                        0.125 * (2.0 ** 100 if scale > 1 else 2.0 ** -100), [297], [3], [300])
+    assert np.array_equal(plain, other)
 
 
 def test_exp2():
