@@ -687,15 +687,14 @@ class Rotation(ctypes.Structure):
         half, n = max(rot_dim // 2, 1), cos.numel()
         if n % half or n != sin.numel():
             raise ValueError(f"cos and sin: [positions, {rot_dim // 2}] are needed, not {tuple(cos.shape)} and {tuple(sin.shape)}")
-        self.tensors, self.device = (cos, sin), cos.get_device()
-        super().__init__(rot_dim, int(interleaved), n // half if rot_dim > 0 else 0, _arg(cos, "cos", n, _T32, self.device),
-                         _arg(sin, "sin", n, _T32, self.device))
+        self.tensors, self.numel = (cos, sin), n
+        super().__init__(rot_dim, int(interleaved), n // half if rot_dim > 0 else 0)
+        self._of(cos.get_device())
 
     def _of(self, dev):
-        """The record's address, with the present addresses of tables that were checked when they came."""
-        if dev != self.device:
-            raise ValueError(f"a rotation's tables on the current device are needed, not on device {self.device}")
-        self.cos, self.sin = self.tensors[0].data_ptr(), self.tensors[1].data_ptr()
+        """The record's address, once its tables are what they were when it was made, wherever they are now."""
+        cos, sin = self.tensors
+        self.cos, self.sin = _arg(cos, "cos", self.numel, _T32, dev), _arg(sin, "sin", self.numel, _T32, dev)
         return ctypes.byref(self)
 
 
@@ -720,31 +719,28 @@ class KVCache(ctypes.Structure):
         one = page * kv_heads * dim
         if not isinstance(k_codes, torch.Tensor) or page < 1 or kv_heads < 1 or dim < 1 or k_codes.numel() % one:
             raise ValueError(f"k_codes: a tensor of pages of {one} codes is needed")
-        codes = k_codes.numel()
-        self.tensors, self.device = (k_codes, v_codes, k_steps, v_steps), k_codes.get_device()
-        super().__init__(codes // one, page, kv_heads, dim, _arg(k_codes, "k_codes", codes, _TI8, self.device),
-                         _arg(v_codes, "v_codes", codes, _TI8, self.device),
-                         _arg(k_steps, "k_steps", codes // dim, _T32, self.device),
-                         _arg(v_steps, "v_steps", codes // dim, _T32, self.device))
         if not all(isinstance(t, torch.Tensor) for t in (v_codes, k_steps, v_steps)):
             raise ValueError("codes and steps: tensors are needed")
+        self.tensors, self.numel = (k_codes, v_codes, k_steps, v_steps), k_codes.numel()
+        super().__init__(self.numel // one, page, kv_heads, dim)
         self.set_table(table)
+        self._of(k_codes.get_device())
 
     def set_table(self, table):
         """The pages of other sequences, or more of the same ones'."""
         if not isinstance(table, torch.Tensor) or table.dim() != 2:
             raise ValueError("table: a tensor [batch, table_len] is needed")
         batch, table_len = table.shape
-        self.table = _arg(table, "table", batch * table_len, _TI32, self.device)
+        self.table = _arg(table, "table", batch * table_len, _TI32, self.tensors[0].get_device())
         self.pages, self.batch, self.table_len = table, batch, table_len
 
     def _of(self, dev):
-        """The record's address, with the present addresses of tensors that were checked when they came."""
-        if dev != self.device:
-            raise ValueError(f"a cache on the current device is needed, not on device {self.device}")
+        """The record's address, once its tensors are what they were when it was made, wherever they are now."""
         k, v, ks, vs = self.tensors
-        self.k_codes, self.v_codes, self.k_steps, self.v_steps = k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr()
-        self.table = self.pages.data_ptr()
+        codes, steps = self.numel, self.numel // self.head_dim
+        self.k_codes, self.v_codes = _arg(k, "k_codes", codes, _TI8, dev), _arg(v, "v_codes", codes, _TI8, dev)
+        self.k_steps, self.v_steps = _arg(ks, "k_steps", steps, _T32, dev), _arg(vs, "v_steps", steps, _T32, dev)
+        self.table = _arg(self.pages, "table", self.batch * self.table_len, _TI32, dev)
         return ctypes.byref(self)
 
 
