@@ -597,8 +597,9 @@ canon_status canon_rope(int32_t backward, int64_t tokens, int64_t n_heads, int64
      canon_cache_append: k and v [batch * q_len][n_kv_heads][head_dim], tokens k_stride (v_stride) elements apart, both fp32
        or both bf16.  rotation (may be NULL): k is turned first (R24, to fp32, kept from that value) at its token's
        position.  A token at a position below 0 or at or behind table_len * page, or in a page that the cache does not have
-       (an entry of the table outside [0, n_pages)), is left out; every other slot stays as it was.  Two tokens of one call
-       in the same slot (sequences that share a page) leave either in it.
+       (an entry of the table outside [0, n_pages)), is left out; every other slot stays as it was.  Sequences may share
+       pages and append to different slots of them in one call; what a slot holds after two different tokens of one call were
+       written to it is not defined (codes and steps of both may be mixed; no other slot is touched).
      canon_cache_read: what is kept of the same rows, k and v [batch * q_len][n_kv_heads][head_dim], fp32 RN(step * code) or
        (rounded once more) bf16, either may be NULL; rows that do not exist are +0, tokens that append would leave out NaN. */
 typedef struct {

@@ -764,7 +764,8 @@ class CacheRows(ctypes.Structure):
 
 
 def cache_append(cache: KVCache, rows: CacheRows, k, v, rotation: Rotation | None = None, stream=None):
-    """Keys (turned first by `rotation`, if given) and values [batch * q_len, kv_heads * dim] of new tokens into their pages."""
+    """Keys (turned first by `rotation`, if given) and values [batch * q_len, kv_heads * dim] of new tokens into their pages: no
+    two of them into one slot, whose contents would not be defined."""
     dev = _device()
     n, width = cache.batch * rows.q_len, cache.n_kv_heads * cache.head_dim
     pk, ks = _rows(k, "k", n, width, _TF, dev)

@@ -177,7 +177,8 @@ __device__ __forceinline__ int64_t cache_slot(const CacheView& c, int64_t b, int
 
 // Workgroup: 16 positions that share a group of the value codes, of one head of one sequence.  LPT lanes hold a token, four
 // consecutive elements each (those behind head_dim idle).  Keys go out as they are, four codes a lane; values through LDS,
-// so that a whole group leaves as 16-byte stores; a group with tokens missing leaves byte by byte, the others untouched.
+// so that a whole group leaves as 16-byte stores; a group with tokens missing leaves byte by byte, the others untouched (they may
+// be another sequence's of the same call; two tokens in one slot are not kept apart).
 // Bound by memory: 5120 tokens of 4 sequences, 8 heads of 128 from fp32, 16.4 us; a token each of 16 sequences 4.2.
 template <bool XB, int LPT>
 __global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, CacheRowsArgs r, const void* __restrict__ k,
