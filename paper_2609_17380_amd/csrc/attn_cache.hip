@@ -143,6 +143,17 @@ __device__ __forceinline__ Column column_of(const CacheAttnArgs& a, int64_t b, i
   if (c.lo >= c.hi) c.lo = c.hi = 0;
   return c;
 }
+// the first tile that one of a block of 16 columns sees, one behind all if none does
+__device__ __forceinline__ int64_t first_tile(const CacheAttnArgs& a, int64_t b, int32_t kvh, int64_t block) {
+  const Column c = column_of(a, b, kvh, block * 16 + (threadIdx.x & 15));
+  int32_t lo = c.hi > c.lo ? (int32_t)c.lo : 0x7FFFFFFF;
+#pragma unroll
+  for (int s = 1; s < 16; s <<= 1) {
+    const int32_t l = __shfl_xor(lo, s, 64);
+    lo = l < lo ? l : lo;
+  }
+  return __builtin_amdgcn_readfirstlane(lo) / kTile;
+}
 // which of a tile's keys a column sees: those from lo on, n of them
 struct Seen {
   int32_t lo, n;
@@ -279,8 +290,8 @@ __device__ __forceinline__ void store_out(const CacheAttnArgs& a, int64_t row, i
 // with the values (the weights cross through LDS, 12 KB): a workgroup has all of its 2 * 256 * head_dim bytes of the cache on
 // their way at once and waits for them once.  What a tile gives goes to `parts`, a row's tiles one after the other, to be
 // joined by attn_join_kernel; where there is one tile only, straight to the output.
-// With a window, `span` workgroups a block of queries, from the first tile that one of them sees on (of all tiles, 12 of 257
-// queries behind 2744 keys, most workgroups had nothing to do).
+// With a window, `span` workgroups (and places in `parts`) a block of queries, from the first tile that one of them sees on (of
+// all tiles, 12 of 257 queries behind 2744 keys, most workgroups had nothing to do).
 // Bound by memory where there is enough of it: 4 x 16 heads x 32768 keys of 128, 554 MB, 111 us, 5.0 TB/s; 8 x 2 heads of up to
 // 4096 keys 8 us, the latencies of table entry, codes and join in a row.
 template <int HD>
@@ -290,23 +301,14 @@ __global__ __launch_bounds__(256) void attn_tile_kernel(CacheAttnArgs a, int64_t
   __shared__ float ms[4][16], ss[4][16];
   __shared__ uint32_t vs[4][16];
   const uint32_t id = blockIdx.x, bt = id / (uint32_t)span, bk = bt / (uint32_t)blocks;
-  int64_t tile = id - bt * (uint32_t)span;
+  const int64_t place = id - bt * (uint32_t)span;
   const int64_t cb = bt - bk * (uint32_t)blocks;
   const int64_t b = bk / (uint32_t)a.c.heads;
   const int32_t kvh = (int32_t)(bk - (uint32_t)b * (uint32_t)a.c.heads);
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, cc = lane & 15, g = lane >> 4;
   const int at0 = 64 * w + 16 * g;  // of this lane's 16 keys in the tile
-  if (span < tiles) {
-    const Column c = column_of(a, b, kvh, cb * 16 + cc);
-    int32_t lo = c.hi > c.lo ? (int32_t)c.lo : 0x7FFFFFFF;
-#pragma unroll
-    for (int s = 1; s < 16; s <<= 1) {
-      const int32_t l = __shfl_xor(lo, s, 64);
-      lo = l < lo ? l : lo;
-    }
-    tile += __builtin_amdgcn_readfirstlane(lo) / kTile;
-    if (tile >= tiles) return;
-  }
+  const int64_t tile = place + (span < tiles ? first_tile(a, b, kvh, cb) : 0);
+  if (tile >= tiles) return;
   const int64_t t0 = tile * kTile;
   // which pages, and the queries: asked for before anything is waited for
   const int32_t kpage = page_of(a, b, t0 + 64 * w + 16 * (cc >> 2));
@@ -417,7 +419,7 @@ __global__ __launch_bounds__(256) void attn_tile_kernel(CacheAttnArgs a, int64_t
   __syncthreads();
   const float S = rf.sum((ss[0][cc] + ss[1][cc]) + (ss[2][cc] + ss[3][cc]));
   const float inv = S == 0.0f ? 0.0f : 1.0f / S;
-  float* parts = a.parts + (col.row * tiles + tile) * (HD + 4);
+  float* parts = a.parts + (col.row * span + place) * (HD + 4);
   if (tiles > 1 && col.real && w == 0 && g == 0)
     *reinterpret_cast<f32x4*>(parts + HD) = f32x4{rf.r, S, whole.down, 0.0f};
 #pragma unroll
@@ -452,15 +454,16 @@ __global__ __launch_bounds__(256) void attn_tile_kernel(CacheAttnArgs a, int64_t
 // operations an element; and 16 tiles' sums are on their way together.  (One tile after the other, each waited for: a row of 128
 // tiles took 156 us, so 12; of 16 16, so 4.)
 template <int HD>
-__global__ __launch_bounds__(64) void attn_join_kernel(CacheAttnArgs a, int64_t tiles) {
+__global__ __launch_bounds__(64) void attn_join_kernel(CacheAttnArgs a, int64_t tiles, int64_t span) {
   constexpr int E = HD > 128 ? 4 : 2, U = 16;
   typedef float Vec __attribute__((ext_vector_type(E)));
   const int64_t row = blockIdx.x;
   const int lane = threadIdx.x, at = lane * E < HD ? lane * E : 0;
   const int64_t tok = (uint32_t)row / (uint32_t)a.heads, b = (uint32_t)tok / (uint32_t)a.q_len;  // rows of a call: below 2^24
   const int32_t G = a.heads / a.c.heads, h = (int32_t)(row - tok * a.heads);
-  const Column col = column_of(a, b, h / G, (tok - b * a.q_len) * G + h % G);
-  const float* parts = a.parts + row * tiles * (HD + 4);
+  const int64_t idx = (tok - b * a.q_len) * G + h % G, base = span < tiles ? first_tile(a, b, h / G, idx / 16) : 0;
+  const Column col = column_of(a, b, h / G, idx);
+  const float* parts = a.parts + row * span * (HD + 4);
   float R = kNegInf, S = 0.0f;
   Vec o;
 #pragma unroll
@@ -468,7 +471,7 @@ __global__ __launch_bounds__(64) void attn_join_kernel(CacheAttnArgs a, int64_t 
   const int64_t first = col.lo / kTile, end = col.hi > col.lo ? (col.hi + kTile - 1) / kTile : first;
   for (int64_t c0 = first; c0 < end; c0 += 64) {
     const int n = end - c0 < 64 ? (int)(end - c0) : 64;
-    const float* p = parts + c0 * (HD + 4);
+    const float* p = parts + (c0 - base) * (HD + 4);
     const f32x4 d = *reinterpret_cast<const f32x4*>(p + (lane < n ? lane : n - 1) * (HD + 4) + HD);
     // R of the rule before and after this lane's tile
     float up = d[0];
@@ -853,7 +856,7 @@ Plan plan_of(const CacheAttnArgs& a) {
 size_t cache_attention_workspace(const CacheAttnArgs& a) {
   const Plan p = plan_of(a);
   if (!p.split || p.tiles <= 1) return 0;
-  return sizeof(float) * (size_t)(a.c.batch * a.q_len * a.heads * p.tiles) * (size_t)(a.c.dim + 4);
+  return sizeof(float) * (size_t)(a.c.batch * a.q_len * a.heads * p.span) * (size_t)(a.c.dim + 4);
 }
 
 template <int HD>
@@ -870,7 +873,7 @@ static hipError_t attn_go(const CacheAttnArgs& a, hipStream_t s) {
   hipLaunchKernelGGL((attn_tile_kernel<HD>), dim3((unsigned)(span * blocks * a.c.heads * a.c.batch)), dim3(256), 0, s, a,
                      tiles, blocks, span);
   if (tiles > 1)
-    hipLaunchKernelGGL((attn_join_kernel<HD>), dim3((unsigned)(a.c.batch * a.q_len * a.heads)), dim3(64), 0, s, a, tiles);
+    hipLaunchKernelGGL((attn_join_kernel<HD>), dim3((unsigned)(a.c.batch * a.q_len * a.heads)), dim3(64), 0, s, a, tiles, span);
   return hipGetLastError();
 }
 
