@@ -532,7 +532,7 @@ size_t canon_softmax_relbias_bwd_workspace_bytes(const canon_attn_rows* rows, co
      canon_gemm_i8_tokens: acc[i][j] = sum_k a[i][k] * b[j][k] exactly, a int8 [m][k] (leading dimension lda), b int8 [n][k]
        (ldb; one channel per row, as weights [out][in]); y[i][j] = RN(RN(RN32(acc) * sa[i]) * sb[j]), fp32 or (rounded once
        more) bf16 by y_dtype, leading dimension ldc.  sa fp32 [m], sb fp32 [n].  k in [0, 65536] keeps |acc| < 2^31;
-       ceil(m / 64) n up to 2^26.
+       ceil(m / 64) ceil(n / 8) up to 2^23, m and n up to 2^31, m lda, n ldb and m ldc up to 2^40 (else CANON_EUNSUPPORTED).
    Both take any alignment that the types allow and refuse outputs that overlap an input or each other (CANON_EINVAL), as
    every entry point of the four groups here does.  The straight-through gradients of such a product are those of
    canon_qlinear_bwd where the tensor has one step. */

@@ -126,14 +126,14 @@ canon_status canon_gemm_i8_tokens(int64_t m, int64_t n, int64_t k, const int8_t*
   if (k > 65536 || m > (int64_t(1) << 31) || n > (int64_t(1) << 31) || !product_ok(m, ldc, kMaxElements) ||
       !product_ok(m, lda, kMaxElements) || !product_ok(n, ldb, kMaxElements))
     return CANON_EUNSUPPORTED;
+  // workgroups of a launch stay below 2^32 threads (at least 64 x 8 outputs each)
+  if (!product_ok((m + 63) / 64, (n + 7) / 8, int64_t(1) << 23)) return CANON_EUNSUPPORTED;
   if (m == 0 || n == 0) return CANON_OK;
   if ((k > 0 && (!a || !b)) || !y || !sa || !sb || !aligned(y, dtype_size(y_dtype)) || !aligned(sa, 4) || !aligned(sb, 4))
     return CANON_EINVAL;
   if (!apart({{a, span(m, k, lda, 1), false}, {b, span(n, k, ldb, 1), false}, {sa, 4 * m, false}, {sb, 4 * n, false},
               {y, span(m, n, ldc, dtype_size(y_dtype)), true}}))
     return CANON_EINVAL;
-  // workgroups of a launch stay below 2^32 threads (at least 64 x 8 outputs each)
-  if (!product_ok((m + 63) / 64, (n + 7) / 8, int64_t(1) << 23)) return CANON_EUNSUPPORTED;
   GemmI8Args g{};
   g.a = a; g.b = b; g.y = (float*)y; g.sa = sa; g.sb = sb;
   g.m = m; g.n = n; g.k = k; g.lda = lda; g.ldb = ldb; g.ldc = ldc;
