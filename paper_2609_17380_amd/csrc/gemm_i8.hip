@@ -249,7 +249,9 @@ __device__ __forceinline__ void vm_wait() {
 // have landed.
 // NW = 8: eight wavefronts (two per SIMD), each a 128 x 64 block of 4 x 2 instructions (128 accumulators), four
 // direct loads per wavefront and stage.
-template <int NBUF, int NW>
+// ROWS: a step for each row (fp32 or bf16 out), all of a lane's asked for before the first store, which a load behind it would
+// wait for; else one for the tensor.
+template <int NBUF, int NW, bool ROWS>
 __global__ __launch_bounds__(64 * NW, 1) void gemm_i8_tile_kernel(GemmI8Args g) {
   constexpr int BM = 256, BN = 256, KS = 64, ROWB = 64;
   constexpr int STAGE = (BM + BN) * KS;  // bytes per stage: A rows, then B rows
@@ -387,9 +389,16 @@ __global__ __launch_bounds__(64 * NW, 1) void gemm_i8_tile_kernel(GemmI8Args g) 
   int32_t* eb = reinterpret_cast<int32_t*>(lds) + w * (32 * ELD);
   const int64_t wrow = row0 + 128 * wr, wcol = col0 + WCOLS * wc;
   const int c4 = 4 * (lane % LPR), rq = lane / LPR;  // this lane's 4 columns and row offset in the read-back
-  float sa = 0.0f, sb4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  float sa = 0.0f, sb4[4] = {0.0f, 0.0f, 0.0f, 0.0f}, sr[ROWS ? 4 : 1][ROWS ? 32 / RPI : 1];
   if (g.y) {
-    if (!g.sa_rows) sa = *g.sa;
+    if constexpr (ROWS) {
+#pragma unroll
+      for (int h = 0; h < 4; ++h)
+#pragma unroll
+        for (int q = 0; q < 32 / RPI; ++q) sr[h][q] = g.sa[wrow + 32 * h + RPI * q + rq];
+    } else {
+      sa = *g.sa;
+    }
 #pragma unroll
     for (int e = 0; e < 4; ++e) sb4[e] = g.sb[g.sb_scalar ? 0 : wcol + c4 + e];
   }
@@ -405,13 +414,13 @@ __global__ __launch_bounds__(64 * NW, 1) void gemm_i8_tile_kernel(GemmI8Args g) 
       const i32x4 x = *reinterpret_cast<const i32x4*>(eb + r * ELD + c4);
       const int64_t o = (wrow + 32 * h + r) * g.ldc + wcol + c4;
       if (g.y) {  // streamed out: nontemporal
-        if (g.sa_rows) sa = g.sa[wrow + 32 * h + r];
+        if constexpr (ROWS) sa = sr[h][q];
         f32x4 y;
         y[0] = ((float)x[0] * sa) * sb4[0];  // RN(RN(RN32(acc) sa) sb), one rounding per operation
         y[1] = ((float)x[1] * sa) * sb4[1];
         y[2] = ((float)x[2] * sa) * sb4[2];
         y[3] = ((float)x[3] * sa) * sb4[3];
-        if (g.y_bf16) {
+        if (ROWS && g.y_bf16) {
           u32x2 y16;
           y16[0] = pack_bf16(y[0], y[1]);
           y16[1] = pack_bf16(y[2], y[3]);
@@ -429,7 +438,10 @@ constexpr int kI8TileWaves = 8;
 
 static hipError_t launch_i8_tile(const GemmI8Args& g, hipStream_t s) {
   const int64_t tiles = (g.m / 256) * (g.n / 256);
-  hipLaunchKernelGGL((gemm_i8_tile_kernel<4, kI8TileWaves>), dim3((unsigned)tiles), dim3(64 * kI8TileWaves), 0, s, g);
+  if (g.sa_rows)
+    hipLaunchKernelGGL((gemm_i8_tile_kernel<4, kI8TileWaves, true>), dim3((unsigned)tiles), dim3(64 * kI8TileWaves), 0, s, g);
+  else
+    hipLaunchKernelGGL((gemm_i8_tile_kernel<4, kI8TileWaves, false>), dim3((unsigned)tiles), dim3(64 * kI8TileWaves), 0, s, g);
   return hipGetLastError();
 }
 
