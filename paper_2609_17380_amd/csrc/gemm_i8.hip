@@ -462,12 +462,13 @@ hipError_t gemm_i8_launch(const GemmI8Args& gin, hipStream_t s) {
   if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) !=
                                               hipSuccess || cus <= 0)
     cus = 256;
-  // Whole 256 x 256 tiles (and 16-byte output stores: y, acc and ldc aligned to 4 elements) that fill three quarters of the CUs
-  // or more: the pipelined kernel (8192 x 16384 x 2048 320 us with bf16 out, 335 with fp32;
-  // 256 x 2048 x 8192 in its 8 tiles 113, in 256 smaller ones 15).
+  // Whole 256 x 256 tiles (and 16-byte output stores: y, acc and ldc aligned to 4 elements) that fill half of the CUs or more:
+  // the pipelined kernel (8192 x 16384 x 2048 288 us with bf16 out, 315 with fp32).  As many 128 x 128 tiles have places on
+  // the chip as there are in half a round of these: 2304 x 4096 x 8192 takes 88 us, in the smaller ones' two rounds 131; 2048 x
+  // 4096 x 8192 85 and 90; 1536 x 4096 x 8192, less than half, 83 and 79; 256 x 2048 x 8192 113, in its 8, and 15.
   const bool whole = g.vec && g.m % 256 == 0 && g.n % 256 == 0 && g.ldc % 4 == 0 && ((uintptr_t)g.y & 15) == 0 &&
                      ((uintptr_t)g.acc & 15) == 0 && g.k % 64 == 0 && g.k > 0;
-  if (whole && (g.m / 256) * (g.n / 256) >= 3 * cus / 4) return launch_i8_tile(g, s);
+  if (whole && (g.m / 256) * (g.n / 256) >= cus / 2) return launch_i8_tile(g, s);
   // 128 x 128 tiles where they fill three quarters of the CUs (440 x 7296 x 256: 10 us, with k split over the wavefronts of
   // smaller tiles 19), with little to split half as many (700 x 2048 x 256: 7.4 and 10; x 4096: 30 and 22).
   const int64_t tiles = ((g.m + 127) / 128) * ((g.n + 127) / 128);
