@@ -408,6 +408,7 @@ __global__ __launch_bounds__(64 * NW, 1) void gemm_i8_tile_kernel(GemmI8Args g) 
     for (int v2 = 0; v2 < V2N; ++v2)
 #pragma unroll
       for (int v = 0; v < 16; ++v) eb[((v & 3) + 4 * hi + 8 * (v >> 2)) * ELD + 32 * v2 + rl] = acc[h][v2][v];
+    in_order();
 #pragma unroll
     for (int q = 0; q < 32 / RPI; ++q) {
       const int r = RPI * q + rq;
@@ -431,6 +432,7 @@ __global__ __launch_bounds__(64 * NW, 1) void gemm_i8_tile_kernel(GemmI8Args g) 
       }
       if (g.acc) __builtin_nontemporal_store(x, reinterpret_cast<i32x4*>(g.acc + o));
     }
+    in_order();
   }
 }
 

@@ -87,6 +87,7 @@ __global__ __launch_bounds__(512) void gemm_i8_split_kernel(GemmI8Args g, int64_
     for (int i = 0; i < AV; ++i) *reinterpret_cast<i32x4*>(mine + (8 * i + lr) * LD + ls) = ra[i];
 #pragma unroll
     for (int i = 0; i < BV; ++i) *reinterpret_cast<i32x4*>(mine + (TM + 8 * i + lr) * LD + ls) = rb[i];
+    in_order();
     if (j + 1 < count) load(at(j + 1));
 #pragma unroll
     for (int ks = 0; ks < KS / 32; ++ks) {
@@ -101,6 +102,7 @@ __global__ __launch_bounds__(512) void gemm_i8_split_kernel(GemmI8Args g, int64_
         for (int v2 = 0; v2 < WN; ++v2)
           acc[h][v2] = __builtin_amdgcn_mfma_i32_32x32x32_i8(a[h], b[v2], acc[h][v2], 0, 0, 0);
     }
+    in_order();
   }
 
   // the sums: four registers of a lane are rows r .. r + 3 of column lane % 32 of a 32 x 32 block, r = 8 (v / 4) + 4 (lane / 32)

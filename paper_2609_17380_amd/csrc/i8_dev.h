@@ -1,4 +1,4 @@
-// i8_dev.h - what the int8 products share: 16 bytes of a row at any alignment, whole or cut by the row's end.
+// i8_dev.h - what the int8 products share: 16 bytes of a row at any alignment, whole or cut by the row's end; order in LDS.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -9,6 +9,9 @@ typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 struct __attribute__((packed, aligned(1))) Bytes16 {
   uint32_t w[4];
 };
+// A wavefront's LDS operations complete in order; this holds the compiler to it where lanes read what others of the wavefront wrote,
+// or write where they read.
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 // rows off 16-byte boundaries load as wide
 __device__ __forceinline__ i32x4 whole16(const int8_t* p) {
   const Bytes16 v = *reinterpret_cast<const Bytes16*>(p);
