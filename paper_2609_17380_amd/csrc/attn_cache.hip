@@ -18,6 +18,7 @@
 #include "act8_dev.h"
 #include "canon_dev.h"
 #include "canon_internal.h"
+#include "dma_dev.h"
 #include "rows_dev.h"
 
 namespace canon {
@@ -522,22 +523,6 @@ __global__ __launch_bounds__(64) void attn_join_kernel(CacheAttnArgs a, int64_t 
 // reading has no bank conflicts and no address is computed per lane), a wavefront fetching its quarter of the tile: the next
 // tile's keys while the present one's weights are computed, its values while the next scores are.  Two workgroups a CU (heads
 // of up to 128) run out of step, one's products under the other's exponentials.
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-// 16 (or 4) bytes a lane from global memory to LDS, lane l's at lds + 16 l (4 l); not tracked by the compiler: vm_left waits
-__device__ __forceinline__ void dma16(const void* p, unsigned lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory", "m0");
-}
-__device__ __forceinline__ void dma4(const void* p, unsigned lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(p) : "memory", "m0");
-}
-#pragma clang diagnostic pop
-template <int N>
-__device__ __forceinline__ void vm_left() {  // at most N vector-memory operations of this wavefront outstanding
-  static_assert(N >= 0 && N < 64, "vmcnt range");
-  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x70 | 0xF00);
-}
-
 template <int HD>
 struct RowsLds {
   static constexpr int NS = Query<HD>::NS, ND = HD / 16;

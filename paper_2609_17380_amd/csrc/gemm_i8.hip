@@ -23,6 +23,7 @@
 
 #include "canon_dev.h"
 #include "canon_internal.h"
+#include "dma_dev.h"
 #include "i8_dev.h"
 
 namespace canon {
@@ -30,10 +31,10 @@ namespace canon {
 typedef int32_t i32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-// Workgroup configuration: NW wavefronts in (NW / 2) x 2, wavefront (wr, wc) owning rows [32 HB wr, 32 HB (wr + 1))
+// A workgroup's tile: NW wavefronts in (NW / 2) x 2, wavefront (wr, wc) owning rows [32 HB wr, 32 HB (wr + 1))
 // and columns [32 WN wc, 32 WN (wc + 1)) of a BM x (64 WN) tile (HB x WN instruction blocks); stages of KS k bytes.
-template <int HB, int WN, int KS, int NW>
 struct I8Cfg {
+  static constexpr int HB = 1, WN = 2, KS = 128, NW = 8;
   static constexpr int BM = 16 * NW * HB;     // workgroup tile rows
   static constexpr int NT = 64 * NW;          // threads
   static constexpr int BN = 64 * WN;          // workgroup tile columns
@@ -43,17 +44,17 @@ struct I8Cfg {
   static_assert(AV * NT * 16 == BM * KS && BV * NT * 16 == BN * KS, "whole vectors per thread");
 };
 
-template <class Cf>
 struct I8Raw {
-  i32x4 a[Cf::AV], b[Cf::BV];
+  i32x4 a[I8Cfg::AV], b[I8Cfg::BV];
 };
 
 // Global -> registers for the stage starting at k0: vector idx = t + NT it covers row idx / (KS/16),
 // 16-byte segment idx % (KS/16) of the row's KS bytes.  Rows behind the last are read as the last: what they give is not
 // stored.  WHOLE: the stage lies within k.
-template <class Cf, int KS, bool WHOLE>
-__device__ __forceinline__ void load_stage(const GemmI8Args& g, int64_t row0, int64_t col0, int64_t k0, I8Raw<Cf>& r) {
-  constexpr int SEG = KS / 16;
+template <bool WHOLE>
+__device__ __forceinline__ void load_stage(const GemmI8Args& g, int64_t row0, int64_t col0, int64_t k0, I8Raw& r) {
+  using Cf = I8Cfg;
+  constexpr int SEG = Cf::KS / 16;
   const int t = threadIdx.x;
 #pragma unroll
   for (int it = 0; it < Cf::AV; ++it) {
@@ -71,9 +72,9 @@ __device__ __forceinline__ void load_stage(const GemmI8Args& g, int64_t row0, in
   }
 }
 
-template <class Cf, int KS>
-__device__ __forceinline__ void store_stage(int8_t* As, int8_t* Bs, const I8Raw<Cf>& r) {
-  constexpr int SEG = KS / 16;
+__device__ __forceinline__ void store_stage(int8_t* As, int8_t* Bs, const I8Raw& r) {
+  using Cf = I8Cfg;
+  constexpr int SEG = Cf::KS / 16;
   const int t = threadIdx.x;
 #pragma unroll
   for (int it = 0; it < Cf::AV; ++it) {
@@ -87,10 +88,9 @@ __device__ __forceinline__ void store_stage(int8_t* As, int8_t* Bs, const I8Raw<
   }
 }
 
-template <int HB, int WN, int KS, int NW>
-__global__ __launch_bounds__(64 * NW, NW / 2) void gemm_i8_kernel(GemmI8Args g) {
-  using Cf = I8Cfg<HB, WN, KS, NW>;
-  constexpr int BM = Cf::BM, BN = Cf::BN, LD = Cf::LD;
+__global__ __launch_bounds__(I8Cfg::NT, I8Cfg::NW / 2) void gemm_i8_kernel(GemmI8Args g) {
+  using Cf = I8Cfg;
+  constexpr int HB = Cf::HB, WN = Cf::WN, KS = Cf::KS, BM = Cf::BM, BN = Cf::BN, LD = Cf::LD;
   __shared__ __attribute__((aligned(16))) int8_t As[2][BM * LD];
   __shared__ __attribute__((aligned(16))) int8_t Bs[2][BN * LD];
 
@@ -124,12 +124,12 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void gemm_i8_kernel(GemmI8Args g) 
   // Stage s is multiplied out of LDS while stage s + 1 waits in registers and stage s + 2 is on its way (with one stage ahead,
   // a memory latency passed in every stage: 1541 x 5001 x 2056 in 256 x 256 tiles 85 us, then 77).
   const int64_t ns = (g.k + KS - 1) / KS;
-  I8Raw<Cf> raw[2];
-  auto load = [&](int64_t st, I8Raw<Cf>& r) {
-    if ((st + 1) * KS <= g.k) load_stage<Cf, KS, true>(g, row0, col0, st * KS, r);
-    else load_stage<Cf, KS, false>(g, row0, col0, st * KS, r);
+  I8Raw raw[2];
+  auto load = [&](int64_t st, I8Raw& r) {
+    if ((st + 1) * KS <= g.k) load_stage<true>(g, row0, col0, st * KS, r);
+    else load_stage<false>(g, row0, col0, st * KS, r);
   };
-  auto stage = [&](int64_t st, int buf, I8Raw<Cf>& next, I8Raw<Cf>& after) {
+  auto stage = [&](int64_t st, int buf, I8Raw& next, I8Raw& after) {
     if (st + 2 < ns) load(st + 2, after);
     __builtin_amdgcn_sched_barrier(0);
     const int8_t* as = As[buf];
@@ -149,13 +149,13 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void gemm_i8_kernel(GemmI8Args g) 
           acc[h][v2] = __builtin_amdgcn_mfma_i32_32x32x32_i8(a[h], b[v2], acc[h][v2], 0, 0, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
-    if (st + 1 < ns) store_stage<Cf, KS>(As[buf ^ 1], Bs[buf ^ 1], next);
+    if (st + 1 < ns) store_stage(As[buf ^ 1], Bs[buf ^ 1], next);
     __syncthreads();
   };
   if (ns > 0) {
     load(0, raw[0]);
     if (ns > 1) load(1, raw[1]);
-    store_stage<Cf, KS>(As[0], Bs[0], raw[0]);
+    store_stage(As[0], Bs[0], raw[0]);
   }
   __syncthreads();
   for (int64_t s = 0; s < ns; s += 2) {
@@ -210,24 +210,6 @@ __global__ __launch_bounds__(64 * NW, NW / 2) void gemm_i8_kernel(GemmI8Args g) 
         else g.y[i * g.ldc + j] = y[v2][v];
       }
   }
-}
-
-// 16 bytes per lane from global memory straight into LDS: lane l of the wavefront writes lds_addr + 16 l
-// (lds_addr wavefront-uniform, in m0).  Written as assembly so that the compiler does not track these loads:
-// it would otherwise wait for all of them before every LDS read, which defeats loading stages ahead; the
-// kernel waits for them itself (vm_wait).  The kernel issues no other instruction that uses m0.
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void dma16(const int8_t* g, unsigned lds_addr) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_addr), "v"(g)
-               : "memory", "m0");
-}
-#pragma clang diagnostic pop
-// wait until at most N vector-memory loads of this wavefront are outstanding (they complete in order)
-template <int N>
-__device__ __forceinline__ void vm_wait() {
-  static_assert(N >= 0 && N < 64, "vmcnt range");
-  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x70 | 0xF00);  // expcnt, lgkmcnt left at max
 }
 
 // Whole 256 x 256 tiles (m, n multiples of 256, k of 64, 16-byte aligned rows), one workgroup per CU.  NW = 4:
@@ -329,9 +311,9 @@ __global__ __launch_bounds__(64 * NW, 1) void gemm_i8_tile_kernel(GemmI8Args g) 
   if (ns > 1) issue(1);
   if (ns > 2) issue(2);
   // stage 0 landed (this wavefront's loads of stages 1 and 2 may still be in flight), then everyone's
-  if (ns > 2) vm_wait<2 * LPW>();
-  else if (ns > 1) vm_wait<LPW>();
-  else vm_wait<0>();
+  if (ns > 2) vm_left<2 * LPW>();
+  else if (ns > 1) vm_left<LPW>();
+  else vm_left<0>();
   __syncthreads();
   frags(0, 0, 0);
   // Every stage but the last: no branch around LDS operations inside the loop, so the compiler's wait counts
@@ -362,9 +344,9 @@ __global__ __launch_bounds__(64 * NW, 1) void gemm_i8_tile_kernel(GemmI8Args g) 
     mma0_loads(st + 3, st + 3 < ns);
     __builtin_amdgcn_sched_barrier(0);
     // this wavefront's loads of stage st + 1 landed (those of later stages may stay in flight), then everyone's
-    if (st + 3 < ns) vm_wait<2 * LPW>();
-    else if (st + 2 < ns) vm_wait<LPW>();
-    else vm_wait<0>();
+    if (st + 3 < ns) vm_left<2 * LPW>();
+    else if (st + 2 < ns) vm_left<LPW>();
+    else vm_left<0>();
     __syncthreads();
     frags(0, st + 1, 0);
     mma(1);
@@ -447,11 +429,10 @@ static hipError_t launch_i8_tile(const GemmI8Args& g, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <int HB, int WN, int KS, int NW>
 static hipError_t launch_i8(const GemmI8Args& g, hipStream_t s) {
-  using Cf = I8Cfg<HB, WN, KS, NW>;
+  using Cf = I8Cfg;
   const int64_t tiles = ((g.m + Cf::BM - 1) / Cf::BM) * ((g.n + Cf::BN - 1) / Cf::BN);
-  hipLaunchKernelGGL((gemm_i8_kernel<HB, WN, KS, NW>), dim3((unsigned)tiles), dim3(Cf::NT), 0, s, g);
+  hipLaunchKernelGGL(gemm_i8_kernel, dim3((unsigned)tiles), dim3(Cf::NT), 0, s, g);
   return hipGetLastError();
 }
 
@@ -475,7 +456,7 @@ hipError_t gemm_i8_launch(const GemmI8Args& gin, hipStream_t s) {
   // smaller tiles 19), with little to split half as many (700 x 2048 x 256: 7.4 and 10; x 4096: 30 and 22).
   const int64_t tiles = ((g.m + 127) / 128) * ((g.n + 127) / 128);
   if (tiles < 3 * cus / 4 && !(g.k <= 512 && g.m > 64 && tiles >= 3 * cus / 8)) return gemm_i8_split_launch(g, cus, s);
-  return launch_i8<1, 2, 128, 8>(g, s);
+  return launch_i8(g, s);
 }
 
 }  // namespace canon
