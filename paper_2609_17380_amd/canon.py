@@ -675,7 +675,30 @@ def rope_tables(rot_dim, positions, theta=5e5, scaling: RopeScaling | None = Non
     return cos, sin
 
 
-class Rotation(ctypes.Structure):
+class _Kept(ctypes.Structure):
+    """A record that is kept from call to call.  Its tensors may be resized or given other memory in between: every call looks
+    whether they are as they were last taken (`kept`: tensor, address, elements, type), and takes them again if not."""
+
+    def _of(self, dev):
+        """The record's address, once its tensors are what they were when it was made, wherever they are now."""
+        if self.kept is None or dev != self.device:
+            self._take(dev)
+        for t, address, numel, dtype in self.kept:
+            if t.data_ptr() != address or t.numel() != numel or t.dtype is not dtype or not t.is_contiguous():
+                self._take(dev)
+                break
+        return ctypes.byref(self)
+
+    def _take(self, dev):
+        self.kept, kept = None, ()  # None: the next call takes them, if one is refused here
+        for name, t, numel, dtypes in self._tensors():
+            address = _arg(t, name, numel, dtypes, dev)
+            setattr(self, name, address)
+            kept += ((t, address, numel, dtypes[0]),)
+        self.kept, self.device = kept, dev
+
+
+class Rotation(_Kept):
     """The turns of the first rot_dim elements of a head: cos and sin fp32 [positions, rot_dim / 2] on the device; halves of
     those elements together, or (interleaved) neighbours."""
     _fields_ = [("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("positions", ctypes.c_int64),
@@ -687,15 +710,14 @@ class Rotation(ctypes.Structure):
         half, n = max(rot_dim // 2, 1), cos.numel()
         if n % half or n != sin.numel():
             raise ValueError(f"cos and sin: [positions, {rot_dim // 2}] are needed, not {tuple(cos.shape)} and {tuple(sin.shape)}")
-        self.tensors, self.numel = (cos, sin), n
-        super().__init__(rot_dim, int(interleaved), n // half if rot_dim > 0 else 0)
-        self._of(cos.get_device())
+        dev = cos.get_device()
+        c, s = _arg(cos, "cos", n, _T32, dev), _arg(sin, "sin", n, _T32, dev)
+        super().__init__(rot_dim, int(interleaved), n // half if rot_dim > 0 else 0, c, s)
+        self.tensors, self.numel, self.device = (cos, sin), n, dev
+        self.kept = (cos, c, n, torch.float32), (sin, s, n, torch.float32)
 
-    def _of(self, dev):
-        """The record's address, once its tables are what they were when it was made, wherever they are now."""
-        cos, sin = self.tensors
-        self.cos, self.sin = _arg(cos, "cos", self.numel, _T32, dev), _arg(sin, "sin", self.numel, _T32, dev)
-        return ctypes.byref(self)
+    def _tensors(self):
+        return [(name, t, self.numel, _T32) for name, t in zip(("cos", "sin"), self.tensors)]
 
 
 def rope(tokens, heads, dim, rotation: Rotation, x, y, positions=None, backward=False, stream=None):
@@ -708,7 +730,7 @@ def rope(tokens, heads, dim, rotation: Rotation, x, y, positions=None, backward=
                              _DTYPES[x.dtype], px, xs, _DTYPES[y.dtype], py, ys, _stream_on(stream, dev)), "canon_rope")
 
 
-class KVCache(ctypes.Structure):
+class KVCache(_Kept):
     """A paged cache of keys and values in 8 bits: k_codes int8 [pages, kv_heads, page, dim], v_codes int8 [pages, kv_heads,
     page / 16, dim, 16], k_steps and v_steps fp32 [pages, kv_heads, page], table int32 [batch, table_len]."""
     _fields_ = [(n, ctypes.c_int64) for n in ("n_pages", "page", "n_kv_heads", "head_dim")] + \
@@ -721,27 +743,31 @@ class KVCache(ctypes.Structure):
             raise ValueError(f"k_codes: a tensor of pages of {one} codes is needed")
         if not all(isinstance(t, torch.Tensor) for t in (v_codes, k_steps, v_steps)):
             raise ValueError("codes and steps: tensors are needed")
-        self.tensors, self.numel = (k_codes, v_codes, k_steps, v_steps), k_codes.numel()
-        super().__init__(self.numel // one, page, kv_heads, dim)
+        codes, dev = k_codes.numel(), k_codes.get_device()
+        steps = codes // dim
+        k, v = _arg(k_codes, "k_codes", codes, _TI8, dev), _arg(v_codes, "v_codes", codes, _TI8, dev)
+        ks, vs = _arg(k_steps, "k_steps", steps, _T32, dev), _arg(v_steps, "v_steps", steps, _T32, dev)
+        super().__init__(codes // one, page, kv_heads, dim, k, v, ks, vs)
+        self.tensors, self.numel, self.device = (k_codes, v_codes, k_steps, v_steps), codes, dev
+        self.kept = ((k_codes, k, codes, torch.int8), (v_codes, v, codes, torch.int8), (k_steps, ks, steps, torch.float32),
+                     (v_steps, vs, steps, torch.float32))
         self.set_table(table)
-        self._of(k_codes.get_device())
 
     def set_table(self, table):
         """The pages of other sequences, or more of the same ones'."""
         if not isinstance(table, torch.Tensor) or table.dim() != 2:
             raise ValueError("table: a tensor [batch, table_len] is needed")
         batch, table_len = table.shape
-        self.table = _arg(table, "table", batch * table_len, _TI32, self.tensors[0].get_device())
-        self.pages, self.batch, self.table_len = table, batch, table_len
+        address = _arg(table, "table", batch * table_len, _TI32, self.device)
+        self.table, self.pages, self.batch, self.table_len = address, table, batch, table_len
+        if self.kept is not None:
+            self.kept = self.kept[:4] + ((table, address, batch * table_len, torch.int32),)
 
-    def _of(self, dev):
-        """The record's address, once its tensors are what they were when it was made, wherever they are now."""
+    def _tensors(self):
         k, v, ks, vs = self.tensors
-        codes, steps = self.numel, self.numel // self.head_dim
-        self.k_codes, self.v_codes = _arg(k, "k_codes", codes, _TI8, dev), _arg(v, "v_codes", codes, _TI8, dev)
-        self.k_steps, self.v_steps = _arg(ks, "k_steps", steps, _T32, dev), _arg(vs, "v_steps", steps, _T32, dev)
-        self.table = _arg(self.pages, "table", self.batch * self.table_len, _TI32, dev)
-        return ctypes.byref(self)
+        steps = self.numel // self.head_dim
+        return (("k_codes", k, self.numel, _TI8), ("v_codes", v, self.numel, _TI8), ("k_steps", ks, steps, _T32),
+                ("v_steps", vs, steps, _T32), ("table", self.pages, self.batch * self.table_len, _TI32))
 
 
 class CacheRows(ctypes.Structure):

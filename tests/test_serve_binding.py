@@ -81,7 +81,38 @@ def test_other_memory_of_the_same_kind(host):
     c._of(-1), turn._of(-1)
     assert [c.k_codes, c.v_codes, c.k_steps, c.v_steps, c.table] == [t.data_ptr() for t in p.values()]
     assert [turn.cos, turn.sin] == [t.data_ptr() for t in tables]
+    assert c._of(-1) and c.kept and c.k_steps == p["k_steps"].data_ptr()
     with pytest.raises(ValueError, match="device"):
         c._of(0)
     with pytest.raises(ValueError, match="device"):
         turn._of(0)
+
+
+def test_a_refusal_leaves_nothing_half_taken(host):
+    p = parts()
+    c = C.KVCache(16, 2, 64, *p.values())
+    first = p["k_codes"].data  # the memory that it had
+    p["k_codes"].set_(torch.ones_like(first))
+    steps = p["k_steps"].data
+    p["k_steps"].set_(torch.ones(3))
+    with pytest.raises(ValueError, match="k_steps"):
+        c._of(-1)
+    p["k_codes"].set_(first)
+    p["k_steps"].set_(steps)
+    c._of(-1)
+    assert c.k_codes == first.data_ptr() and c.k_steps == steps.data_ptr()
+    p["v_steps"].resize_(1)
+    longer = z(7, 9, t=torch.int32)
+    c.set_table(longer)
+    for _ in range(2):
+        with pytest.raises(ValueError, match="v_steps"):
+            c._of(-1)
+    longer = z(7, 9, t=torch.int32)
+    c.set_table(longer)
+    p["v_steps"].resize_(4, 2, 16)
+    c._of(-1)
+    assert (c.batch, c.table_len, c.table) == (7, 9, longer.data_ptr())
+    with pytest.raises(ValueError, match="table"):
+        c.set_table(z(3, 2, t=torch.int64))
+    c._of(-1)
+    assert (c.batch, c.table_len, c.table) == (7, 9, longer.data_ptr())
