@@ -293,7 +293,7 @@ __device__ __forceinline__ void store_out(const CacheAttnArgs& a, int64_t row, i
 // joined by attn_join_kernel; where there is one tile only, straight to the output.
 // With a window, `span` workgroups (and places in `parts`) a block of queries, from the first tile that one of them sees on (of
 // all tiles, 12 of 257 queries behind 2744 keys, most workgroups had nothing to do).
-// Bound by memory where there is enough of it: 4 x 16 heads x 32768 keys of 128, 554 MB, 111 us, 5.0 TB/s; 8 x 2 heads of up to
+// Bound by memory where there is enough of it: 4 x 16 heads x 32768 keys of 128, 554 MB, 112 us, 4.9 TB/s; 8 x 2 heads of up to
 // 4096 keys 8 us, the latencies of table entry, codes and join in a row.
 template <int HD>
 __global__ __launch_bounds__(256) void attn_tile_kernel(CacheAttnArgs a, int64_t tiles, int64_t blocks, int64_t span) {
@@ -453,7 +453,7 @@ __global__ __launch_bounds__(256) void attn_tile_kernel(CacheAttnArgs a, int64_t
 // A row's tiles joined, ascending: one wavefront a row, E elements a lane.  What the references change by is worked out for 64
 // tiles at once, a tile a lane (the largest reference up to a tile is a prefix maximum), so that the chain over the tiles is two
 // operations an element; and 16 tiles' sums are on their way together.  (One tile after the other, each waited for: a row of 128
-// tiles took 156 us, so 12; of 16 16, so 4.)
+// tiles took 156 us, so 13; of 16 16, so 4.)
 template <int HD>
 __global__ __launch_bounds__(64) void attn_join_kernel(CacheAttnArgs a, int64_t tiles, int64_t span) {
   constexpr int E = HD > 128 ? 4 : 2, U = 16;
@@ -523,6 +523,9 @@ __global__ __launch_bounds__(64) void attn_join_kernel(CacheAttnArgs a, int64_t 
 // reading has no bank conflicts and no address is computed per lane), a wavefront fetching its quarter of the tile: the next
 // tile's keys while the present one's weights are computed, its values while the next scores are.  Two workgroups a CU (heads
 // of up to 128) run out of step, one's products under the other's exponentials.
+// Bound by its vector instructions: 16 heads x 4096 x 128 152 us in a graph, 32 of them for each 64 visible scores, 85% of a
+// SIMD's cycles issuing one; the third digits of queries and weights and the exponential's last term are a fifth of them.
+// Registers: heads of 128 leave 12 a lane in scratch, of 96 3, of 224 26 and of 256 18, addresses for the most part.
 template <int HD>
 struct RowsLds {
   static constexpr int NS = Query<HD>::NS, ND = HD / 16;
@@ -718,7 +721,7 @@ __global__ __launch_bounds__(256, HD <= 128 ? 2 : 1) void attn_rows_kernel(Cache
           }
         }
         sums[q] = sum4(sum);
-        // one quarter's steps in registers at a time (all four's: 45 registers spilled, 16 heads x 4096 160 us instead of 142)
+        // one quarter's steps in registers at a time (all four's: 45 registers in scratch, 16 heads x 4096 160 us instead of 142, with queries of two digits)
         __builtin_amdgcn_sched_barrier(0);
       }
     };
@@ -828,9 +831,9 @@ Plan plan_of(const CacheAttnArgs& a) {
     const int64_t keys = (a.causal ? a.window : 2 * a.window - 1) + 15 / G + 1;
     span = keys / kTile + 2 < tiles ? keys / kTile + 2 : tiles;
   }
-  // A workgroup for every tile where those for 64 queries would be few (2 heads of 8 over 2048 keys: 64 of them 38 us, 49 in
-  // whole rows; 128 of them 64 and 50; of one tile, 128 of them 10.8 and 13.7, 224 16 and 14), or would have at most two
-  // wavefronts with queries; launches stay below 2^32 threads.
+  // A workgroup for every tile where those for 64 queries would be few (2 heads of 8 over 2048 keys: 64 of them 38 us, 55 in
+  // whole rows; 128 of them 63 and 55; of one tile, 192 of them 12.8 and 14.1, 256 16.5 and 14.5), or would have at most two
+  // wavefronts with queries (8 x 8 heads x 48 of 4000 50 and 102); launches stay below 2^32 threads.
   const int64_t groups = a.c.batch * a.c.heads, wgs = groups * ((cols + 63) / 64);
   const int64_t split_wgs = span * groups * ((cols + 15) / 16);
   // Without keys there may be no cache either (no pages, null pointers): whole rows, which load nothing of it then.
