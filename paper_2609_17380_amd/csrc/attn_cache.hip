@@ -525,7 +525,7 @@ __global__ __launch_bounds__(64) void attn_join_kernel(CacheAttnArgs a, int64_t 
 // of up to 128) run out of step, one's products under the other's exponentials.
 // Bound by its vector instructions: 16 heads x 4096 x 128 152 us in a graph, 32 of them for each 64 visible scores, 85% of a
 // SIMD's cycles issuing one; the third digits of queries and weights and the exponential's last term are a fifth of them.
-// Registers: heads of 128 leave 12 a lane in scratch, of 96 3, of 224 26 and of 256 18, addresses for the most part.
+// Registers: heads of 128 leave 12 a lane in scratch, of 96 3, of 224 18 and of 256 26, addresses for the most part.
 template <int HD>
 struct RowsLds {
   static constexpr int NS = Query<HD>::NS, ND = HD / 16;
